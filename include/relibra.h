@@ -55,7 +55,7 @@ enum {
 
 /* which = */
 enum { RELIBRA_WS_PERMUTE = 0, RELIBRA_WS_FFN_FWD = 1, RELIBRA_WS_FFN_BWD = 2, RELIBRA_WS_WGRAD_BATCHED = 3,
-       RELIBRA_WS_DGATE = 4 };
+       RELIBRA_WS_DGATE = 4, RELIBRA_WS_ROUTER = 5, RELIBRA_WS_BLOCK_NORM = 6 };
 
 /* flags of relibra_moe_ffn_bwd */
 enum {
@@ -579,6 +579,67 @@ int relibra_unpermute_combine(int mode, const void *rows_dev, const void *tok_de
                               int32_t *err_flag_dev, relibra_stream stream);
 
 /*
+ * Router gates of replayed ids and the load-balance loss over per-expert counts, for n_mb micro-batches in one call.  A token's
+ * logits z give log scores u = z, or u = log sigmoid(z) with RELIBRA_ROUTER_SIGMOID, and probabilities p = softmax(u) over the
+ * E experts.  The gate of selection s is scale * part_s with
+ *   part = softmax of u over the token's k selected experts            with RELIBRA_ROUTER_NORMALIZE,
+ *   part = p at the selected expert (softmax), sigmoid(z) (sigmoid)    without.
+ * Over a micro-batch's n valid tokens, f_e = counts_e / (k n) and P_e = mean p_e, the loss is
+ *   loss = balance_coef * E * sum_e f_e P_e     (0 if n = 0).
+ *   logits_dev [n_mb, T, E] bf16, or fp32 with RELIBRA_ROUTER_FP32, dev, in; -infinity takes an expert out of a token's reach
+ *              (a set with nothing else in it has probabilities, parts and gates 0); +infinity and NaN make the token's p, and
+ *              with them prob_mean and loss, NaN
+ *   ids_dev    [n_mb, T, k] int32, dev, in: the replayed experts; an id outside [0, E) has gate 0, is not counted and raises
+ *              RELIBRA_ERR_ID_RANGE; the same expert twice counts twice
+ *   valid_dev  [n_mb, T] uint8, dev, in, or NULL: tokens with 0 (padding) have gates 0 and enter no sum; their logits and ids
+ *              are not looked at
+ *   gates_dev [n_mb, T, k] fp32 out: what relibra_unpermute_combine and relibra_row_gates take; counts_dev [n_mb, E], n_valid_dev
+ *   [n_mb] int32 out; prob_mean_dev [n_mb, E], loss_dev [n_mb] fp32 out
+ *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ROUTER, T, k, E, n_mb, 0, 0) bytes (G is n_mb)
+ * Sums in fp32 and double in a fixed order: results are reproducible bit for bit.
+ * Limits: E <= 4096, k <= min(E, 64), n_mb <= 65535, n_mb * T <= 2^30 (RELIBRA_EUNSUPPORTED beyond), 16-byte aligned logits.
+ */
+enum { RELIBRA_ROUTER_SIGMOID = 1, RELIBRA_ROUTER_NORMALIZE = 2, RELIBRA_ROUTER_FP32 = 4 };
+int relibra_router_fwd(const void *logits_dev, const int32_t *ids_dev, const uint8_t *valid_dev, int n_mb, int T, int k, int E, int flags,
+                       float scale, float balance_coef, float *gates_dev, int32_t *counts_dev, int32_t *n_valid_dev, float *prob_mean_dev,
+                       float *loss_dev, void *workspace_dev, size_t workspace_bytes, int32_t *err_flag_dev, relibra_stream stream);
+
+/*
+ * Its backward pass: dlogits [n_mb, T, E] in the logits' type from dgates [n_mb, T, k] fp32 (the dgate of relibra_unpermute_combine or
+ * relibra_moe_ffn_bwd_gated; NULL: none) and dloss [n_mb] fp32 (NULL: no balance loss; counts and n_valid are then not read).
+ * The counts are constants of the loss.  Rows of invalid tokens become 0; ids outside [0, E) give nothing and raise
+ * RELIBRA_ERR_ID_RANGE.  flags, scale, balance_coef, valid as in the forward call.  dlogits may not overlap the logits.
+ */
+int relibra_router_bwd(const void *logits_dev, const int32_t *ids_dev, const uint8_t *valid_dev, const float *dgates_dev, const int32_t *counts_dev,
+                       const int32_t *n_valid_dev, const float *dloss_dev, int n_mb, int T, int k, int E, int flags, float scale, float balance_coef,
+                       void *dlogits_dev, int32_t *err_flag_dev, relibra_stream stream);
+
+/*
+ * The RMS norms behind one block and in front of the next, with the residual stream between them:
+ *   z = y / rms(y) * w_post  (z = y with w_post = NULL),   x' = res_scale * x + gate * z,   n = x' / rms(x') * w_pre,
+ *   rms(v) = sqrt(mean v^2 + eps) over the h values of a row.
+ * y is what a block put out (for the expert layer: relibra_unpermute_combine's out_tok), n the next block's input.
+ *   y_dev NULL (with w_post NULL and no gate): only the norm in front, n from x' = x, nothing stored to x_out
+ *   w_pre_dev NULL: no norm in front, n is not written
+ *   gate_dev: with RELIBRA_NORM_GATE_TOKEN [T] fp32, one gate a row; with RELIBRA_NORM_GATE_ELEMENT [T, h] bf16; else 1
+ *   x_dev, x_out_dev [T, h] bf16, or fp32 with RELIBRA_NORM_STREAM_FP32; y_dev, n_dev [T, h], w_post_dev, w_pre_dev [h] bf16
+ * n comes from x' before its rounding to the stream's type.  x_out may be x, n may be y (row by row, read before it is written).
+ * Backward: dx, dy, dgate, dw_post, dw_pre from dx_out (the gradient of x', NULL: 0) and dn (of n; with w_pre only), with
+ * x_out as the forward call left it (x where y is NULL).  dx, dx_out in the stream's type, dy bf16, dgate like the gate, dw_post,
+ * dw_pre [h] fp32: overwritten, or added to with RELIBRA_NORM_ACCUMULATE.  dx may be dx_out, dy may be y or dn.
+ *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_BLOCK_NORM, T, 1, 1, 1, h, 0) bytes
+ * Row sums and weight gradients are added up in fp32 in a fixed order: results are reproducible bit for bit.
+ * Limits: eps > 0, h % 8 == 0, h <= 8192, T <= 2^30, 16-byte aligned tensors (one gate a row: 4 bytes).
+ */
+enum { RELIBRA_NORM_STREAM_FP32 = 1, RELIBRA_NORM_GATE_TOKEN = 2, RELIBRA_NORM_GATE_ELEMENT = 4, RELIBRA_NORM_ACCUMULATE = 8 };
+int relibra_block_norm_fwd(const void *x_dev, const void *y_dev, const void *w_post_dev, const void *w_pre_dev, const void *gate_dev, int T, int h,
+                           float res_scale, float eps, int flags, void *x_out_dev, void *n_dev, relibra_stream stream);
+int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const void *dn_dev, const void *y_dev, const void *w_post_dev,
+                           const void *w_pre_dev, const void *gate_dev, int T, int h, float res_scale, float eps, int flags,
+                           void *dx_dev, void *dy_dev, void *dgate_dev, float *dw_post_dev, float *dw_pre_dev,
+                           void *workspace_dev, size_t workspace_bytes, relibra_stream stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  Between relibra_prof_start and
  * relibra_prof_stop every kernel launch of the chosen level is bracketed by two HIP events on
  * its launch stream: level 1 = the grouped-GEMM kernels, level 2 = every kernel, 0 = off.
@@ -597,7 +658,8 @@ enum {
     RELIBRA_K_FWD_GATE_UP, RELIBRA_K_FWD_DOWN, RELIBRA_K_BWD_ACT, RELIBRA_K_BWD_DX,
     RELIBRA_K_WGRAD_DOWN, RELIBRA_K_WGRAD_GATE_UP, RELIBRA_K_REPLICA_SUM, RELIBRA_K_REPLICA_PUSH,
     RELIBRA_K_WGRAD_ORDER, RELIBRA_K_TRANSPOSE, RELIBRA_K_ROW_TOKENS, RELIBRA_K_ROW_GATES, RELIBRA_K_DGATE_REDUCE,
-    RELIBRA_K_REPLICA_PULL, RELIBRA_K_WGRAD_PAIR, RELIBRA_K_PERM_SMALL, RELIBRA_K_COUNT
+    RELIBRA_K_REPLICA_PULL, RELIBRA_K_WGRAD_PAIR, RELIBRA_K_PERM_SMALL,
+    RELIBRA_K_ROUTER_FWD, RELIBRA_K_ROUTER_FINISH, RELIBRA_K_ROUTER_BWD, RELIBRA_K_NORM_FWD, RELIBRA_K_NORM_BWD, RELIBRA_K_NORM_REDUCE, RELIBRA_K_COUNT
 };
 int relibra_prof_start(int level, int max_records);
 int relibra_prof_stop(double *ms_by_kernel_host, int64_t *launches_by_kernel_host);

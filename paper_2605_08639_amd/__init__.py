@@ -18,12 +18,14 @@ LIB_PATH = os.path.join(_HERE, "librelibra.so")
 
 OK, EINVAL, ERANGE, EWORKSPACE, EHIP, EUNSUPPORTED, ENOMEM = 0, -1, -2, -3, -4, -5, -6
 ERR_ID_RANGE, ERR_PLAN_COVER, ERR_GROUP_TABLE = 1, 2, 4
-WS_PERMUTE, WS_FFN_FWD, WS_FFN_BWD, WS_WGRAD_BATCHED, WS_DGATE = 0, 1, 2, 3, 4
+WS_PERMUTE, WS_FFN_FWD, WS_FFN_BWD, WS_WGRAD_BATCHED, WS_DGATE, WS_ROUTER, WS_BLOCK_NORM = 0, 1, 2, 3, 4, 5, 6
 BWD_ACCUMULATE, BWD_NO_REPLICA_SUM, BWD_REPLICA_WEIGHTS, BWD_DEFER_WGRAD, BWD_TRANSPOSED_WEIGHTS = 1, 2, 4, 8, 16
 FWD_TRANSPOSED_WEIGHTS = 1
 WGRAD_ACCUMULATE, WGRAD_TILE_NARROW, WGRAD_TILE_WIDE = 1, 2, 4
 MAX_WGRAD_MB = 48
 COMBINE_FWD, COMBINE_BWD, COMBINE_SUM = 0, 1, 2
+ROUTER_SIGMOID, ROUTER_NORMALIZE, ROUTER_FP32 = 1, 2, 4
+NORM_STREAM_FP32, NORM_GATE_TOKEN, NORM_GATE_ELEMENT, NORM_ACCUMULATE = 1, 2, 4, 8
 
 EXPORTS = ("relibra_route_hist", "relibra_plan", "relibra_plan_placed", "relibra_moe_time", "relibra_reorder_sa", "relibra_load_stats",
            "relibra_cost_model_init", "relibra_reorder_sa_trace",
@@ -31,13 +33,15 @@ EXPORTS = ("relibra_route_hist", "relibra_plan", "relibra_plan_placed", "relibra
            "relibra_permute", "relibra_permute_static", "relibra_row_tokens", "relibra_row_gates", "relibra_moe_ffn_fwd_gather", "relibra_moe_ffn_fwd_gated",
            "relibra_moe_ffn_bwd_gated", "relibra_moe_ffn_fwd",
            "relibra_moe_ffn_bwd", "relibra_moe_ffn_wgrad_batched", "relibra_transpose_experts", "relibra_unpermute_combine", "relibra_replica_push", "relibra_replica_pull",
+           "relibra_router_fwd", "relibra_router_bwd", "relibra_block_norm_fwd", "relibra_block_norm_bwd",
            "relibra_workspace_bytes",
            "relibra_status_string", "relibra_prof_start", "relibra_prof_stop")
 
 KERNELS = ("hist", "perm_count", "perm_scan", "perm_rank", "gather", "combine_fwd", "combine_bwd",
            "combine_sum", "sched", "fwd_gate_up", "fwd_down", "bwd_act", "bwd_dx", "wgrad_down",
            "wgrad_gate_up", "replica_sum", "replica_push", "wgrad_order", "transpose", "row_tokens", "row_gates",
-           "dgate_reduce", "replica_pull", "wgrad_pair", "perm_small")
+           "dgate_reduce", "replica_pull", "wgrad_pair", "perm_small",
+           "router_fwd", "router_finish", "router_bwd", "norm_fwd", "norm_bwd", "norm_reduce")
 
 _lib = None
 
@@ -669,6 +673,119 @@ def relibra_unpermute_combine(mode, rows, row_of, T, k, gates=None, tok=None,
                                          _dp(dgate), _dp(err_flag), _stream())
     _check("relibra_unpermute_combine", rc)
     return (out_rows, dgate) if mode == COMBINE_BWD else out_tok
+
+
+def _router_args(logits, ids, valid, sigmoid, normalize):
+    n_mb, T, E = logits.shape
+    k = ids.shape[2]
+    assert logits.dtype in (torch.bfloat16, torch.float32), f"logits in bf16 or fp32, got {logits.dtype}"
+    assert ids.shape == (n_mb, T, k), "ids are [n_mb, T, k]"
+    assert valid is None or (valid.shape == (n_mb, T) and valid.dtype in (torch.uint8, torch.bool)), "valid is [n_mb, T] of bytes"
+    flags = (ROUTER_SIGMOID if sigmoid else 0) | (ROUTER_NORMALIZE if normalize else 0) | (ROUTER_FP32 if logits.dtype == torch.float32 else 0)
+    return n_mb, T, k, E, flags
+
+
+def router_workspace(n_mb, T, k, E, device="cuda"):
+    return torch.empty(max(workspace_bytes(WS_ROUTER, T, k, E, max(n_mb, 1), 0, 0), 1), dtype=torch.uint8, device=device)
+
+
+def _out(t, shape, dtype, like):
+    """An output the caller gave, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    assert tuple(t.shape) == tuple(shape) and t.dtype == dtype, f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
+    return t
+
+
+def relibra_router_fwd(logits, ids, sigmoid=False, normalize=True, scale=1.0, balance_coef=0.0, valid=None,
+                       gates=None, counts=None, n_valid=None, prob_mean=None, loss=None, workspace=None, err_flag=None):
+    """logits [n_mb,T,E] bf16 or fp32, replayed ids [n_mb,T,k] int32 -> gates [n_mb,T,k] fp32, counts [n_mb,E] and n_valid [n_mb]
+    int32, prob_mean [n_mb,E] and the balance loss [n_mb] fp32.  valid [n_mb,T] (bool or uint8): tokens that count."""
+    n_mb, T, k, E, flags = _router_args(logits, ids, valid, sigmoid, normalize)
+    gates = _out(gates, (n_mb, T, k), torch.float32, logits)
+    counts = _out(counts, (n_mb, E), torch.int32, logits)
+    n_valid = _out(n_valid, (n_mb,), torch.int32, logits)
+    prob_mean = _out(prob_mean, (n_mb, E), torch.float32, logits)
+    loss = _out(loss, (n_mb,), torch.float32, logits)
+    if workspace is None:
+        workspace = router_workspace(n_mb, T, k, E, logits.device)
+    if err_flag is None:
+        err_flag = new_err_flag(logits.device)
+    rc = lib().relibra_router_fwd(_dp(logits), _dp(ids, torch.int32), _dp(valid), n_mb, T, k, E, flags, C.c_float(scale), C.c_float(balance_coef),
+                                  _dp(gates), _dp(counts), _dp(n_valid), _dp(prob_mean), _dp(loss),
+                                  _dp(workspace), C.c_size_t(workspace.numel()), _dp(err_flag, torch.int32), _stream())
+    _check("relibra_router_fwd", rc)
+    return gates, counts, n_valid, prob_mean, loss
+
+
+def relibra_router_bwd(logits, ids, dgates, counts=None, n_valid=None, dloss=None, sigmoid=False, normalize=True, scale=1.0, balance_coef=0.0,
+                       valid=None, dlogits=None, err_flag=None):
+    """dgates [n_mb,T,k] fp32 (or None) and dloss [n_mb] fp32 (or None; else with the forward call's counts and n_valid) -> dlogits
+    [n_mb,T,E] in the logits' type."""
+    n_mb, T, k, E, flags = _router_args(logits, ids, valid, sigmoid, normalize)
+    assert dgates is None or dgates.shape == (n_mb, T, k), "dgates are [n_mb, T, k]"
+    assert dloss is None or (dloss.shape == (n_mb,) and counts.shape == (n_mb, E) and n_valid.shape == (n_mb,)), "dloss comes with counts and n_valid"
+    dlogits = _out(dlogits, logits.shape, logits.dtype, logits)
+    if err_flag is None:
+        err_flag = new_err_flag(logits.device)
+    rc = lib().relibra_router_bwd(_dp(logits), _dp(ids, torch.int32), _dp(valid), _dp(dgates, torch.float32), _dp(counts, torch.int32),
+                                  _dp(n_valid, torch.int32), _dp(dloss, torch.float32), n_mb, T, k, E, flags, C.c_float(scale), C.c_float(balance_coef),
+                                  _dp(dlogits), _dp(err_flag, torch.int32), _stream())
+    _check("relibra_router_bwd", rc)
+    return dlogits
+
+
+def _norm_args(x, y, w_post, w_pre, gate):
+    T, h = x.shape
+    assert x.dtype in (torch.bfloat16, torch.float32), f"the residual stream is bf16 or fp32, got {x.dtype}"
+    assert y is None or y.shape == (T, h), "y is [T, h]"
+    assert (w_post is None or w_post.shape == (h,)) and (w_pre is None or w_pre.shape == (h,)), "norm weights are [h]"
+    flags = NORM_STREAM_FP32 if x.dtype == torch.float32 else 0
+    gate_type = None
+    if gate is not None:
+        assert gate.shape in ((T,), (T, h)), "one gate a token or one an element"
+        flags |= NORM_GATE_TOKEN if gate.dim() == 1 else NORM_GATE_ELEMENT
+        gate_type = torch.float32 if gate.dim() == 1 else torch.bfloat16
+    return T, h, flags, gate_type
+
+
+def relibra_block_norm_fwd(x, y=None, w_post=None, w_pre=None, gate=None, res_scale=1.0, eps=1e-6, x_out=None, n=None):
+    """x' = res_scale * x + gate * RMSNorm(y; w_post), n = RMSNorm(x'; w_pre) -> (x', n).  x [T,h] bf16 or fp32, y [T,h] bf16, weights [h] bf16,
+    gate [T] fp32 or [T,h] bf16 (or None).  Without y: x' is x and only n is computed; without w_pre: n is None."""
+    T, h, flags, gate_type = _norm_args(x, y, w_post, w_pre, gate)
+    x_out = x if y is None else _out(x_out, (T, h), x.dtype, x)
+    n = None if w_pre is None else _out(n, (T, h), torch.bfloat16, x)
+    rc = lib().relibra_block_norm_fwd(_dp(x), _dp(y, torch.bfloat16), _dp(w_post, torch.bfloat16), _dp(w_pre, torch.bfloat16), _dp(gate, gate_type),
+                                      T, h, C.c_float(res_scale), C.c_float(eps), flags, _dp(None if y is None else x_out), _dp(n), _stream())
+    _check("relibra_block_norm_fwd", rc)
+    return x_out, n
+
+
+def block_norm_workspace(T, h, device="cuda"):
+    return torch.empty(max(workspace_bytes(WS_BLOCK_NORM, T, 1, 1, 1, h, 0), 1), dtype=torch.uint8, device=device)
+
+
+def relibra_block_norm_bwd(x_out, dx_out, dn, y=None, w_post=None, w_pre=None, gate=None, res_scale=1.0, eps=1e-6, accumulate=False,
+                           dx=None, dy=None, dgate=None, dw_post=None, dw_pre=None, workspace=None):
+    """x_out as the forward call left it, dx_out (or None) and dn [T,h] -> (dx, dy, dgate, dw_post, dw_pre), None where there is no such input.
+    accumulate: dw_post and dw_pre (fp32 [h], given) are added to."""
+    T, h, flags, gate_type = _norm_args(x_out, y, w_post, w_pre, gate)
+    assert dx_out is None or (dx_out.shape == (T, h) and dx_out.dtype == x_out.dtype), "dx_out is like x_out"
+    assert (dn is None) == (w_pre is None) and (dn is None or dn.shape == (T, h)), "dn [T, h] goes with w_pre"
+    assert not accumulate or ((w_post is None or dw_post is not None) and (w_pre is None or dw_pre is not None)), "nothing to add to"
+    dx = _out(dx, (T, h), x_out.dtype, x_out)
+    dy = None if y is None else _out(dy, (T, h), torch.bfloat16, x_out)
+    dgate = None if gate is None else _out(dgate, gate.shape, gate_type, x_out)
+    dw_post = None if w_post is None else _out(dw_post, (h,), torch.float32, x_out)
+    dw_pre = None if w_pre is None else _out(dw_pre, (h,), torch.float32, x_out)
+    if workspace is None:
+        workspace = block_norm_workspace(T, h, x_out.device)
+    rc = lib().relibra_block_norm_bwd(_dp(x_out), _dp(dx_out), _dp(dn, torch.bfloat16), _dp(y, torch.bfloat16), _dp(w_post, torch.bfloat16),
+                                      _dp(w_pre, torch.bfloat16), _dp(gate, gate_type), T, h, C.c_float(res_scale), C.c_float(eps),
+                                      flags | (NORM_ACCUMULATE if accumulate else 0), _dp(dx), _dp(dy), _dp(dgate), _dp(dw_post), _dp(dw_pre),
+                                      _dp(workspace), C.c_size_t(workspace.numel()), _stream())
+    _check("relibra_block_norm_bwd", rc)
+    return dx, dy, dgate, dw_post, dw_pre
 
 
 def prof_start(level=1, max_records=4096):

@@ -54,7 +54,13 @@ __device__ __forceinline__ int block_scan256(int v, int32_t *sums, int &total)
     return v;
 }
 
+inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Workspace sizes of the entry points in other translation units (relibra_workspace_bytes).
+size_t router_ws_bytes(int n_mb, int T, int E);
+size_t norm_ws_bytes(int T, int h);
 
 inline hipError_t launch_check() { return hipGetLastError(); }
 

@@ -53,7 +53,6 @@ struct Sched {
     bf16_t *dGt, *dU;      // [n_rows, hff] (backward only)
 };
 
-inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline int max_row_tiles(int n_rows, int Gr) { return (n_rows + BM - 1) / BM + Gr; }
 constexpr int kLdsBytes = NSTAGES * (256 + BM) * BK * 2;   // NSTAGES slabs of 256 + BM operand rows
 // The row-tiled GEMMs also come with a tile twice as wide (512 columns, or 2 x 256 for gate and up)
@@ -1295,6 +1294,8 @@ extern "C" size_t relibra_workspace_bytes(int which, int T, int k, int E, int G,
     case RELIBRA_WS_FFN_BWD: return ffn_ws_bytes(N, G, hff, true);
     case RELIBRA_WS_WGRAD_BATCHED: return round256(wgrad_plan_ints(E, G) * sizeof(int32_t));
     case RELIBRA_WS_DGATE: return dgate_scratch_bytes(N, hff);
+    case RELIBRA_WS_ROUTER: return (long long)G * T <= 1 << 30 ? router_ws_bytes(G, T, E) : 0;
+    case RELIBRA_WS_BLOCK_NORM: return h >= 8 && h % 8 == 0 ? norm_ws_bytes(T, h) : 0;
     default: return 0;
     }
     (void)h;
