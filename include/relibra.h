@@ -55,7 +55,8 @@ enum {
 
 /* which = */
 enum { RELIBRA_WS_PERMUTE = 0, RELIBRA_WS_FFN_FWD = 1, RELIBRA_WS_FFN_BWD = 2, RELIBRA_WS_WGRAD_BATCHED = 3,
-       RELIBRA_WS_DGATE = 4, RELIBRA_WS_ROUTER = 5, RELIBRA_WS_BLOCK_NORM = 6 };
+       RELIBRA_WS_DGATE = 4, RELIBRA_WS_ROUTER = 5, RELIBRA_WS_BLOCK_NORM = 6,
+       RELIBRA_WS_ORTHOGONALIZE = 7 };
 
 /* flags of relibra_moe_ffn_bwd */
 enum {
@@ -640,6 +641,25 @@ int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const 
                            void *workspace_dev, size_t workspace_bytes, relibra_stream stream);
 
 /*
+ * Orthogonalised updates of n matrices (the experts' weight gradients) by Newton-Schulz products, as the Muon optimiser takes them:
+ *   M' = mu M + G;   U = G + mu M' with RELIBRA_ORTHO_NESTEROV, else M';   without momentum U = G
+ *   X = U / |U|_F, then `steps` times  A = X X^T,  X = a X + (b A + c A^2) X   with (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *   out = scale * X
+ * Singular values of at most 1 go towards 1 (between about 0.7 and 1.2 after 5 steps); a matrix of zeros stays zero, an infinity or
+ * NaN makes its own matrix NaN.
+ *   grad_dev [n, rows, cols] fp32, or bf16 with RELIBRA_ORTHO_BF16, dev, in: dWg, dWu or dWd of relibra_moe_ffn_wgrad_batched
+ *   momentum_dev [n, rows, cols] fp32, dev, in, or NULL; momentum_out_dev the same, out (may be momentum_dev), NULL without
+ *   out_dev [n, rows, cols] bf16, dev, out
+ *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ORTHOGONALIZE, 0, 1, n, 1, rows, cols) bytes (E, h, hff are n, rows, cols)
+ * Products of half-precision operands with fp32 sums, the linear term in 22 bits: the result's error is that of its rounding to bf16
+ * (about 2e-3 of its norm), for gradients of low rank too.  Fixed order, no atomics: results are reproducible bit for bit.
+ * Limits: rows, cols <= 32768, n <= 65535, 1 <= steps <= 64.
+ */
+enum { RELIBRA_ORTHO_BF16 = 1, RELIBRA_ORTHO_NESTEROV = 2 };
+int relibra_orthogonalize(const void *grad_dev, const float *momentum_dev, int n, int rows, int cols, float mu, float scale, int steps, int flags,
+                          float *momentum_out_dev, void *out_dev, void *workspace_dev, size_t workspace_bytes, relibra_stream stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  Between relibra_prof_start and
  * relibra_prof_stop every kernel launch of the chosen level is bracketed by two HIP events on
  * its launch stream: level 1 = the grouped-GEMM kernels, level 2 = every kernel, 0 = off.
@@ -659,7 +679,8 @@ enum {
     RELIBRA_K_WGRAD_DOWN, RELIBRA_K_WGRAD_GATE_UP, RELIBRA_K_REPLICA_SUM, RELIBRA_K_REPLICA_PUSH,
     RELIBRA_K_WGRAD_ORDER, RELIBRA_K_TRANSPOSE, RELIBRA_K_ROW_TOKENS, RELIBRA_K_ROW_GATES, RELIBRA_K_DGATE_REDUCE,
     RELIBRA_K_REPLICA_PULL, RELIBRA_K_WGRAD_PAIR, RELIBRA_K_PERM_SMALL,
-    RELIBRA_K_ROUTER_FWD, RELIBRA_K_ROUTER_FINISH, RELIBRA_K_ROUTER_BWD, RELIBRA_K_NORM_FWD, RELIBRA_K_NORM_BWD, RELIBRA_K_NORM_REDUCE, RELIBRA_K_COUNT
+    RELIBRA_K_ROUTER_FWD, RELIBRA_K_ROUTER_FINISH, RELIBRA_K_ROUTER_BWD, RELIBRA_K_NORM_FWD, RELIBRA_K_NORM_BWD, RELIBRA_K_NORM_REDUCE,
+    RELIBRA_K_ORTHO_NORM, RELIBRA_K_ORTHO_LOAD, RELIBRA_K_ORTHO_GRAM, RELIBRA_K_ORTHO_POLY, RELIBRA_K_ORTHO_UPDATE, RELIBRA_K_COUNT
 };
 int relibra_prof_start(int level, int max_records);
 int relibra_prof_stop(double *ms_by_kernel_host, int64_t *launches_by_kernel_host);

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "librelibra.so")
 
 OK, EINVAL, ERANGE, EWORKSPACE, EHIP, EUNSUPPORTED, ENOMEM = 0, -1, -2, -3, -4, -5, -6
 ERR_ID_RANGE, ERR_PLAN_COVER, ERR_GROUP_TABLE = 1, 2, 4
-WS_PERMUTE, WS_FFN_FWD, WS_FFN_BWD, WS_WGRAD_BATCHED, WS_DGATE, WS_ROUTER, WS_BLOCK_NORM = 0, 1, 2, 3, 4, 5, 6
+WS_PERMUTE, WS_FFN_FWD, WS_FFN_BWD, WS_WGRAD_BATCHED, WS_DGATE, WS_ROUTER, WS_BLOCK_NORM, WS_ORTHOGONALIZE = 0, 1, 2, 3, 4, 5, 6, 7
 BWD_ACCUMULATE, BWD_NO_REPLICA_SUM, BWD_REPLICA_WEIGHTS, BWD_DEFER_WGRAD, BWD_TRANSPOSED_WEIGHTS = 1, 2, 4, 8, 16
 FWD_TRANSPOSED_WEIGHTS = 1
 WGRAD_ACCUMULATE, WGRAD_TILE_NARROW, WGRAD_TILE_WIDE = 1, 2, 4
@@ -26,6 +26,7 @@ MAX_WGRAD_MB = 48
 COMBINE_FWD, COMBINE_BWD, COMBINE_SUM = 0, 1, 2
 ROUTER_SIGMOID, ROUTER_NORMALIZE, ROUTER_FP32 = 1, 2, 4
 NORM_STREAM_FP32, NORM_GATE_TOKEN, NORM_GATE_ELEMENT, NORM_ACCUMULATE = 1, 2, 4, 8
+ORTHO_BF16, ORTHO_NESTEROV = 1, 2
 
 EXPORTS = ("relibra_route_hist", "relibra_plan", "relibra_plan_placed", "relibra_moe_time", "relibra_reorder_sa", "relibra_load_stats",
            "relibra_cost_model_init", "relibra_reorder_sa_trace",
@@ -33,7 +34,7 @@ EXPORTS = ("relibra_route_hist", "relibra_plan", "relibra_plan_placed", "relibra
            "relibra_permute", "relibra_permute_static", "relibra_row_tokens", "relibra_row_gates", "relibra_moe_ffn_fwd_gather", "relibra_moe_ffn_fwd_gated",
            "relibra_moe_ffn_bwd_gated", "relibra_moe_ffn_fwd",
            "relibra_moe_ffn_bwd", "relibra_moe_ffn_wgrad_batched", "relibra_transpose_experts", "relibra_unpermute_combine", "relibra_replica_push", "relibra_replica_pull",
-           "relibra_router_fwd", "relibra_router_bwd", "relibra_block_norm_fwd", "relibra_block_norm_bwd",
+           "relibra_router_fwd", "relibra_router_bwd", "relibra_block_norm_fwd", "relibra_block_norm_bwd", "relibra_orthogonalize",
            "relibra_workspace_bytes",
            "relibra_status_string", "relibra_prof_start", "relibra_prof_stop")
 
@@ -41,7 +42,8 @@ KERNELS = ("hist", "perm_count", "perm_scan", "perm_rank", "gather", "combine_fw
            "combine_sum", "sched", "fwd_gate_up", "fwd_down", "bwd_act", "bwd_dx", "wgrad_down",
            "wgrad_gate_up", "replica_sum", "replica_push", "wgrad_order", "transpose", "row_tokens", "row_gates",
            "dgate_reduce", "replica_pull", "wgrad_pair", "perm_small",
-           "router_fwd", "router_finish", "router_bwd", "norm_fwd", "norm_bwd", "norm_reduce")
+           "router_fwd", "router_finish", "router_bwd", "norm_fwd", "norm_bwd", "norm_reduce",
+           "ortho_norm", "ortho_load", "ortho_gram", "ortho_poly", "ortho_update")
 
 _lib = None
 
@@ -786,6 +788,29 @@ def relibra_block_norm_bwd(x_out, dx_out, dn, y=None, w_post=None, w_pre=None, g
                                       _dp(workspace), C.c_size_t(workspace.numel()), _stream())
     _check("relibra_block_norm_bwd", rc)
     return dx, dy, dgate, dw_post, dw_pre
+
+
+def orthogonalize_workspace(n, rows, cols, device="cuda"):
+    return torch.empty(max(workspace_bytes(WS_ORTHOGONALIZE, 0, 1, max(n, 1), 1, rows, cols), 1), dtype=torch.uint8, device=device)
+
+
+def relibra_orthogonalize(grad, momentum=None, mu=0.95, nesterov=True, scale=1.0, steps=5, out=None, momentum_out=None, workspace=None):
+    """grad [n,rows,cols] fp32 or bf16 (dWg, dWu, dWd of the experts) and momentum fp32 (or None) -> (the orthogonalised update [n,rows,cols] bf16,
+    the new momentum (None without)).  momentum_out may be the momentum itself; nesterov counts with momentum only."""
+    n, rows, cols = grad.shape
+    assert grad.dtype in (torch.bfloat16, torch.float32), f"gradients in bf16 or fp32, got {grad.dtype}"
+    assert momentum is None or momentum.shape == grad.shape, "momentum is like grad"
+    assert momentum is not None or momentum_out is None, "no momentum to update"
+    out = _out(out, grad.shape, torch.bfloat16, grad)
+    if momentum is not None:
+        momentum_out = _out(momentum_out, grad.shape, torch.float32, grad)
+    if workspace is None:
+        workspace = orthogonalize_workspace(n, rows, cols, grad.device)
+    flags = (ORTHO_BF16 if grad.dtype == torch.bfloat16 else 0) | (ORTHO_NESTEROV if nesterov and momentum is not None else 0)
+    rc = lib().relibra_orthogonalize(_dp(grad), _dp(momentum, torch.float32), n, rows, cols, C.c_float(mu), C.c_float(scale), int(steps), flags,
+                                     _dp(momentum_out), _dp(out), _dp(workspace), C.c_size_t(workspace.numel()), _stream())
+    _check("relibra_orthogonalize", rc)
+    return out, momentum_out
 
 
 def prof_start(level=1, max_records=4096):

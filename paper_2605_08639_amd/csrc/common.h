@@ -61,6 +61,7 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 // Workspace sizes of the entry points in other translation units (relibra_workspace_bytes).
 size_t router_ws_bytes(int n_mb, int T, int E);
 size_t norm_ws_bytes(int T, int h);
+size_t ortho_ws_bytes(int n, int rows, int cols);
 
 inline hipError_t launch_check() { return hipGetLastError(); }
 

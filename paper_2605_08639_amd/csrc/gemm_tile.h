@@ -20,6 +20,7 @@
 namespace relibra {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
@@ -379,7 +380,7 @@ __device__ __forceinline__ bf16x8_t mask_frag(bf16x8_t f, int k_first, int k_val
 // each, gate/up 5.08 -> 4.01 ms, down 2.45 -> 2.22; 128 of 2048 x 768, 300 rows each, 391 -> 325 and 205 -> 176 us:
 // what the same kernels take on transposed weight copies (4.09, 2.21 ms; 326, 170 us).
 template <class AT, class BT, int NA, int NB, int BA, int BB, int WA, int WB, int NPH, bool RAGGED_K, int STAGES = 4,
-          bool SPREAD = false, bool B_FIRST = false, bool ALT = false>
+          bool SPREAD = false, bool B_FIRST = false, bool ALT = false, bool F16 = false>
 struct KLoop {
     static constexpr int NW = WA * WB;
     static constexpr int DEPTH = AT::DEPTH;           // k-values per slab
@@ -586,6 +587,13 @@ struct KLoop {
         }
     }
 
+    // F16: the operands' 16 bits are IEEE half precision.
+    static __device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c)
+    {
+        if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+
     // MFMAs number lo .. hi-1 of the NS*NB*TA*TB of one k16 step (all of them: 0 .. N_MFMA)
     static constexpr int N_MFMA = NS * NB * TA * TB;
     template <int LO, int HI>
@@ -601,8 +609,7 @@ struct KLoop {
                     for (int tb = 0; tb < TB; ++tb) {
                         const int idx = ((a * NB + b) * TA + ta) * TB + tb;
                         if (idx >= LO && idx < HI)
-                            acc[a * NB + b][ta][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                f.a[a][ta], f.b[b][tb], acc[a * NB + b][ta][tb], 0, 0, 0);
+                            acc[a * NB + b][ta][tb] = mfma(f.a[a][ta], f.b[b][tb], acc[a * NB + b][ta][tb]);
                     }
     }
     static __device__ __forceinline__ void mfma_all(Acc &acc, const Frags &f) { mfma_range<0, N_MFMA>(acc, f); }
@@ -611,7 +618,7 @@ struct KLoop {
     static __device__ __forceinline__ void mfma_one(Acc &acc, const Frags &f, int idx)
     {
         const int tb = idx % TB, ta = (idx / TB) % TA, ab = ALT ? PAR : idx / (TA * TB);
-        acc[ab][ta][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[ALT ? 0 : ab / NB][ta], f.b[ab % NB][tb], acc[ab][ta][tb], 0, 0, 0);
+        acc[ab][ta][tb] = mfma(f.a[ALT ? 0 : ab / NB][ta], f.b[ab % NB][tb], acc[ab][ta][tb]);
     }
 
     // Spread loads (SPREAD): a slab's loads go out one by one between the MFMAs of a slab period

@@ -106,10 +106,10 @@ __device__ __forceinline__ void pick_selections(const float (&z)[CH][8], float *
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) store8(row + (c * LT + sub) * 8, z[c]);
-    wave_lds_handover();
+    wave_lds_fence();
 #pragma unroll
     for (int i = 0; i < kRouterMaxSel; ++i) sel.z[i] = i < n_sel && sel.id[i] >= 0 ? row[sel.id[i]] : -INFINITY;
-    wave_lds_handover();                                     // the row may be overwritten
+    wave_lds_fence();                                     // the row may be overwritten
 }
 
 // The part of each selection of this lane: its share of the token's selected (normalised), or its score as it is.
@@ -219,6 +219,7 @@ router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
             }
     }
     if (bad) atomicOr(err_flag, RELIBRA_ERR_ID_RANGE);
+    __syncthreads();                                         // every wave is done with its rows
     // the wave's token groups, then the waves, in a fixed order
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -343,7 +344,7 @@ router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
             for (int i = 0; i < kRouterMaxSel; ++i) mean += part[i] * dg[i];
             mean = group_sum<LT>(mean);
         }
-        wave_lds_handover();
+        wave_lds_fence();
 #pragma unroll
         for (int i = 0; i < kRouterMaxSel; ++i)
             if (i < n_sel) {
@@ -352,10 +353,10 @@ router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
                 for (int q = 0; q < last; ++q)
                     if (sub == q && sel.id[i] >= 0) unsafeAtomicAdd(row + sel.id[i], v);
             }
-        wave_lds_handover();
+        wave_lds_fence();
 #pragma unroll
         for (int c = 0; c < CH; ++c) load8(row + (c * LT + sub) * 8, add[c]);
-        wave_lds_handover();
+        wave_lds_fence();
         // softmax gates as they are: the upstream gradient joins c; otherwise it is a du of its own
         const bool joins = !normalize && !SIGMOID;
         float dot = 0.0f;

@@ -2,6 +2,7 @@
 // they are DPP moves (no LDS, no index registers), beyond that the row and half swaps of gfx950.
 #pragma once
 #include "common.h"
+#include "wave_stage.h"
 
 namespace relibra {
 
@@ -37,16 +38,6 @@ template <int LANES, class Op> __device__ __forceinline__ float group_reduce(flo
 }
 template <int LANES> __device__ __forceinline__ float group_sum(float v) { return group_reduce<LANES, SumOp>(v); }
 template <int LANES> __device__ __forceinline__ float group_max(float v) { return group_reduce<LANES, MaxOp>(v); }
-
-// LDS operations of one wave execute in order; this keeps the compiler from moving them across a hand-over of data between
-// the wave's lanes, and waits for what was read.
-__device__ __forceinline__ void wave_lds_handover()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0)
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 
 // Eight consecutive values of memory (16-byte aligned) as loaded, as fp32, and back (one rounding to bf16).
 template <class T> struct Raw8;

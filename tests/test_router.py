@@ -129,6 +129,17 @@ def check(kw, sigmoid, normalize, dtype, padded, masked, seed=0, spread=3.0, z=N
 
 
 @gpu
+def test_router_long_micro_batches_give_the_same_every_time():
+    """Many rounds of tokens in every block, its waves running apart, over several passes."""
+    kw = dict(n_mb=12, T=6000, E=128, k=8)
+    got, dz = check(kw, False, True, torch.bfloat16, True, 0.0, seed=31)
+    z, ids, valid = make(12, 6000, 128, 8, torch.bfloat16, 31, 3.0, True, 0.0)
+    for _ in range(10):
+        again = rl.relibra_router_fwd(z.to(DEV), ids.to(DEV), scale=2.5, balance_coef=0.01, valid=valid.to(DEV))
+        assert all(torch.equal(a, b) for a, b in zip(again, got))
+
+
+@gpu
 def test_router_gradient_against_differences():
     """Central differences of the library's own forward pass: loss and gates as functions of single logits."""
     n_mb, T, E, k = 1, 4, 12, 3
