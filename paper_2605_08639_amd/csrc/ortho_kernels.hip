@@ -8,9 +8,14 @@
 // because singular values stay below 1.3: everything is stored times 2^12 (kScale), which keeps the entries of a large matrix
 // (about 1 / sqrt(m n)) out of the subnormals.  The linear term a X is another matter: what rounding puts outside of X's row and column
 // spaces is multiplied by a = 3.4 in every step, by 485 in all, and a gradient of few tokens has few dimensions.  X is therefore
-// kept as the sum of two halves (22 bits), of which only the first enters products.  Relative error of the result (norm) against
-// double precision, bf16 operands / one half / this, before the result's own rounding to bf16 (1.7e-3): 256 x 640
-// Gaussian 1.1e-2 / 1.4e-3 / 1.7e-3; rank 4: 0.55 / 6.9e-2 / 3.4e-4; rank 1: 1.2 / 0.15 / 3.1e-4.
+// kept as the sum of two halves, hi + lo (22 bits), of which only hi enters products.  Near the end X X^T is close to a multiple of
+// I, and so is B (-2.4 I): the diagonals of A and B are kept apart in fp32 and the products' operands have a diagonal of zeros, so
+// that what is rounded is small:  X' = (a + dB) hi + (a + w dB) lo + (B - dB) hi  row by row.  B hi stands for B X: what the
+// product leaves out of lo is put back for the diagonal, w = 1, but only in the last three steps, since dB lo, unlike B lo, does leave X's
+// row space.  Relative error of the result (norm) in a simulation against double precision, before the result's own
+// rounding to bf16 (1.7e-3), with bf16 operands / halves alone / lo kept too / and the diagonals apart: 128 x 256 Gaussian 1.2e-2 /
+// 1.7e-3 / 1.7e-3 / 5.9e-4, 64 x 1000 1.3e-2 / 1.8e-3 / 2.1e-3 / 3.1e-4, rank 1 1.2 / 0.15 / 4.0e-4 / 5.5e-4, rank 16 of 256 x 500
+// 0.3 / 3e-2 / 5.5e-4 / 7.4e-4.
 //
 // Matrices are padded to multiples of 64 with zeros, which every step leaves zero.  X lies as the gradient does; the Gram matrix is
 // taken over the longer side, along memory (wide) or across it (tall), and X is multiplied from the left or the right.  A and B
@@ -38,9 +43,10 @@ struct OrthoShape {
     int rp, cp;                                  // padded
     bool tall;                                   // rows > cols
 };
-// Workspace: two copies of X's first halves (a step reads one and writes the other), the second halves, A, B, partial sums.
+// Workspace: two copies of X's first halves (a step reads one and writes the other), the second halves, A, B, their diagonals, partial sums.
 struct OrthoWs {
     uint16_t *x[2], *lo, *a, *b;
+    float *da, *db;
     double *parts;
 };
 inline size_t ortho_x_bytes(const OrthoShape &s) { return round256((size_t)s.n * s.rp * s.cp * 2); }
@@ -49,6 +55,7 @@ inline size_t ortho_gram_bytes(const OrthoShape &s)
     const size_t m = s.tall ? s.cp : s.rp;
     return round256((size_t)s.n * m * m * 2);
 }
+inline size_t ortho_diag_bytes(const OrthoShape &s) { return round256((size_t)s.n * (s.tall ? s.cp : s.rp) * sizeof(float)); }
 inline OrthoShape ortho_shape(int n, int rows, int cols)
 {
     auto pad = [](int v) { return (v + kOrthoPad - 1) / kOrthoPad * kOrthoPad; };
@@ -57,7 +64,7 @@ inline OrthoShape ortho_shape(int n, int rows, int cols)
 size_t ortho_ws_bytes(int n, int rows, int cols)
 {
     const OrthoShape s = ortho_shape(n, rows, cols);
-    return 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + round256((size_t)n * kNormParts * sizeof(double));
+    return 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + 2 * ortho_diag_bytes(s) + round256((size_t)n * kNormParts * sizeof(double));
 }
 
 // ---------------------------------------------------------------- momentum, norm, first halves
@@ -189,12 +196,14 @@ __device__ __forceinline__ int xcd_tile(int block, int total)
 }
 
 // Symmetric product S = P P^T over k (P [m, k], k along memory: ACROSS = false; or P^T stored, [k, m]: ACROSS = true).
-// POLY: out = b P + c P P / kScale instead of P P^T / kScale (P symmetric, m = k).
+// POLY: out = b P + c P P / kScale instead of P P^T / kScale (P symmetric, m = k).  The diagonals are kept apart: `diag_out` takes
+// the result's, out has zeros there; P = p + diag(diag_in) in the POLY form, so that P P = p p + (d_r + d_c) p_rc + d^2.
 // Tiles (i, j), j <= i: rows i * TILE on the lanes, columns j * TILE in the registers; a tile below the diagonal is stored
 // a second time with rows and columns exchanged, read back from the staging area by transposing LDS reads.
 template <int TILE, bool ACROSS, bool POLY>
 __global__ void __launch_bounds__(OrthoCfg<TILE>::THREADS, TILE == 256 ? 2 : 2)
-ortho_gram_kernel(const uint16_t *__restrict__ p, int m, int k, int tiles_1d, int total, uint16_t *__restrict__ out)
+ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag_in, int m, int k, int tiles_1d, int total, uint16_t *__restrict__ out,
+                  float *__restrict__ diag_out)
 {
     using CF = OrthoCfg<TILE>;
     using OT = typename std::conditional<ACROSS, KsTile<TILE>, KcTile<TILE>>::type;
@@ -224,8 +233,12 @@ ortho_gram_kernel(const uint16_t *__restrict__ p, int m, int k, int tiles_1d, in
     for (int half = 0; half < COLS / 64; ++half) {
         const int wcol0 = col0 + (wave / CF::WB) * COLS + half * 64;
         if (wrow0 >= m || wcol0 >= m) break;                  // uniform in the wave; padding is in whole runs of 64
+        const float *din = diag_in + (size_t)mat * m;
+        float d_r[2] = {0.0f, 0.0f};
         if (POLY) {
             ST::fill(buf, src, m, wrow0, m, wcol0, m, lane);
+            d_r[0] = din[wrow0 + (lane & 31)];
+            d_r[1] = din[wrow0 + 32 + (lane & 31)];
             wave_lds_fence();
         }
 #pragma unroll
@@ -235,12 +248,19 @@ ortho_gram_kernel(const uint16_t *__restrict__ p, int m, int k, int tiles_1d, in
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int r = tb * 32 + (lane & 31), c = ta * 32 + q * 8 + (lane >> 5) * 4;
-                    float v[4], old[4];
-                    if (POLY) unpack4h(ST::get(buf, r, c), old);
+                    float v[4], old[4], d_c[4];
+                    if (POLY) {
+                        unpack4h(ST::get(buf, r, c), old);
+                        *reinterpret_cast<float4 *>(d_c) = *reinterpret_cast<const float4 *>(din + wcol0 + c);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float s = acc[0][half * 2 + ta][tb][q * 4 + e] * (1.0f / kScale);
-                        v[e] = POLY ? kNsB * old[e] + kNsC * s : s;
+                        const float s = acc[0][half * 2 + ta][tb][q * 4 + e];
+                        v[e] = POLY ? kNsB * old[e] + (kNsC / kScale) * (s + (d_r[tb] + d_c[e]) * old[e]) : s * (1.0f / kScale);
+                        if (i == j && wrow0 + r == wcol0 + c + e) {
+                            diag_out[(size_t)mat * m + wrow0 + r] = POLY ? kNsB * d_c[e] + (kNsC / kScale) * (s + d_c[e] * d_c[e]) : v[e];
+                            v[e] = 0.0f;
+                        }
                     }
                     ST::put(buf, r, c, pack4h(v));
                 }
@@ -263,7 +283,7 @@ ortho_gram_kernel(const uint16_t *__restrict__ p, int m, int k, int tiles_1d, in
     }
 }
 
-// X' = a X + B X (wide: X [m, n], rows of B on the lanes, X's columns across memory in the registers) or a X + X B (tall: X [n, m], rows of
+// X' = (a + d) hi + (a + w d) lo + B hi, d the diagonal kept apart (wide: X [m, n], rows of B on the lanes, X's columns across memory in the registers or, tall: X [n, m] with B from the right, rows of
 // X on the lanes, B's columns, which are its rows, in the registers).  The last step writes the caller's matrix instead.
 struct OrthoLast {
     uint16_t *out;                               // bf16 [n, rows, cols], or nullptr: not the last step
@@ -272,8 +292,8 @@ struct OrthoLast {
 };
 template <int TILE, bool TALL>
 __global__ void __launch_bounds__(OrthoCfg<TILE>::THREADS, 2)
-ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t *__restrict__ bmat, OrthoShape s, int tiles_r, int tiles_c, int total,
-                    uint16_t *__restrict__ x_out, OrthoLast last)
+ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t *__restrict__ bmat, const float *__restrict__ diag, float w, OrthoShape s,
+                    int tiles_r, int tiles_c, int total, uint16_t *__restrict__ x_out, OrthoLast last)
 {
     using CF = OrthoCfg<TILE>;
     using AT = typename std::conditional<TALL, KcTile<TILE>, KsTile<TILE>>::type;
@@ -304,6 +324,12 @@ ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t
         const int wcol0 = col0 + (wave / CF::WB) * COLS + half * 64;
         if (wrow0 >= s.rp || wcol0 >= s.cp) break;
         ST::fill2(buf_h, buf_l, X, L, s.cp, wrow0, s.rp, wcol0, s.cp, lane);
+        const float *d = diag + (size_t)mat * m;
+        float d_r[2] = {0.0f, 0.0f};
+        if (!TALL) {
+            d_r[0] = d[wrow0 + (lane & 31)] * (1.0f / kScale);
+            d_r[1] = d[wrow0 + 32 + (lane & 31)] * (1.0f / kScale);
+        }
         wave_lds_fence();
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb)
@@ -312,11 +338,15 @@ ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int r = tb * 32 + (lane & 31), c = ta * 32 + q * 8 + (lane >> 5) * 4;
-                    float h[4], l[4], v[4];
+                    float h[4], l[4], v[4], d_c[4];
+                    if (TALL) *reinterpret_cast<float4 *>(d_c) = *reinterpret_cast<const float4 *>(d + wcol0 + c);
                     unpack4h(ST::get(buf_h, r, c), h);
                     unpack4h(ST::get(buf_l, r, c), l);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = kNsA * (h[e] + l[e]) + acc[0][half * 2 + ta][tb][q * 4 + e] * (1.0f / kScale);
+                    for (int e = 0; e < 4; ++e) {
+                        const float de = TALL ? d_c[e] * (1.0f / kScale) : d_r[tb];
+                        v[e] = (kNsA + de) * h[e] + ((kNsA + w * de) * l[e] + acc[0][half * 2 + ta][tb][q * 4 + e] * (1.0f / kScale));
+                    }
                     if (last.out) {
                         const float f = last.scale * (1.0f / kScale);
                         ST::put(buf_h, r, c, make_uint2(pack2bf(f * v[0], f * v[1]), pack2bf(f * v[2], f * v[3])));
@@ -370,14 +400,15 @@ int ortho_steps(const OrthoShape &s, const OrthoWs &w, int steps, float scale, u
     const int tr = (s.rp + TILE - 1) / TILE, tc = (s.cp + TILE - 1) / TILE, upd = s.n * tr * tc;
     for (int i = 0; i < steps; ++i) {
         const uint16_t *x = w.x[i & 1];
-        if (s.tall) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<TILE, true, false><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(x, m, n, t1, gram, w.a)));
-        else RELIBRA_LAUNCH(RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<TILE, false, false><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(x, m, n, t1, gram, w.a)));
-        RELIBRA_LAUNCH(RELIBRA_K_ORTHO_POLY, stream, (ortho_gram_kernel<TILE, false, true><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(w.a, m, m, t1, gram, w.b)));
+        const float weight = i + 3 >= steps ? 1.0f : 0.0f;
+        if (s.tall) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<TILE, true, false><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(x, nullptr, m, n, t1, gram, w.a, w.da)));
+        else RELIBRA_LAUNCH(RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<TILE, false, false><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(x, nullptr, m, n, t1, gram, w.a, w.da)));
+        RELIBRA_LAUNCH(RELIBRA_K_ORTHO_POLY, stream, (ortho_gram_kernel<TILE, false, true><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(w.a, w.da, m, m, t1, gram, w.b, w.db)));
         const OrthoLast last{i + 1 == steps ? out : nullptr, scale, s.cols % 8 == 0 && aligned16(out)};
         if (s.tall) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_UPDATE, stream, (ortho_update_kernel<TILE, true><<<xcd_grid(upd), CF::THREADS, CF::LDS, stream>>>(
-            x, w.lo, w.b, s, tr, tc, upd, w.x[(i + 1) & 1], last)));
+            x, w.lo, w.b, w.db, weight, s, tr, tc, upd, w.x[(i + 1) & 1], last)));
         else RELIBRA_LAUNCH(RELIBRA_K_ORTHO_UPDATE, stream, (ortho_update_kernel<TILE, false><<<xcd_grid(upd), CF::THREADS, CF::LDS, stream>>>(
-            x, w.lo, w.b, s, tr, tc, upd, w.x[(i + 1) & 1], last)));
+            x, w.lo, w.b, w.db, weight, s, tr, tc, upd, w.x[(i + 1) & 1], last)));
     }
     return RELIBRA_OK;
 }
@@ -420,7 +451,9 @@ extern "C" int relibra_orthogonalize(const void *grad, const float *momentum, in
     w.lo = (uint16_t *)(p += ortho_x_bytes(s));
     w.a = (uint16_t *)(p += ortho_x_bytes(s));
     w.b = (uint16_t *)(p += ortho_gram_bytes(s));
-    w.parts = (double *)(p + ortho_gram_bytes(s));
+    w.da = (float *)(p += ortho_gram_bytes(s));
+    w.db = (float *)(p += ortho_diag_bytes(s));
+    w.parts = (double *)(p + ortho_diag_bytes(s));
     const int mode = !momentum ? U_GRAD : flags & RELIBRA_ORTHO_NESTEROV ? U_NESTEROV : U_MOMENTUM;
     if (flags & RELIBRA_ORTHO_BF16) ortho_load(s, w, (const bf16_t *)grad, momentum, mu, mode, momentum_out, stream);
     else ortho_load(s, w, (const float *)grad, momentum, mu, mode, momentum_out, stream);
