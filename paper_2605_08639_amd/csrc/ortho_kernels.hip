@@ -25,14 +25,13 @@
 #include "wave_stage.h"
 
 #include <algorithm>
-#include <mutex>
 
 namespace relibra {
 
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kScale = 4096.0f;
 constexpr int kOrthoPad = 64;
-constexpr int kNormParts = 64;                   // partial sums of a matrix's squares
+constexpr int kMinParts = 16, kMaxParts = 1024;  // partial sums of a matrix's squares
 constexpr int kOrthoMaxSide = 32768;
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
@@ -61,21 +60,27 @@ inline OrthoShape ortho_shape(int n, int rows, int cols)
     auto pad = [](int v) { return (v + kOrthoPad - 1) / kOrthoPad * kOrthoPad; };
     return OrthoShape{n, rows, cols, pad(rows), pad(cols), rows > cols};
 }
+// Blocks that share a matrix's squares: 2048 over all matrices, each with at least 4096 values.  With 64 a matrix one of
+// 4096 x 4096 took 197 us (0.25 of the copy rate).
+inline int norm_parts(const OrthoShape &s)
+{
+    const size_t values = (size_t)s.rows * s.cols;
+    return (int)std::min<size_t>(std::max<size_t>(std::min<size_t>((2048 + s.n - 1) / s.n, values / 4096), kMinParts), kMaxParts);
+}
 size_t ortho_ws_bytes(int n, int rows, int cols)
 {
     const OrthoShape s = ortho_shape(n, rows, cols);
-    return 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + 2 * ortho_diag_bytes(s) + round256((size_t)n * kNormParts * sizeof(double));
+    return 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + 2 * ortho_diag_bytes(s) + round256((size_t)n * norm_parts(s) * sizeof(double));
 }
 
 // ---------------------------------------------------------------- momentum, norm, first halves
-template <class GT> __device__ __forceinline__ float update_of(GT g, float m_new, float mu, int mode)
-{
-    const float gf = to_f32(g);
-    return mode == 0 ? gf : mode == 1 ? m_new : fmaf(mu, m_new, gf);
-}
 enum { U_GRAD = 0, U_MOMENTUM = 1, U_NESTEROV = 2 };
+__device__ __forceinline__ float update_of(float g, float m_new, float mu, int mode)
+{
+    return mode == U_GRAD ? g : mode == U_MOMENTUM ? m_new : fmaf(mu, m_new, g);
+}
 
-// M' and the sum of U^2, blockIdx.x of kNormParts parts of matrix blockIdx.y.  Squares in double: no gradient is too large or small.
+// M' and the sum of U^2, part blockIdx.x of matrix blockIdx.y.  Squares in double: no gradient is too large or small.
 // vec: elements per matrix and all pointers allow 16-byte accesses (four fp32 or eight bytes of bf16 at a time).
 template <class GT>
 __global__ void __launch_bounds__(256)
@@ -86,12 +91,12 @@ ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mo
     double sum = 0.0;
     auto one = [&](GT gv, float mv) __attribute__((always_inline)) {
         const float mn = mode == U_GRAD ? 0.0f : fmaf(mu, mv, to_f32(gv));
-        const double u = update_of(gv, mn, mu, mode);
+        const double u = update_of(to_f32(gv), mn, mu, mode);
         sum += u * u;
         return mn;
     };
     if (vec) {
-        const size_t quads = per_matrix / 4, stride = (size_t)kNormParts * 256;
+        const size_t quads = per_matrix / 4, stride = (size_t)gridDim.x * 256;
         for (size_t q = (size_t)blockIdx.x * 256 + threadIdx.x; q < quads; q += stride) {
             GT gv[4];
             if constexpr (sizeof(GT) == 4) *reinterpret_cast<float4 *>(gv) = *reinterpret_cast<const float4 *>(g + base + q * 4);
@@ -102,7 +107,7 @@ ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mo
             if (mode != U_GRAD) *reinterpret_cast<float4 *>(m_out + base + q * 4) = mn;
         }
     } else {
-        for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < per_matrix; i += (size_t)kNormParts * 256) {
+        for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < per_matrix; i += (size_t)gridDim.x * 256) {
             const float mn = one(g[base + i], mode != U_GRAD ? m[base + i] : 0.0f);
             if (mode != U_GRAD) m_out[base + i] = mn;
         }
@@ -111,19 +116,20 @@ ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mo
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) parts[(size_t)blockIdx.y * kNormParts + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+    if (threadIdx.x == 0) parts[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
 // X = kScale U / |U| as two halves, padding included.  A thread takes 8 consecutive padded columns of a row.
 template <class GT>
 __global__ void __launch_bounds__(256)
 ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, float mu, int mode, OrthoShape s, int vec, const double *__restrict__ parts,
-                  uint16_t *__restrict__ hi, uint16_t *__restrict__ lo)
+                  int n_parts, uint16_t *__restrict__ hi, uint16_t *__restrict__ lo)
 {
     __shared__ double scale_of;
     const int b = blockIdx.y;
     if (threadIdx.x < 64) {
-        double sum = parts[(size_t)b * kNormParts + threadIdx.x];
+        double sum = 0.0;
+        for (int i = threadIdx.x; i < n_parts; i += 64) sum += parts[(size_t)b * n_parts + i];
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
         if (threadIdx.x == 0) scale_of = sum == 0.0 ? 0.0 : (double)kScale / sqrt(sum);
@@ -135,18 +141,18 @@ ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, flo
     const size_t from = (size_t)b * s.rows * s.cols, to = (size_t)b * s.rp * s.cp;
     for (size_t p = (size_t)blockIdx.x * 256 + threadIdx.x; p < pieces; p += (size_t)gridDim.x * 256) {
         const int r = (int)(p / per_row), c = (int)(p % per_row) * 8;
-        float gv[8], mv[8], u[8];
+        float gv[8] = {}, mv[8] = {}, u[8];
         const size_t at = from + (size_t)r * s.cols + c;
         const bool whole = vec && r < s.rows && c < s.cols;          // cols % 8 == 0 then
         if (whole) {
-            load8(g + at, gv);
+            if (mode != U_MOMENTUM) load8(g + at, gv);
             if (mode != U_GRAD) load8(m_new + at, mv);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const bool in = r < s.rows && c + j < s.cols;
             if (!whole) {
-                gv[j] = in ? to_f32(g[at + j]) : 0.0f;
+                gv[j] = in && mode != U_MOMENTUM ? to_f32(g[at + j]) : 0.0f;
                 mv[j] = in && mode != U_GRAD ? m_new[at + j] : 0.0f;
             }
             u[j] = in ? (float)((double)update_of(gv[j], mv[j], mu, mode) * scale) : 0.0f;
@@ -165,15 +171,17 @@ ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, flo
 }
 
 // ---------------------------------------------------------------- products
-// TILE = 256: eight waves of 128 x 64 (columns in the accumulator registers x rows on the lanes), one workgroup per compute unit;
-// TILE = 128: four waves of 64 x 64, two.
-template <int TILE> struct OrthoCfg {
-    static constexpr int WA = 2, WB = TILE / 64, NWV = WA * WB, THREADS = NWV * 64;
-    static constexpr int STAGES = 4;
-    static constexpr int LDS = STAGES * 2 * TILE * BK * 2;
-    static constexpr int OCC = TILE == 256 ? 1 : 2;                  // workgroups per compute unit
+// A tile has BB rows (on the lanes) and BA columns (in the accumulator registers); a wave owns 64 rows and BA / WA_ columns.
+template <int BA_, int BB_, int STAGES_, int OCC_, bool DEEP_ = false, int WA_ = 2> struct OrthoCfg {
+    static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = BB / 64, THREADS = WA * WB * 64, STAGES = STAGES_;
+    static constexpr int COLS = BA / WA;                             // of a wave
+    static constexpr int BDEPTH = DEEP_ ? 2 * BK : BK;               // of the row operand's LDS tiles
+    static constexpr int WAVES_PER_SIMD = OCC_ * WA * WB / 4;        // OCC_: workgroups per compute unit
+    static constexpr int SLABS = STAGES * (BA + (DEEP_ ? 0 : BB)) * BK * 2 + (DEEP_ ? (STAGES + 3) / 2 * BB * BDEPTH * 2 : 0);
+    static constexpr int STAGING = WA * WB * 2 * WaveStage<64>::BYTES;
+    static constexpr int LDS = SLABS > STAGING ? SLABS : STAGING;
+    template <class AT> using Loop = KLoop<AT, KcTile<BB, BDEPTH>, 1, 1, BA, BB, WA, WB, 1, false, STAGES, true, false, false, true>;
 };
-static_assert(OrthoCfg<256>::LDS >= 8 * 2 * WaveStage<64>::BYTES && OrthoCfg<128>::LDS >= 4 * 2 * WaveStage<64>::BYTES, "two staging areas a wave");
 
 __device__ __forceinline__ uint2 pack4h(const float (&v)[4])
 {
@@ -198,27 +206,25 @@ __device__ __forceinline__ int xcd_tile(int block, int total)
 // Symmetric product S = P P^T over k (P [m, k], k along memory: ACROSS = false; or P^T stored, [k, m]: ACROSS = true).
 // POLY: out = b P + c P P / kScale instead of P P^T / kScale (P symmetric, m = k).  The diagonals are kept apart: `diag_out` takes
 // the result's, out has zeros there; P = p + diag(diag_in) in the POLY form, so that P P = p p + (d_r + d_c) p_rc + d^2.
-// Tiles (i, j), j <= i: rows i * TILE on the lanes, columns j * TILE in the registers; a tile below the diagonal is stored
-// a second time with rows and columns exchanged, read back from the staging area by transposing LDS reads.
-template <int TILE, bool ACROSS, bool POLY>
-__global__ void __launch_bounds__(OrthoCfg<TILE>::THREADS, TILE == 256 ? 2 : 2)
-ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag_in, int m, int k, int tiles_1d, int total, uint16_t *__restrict__ out,
+// Tiles that hold anything on or below the diagonal, row block after row block; of these the 64 x 64 blocks on or below it are
+// stored, those below a second time with rows and columns exchanged, read back from the staging area by transposing LDS reads.
+template <class CF> __host__ __device__ constexpr int gram_tiles_of_row(int i) { return ((i + 1) * CF::BB - 1) / CF::BA + 1; }
+template <class CF, bool ACROSS, bool POLY>
+__global__ void __launch_bounds__(CF::THREADS, CF::WAVES_PER_SIMD)
+ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag_in, int m, int k, int per_matrix, int total, uint16_t *__restrict__ out,
                   float *__restrict__ diag_out)
 {
-    using CF = OrthoCfg<TILE>;
-    using OT = typename std::conditional<ACROSS, KsTile<TILE>, KcTile<TILE>>::type;
-    using KL = KLoop<OT, OT, 1, 1, TILE, TILE, CF::WA, CF::WB, 1, false, CF::STAGES, true, false, false, true>;
+    using KL = typename std::conditional<ACROSS, KLoop<KsTile<CF::BA>, KsTile<CF::BB>, 1, 1, CF::BA, CF::BB, CF::WA, CF::WB, 1, false, CF::STAGES, true, false, false, true>,
+                                         typename CF::template Loop<KcTile<CF::BA>>>::type;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int t = xcd_tile(blockIdx.x, total);
     if (t < 0) return;
-    const int per_matrix = tiles_1d * (tiles_1d + 1) / 2, mat = t / per_matrix, rem = t % per_matrix;
-    int i = (int)((sqrtf(8.0f * rem + 1.0f) - 1.0f) * 0.5f);
-    while (i * (i + 1) / 2 > rem) --i;
-    while ((i + 1) * (i + 2) / 2 <= rem) ++i;
-    const int j = rem - i * (i + 1) / 2;
+    const int mat = t / per_matrix;
+    int i = 0, j = t % per_matrix;
+    while (j >= gram_tiles_of_row<CF>(i)) j -= gram_tiles_of_row<CF>(i++);
     const uint16_t *src = p + (size_t)mat * m * k;
     uint16_t *dst = out + (size_t)mat * m * m;
-    const int ld = ACROSS ? m : k, row0 = i * TILE, col0 = j * TILE;
+    const int ld = ACROSS ? m : k, row0 = i * CF::BB, col0 = j * CF::BA;
     const Operand A[1][1] = {{{src, ld, col0, m - 1}}}, B[1][1] = {{{src, ld, row0, m - 1}}};
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     typename KL::Acc acc;
@@ -228,14 +234,18 @@ ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag
     using ST = WaveStage<64>;
     char *buf = lds + wave * 2 * ST::BYTES;
     const int wrow0 = row0 + (wave % CF::WB) * 64;
-    constexpr int COLS = TILE / CF::WA;
 #pragma unroll
-    for (int half = 0; half < COLS / 64; ++half) {
-        const int wcol0 = col0 + (wave / CF::WB) * COLS + half * 64;
-        if (wrow0 >= m || wcol0 >= m) break;                  // uniform in the wave; padding is in whole runs of 64
+    for (int half = 0; half < CF::COLS / 64; ++half) {
+        const int wcol0 = col0 + (wave / CF::WB) * CF::COLS + half * 64;
+        if (wrow0 >= m || wcol0 > wrow0) break;               // uniform in the wave; padding is in whole runs of 64
         const float *din = diag_in + (size_t)mat * m;
-        float d_r[2] = {0.0f, 0.0f};
+        float d_r[2] = {0.0f, 0.0f}, d_c[2][4][4];
         if (POLY) {
+#pragma unroll
+            for (int ta = 0; ta < 2; ++ta)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<float4 *>(d_c[ta][q]) = *reinterpret_cast<const float4 *>(din + wcol0 + ta * 32 + q * 8 + (lane >> 5) * 4);
             ST::fill(buf, src, m, wrow0, m, wcol0, m, lane);
             d_r[0] = din[wrow0 + (lane & 31)];
             d_r[1] = din[wrow0 + 32 + (lane & 31)];
@@ -248,17 +258,14 @@ ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int r = tb * 32 + (lane & 31), c = ta * 32 + q * 8 + (lane >> 5) * 4;
-                    float v[4], old[4], d_c[4];
-                    if (POLY) {
-                        unpack4h(ST::get(buf, r, c), old);
-                        *reinterpret_cast<float4 *>(d_c) = *reinterpret_cast<const float4 *>(din + wcol0 + c);
-                    }
+                    float v[4], old[4];
+                    if (POLY) unpack4h(ST::get(buf, r, c), old);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float s = acc[0][half * 2 + ta][tb][q * 4 + e];
-                        v[e] = POLY ? kNsB * old[e] + (kNsC / kScale) * (s + (d_r[tb] + d_c[e]) * old[e]) : s * (1.0f / kScale);
-                        if (i == j && wrow0 + r == wcol0 + c + e) {
-                            diag_out[(size_t)mat * m + wrow0 + r] = POLY ? kNsB * d_c[e] + (kNsC / kScale) * (s + d_c[e] * d_c[e]) : v[e];
+                        v[e] = POLY ? kNsB * old[e] + (kNsC / kScale) * (s + (d_r[tb] + d_c[ta][q][e]) * old[e]) : s * (1.0f / kScale);
+                        if (wrow0 == wcol0 && r == c + e) {
+                            diag_out[(size_t)mat * m + wrow0 + r] = POLY ? kNsB * d_r[tb] + (kNsC / kScale) * (s + d_r[tb] * d_r[tb]) : v[e];
                             v[e] = 0.0f;
                         }
                     }
@@ -266,9 +273,10 @@ ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag
                 }
         wave_lds_fence();
         ST::flush(buf, dst, m, wrow0, m, wcol0, m, lane);
-        if (i != j) {
+        if (wrow0 != wcol0) {
+            char *turned = buf + ST::BYTES;
 #pragma unroll
-            for (int r0 = 0; r0 < 64; r0 += 32)               // rows of the exchanged tile: columns r0 .. r0 + 31 of the staged one
+            for (int r0 = 0; r0 < 64; r0 += 32)               // rows of the exchanged block: columns r0 .. r0 + 31 of the staged one
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk) {
                     const int bq = lane >> 4, iq = lane & 15;
@@ -276,28 +284,29 @@ ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag
                     const s16x4_t l = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(buf + ST::acc_addr(r, c)));
                     const s16x4_t h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(buf + ST::acc_addr(r + 4, c)));
                     const s16x8_t v = __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
-                    *reinterpret_cast<s16x8_t *>(dst + (size_t)(wcol0 + r0 + (lane & 31)) * m + wrow0 + kk * 16 + (lane >> 5) * 8) = v;
+                    *reinterpret_cast<s16x8_t *>(turned + ST::acc_addr(r0 + (lane & 31), kk * 16 + (lane >> 5) * 8)) = v;
                 }
+            wave_lds_fence();
+            ST::flush(turned, dst, m, wcol0, m, wrow0, m, lane);
         }
         wave_lds_fence();
     }
 }
 
-// X' = (a + d) hi + (a + w d) lo + B hi, d the diagonal kept apart (wide: X [m, n], rows of B on the lanes, X's columns across memory in the registers or, tall: X [n, m] with B from the right, rows of
-// X on the lanes, B's columns, which are its rows, in the registers).  The last step writes the caller's matrix instead.
+// X' = (a + d) hi + (a + w d) lo + B hi, d the diagonal of B kept apart.  Wide: X [m, n], B from the left, its rows on the lanes, X's
+// columns across memory in the registers.  Tall: X [n, m], its rows on the lanes, B from the right, B's columns (which are its rows) in
+// the registers.  The last step writes the caller's matrix instead.
 struct OrthoLast {
     uint16_t *out;                               // bf16 [n, rows, cols], or nullptr: not the last step
     float scale;
     int vec;                                     // rows of 8-value pieces: 16-byte stores
 };
-template <int TILE, bool TALL>
-__global__ void __launch_bounds__(OrthoCfg<TILE>::THREADS, 2)
+template <class CF, bool TALL>
+__global__ void __launch_bounds__(CF::THREADS, CF::WAVES_PER_SIMD)
 ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t *__restrict__ bmat, const float *__restrict__ diag, float w, OrthoShape s,
                     int tiles_r, int tiles_c, int total, uint16_t *__restrict__ x_out, OrthoLast last)
 {
-    using CF = OrthoCfg<TILE>;
-    using AT = typename std::conditional<TALL, KcTile<TILE>, KsTile<TILE>>::type;
-    using KL = KLoop<AT, KcTile<TILE>, 1, 1, TILE, TILE, CF::WA, CF::WB, 1, false, CF::STAGES, true, false, false, true>;
+    using KL = typename CF::template Loop<typename std::conditional<TALL, KcTile<CF::BA>, KsTile<CF::BA>>::type>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int t = xcd_tile(blockIdx.x, total);
     if (t < 0) return;
@@ -306,7 +315,7 @@ ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t
     const int i = TALL ? rem / tiles_c : rem % tiles_r, j = TALL ? rem % tiles_c : rem / tiles_r;
     const int m = TALL ? s.cp : s.rp;
     const uint16_t *X = x + (size_t)mat * s.rp * s.cp, *Bm = bmat + (size_t)mat * m * m;
-    const int row0 = i * TILE, col0 = j * TILE;
+    const int row0 = i * CF::BB, col0 = j * CF::BA;
     const Operand A[1][1] = {{TALL ? Operand{Bm, m, col0, m - 1} : Operand{X, s.cp, col0, s.cp - 1}}};
     const Operand B[1][1] = {{TALL ? Operand{X, s.cp, row0, s.rp - 1} : Operand{Bm, m, row0, m - 1}}};
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -318,10 +327,9 @@ ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t
     char *buf_h = lds + wave * 2 * ST::BYTES, *buf_l = buf_h + ST::BYTES;
     uint16_t *L = lo + (size_t)mat * s.rp * s.cp, *Xo = x_out + (size_t)mat * s.rp * s.cp;
     const int wrow0 = row0 + (wave % CF::WB) * 64;
-    constexpr int COLS = TILE / CF::WA;
 #pragma unroll
-    for (int half = 0; half < COLS / 64; ++half) {
-        const int wcol0 = col0 + (wave / CF::WB) * COLS + half * 64;
+    for (int half = 0; half < CF::COLS / 64; ++half) {
+        const int wcol0 = col0 + (wave / CF::WB) * CF::COLS + half * 64;
         if (wrow0 >= s.rp || wcol0 >= s.cp) break;
         ST::fill2(buf_h, buf_l, X, L, s.cp, wrow0, s.rp, wcol0, s.cp, lane);
         const float *d = diag + (size_t)mat * m;
@@ -375,40 +383,81 @@ ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t
     }
 }
 
-static int ortho_lds_limits()
+template <class... Fs> int raise_lds_limits(int bytes, Fs... kernels)
 {
-    static std::once_flag once;
-    static int status = RELIBRA_OK;
-    std::call_once(once, [] {
-        const void *wide[] = {(const void *)ortho_gram_kernel<256, false, false>, (const void *)ortho_gram_kernel<256, true, false>,
-                              (const void *)ortho_gram_kernel<256, false, true>, (const void *)ortho_update_kernel<256, false>,
-                              (const void *)ortho_update_kernel<256, true>};
-        for (const void *f : wide)
-            if (hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, OrthoCfg<256>::LDS) != hipSuccess) status = RELIBRA_EHIP;
-    });
-    return status;
+    for (const void *f : {(const void *)kernels...})
+        if (hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return RELIBRA_EHIP;
+    return RELIBRA_OK;
 }
 
 inline unsigned xcd_grid(long long tiles) { return (unsigned)((tiles + 7) / 8 * 8); }
 
-template <int TILE>
+template <class CF> int gram_tiles(int n, int m)
+{
+    int per_matrix = 0;
+    for (int i = 0; i * CF::BB < m; ++i) per_matrix += gram_tiles_of_row<CF>(i);
+    return n * per_matrix;
+}
+template <class CF, bool ACROSS, bool POLY>
+int launch_gram(const uint16_t *p, const float *diag_in, int n, int m, int k, uint16_t *out, float *diag_out, hipStream_t stream)
+{
+    static const int limits = raise_lds_limits(CF::LDS, ortho_gram_kernel<CF, ACROSS, POLY>);
+    if (limits != RELIBRA_OK) return limits;
+    const int per_matrix = gram_tiles<CF>(1, m);
+    RELIBRA_LAUNCH(POLY ? RELIBRA_K_ORTHO_POLY : RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<CF, ACROSS, POLY>
+        <<<xcd_grid((long long)n * per_matrix), CF::THREADS, CF::LDS, stream>>>(p, diag_in, m, k, per_matrix, n * per_matrix, out, diag_out)));
+    return RELIBRA_OK;
+}
+template <class CF, bool TALL>
+int launch_update(const OrthoShape &s, const OrthoWs &w, const uint16_t *x, uint16_t *x_out, float weight, const OrthoLast &last, hipStream_t stream)
+{
+    static const int limits = raise_lds_limits(CF::LDS, ortho_update_kernel<CF, TALL>);
+    if (limits != RELIBRA_OK) return limits;
+    const int tr = (s.rp + CF::BB - 1) / CF::BB, tc = (s.cp + CF::BA - 1) / CF::BA, total = s.n * tr * tc;
+    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_UPDATE, stream, (ortho_update_kernel<CF, TALL><<<xcd_grid(total), CF::THREADS, CF::LDS, stream>>>(
+        x, w.lo, w.b, w.db, weight, s, tr, tc, total, x_out, last)));
+    return RELIBRA_OK;
+}
+
+typedef OrthoCfg<256, 256, 4, 1> OrthoWide;
+typedef OrthoCfg<256, 256, 3, 1, true> OrthoWideDeep;
+typedef OrthoCfg<128, 128, 4, 2> OrthoNarrow;
+typedef OrthoCfg<128, 64, 4, 2> OrthoFlat;
+
+template <class CF> int update_tiles(const OrthoShape &s) { return s.n * ((s.rp + CF::BB - 1) / CF::BB) * ((s.cp + CF::BA - 1) / CF::BA); }
+
+// Wide tiles where they occupy nearly half of the compute units or more, smaller ones where wide tiles would leave the rest idle.
+// us a launch, 256 x 256 / 128 x 128 (wide tiles): A of 4096 x 4096 (136) 88 / 114, of 16 of 768 x 2048 (96) 48 / 40, of 64 of 256 x 512 (64)
+// 17.9 / 11.8, of 2048 x 2048 (36) 42 / 23, of 2 of 1000 x 3000 (20) 54 / 27; X' of 16 of 768 x 2048 (384) 74 / 76, of 64 of 256 x 512 (128) 22.3 /
+// 22.2, of 2048 x 2048 (64) 47 / 33.  The row operand twice as deep gains the wide X' 2 to 5 % (full lines of B) and costs A 3 %.  Half as
+// many rows again (128 x 64) where X' has few tiles: 5 of 1001 x 333 (120 of 128 x 128) 15.3 -> 13.2, 8 of 512 x 512 (128) 13.9 -> 12.7, 2048 x 2048
+// (256) 32.9 -> 34.4.
+constexpr int kEnoughWideTiles = 112, kFewNarrowTiles = 192;
+
 int ortho_steps(const OrthoShape &s, const OrthoWs &w, int steps, float scale, uint16_t *out, hipStream_t stream)
 {
-    using CF = OrthoCfg<TILE>;
-    const int m = s.tall ? s.cp : s.rp, n = s.tall ? s.rp : s.cp;
-    const int t1 = (m + TILE - 1) / TILE, gram = s.n * (t1 * (t1 + 1) / 2);
-    const int tr = (s.rp + TILE - 1) / TILE, tc = (s.cp + TILE - 1) / TILE, upd = s.n * tr * tc;
+    const int m = s.tall ? s.cp : s.rp, k = s.tall ? s.rp : s.cp;
+    const bool wide_gram = gram_tiles<OrthoWide>(s.n, m) >= kEnoughWideTiles, wide_update = update_tiles<OrthoWideDeep>(s) >= kEnoughWideTiles;
+    const bool flat_update = update_tiles<OrthoNarrow>(s) <= kFewNarrowTiles;
+    auto gram = [&](auto across, auto poly, const uint16_t *p, const float *d, int depth, uint16_t *out_, float *d_out) {
+        return wide_gram ? launch_gram<OrthoWide, decltype(across)::value, decltype(poly)::value>(p, d, s.n, m, depth, out_, d_out, stream)
+                         : launch_gram<OrthoNarrow, decltype(across)::value, decltype(poly)::value>(p, d, s.n, m, depth, out_, d_out, stream);
+    };
     for (int i = 0; i < steps; ++i) {
         const uint16_t *x = w.x[i & 1];
+        uint16_t *x_out = w.x[(i + 1) & 1];
         const float weight = i + 3 >= steps ? 1.0f : 0.0f;
-        if (s.tall) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<TILE, true, false><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(x, nullptr, m, n, t1, gram, w.a, w.da)));
-        else RELIBRA_LAUNCH(RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<TILE, false, false><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(x, nullptr, m, n, t1, gram, w.a, w.da)));
-        RELIBRA_LAUNCH(RELIBRA_K_ORTHO_POLY, stream, (ortho_gram_kernel<TILE, false, true><<<xcd_grid(gram), CF::THREADS, CF::LDS, stream>>>(w.a, w.da, m, m, t1, gram, w.b, w.db)));
         const OrthoLast last{i + 1 == steps ? out : nullptr, scale, s.cols % 8 == 0 && aligned16(out)};
-        if (s.tall) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_UPDATE, stream, (ortho_update_kernel<TILE, true><<<xcd_grid(upd), CF::THREADS, CF::LDS, stream>>>(
-            x, w.lo, w.b, w.db, weight, s, tr, tc, upd, w.x[(i + 1) & 1], last)));
-        else RELIBRA_LAUNCH(RELIBRA_K_ORTHO_UPDATE, stream, (ortho_update_kernel<TILE, false><<<xcd_grid(upd), CF::THREADS, CF::LDS, stream>>>(
-            x, w.lo, w.b, w.db, weight, s, tr, tc, upd, w.x[(i + 1) & 1], last)));
+        auto update = [&](auto tall) {
+            constexpr bool T = decltype(tall)::value;
+            return wide_update ? launch_update<OrthoWideDeep, T>(s, w, x, x_out, weight, last, stream)
+                   : flat_update ? launch_update<OrthoFlat, T>(s, w, x, x_out, weight, last, stream)
+                                 : launch_update<OrthoNarrow, T>(s, w, x, x_out, weight, last, stream);
+        };
+        int rc = s.tall ? gram(std::true_type{}, std::false_type{}, x, nullptr, k, w.a, w.da) : gram(std::false_type{}, std::false_type{}, x, nullptr, k, w.a, w.da);
+        if (rc == RELIBRA_OK) rc = gram(std::false_type{}, std::true_type{}, w.a, w.da, m, w.b, w.db);
+        if (rc == RELIBRA_OK) rc = s.tall ? update(std::true_type{}) : update(std::false_type{});
+        if (rc != RELIBRA_OK) return rc;
     }
     return RELIBRA_OK;
 }
@@ -417,12 +466,13 @@ template <class GT>
 void ortho_load(const OrthoShape &s, const OrthoWs &w, const GT *g, const float *m, float mu, int mode, float *m_out, hipStream_t stream)
 {
     const size_t per_matrix = (size_t)s.rows * s.cols;
+    const int parts = norm_parts(s);
     const bool aligned = aligned16(g) && (mode == U_GRAD || (aligned16(m) && aligned16(m_out)));
-    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_NORM, stream, ortho_momentum_kernel<GT><<<dim3(kNormParts, s.n), 256, 0, stream>>>(
+    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_NORM, stream, ortho_momentum_kernel<GT><<<dim3(parts, s.n), 256, 0, stream>>>(
         g, m, mu, mode, per_matrix, aligned && per_matrix % 4 == 0, m_out, w.parts));
     const size_t pieces = (size_t)s.rp * s.cp / 8;
     RELIBRA_LAUNCH(RELIBRA_K_ORTHO_LOAD, stream, ortho_load_kernel<GT><<<dim3((unsigned)std::min<size_t>((pieces + 255) / 256, 256), s.n), 256, 0, stream>>>(
-        g, m_out, mu, mode, s, aligned && s.cols % 8 == 0, w.parts, w.x[0], w.lo));
+        g, m_out, mu, mode, s, aligned && s.cols % 8 == 0, w.parts, parts, w.x[0], w.lo));
 }
 
 }  // namespace relibra
@@ -443,7 +493,6 @@ extern "C" int relibra_orthogonalize(const void *grad, const float *momentum, in
     if ((long long)n * ((s.rp + t - 1) / t) * ((s.cp + t - 1) / t) > 0x3fffffff) return RELIBRA_EUNSUPPORTED;
     if (!workspace || workspace_bytes < ortho_ws_bytes(n, rows, cols)) return RELIBRA_EWORKSPACE;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
-    if (const int rc = ortho_lds_limits(); rc != RELIBRA_OK) return rc;
     OrthoWs w;
     char *p = (char *)workspace;
     w.x[0] = (uint16_t *)p;
@@ -457,8 +506,7 @@ extern "C" int relibra_orthogonalize(const void *grad, const float *momentum, in
     const int mode = !momentum ? U_GRAD : flags & RELIBRA_ORTHO_NESTEROV ? U_NESTEROV : U_MOMENTUM;
     if (flags & RELIBRA_ORTHO_BF16) ortho_load(s, w, (const bf16_t *)grad, momentum, mu, mode, momentum_out, stream);
     else ortho_load(s, w, (const float *)grad, momentum, mu, mode, momentum_out, stream);
-    const int m = s.tall ? s.cp : s.rp;
-    const int rc = m >= 256 ? ortho_steps<256>(s, w, steps, scale, (uint16_t *)out, stream) : ortho_steps<128>(s, w, steps, scale, (uint16_t *)out, stream);
+    const int rc = ortho_steps(s, w, steps, scale, (uint16_t *)out, stream);
     if (rc != RELIBRA_OK) return rc;
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
