@@ -45,6 +45,17 @@ KERNELS = ("hist", "perm_count", "perm_scan", "perm_rank", "gather", "combine_fw
            "router_fwd", "router_finish", "router_bwd", "norm_fwd", "norm_bwd", "norm_reduce",
            "ortho_norm", "ortho_load", "ortho_gram", "ortho_poly", "ortho_update")
 
+# Argument types of the calls that are short on the GPU: ctypes then takes plain integers and floats, which costs the host half
+# of what building an object for every argument does.
+_P, _I, _F, _Z = C.c_void_p, C.c_int, C.c_float, C.c_size_t
+_ARGTYPES = {
+    "relibra_router_fwd": [_P] * 3 + [_I] * 5 + [_F] * 2 + [_P] * 6 + [_Z] + [_P] * 2,
+    "relibra_router_bwd": [_P] * 7 + [_I] * 5 + [_F] * 2 + [_P] * 3,
+    "relibra_block_norm_fwd": [_P] * 5 + [_I] * 2 + [_F] * 2 + [_I] + [_P] * 3,
+    "relibra_block_norm_bwd": [_P] * 7 + [_I] * 2 + [_F] * 2 + [_I] + [_P] * 6 + [_Z, _P],
+    "relibra_orthogonalize": [_P] * 2 + [_I] * 3 + [_F] * 2 + [_I] * 2 + [_P] * 3 + [_Z, _P],
+}
+
 _lib = None
 
 
@@ -66,6 +77,8 @@ def lib():
         L.relibra_status_string.restype = C.c_char_p
         for name in EXPORTS:
             getattr(L, name)
+        for name, types in _ARGTYPES.items():
+            getattr(L, name).argtypes = types
         _lib = L
     return _lib
 
@@ -99,6 +112,22 @@ def _dp(t, dtype=None):
     if dtype is not None:
         assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
     return C.c_void_p(t.data_ptr())
+
+
+def _ptr(t, dtype=None):
+    """_dp as a plain integer, for calls with declared argument types."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous"
+    assert dtype is None or t.dtype is dtype, f"expected {dtype}, got {t.dtype}"
+    return t.data_ptr()
+
+
+def _raw():
+    """The current stream as a plain integer."""
+    if _raw_stream is None or _device is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_device())
 
 
 def _hp(a):
@@ -695,7 +724,7 @@ def _out(t, shape, dtype, like):
     """An output the caller gave, checked, or a new one."""
     if t is None:
         return torch.empty(shape, dtype=dtype, device=like.device)
-    assert tuple(t.shape) == tuple(shape) and t.dtype == dtype, f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
+    assert t.shape == shape and t.dtype is dtype, f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
     return t
 
 
@@ -713,9 +742,9 @@ def relibra_router_fwd(logits, ids, sigmoid=False, normalize=True, scale=1.0, ba
         workspace = router_workspace(n_mb, T, k, E, logits.device)
     if err_flag is None:
         err_flag = new_err_flag(logits.device)
-    rc = lib().relibra_router_fwd(_dp(logits), _dp(ids, torch.int32), _dp(valid), n_mb, T, k, E, flags, C.c_float(scale), C.c_float(balance_coef),
-                                  _dp(gates), _dp(counts), _dp(n_valid), _dp(prob_mean), _dp(loss),
-                                  _dp(workspace), C.c_size_t(workspace.numel()), _dp(err_flag, torch.int32), _stream())
+    rc = lib().relibra_router_fwd(_ptr(logits), _ptr(ids, torch.int32), _ptr(valid), n_mb, T, k, E, flags, scale, balance_coef,
+                                  _ptr(gates), _ptr(counts), _ptr(n_valid), _ptr(prob_mean), _ptr(loss),
+                                  _ptr(workspace), workspace.numel(), _ptr(err_flag, torch.int32), _raw())
     _check("relibra_router_fwd", rc)
     return gates, counts, n_valid, prob_mean, loss
 
@@ -730,9 +759,9 @@ def relibra_router_bwd(logits, ids, dgates, counts=None, n_valid=None, dloss=Non
     dlogits = _out(dlogits, logits.shape, logits.dtype, logits)
     if err_flag is None:
         err_flag = new_err_flag(logits.device)
-    rc = lib().relibra_router_bwd(_dp(logits), _dp(ids, torch.int32), _dp(valid), _dp(dgates, torch.float32), _dp(counts, torch.int32),
-                                  _dp(n_valid, torch.int32), _dp(dloss, torch.float32), n_mb, T, k, E, flags, C.c_float(scale), C.c_float(balance_coef),
-                                  _dp(dlogits), _dp(err_flag, torch.int32), _stream())
+    rc = lib().relibra_router_bwd(_ptr(logits), _ptr(ids, torch.int32), _ptr(valid), _ptr(dgates, torch.float32), _ptr(counts, torch.int32),
+                                  _ptr(n_valid, torch.int32), _ptr(dloss, torch.float32), n_mb, T, k, E, flags, scale, balance_coef,
+                                  _ptr(dlogits), _ptr(err_flag, torch.int32), _raw())
     _check("relibra_router_bwd", rc)
     return dlogits
 
@@ -757,8 +786,8 @@ def relibra_block_norm_fwd(x, y=None, w_post=None, w_pre=None, gate=None, res_sc
     T, h, flags, gate_type = _norm_args(x, y, w_post, w_pre, gate)
     x_out = x if y is None else _out(x_out, (T, h), x.dtype, x)
     n = None if w_pre is None else _out(n, (T, h), torch.bfloat16, x)
-    rc = lib().relibra_block_norm_fwd(_dp(x), _dp(y, torch.bfloat16), _dp(w_post, torch.bfloat16), _dp(w_pre, torch.bfloat16), _dp(gate, gate_type),
-                                      T, h, C.c_float(res_scale), C.c_float(eps), flags, _dp(None if y is None else x_out), _dp(n), _stream())
+    rc = lib().relibra_block_norm_fwd(_ptr(x), _ptr(y, torch.bfloat16), _ptr(w_post, torch.bfloat16), _ptr(w_pre, torch.bfloat16), _ptr(gate, gate_type),
+                                      T, h, res_scale, eps, flags, _ptr(None if y is None else x_out), _ptr(n), _raw())
     _check("relibra_block_norm_fwd", rc)
     return x_out, n
 
@@ -782,10 +811,10 @@ def relibra_block_norm_bwd(x_out, dx_out, dn, y=None, w_post=None, w_pre=None, g
     dw_pre = None if w_pre is None else _out(dw_pre, (h,), torch.float32, x_out)
     if workspace is None:
         workspace = block_norm_workspace(T, h, x_out.device)
-    rc = lib().relibra_block_norm_bwd(_dp(x_out), _dp(dx_out), _dp(dn, torch.bfloat16), _dp(y, torch.bfloat16), _dp(w_post, torch.bfloat16),
-                                      _dp(w_pre, torch.bfloat16), _dp(gate, gate_type), T, h, C.c_float(res_scale), C.c_float(eps),
-                                      flags | (NORM_ACCUMULATE if accumulate else 0), _dp(dx), _dp(dy), _dp(dgate), _dp(dw_post), _dp(dw_pre),
-                                      _dp(workspace), C.c_size_t(workspace.numel()), _stream())
+    rc = lib().relibra_block_norm_bwd(_ptr(x_out), _ptr(dx_out), _ptr(dn, torch.bfloat16), _ptr(y, torch.bfloat16), _ptr(w_post, torch.bfloat16),
+                                      _ptr(w_pre, torch.bfloat16), _ptr(gate, gate_type), T, h, res_scale, eps,
+                                      flags | (NORM_ACCUMULATE if accumulate else 0), _ptr(dx), _ptr(dy), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre),
+                                      _ptr(workspace), workspace.numel(), _raw())
     _check("relibra_block_norm_bwd", rc)
     return dx, dy, dgate, dw_post, dw_pre
 
@@ -807,8 +836,8 @@ def relibra_orthogonalize(grad, momentum=None, mu=0.95, nesterov=True, scale=1.0
     if workspace is None:
         workspace = orthogonalize_workspace(n, rows, cols, grad.device)
     flags = (ORTHO_BF16 if grad.dtype == torch.bfloat16 else 0) | (ORTHO_NESTEROV if nesterov and momentum is not None else 0)
-    rc = lib().relibra_orthogonalize(_dp(grad), _dp(momentum, torch.float32), n, rows, cols, C.c_float(mu), C.c_float(scale), int(steps), flags,
-                                     _dp(momentum_out), _dp(out), _dp(workspace), C.c_size_t(workspace.numel()), _stream())
+    rc = lib().relibra_orthogonalize(_ptr(grad), _ptr(momentum, torch.float32), n, rows, cols, mu, scale, int(steps), flags,
+                                     _ptr(momentum_out), _ptr(out), _ptr(workspace), workspace.numel(), _raw())
     _check("relibra_orthogonalize", rc)
     return out, momentum_out
 

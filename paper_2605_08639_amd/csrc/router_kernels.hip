@@ -8,70 +8,100 @@
 // r = 1 / (1 + exp(-|z|)), and m the largest v of the set that is summed over: the row for p, the selected alone for normalised gates
 // (their ratio survives however far below the row's maximum they lie).  A set of -infinities only has the sum 0 and yields zeros.
 //
-// Layout: LT lanes share a token (the power of two with 8 LT >= E, at most 64), each holds 8 consecutive experts of every CH-th
+// Layout: LT lanes share a token (2, 8, 16, 32 or 64: the least with 8 LT >= E), each holds 8 consecutive experts of every CH-th
 // run, so a wave has 64 / LT tokens in flight, rows are read in 16-byte pieces, and a lane's experts stay its own
 // over all tokens: sum_t p_te accumulates in registers, and only the finished sums of a block are stored.
 #include "wave_ops.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace relibra {
 
 constexpr int kRouterMaxExperts = 4096;
-constexpr int kRouterMaxSel = 8;                 // selections a lane handles: k <= 64 and k <= E <= 8 LT CH
 
 struct RouterShape {
     int T, k, E, flags;
     float scale;
 };
 
-// Log score of z in the form exp(v) * r.
+// exp(x) for x <= 0, -infinity and NaN: 2^t with t = x log2(e) rounded once, and what that rounding left out put back to first
+// order.  (For x = -infinity that rest is a NaN, which the median takes out; 2^t is 0 then.)  Six instructions instead of
+// expf's fourteen; off by 2 units in the last place and |x| 2^-26.
+__device__ __forceinline__ float exp_down(float x)
+{
+    const float t = x * 1.44269504f;
+    const float rest = __builtin_amdgcn_fmed3f(fmaf(x, 1.44269504f, -t), -1.0f, 1.0f);
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, rest * 0.693147181f, e);
+}
+// Largest of three, NaN left out (fmaxf spends an instruction on each operand to quiet signalling ones).
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// The score of z in the form exp(v) * r, and sigmoid(-z).
 struct Score {
-    float v, r;
+    float v, r, down;
 };
 template <bool SIGMOID> __device__ __forceinline__ Score score_of(float z)
 {
-    if constexpr (SIGMOID) return Score{z < 0.0f ? z : z >= 0.0f ? 0.0f : z, 1.0f / (1.0f + expf(-fabsf(z)))};      // NaN stays
-    else return Score{z, 1.0f};
+    if constexpr (SIGMOID) {
+        const float e = exp_down(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + e);
+        return Score{z < 0.0f ? z : z >= 0.0f ? 0.0f : z, r, z < 0.0f ? r : e * r};      // (v: NaN stays)
+    }
+    return Score{z, 1.0f, 1.0f};
 }
+template <bool SIGMOID> __device__ __forceinline__ float top_of(float z) { return SIGMOID ? fminf(z, 0.0f) : z; }
 
 // exp(v - m) with m finite or the -infinity of an empty set (then v = -infinity too, and the result is 0)
-__device__ __forceinline__ float exp_below(float v, float m) { return expf(v - (m == -INFINITY ? 0.0f : m)); }
+__device__ __forceinline__ float exp_below(float v, float m) { return exp_down(v - (m == -INFINITY ? 0.0f : m)); }
 
-// One token's row in registers: lane `sub` of LT holds experts (c * LT + sub) * 8 + j; beyond E: -infinity.
+// One token's row as it comes from memory: lane `sub` of LT holds experts (c * LT + sub) * 8 + j; beyond E: -infinity.  Rows
+// start anywhere (E need not be a multiple of 8): whole pieces are 16-byte loads all the same, a row's last piece may be shorter.
+template <class ZT> __device__ __forceinline__ Raw8<ZT> raw_of(const float (&v)[8])
+{
+    if constexpr (sizeof(ZT) == 2) return Raw8<ZT>{make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]))};
+    else return Raw8<ZT>{make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7])};
+}
 template <class ZT, int LT, int CH>
-__device__ __forceinline__ void load_row(const ZT *row, int E, int sub, bool vec, float (&z)[CH][8])
+__device__ __forceinline__ void fetch_row(const ZT *row, int E, int sub, Raw8<ZT> (&raw)[CH])
 {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int e0 = (c * LT + sub) * 8;
-        if (vec) {                                           // E % 8 == 0: a piece is whole or absent
-            if (e0 < E) load8(row + e0, z[c]);
-            else
+        if (E % 8 == 0) {                                    // the same for the whole launch: no lane has a piece of its own kind
+            raw[c] = fetch8_any(row + min(e0, E - 8));
+            if (e0 >= E) raw[c] = raw_of<ZT>({-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY});
+        } else if (e0 + 8 <= E) raw[c] = fetch8_any(row + e0);
+        else {
+            float v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[c][j] = -INFINITY;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[c][j] = e0 + j < E ? to_f32(row[e0 + j]) : -INFINITY;
+            for (int j = 0; j < 8; ++j) v[j] = e0 + j < E ? to_f32(row[e0 + j]) : -INFINITY;
+            raw[c] = raw_of<ZT>(v);
         }
     }
 }
 
-// The token's selections, dealt to its lanes: selection i * LT + sub.  Raw logits through the wave's LDS row.
-struct Selection {
-    int id[kRouterMaxSel];                                   // -1: none, or an id outside [0, E)
-    float z[kRouterMaxSel];
+// The token's selections, dealt to its lanes: selection i * LT + sub, at most NS each: one where the lanes are as many as the
+// selections, which is most routers; else up to 8 (k <= E <= 8 LT).  Raw logits through the wave's LDS row.
+template <int NS> struct Selection {
+    int id[NS];                                              // -1: none, or an id outside [0, E)
+    float z[NS];
 };
 
 // p = w / sum over the row; the row's largest v and the sum's reciprocal (0 for a row of -infinities) come back too.
 template <bool SIGMOID, int LT, int CH>
-__device__ __forceinline__ void row_probabilities(const float (&z)[CH][8], float (&p)[CH][8], float &top, float &inv)
+__device__ __forceinline__ void row_probabilities(const float (&z)[CH][8], float (&p)[CH][8], float &top, float &inv, float (&down)[CH][8])
 {
     top = -INFINITY;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, SIGMOID ? fminf(z[c][j], 0.0f) : z[c][j]);
+        for (int j = 0; j < 8; j += 2) top = max3(top, top_of<SIGMOID>(z[c][j]), top_of<SIGMOID>(z[c][j + 1]));
     top = group_max<LT>(top);
     float total = 0.0f;
 #pragma unroll
@@ -80,27 +110,33 @@ __device__ __forceinline__ void row_probabilities(const float (&z)[CH][8], float
         for (int j = 0; j < 8; ++j) {
             const Score s = score_of<SIGMOID>(z[c][j]);
             p[c][j] = exp_below(s.v, top) * s.r;
+            down[c][j] = s.down;
             total += p[c][j];
         }
     total = group_sum<LT>(total);
-    inv = total == 0.0f ? 0.0f : 1.0f / total;
+    inv = total == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(total);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[c][j] *= inv;
 }
 
-// Puts the row into the wave's LDS and picks the lane's selections from it.  `bad`: an id outside [0, E) in a live token.
-template <int LT, int CH>
-__device__ __forceinline__ void pick_selections(const float (&z)[CH][8], float *row, const int32_t *ids, int k, int E, int sub, int n_sel, bool live,
-                                                Selection &sel, bool &bad)
+template <int LT, int NS> __device__ __forceinline__ void fetch_ids(const int32_t *ids, int k, int sub, int n_sel, int (&id)[NS])
 {
 #pragma unroll
-    for (int i = 0; i < kRouterMaxSel; ++i) {
+    for (int i = 0; i < NS; ++i)
+        if (i < n_sel && i * LT + sub < k) id[i] = ids[i * LT + sub];
+}
+// Puts the row into the wave's LDS and picks the lane's selections from it.  `bad`: an id outside [0, E) in a live token.
+template <int LT, int CH, int NS>
+__device__ __forceinline__ void pick_selections(const float (&z)[CH][8], float *row, const int (&ids)[NS], int k, int E, int sub, int n_sel, bool live,
+                                                Selection<NS> &sel, bool &bad)
+{
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
         sel.id[i] = -1;
         if (i < n_sel && i * LT + sub < k) {
-            const int id = ids[i * LT + sub];
-            if ((unsigned)id < (unsigned)E) sel.id[i] = id;
+            if ((unsigned)ids[i] < (unsigned)E) sel.id[i] = ids[i];
             else bad |= live;
         }
     }
@@ -108,26 +144,26 @@ __device__ __forceinline__ void pick_selections(const float (&z)[CH][8], float *
     for (int c = 0; c < CH; ++c) store8(row + (c * LT + sub) * 8, z[c]);
     wave_lds_fence();
 #pragma unroll
-    for (int i = 0; i < kRouterMaxSel; ++i) sel.z[i] = i < n_sel && sel.id[i] >= 0 ? row[sel.id[i]] : -INFINITY;
-    wave_lds_fence();                                     // the row may be overwritten
+    for (int i = 0; i < NS; ++i) sel.z[i] = i < n_sel && sel.id[i] >= 0 ? row[sel.id[i]] : -INFINITY;
+    wave_lds_fence();                                        // the row may be overwritten
 }
 
 // The part of each selection of this lane: its share of the token's selected (normalised), or its score as it is.
-template <bool SIGMOID, int LT>
-__device__ __forceinline__ void selected_parts(const Selection &sel, int n_sel, bool normalize, float row_top, float row_inv,
-                                               float (&part)[kRouterMaxSel])
+template <bool SIGMOID, int LT, int NS>
+__device__ __forceinline__ void selected_parts(const Selection<NS> &sel, int n_sel, bool normalize, float row_top, float row_inv,
+                                               float (&part)[NS])
 {
     float top = SIGMOID ? 0.0f : row_top, inv = SIGMOID ? 1.0f : row_inv;
     if (normalize) {
         top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kRouterMaxSel; ++i)
-            if (i < n_sel && sel.id[i] >= 0) top = fmaxf(top, SIGMOID ? fminf(sel.z[i], 0.0f) : sel.z[i]);
+        for (int i = 0; i < NS; ++i)
+            if (i < n_sel && sel.id[i] >= 0) top = max3(top, top, top_of<SIGMOID>(sel.z[i]));
         top = group_max<LT>(top);
     }
     float total = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kRouterMaxSel; ++i) {
+    for (int i = 0; i < NS; ++i) {
         part[i] = 0.0f;
         if (i < n_sel && sel.id[i] >= 0) {
             const Score s = score_of<SIGMOID>(sel.z[i]);
@@ -137,10 +173,10 @@ __device__ __forceinline__ void selected_parts(const Selection &sel, int n_sel, 
     }
     if (normalize) {
         total = group_sum<LT>(total);
-        inv = total == 0.0f ? 0.0f : 1.0f / total;
+        inv = total == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(total);
     }
 #pragma unroll
-    for (int i = 0; i < kRouterMaxSel; ++i) part[i] *= inv;
+    for (int i = 0; i < NS; ++i) part[i] *= inv;
 }
 
 // What a block leaves for the micro-batch's sums: per expert sum of p and count, and its number of valid tokens.
@@ -153,6 +189,12 @@ struct RouterSums {
     int32_t *counts, *n_valid;
     float *prob_mean, *loss;
 };
+
+// coef E sum_e f_e P_e from dot = sum_e counts_e sum_t p_te
+__device__ __forceinline__ float balance_loss(double dot, float coef, int E, int k, double n)
+{
+    return n > 0.0 ? (float)((double)coef * E * dot / ((double)k * n * n)) : 0.0f;
+}
 
 __device__ __forceinline__ double block_sum(double v, double *red, int threads)
 {
@@ -168,13 +210,18 @@ __device__ __forceinline__ double block_sum(double v, double *red, int threads)
     return total;
 }
 
+// Whether the next round's loads go out a round ahead: not where the row alone fills the registers.
+template <int CH> constexpr bool router_ahead() { return CH <= 2; }
+
 template <int CH> constexpr int router_waves() { return CH == 8 ? 2 : 4; }
 
-// grid (blocks, n_mb); a block takes `per_block` tokens of its micro-batch.
-template <class ZT, bool SIGMOID, int LT, int CH>
+// grid (blocks, n_mb); a block takes `per_block` tokens of its micro-batch, with SOLO all of them: it finishes the sums itself.  The next round's row, ids and mask are requested before
+// the present round is worked on: a round is a chain of LDS round trips, and with the loads in front of it the chain took 3.5
+// us (524288 tokens, 128 experts, bf16).
+template <class ZT, bool SIGMOID, int LT, int CH, int NS, bool SOLO>
 __global__ void __launch_bounds__(router_waves<CH>() * 64)
 router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids, const uint8_t *__restrict__ valid, RouterShape sh, int per_block,
-                  int vec, float *__restrict__ gates, RouterPartials part_out, int32_t *err_flag)
+                  float *__restrict__ gates, RouterPartials part_out, RouterSums sums, float coef, int32_t *err_flag)
 {
     constexpr int NW = router_waves<CH>(), TPW = 64 / LT, ROW = LT * 8 * CH;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -184,6 +231,17 @@ router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
     const int mb = blockIdx.y, E = sh.E, k = sh.k;
     const int n_sel = (k + LT - 1) / LT;
     const bool normalize = sh.flags & RELIBRA_ROUTER_NORMALIZE;
+    const int t_end = min(sh.T, (int)(blockIdx.x + 1) * per_block);
+    Raw8<ZT> raw[CH];
+    int next_id[NS];
+    uint8_t next_valid = 1;
+    auto fetch = [&](int t0) __attribute__((always_inline)) {
+        const size_t tok = (size_t)mb * sh.T + min(t0 + wave * TPW + group, sh.T - 1);
+        fetch_row<ZT, LT, CH>(logits + tok * E, E, sub, raw);
+        fetch_ids<LT, NS>(ids + tok * k, k, sub, n_sel, next_id);
+        if (valid) next_valid = valid[tok];
+    };
+    if (router_ahead<CH>() && sh.T > 0) fetch(blockIdx.x * per_block);
     for (int i = tid; i <= E; i += NW * 64) bins[i] = 0;
     __syncthreads();
     float *row = stage + (wave * TPW + group) * ROW;
@@ -193,31 +251,39 @@ router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[c][j] = 0.0f;
     bool bad = false;
-    const int t_end = min(sh.T, (int)(blockIdx.x + 1) * per_block);
+    int n_live = 0;
     for (int t0 = blockIdx.x * per_block; t0 < t_end; t0 += NW * TPW) {
+        if (!router_ahead<CH>()) fetch(t0);
         const int t = t0 + wave * TPW + group;
         const size_t tok = (size_t)mb * sh.T + min(t, sh.T - 1);
-        const bool live = t < t_end && (!valid || valid[tok]);
-        float z[CH][8], p[CH][8], top, inv, part[kRouterMaxSel];
-        load_row<ZT, LT, CH>(logits + tok * E, E, sub, vec, z);
-        Selection sel;
-        pick_selections<LT, CH>(z, row, ids + tok * k, k, E, sub, n_sel, live, sel, bad);
-        row_probabilities<SIGMOID, LT, CH>(z, p, top, inv);
-        selected_parts<SIGMOID, LT>(sel, n_sel, normalize, top, inv, part);
+        const bool live = t < t_end && next_valid;
+        float z[CH][8], p[CH][8], top, inv, part[NS];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) unpack8(raw[c], z[c]);
+        int id[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) id[i] = next_id[i];
+        if (router_ahead<CH>() && t0 + NW * TPW < t_end) fetch(t0 + NW * TPW);
+        Selection<NS> sel;
+        pick_selections<LT, CH, NS>(z, row, id, k, E, sub, n_sel, live, sel, bad);
+        float down[CH][8];
+        row_probabilities<SIGMOID, LT, CH>(z, p, top, inv, down);
+        selected_parts<SIGMOID, LT, NS>(sel, n_sel, normalize, top, inv, part);
         if (live) {
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[c][j] += p[c][j];
-            if (sub == 0) atomicAdd(&bins[E], 1);
+            n_live += sub == 0;
         }
 #pragma unroll
-        for (int i = 0; i < kRouterMaxSel; ++i)
+        for (int i = 0; i < NS; ++i)
             if (i < n_sel && i * LT + sub < k) {
                 if (live && sel.id[i] >= 0) atomicAdd(&bins[sel.id[i]], 1);
                 if (t < t_end) gates[tok * k + i * LT + sub] = live ? sh.scale * part[i] : 0.0f;
             }
     }
+    if (n_live) atomicAdd(&bins[E], n_live);
     if (bad) atomicOr(err_flag, RELIBRA_ERR_ID_RANGE);
     __syncthreads();                                         // every wave is done with its rows
     // the wave's token groups, then the waves, in a fixed order
@@ -231,36 +297,53 @@ router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
     }
     __syncthreads();
     const size_t at = (size_t)mb * gridDim.x + blockIdx.x;
+    const int n = bins[E];
+    double dot = 0.0;
     for (int e = tid; e < E; e += NW * 64) {
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) s += stage[w * ROW + e];
-        part_out.prob[at * E + e] = s;
-        part_out.count[at * E + e] = bins[e];
+        if (SOLO) {
+            sums.prob_mean[at * E + e] = n > 0 ? s * (float)(1.0 / n) : 0.0f;
+            sums.counts[at * E + e] = bins[e];
+            dot += (double)s * bins[e];
+        } else {
+            part_out.prob[at * E + e] = s;
+            part_out.count[at * E + e] = bins[e];
+        }
     }
-    if (tid == 0) part_out.tokens[at] = bins[E];
+    if (SOLO) {
+        __syncthreads();                                     // the sums have been read
+        dot = block_sum(dot, reinterpret_cast<double *>(smem), NW * 64);
+        if (tid == 0) {
+            sums.n_valid[mb] = n;
+            sums.loss[mb] = balance_loss(dot, coef, E, k, n);
+        }
+    } else if (tid == 0) part_out.tokens[at] = n;
 }
 
 // One block per micro-batch adds up the blocks' sums in ascending order and finishes the loss.
-__global__ void __launch_bounds__(256)
+constexpr int kFinishThreads = 1024;
+__global__ void __launch_bounds__(kFinishThreads)
 router_finish_kernel(RouterPartials part, int blocks, int k, int E, int lanes_e, float coef, RouterSums out)
 {
-    __shared__ double red[256];
-    __shared__ float s_prob[256];
-    __shared__ int32_t s_count[256];
+    __shared__ double red[kFinishThreads];
+    __shared__ float s_prob[kFinishThreads];
+    __shared__ int32_t s_count[kFinishThreads];
     const int tid = threadIdx.x, mb = blockIdx.x;
     const size_t base = (size_t)mb * blocks;
     double tokens = 0.0;
-    for (int b = tid; b < blocks; b += 256) tokens += part.tokens[base + b];
-    const double n = block_sum(tokens, red, 256);
+    for (int b = tid; b < blocks; b += kFinishThreads) tokens += part.tokens[base + b];
+    const double n = block_sum(tokens, red, kFinishThreads);
     const float inv_n = n > 0.0 ? (float)(1.0 / n) : 0.0f;
-    const int el = tid % lanes_e, strip = tid / lanes_e, strips = 256 / lanes_e;
+    const int el = tid % lanes_e, strip = tid / lanes_e, strips = kFinishThreads / lanes_e;
     double dot = 0.0;
     for (int e0 = 0; e0 < E; e0 += lanes_e) {
         const int e = e0 + el;
         float p = 0.0f;
         int32_t c = 0;
         if (e < E)
+#pragma unroll 4
             for (int b = strip; b < blocks; b += strips) {
                 p += part.prob[(base + b) * E + e];
                 c += part.count[(base + b) * E + e];
@@ -279,10 +362,10 @@ router_finish_kernel(RouterPartials part, int blocks, int k, int E, int lanes_e,
         }
         __syncthreads();
     }
-    dot = block_sum(dot, red, 256);
+    dot = block_sum(dot, red, kFinishThreads);
     if (tid == 0) {
         out.n_valid[mb] = (int)n;
-        out.loss[mb] = n > 0.0 ? (float)((double)coef * E * dot / ((double)k * n * n)) : 0.0f;
+        out.loss[mb] = balance_loss(dot, coef, E, k, n);
     }
 }
 
@@ -292,11 +375,11 @@ router_finish_kernel(RouterPartials part, int blocks, int k, int E, int lanes_e,
 //   dz = du (softmax), du sigmoid(-z) (sigmoid).
 // What falls on the selected experts goes through the token's LDS row, one selection after the other: the same expert twice adds
 // up in the order of the selections.
-template <class ZT, bool SIGMOID, int LT, int CH>
+template <class ZT, bool SIGMOID, int LT, int CH, int NS>
 __global__ void __launch_bounds__(router_waves<CH>() * 64)
 router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids, const uint8_t *__restrict__ valid, const float *__restrict__ dgates,
                   const int32_t *__restrict__ counts, const int32_t *__restrict__ n_valid, const float *__restrict__ dloss, RouterShape sh, float coef,
-                  int per_block, int vec, ZT *__restrict__ dlogits, int32_t *err_flag)
+                  int per_block, ZT *__restrict__ dlogits, int32_t *err_flag)
 {
     constexpr int NW = router_waves<CH>(), TPW = 64 / LT, ROW = LT * 8 * CH;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -305,6 +388,20 @@ router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
     const int n_sel = (k + LT - 1) / LT;
     const bool normalize = sh.flags & RELIBRA_ROUTER_NORMALIZE;
     float *row = reinterpret_cast<float *>(smem) + (wave * TPW + group) * ROW;
+    const int t_end = min(sh.T, (int)(blockIdx.x + 1) * per_block);
+    Raw8<ZT> raw[CH];
+    int next_id[NS];
+    float next_dg[NS];
+    uint8_t next_valid = 1;
+    auto fetch = [&](int t0) __attribute__((always_inline)) {
+        const size_t tok = (size_t)mb * sh.T + min(t0 + wave * TPW + group, sh.T - 1);
+        fetch_row<ZT, LT, CH>(logits + tok * E, E, sub, raw);
+        fetch_ids<LT, NS>(ids + tok * k, k, sub, n_sel, next_id);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) next_dg[i] = dgates && i < n_sel && i * LT + sub < k ? dgates[tok * k + i * LT + sub] : 0.0f;
+        if (valid) next_valid = valid[tok];
+    };
+    if (router_ahead<CH>()) fetch(blockIdx.x * per_block);
     float cost[CH][8];
     {
         const int n = dloss ? n_valid[mb] : 0;
@@ -318,35 +415,41 @@ router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
             }
     }
     bool bad = false;
-    const int t_end = min(sh.T, (int)(blockIdx.x + 1) * per_block);
     for (int t0 = blockIdx.x * per_block; t0 < t_end; t0 += NW * TPW) {
+        if (!router_ahead<CH>()) fetch(t0);
         const int t = t0 + wave * TPW + group;
         const size_t tok = (size_t)mb * sh.T + min(t, sh.T - 1);
-        const bool live = t < t_end && (!valid || valid[tok]);
-        float z[CH][8], p[CH][8], top, inv, part[kRouterMaxSel], add[CH][8];
-        load_row<ZT, LT, CH>(logits + tok * E, E, sub, vec, z);
-        float dg[kRouterMaxSel];
+        const bool live = t < t_end && next_valid;
+        float z[CH][8], p[CH][8], top, inv, part[NS], add[CH][8], dg[NS];
 #pragma unroll
-        for (int i = 0; i < kRouterMaxSel; ++i) dg[i] = dgates && i < n_sel && i * LT + sub < k ? sh.scale * dgates[tok * k + i * LT + sub] : 0.0f;
-        Selection sel;
-        pick_selections<LT, CH>(z, row, ids + tok * k, k, E, sub, n_sel, live, sel, bad);
+        for (int c = 0; c < CH; ++c) unpack8(raw[c], z[c]);
+        int id[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            id[i] = next_id[i];
+            dg[i] = sh.scale * next_dg[i];
+        }
+        if (router_ahead<CH>() && t0 + NW * TPW < t_end) fetch(t0 + NW * TPW);
+        Selection<NS> sel;
+        pick_selections<LT, CH, NS>(z, row, id, k, E, sub, n_sel, live, sel, bad);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) add[c][j] = 0.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) store8(row + (c * LT + sub) * 8, add[c]);
-        row_probabilities<SIGMOID, LT, CH>(z, p, top, inv);
-        selected_parts<SIGMOID, LT>(sel, n_sel, normalize, top, inv, part);
+        float down[CH][8];
+        row_probabilities<SIGMOID, LT, CH>(z, p, top, inv, down);
+        selected_parts<SIGMOID, LT, NS>(sel, n_sel, normalize, top, inv, part);
         float mean = 0.0f;
         if (normalize) {
 #pragma unroll
-            for (int i = 0; i < kRouterMaxSel; ++i) mean += part[i] * dg[i];
+            for (int i = 0; i < NS; ++i) mean += part[i] * dg[i];
             mean = group_sum<LT>(mean);
         }
         wave_lds_fence();
 #pragma unroll
-        for (int i = 0; i < kRouterMaxSel; ++i)
+        for (int i = 0; i < NS; ++i)
             if (i < n_sel) {
                 const float v = !normalize && !SIGMOID ? dg[i] : part[i] * (dg[i] - mean);
                 const int last = min(LT, k - i * LT);
@@ -374,50 +477,46 @@ router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     float du = p[c][j] * ((joins ? cost[c][j] + add[c][j] : cost[c][j]) - dot) + (joins ? 0.0f : add[c][j]);
-                    if (SIGMOID) {
-                        const float e = expf(-fabsf(z[c][j]));
-                        du *= (z[c][j] < 0.0f ? 1.0f : e) / (1.0f + e);
-                    }
+                    if (SIGMOID) du *= down[c][j];
                     v[j] = live ? du : 0.0f;
                 }
-                if (vec) {
-                    if (e0 < E) store8(out + e0, v);
-                } else {
+                if (e0 + 8 <= E) store8_any(out + e0, v);
+                else
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         if (e0 + j < E) from_f32(out + e0 + j, v[j]);
-                }
             }
         }
     }
     if (bad) atomicOr(err_flag, RELIBRA_ERR_ID_RANGE);
 }
 
-// Blocks per micro-batch: enough that the chip is full over all micro-batches, and no fewer than a wave's worth of tokens each.
-constexpr int kRouterBlocks = 1024;
+// Blocks per micro-batch: enough that the chip is full over all micro-batches, and no fewer tokens than a block has in flight.
+// A micro-batch of few tokens is one block's, which finishes its sums without a second launch.
+constexpr int kRouterBlocks = 2048, kSoloRounds = 4;
 struct RouterGrid {
     int lanes, chunks, waves, blocks, per_block;
+    bool solo;
 };
-inline RouterGrid router_grid(int n_mb, int T, int E)
+inline RouterGrid router_grid(int n_mb, int T, int E, bool fwd)
 {
     RouterGrid g;
-    g.lanes = 1;
-    while (g.lanes < 64 && 8 * g.lanes < E) g.lanes *= 2;
+    g.lanes = E <= 16 ? 2 : E <= 64 ? 8 : E <= 128 ? 16 : E <= 256 ? 32 : 64;
     g.chunks = 1;
     while (8 * 64 * g.chunks < E) g.chunks *= 2;
     g.waves = g.chunks == 8 ? 2 : 4;
     const int round = g.waves * (64 / g.lanes);              // tokens in flight in a block
     const int rounds = (T + round - 1) / round;
-    const int want = (kRouterBlocks + n_mb - 1) / n_mb;
+    g.solo = fwd && rounds <= kSoloRounds;
+    const int want = g.solo ? 1 : (kRouterBlocks + n_mb - 1) / n_mb;
     const int each = rounds > want ? (rounds + want - 1) / want : 1;
     g.per_block = each * round;
-    g.blocks = (T + g.per_block - 1) / g.per_block;
-    if (g.blocks < 1) g.blocks = 1;
+    g.blocks = std::max(1, (T + g.per_block - 1) / g.per_block);
     return g;
 }
 size_t router_ws_bytes(int n_mb, int T, int E)
 {
-    const RouterGrid g = router_grid(n_mb, T, E);
+    const RouterGrid g = router_grid(n_mb, T, E, true);
     const size_t cells = (size_t)n_mb * g.blocks;
     return round256(cells * E * sizeof(float)) + round256(cells * E * sizeof(int32_t)) + round256(cells * sizeof(int32_t));
 }
@@ -431,14 +530,17 @@ inline int check_router(int n_mb, int T, int k, int E, int flags, const void *lo
     return RELIBRA_OK;
 }
 
-// Calls fn(ZT, SIGMOID, LT, CH) as constants.
-template <class ZT, bool SIGMOID, class Fn> int router_layout(const RouterGrid &g, const Fn &fn)
+// Calls fn(LT, CH, NS) as constants.
+template <class Fn> int router_layout(const RouterGrid &g, int k, const Fn &fn)
 {
+    auto with = [&](auto lt, auto ch) {
+        if constexpr (decltype(lt)::value < 64)
+            if (k > decltype(lt)::value) return fn(lt, ch, std::integral_constant<int, 8>{});
+        return fn(lt, ch, std::integral_constant<int, 1>{});
+    };
 #define RELIBRA_ROUTER_CASE(l, c) \
-    if (g.lanes == l && g.chunks == c) return fn(std::integral_constant<int, l>{}, std::integral_constant<int, c>{})
-    RELIBRA_ROUTER_CASE(1, 1);
+    if (g.lanes == l && g.chunks == c) return with(std::integral_constant<int, l>{}, std::integral_constant<int, c>{})
     RELIBRA_ROUTER_CASE(2, 1);
-    RELIBRA_ROUTER_CASE(4, 1);
     RELIBRA_ROUTER_CASE(8, 1);
     RELIBRA_ROUTER_CASE(16, 1);
     RELIBRA_ROUTER_CASE(32, 1);
@@ -452,14 +554,15 @@ template <class ZT, bool SIGMOID, class Fn> int router_layout(const RouterGrid &
 
 template <class ZT, bool SIGMOID>
 int router_fwd_impl(const ZT *logits, const int32_t *ids, const uint8_t *valid, int n_mb, const RouterShape &sh, const RouterGrid &g,
-                    float *gates, const RouterPartials &part, int32_t *err_flag, hipStream_t stream)
+                    float *gates, const RouterPartials &part, const RouterSums &sums, float coef, int32_t *err_flag, hipStream_t stream)
 {
-    const int vec = sh.E % 8 == 0;
-    return router_layout<ZT, SIGMOID>(g, [&](auto lt, auto ch) {
-        constexpr int LT = decltype(lt)::value, CH = decltype(ch)::value;
+    return router_layout(g, sh.k, [&](auto lt, auto ch, auto ns) {
+        constexpr int LT = decltype(lt)::value, CH = decltype(ch)::value, NS = decltype(ns)::value;
         const size_t lds = (size_t)g.waves * 512 * CH * sizeof(float) + (sh.E + 1) * sizeof(int32_t);
-        RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FWD, stream, (router_fwd_kernel<ZT, SIGMOID, LT, CH><<<dim3(g.blocks, n_mb), g.waves * 64, lds, stream>>>(
-            logits, ids, valid, sh, g.per_block, vec, gates, part, err_flag)));
+        if (g.solo) RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FWD, stream, (router_fwd_kernel<ZT, SIGMOID, LT, CH, NS, true><<<dim3(1, n_mb), g.waves * 64, lds, stream>>>(
+            logits, ids, valid, sh, g.per_block, gates, part, sums, coef, err_flag)));
+        else RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FWD, stream, (router_fwd_kernel<ZT, SIGMOID, LT, CH, NS, false><<<dim3(g.blocks, n_mb), g.waves * 64, lds, stream>>>(
+            logits, ids, valid, sh, g.per_block, gates, part, sums, coef, err_flag)));
         return RELIBRA_OK;
     });
 }
@@ -468,12 +571,11 @@ template <class ZT, bool SIGMOID>
 int router_bwd_impl(const ZT *logits, const int32_t *ids, const uint8_t *valid, const float *dgates, const int32_t *counts, const int32_t *n_valid,
                     const float *dloss, int n_mb, const RouterShape &sh, float coef, const RouterGrid &g, ZT *dlogits, int32_t *err_flag, hipStream_t stream)
 {
-    const int vec = sh.E % 8 == 0;
-    return router_layout<ZT, SIGMOID>(g, [&](auto lt, auto ch) {
-        constexpr int LT = decltype(lt)::value, CH = decltype(ch)::value;
+    return router_layout(g, sh.k, [&](auto lt, auto ch, auto ns) {
+        constexpr int LT = decltype(lt)::value, CH = decltype(ch)::value, NS = decltype(ns)::value;
         const size_t lds = (size_t)g.waves * 512 * CH * sizeof(float);
-        RELIBRA_LAUNCH(RELIBRA_K_ROUTER_BWD, stream, (router_bwd_kernel<ZT, SIGMOID, LT, CH><<<dim3(g.blocks, n_mb), g.waves * 64, lds, stream>>>(
-            logits, ids, valid, dgates, counts, n_valid, dloss, sh, coef, g.per_block, vec, dlogits, err_flag)));
+        RELIBRA_LAUNCH(RELIBRA_K_ROUTER_BWD, stream, (router_bwd_kernel<ZT, SIGMOID, LT, CH, NS><<<dim3(g.blocks, n_mb), g.waves * 64, lds, stream>>>(
+            logits, ids, valid, dgates, counts, n_valid, dloss, sh, coef, g.per_block, dlogits, err_flag)));
         return RELIBRA_OK;
     });
 }
@@ -491,7 +593,7 @@ extern "C" int relibra_router_fwd(const void *logits, const int32_t *ids, const 
     if (rc != RELIBRA_OK) return rc;
     if (n_mb == 0) return RELIBRA_OK;
     if (!counts || !n_valid || !prob_mean || !loss || !err_flag || (T > 0 && !gates)) return RELIBRA_EINVAL;
-    const RouterGrid g = router_grid(n_mb, T, E);
+    const RouterGrid g = router_grid(n_mb, T, E, true);
     if (!workspace || workspace_bytes < router_ws_bytes(n_mb, T, E)) return RELIBRA_EWORKSPACE;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     const size_t cells = (size_t)n_mb * g.blocks;
@@ -501,18 +603,20 @@ extern "C" int relibra_router_fwd(const void *logits, const int32_t *ids, const 
     part.count = (int32_t *)(ws += round256(cells * E * sizeof(float)));
     part.tokens = (int32_t *)(ws + round256(cells * E * sizeof(int32_t)));
     const RouterShape sh{T, k, E, flags, scale};
+    const RouterSums sums{counts, n_valid, prob_mean, loss};
     int rl;
     if (flags & RELIBRA_ROUTER_FP32)
-        rl = flags & RELIBRA_ROUTER_SIGMOID ? router_fwd_impl<float, true>((const float *)logits, ids, valid, n_mb, sh, g, gates, part, err_flag, stream)
-                                            : router_fwd_impl<float, false>((const float *)logits, ids, valid, n_mb, sh, g, gates, part, err_flag, stream);
+        rl = flags & RELIBRA_ROUTER_SIGMOID ? router_fwd_impl<float, true>((const float *)logits, ids, valid, n_mb, sh, g, gates, part, sums, balance_coef, err_flag, stream)
+                                            : router_fwd_impl<float, false>((const float *)logits, ids, valid, n_mb, sh, g, gates, part, sums, balance_coef, err_flag, stream);
     else
-        rl = flags & RELIBRA_ROUTER_SIGMOID ? router_fwd_impl<bf16_t, true>((const bf16_t *)logits, ids, valid, n_mb, sh, g, gates, part, err_flag, stream)
-                                            : router_fwd_impl<bf16_t, false>((const bf16_t *)logits, ids, valid, n_mb, sh, g, gates, part, err_flag, stream);
+        rl = flags & RELIBRA_ROUTER_SIGMOID ? router_fwd_impl<bf16_t, true>((const bf16_t *)logits, ids, valid, n_mb, sh, g, gates, part, sums, balance_coef, err_flag, stream)
+                                            : router_fwd_impl<bf16_t, false>((const bf16_t *)logits, ids, valid, n_mb, sh, g, gates, part, sums, balance_coef, err_flag, stream);
     if (rl != RELIBRA_OK) return rl;
-    int lanes_e = 1;
-    while (lanes_e < 256 && lanes_e < E) lanes_e *= 2;
-    RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FINISH, stream, router_finish_kernel<<<n_mb, 256, 0, stream>>>(
-        part, g.blocks, k, E, lanes_e, balance_coef, RouterSums{counts, n_valid, prob_mean, loss}));
+    if (!g.solo) {
+        int lanes_e = 1;
+        while (lanes_e < kFinishThreads && lanes_e < E) lanes_e *= 2;
+        RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FINISH, stream, router_finish_kernel<<<n_mb, kFinishThreads, 0, stream>>>(part, g.blocks, k, E, lanes_e, balance_coef, sums));
+    }
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
 }
@@ -526,7 +630,7 @@ extern "C" int relibra_router_bwd(const void *logits, const int32_t *ids, const 
     if (rc != RELIBRA_OK) return rc;
     if (n_mb == 0 || T == 0) return RELIBRA_OK;
     if (!dlogits || !aligned16(dlogits) || !err_flag || (dloss && (!counts || !n_valid))) return RELIBRA_EINVAL;
-    const RouterGrid g = router_grid(n_mb, T, E);
+    const RouterGrid g = router_grid(n_mb, T, E, false);
     const RouterShape sh{T, k, E, flags, scale};
     int rl;
     if (flags & RELIBRA_ROUTER_FP32)

@@ -71,6 +71,17 @@ __device__ __forceinline__ void unpack8(const Raw8<float> &r, float (&v)[8])
     v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
     v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
 }
+// The same at any alignment of the element type (the memory pipeline takes such accesses).
+__device__ __forceinline__ Raw8<bf16_t> fetch8_any(const bf16_t *p)
+{
+    typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+    return Raw8<bf16_t>{__builtin_bit_cast(uint4, *reinterpret_cast<const any4 *>(p))};
+}
+__device__ __forceinline__ Raw8<float> fetch8_any(const float *p)
+{
+    typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+    return Raw8<float>{__builtin_bit_cast(float4, reinterpret_cast<const any4 *>(p)[0]), __builtin_bit_cast(float4, reinterpret_cast<const any4 *>(p)[1])};
+}
 template <class T> __device__ __forceinline__ void load8(const T *p, float (&v)[8]) { unpack8(fetch8(p), v); }
 __device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8])
 {
@@ -80,6 +91,17 @@ __device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
     reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8_any(bf16_t *p, const float (&v)[8])
+{
+    typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+    *reinterpret_cast<any4 *>(p) = any4{pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7])};
+}
+__device__ __forceinline__ void store8_any(float *p, const float (&v)[8])
+{
+    typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+    reinterpret_cast<any4 *>(p)[0] = any4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<any4 *>(p)[1] = any4{v[4], v[5], v[6], v[7]};
 }
 __device__ __forceinline__ float to_f32(bf16_t b) { return bf2f(b); }
 __device__ __forceinline__ float to_f32(float f) { return f; }
