@@ -33,6 +33,7 @@ constexpr float kScale = 4096.0f;
 constexpr int kOrthoPad = 64;
 constexpr int kMinParts = 16, kMaxParts = 1024;  // partial sums of a matrix's squares
 constexpr int kOrthoMaxSide = 32768;
+constexpr int kComputeUnits = 256;
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
@@ -42,11 +43,10 @@ struct OrthoShape {
     int rp, cp;                                  // padded
     bool tall;                                   // rows > cols
 };
-// Workspace: two copies of X's first halves (a step reads one and writes the other), the second halves, A, B, their diagonals, partial sums.
+// Workspace: two copies of X's first halves (a step reads one and writes the other), the second halves, A, B, their diagonals.
 struct OrthoWs {
     uint16_t *x[2], *lo, *a, *b;
     float *da, *db;
-    double *parts;
 };
 inline size_t ortho_x_bytes(const OrthoShape &s) { return round256((size_t)s.n * s.rp * s.cp * 2); }
 inline size_t ortho_gram_bytes(const OrthoShape &s)
@@ -62,17 +62,11 @@ inline OrthoShape ortho_shape(int n, int rows, int cols)
 }
 // Blocks that share a matrix's squares: 2048 over all matrices, each with at least 4096 values.  With 64 a matrix one of
 // 4096 x 4096 took 197 us (0.25 of the copy rate).
-inline int norm_parts(const OrthoShape &s)
+inline int norm_parts(int n, int rows, int cols)
 {
-    const size_t values = (size_t)s.rows * s.cols;
-    return (int)std::min<size_t>(std::max<size_t>(std::min<size_t>((2048 + s.n - 1) / s.n, values / 4096), kMinParts), kMaxParts);
+    const size_t values = (size_t)rows * cols;
+    return (int)std::min<size_t>(std::max<size_t>(std::min<size_t>((2048 + n - 1) / n, values / 4096), kMinParts), kMaxParts);
 }
-size_t ortho_ws_bytes(int n, int rows, int cols)
-{
-    const OrthoShape s = ortho_shape(n, rows, cols);
-    return 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + 2 * ortho_diag_bytes(s) + round256((size_t)n * norm_parts(s) * sizeof(double));
-}
-
 // ---------------------------------------------------------------- momentum, norm, first halves
 enum { U_GRAD = 0, U_MOMENTUM = 1, U_NESTEROV = 2 };
 __device__ __forceinline__ float update_of(float g, float m_new, float mu, int mode)
@@ -80,37 +74,34 @@ __device__ __forceinline__ float update_of(float g, float m_new, float mu, int m
     return mode == U_GRAD ? g : mode == U_MOMENTUM ? m_new : fmaf(mu, m_new, g);
 }
 
-// M' and the sum of U^2, part blockIdx.x of matrix blockIdx.y.  Squares in double: no gradient is too large or small.
-// vec: elements per matrix and all pointers allow 16-byte accesses (four fp32 or eight bytes of bf16 at a time).
+// M' and the sum of U^2, part blockIdx.x of matrix blockIdx.y.  Squares in double: no gradient is too large or small.  Eight values at a
+// time, wherever the matrix starts.
 template <class GT>
 __global__ void __launch_bounds__(256)
-ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mode, size_t per_matrix, int vec, float *m_out, double *__restrict__ parts)
+ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mode, size_t per_matrix, float *m_out, double *__restrict__ parts)
 {
     __shared__ double red[4];
     const size_t base = (size_t)blockIdx.y * per_matrix;
     double sum = 0.0;
-    auto one = [&](GT gv, float mv) __attribute__((always_inline)) {
-        const float mn = mode == U_GRAD ? 0.0f : fmaf(mu, mv, to_f32(gv));
-        const double u = update_of(to_f32(gv), mn, mu, mode);
+    auto one = [&](float gv, float mv) __attribute__((always_inline)) {
+        const float mn = mode == U_GRAD ? 0.0f : fmaf(mu, mv, gv);
+        const double u = update_of(gv, mn, mu, mode);
         sum += u * u;
         return mn;
     };
-    if (vec) {
-        const size_t quads = per_matrix / 4, stride = (size_t)gridDim.x * 256;
-        for (size_t q = (size_t)blockIdx.x * 256 + threadIdx.x; q < quads; q += stride) {
-            GT gv[4];
-            if constexpr (sizeof(GT) == 4) *reinterpret_cast<float4 *>(gv) = *reinterpret_cast<const float4 *>(g + base + q * 4);
-            else *reinterpret_cast<uint2 *>(gv) = *reinterpret_cast<const uint2 *>(g + base + q * 4);
-            float4 mv = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (mode != U_GRAD) mv = *reinterpret_cast<const float4 *>(m + base + q * 4);
-            const float4 mn = make_float4(one(gv[0], mv.x), one(gv[1], mv.y), one(gv[2], mv.z), one(gv[3], mv.w));
-            if (mode != U_GRAD) *reinterpret_cast<float4 *>(m_out + base + q * 4) = mn;
-        }
-    } else {
-        for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < per_matrix; i += (size_t)gridDim.x * 256) {
-            const float mn = one(g[base + i], mode != U_GRAD ? m[base + i] : 0.0f);
-            if (mode != U_GRAD) m_out[base + i] = mn;
-        }
+    const size_t eights = per_matrix / 8, stride = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < eights; i += stride) {
+        float gv[8], mv[8] = {};
+        unpack8(fetch8_any(g + base + i * 8), gv);
+        if (mode != U_GRAD) unpack8(fetch8_any(m + base + i * 8), mv);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mv[j] = one(gv[j], mv[j]);
+        if (mode != U_GRAD) store8_any(m_out + base + i * 8, mv);
+    }
+    const size_t rest = eights * 8 + threadIdx.x;
+    if (blockIdx.x == 0 && rest < per_matrix) {
+        const float mn = one(to_f32(g[base + rest]), mode != U_GRAD ? m[base + rest] : 0.0f);
+        if (mode != U_GRAD) m_out[base + rest] = mn;
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
@@ -122,7 +113,7 @@ ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mo
 // X = kScale U / |U| as two halves, padding included.  A thread takes 8 consecutive padded columns of a row.
 template <class GT>
 __global__ void __launch_bounds__(256)
-ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, float mu, int mode, OrthoShape s, int vec, const double *__restrict__ parts,
+ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, float mu, int mode, OrthoShape s, const double *__restrict__ parts,
                   int n_parts, uint16_t *__restrict__ hi, uint16_t *__restrict__ lo)
 {
     __shared__ double scale_of;
@@ -137,16 +128,16 @@ ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, flo
     __syncthreads();
     const double scale = scale_of;
     const int per_row = s.cp / 8;
-    const size_t pieces = (size_t)s.rp * per_row;
+    const unsigned pieces = (unsigned)((size_t)s.rp * per_row);                     // at most 2^27: sides of at most 32768
     const size_t from = (size_t)b * s.rows * s.cols, to = (size_t)b * s.rp * s.cp;
-    for (size_t p = (size_t)blockIdx.x * 256 + threadIdx.x; p < pieces; p += (size_t)gridDim.x * 256) {
-        const int r = (int)(p / per_row), c = (int)(p % per_row) * 8;
+    for (unsigned p = blockIdx.x * 256 + threadIdx.x; p < pieces; p += gridDim.x * 256) {
+        const int r = p / (unsigned)per_row, c = p % (unsigned)per_row * 8;
         float gv[8] = {}, mv[8] = {}, u[8];
         const size_t at = from + (size_t)r * s.cols + c;
-        const bool whole = vec && r < s.rows && c < s.cols;          // cols % 8 == 0 then
+        const bool whole = r < s.rows && c + 8 <= s.cols;
         if (whole) {
-            if (mode != U_MOMENTUM) load8(g + at, gv);
-            if (mode != U_GRAD) load8(m_new + at, mv);
+            if (mode != U_MOMENTUM) unpack8(fetch8_any(g + at), gv);
+            if (mode != U_GRAD) unpack8(fetch8_any(m_new + at), mv);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -462,17 +453,470 @@ int ortho_steps(const OrthoShape &s, const OrthoWs &w, int steps, float scale, u
     return RELIBRA_OK;
 }
 
-template <class GT>
-void ortho_load(const OrthoShape &s, const OrthoWs &w, const GT *g, const float *m, float mu, int mode, float *m_out, hipStream_t stream)
+// ---------------------------------------------------------------- thin matrices
+// A side of at most 128: A and B fit into a workgroup's LDS, so one launch does a whole step.  The long side is cut into runs of rows,
+// `runs` of them to a workgroup; it adds up the workgroups' partial A's, works out B (every workgroup of a matrix does: 128^3 at most),
+// multiplies its own rows and takes their share of the next A while they are at hand.  X lies with the long side first whatever the
+// gradient's layout, so that every product finds what it needs along memory or through transposing LDS reads; a workgroup alone
+// reads and writes its rows, so they are updated in place.  Partial A's travel in accumulator order.  Where one workgroup holds a
+// matrix it does all the steps in one launch.  us a call, tiles and 17 launches -> this: 8 of 128 x 256 102 -> 70, 4096 x 128 200 -> 91, 64 x 4096 172 -> 74,
+// 128 of 128 x 2048 690 -> 470, 39 of 21 x 2499 238 -> 128.
+// 16 waves, one 32 x 32 tile each in every phase: the phases are short chains of LDS round trips and conversions, and with four waves
+// of four times the tiles a step of 128 x 128 took 16 us (nothing hides a wave's own latency) where this takes 10.
+constexpr int kThinSide = 128, kThinWaves = 16, kThinThreads = kThinWaves * 64, kThinBatch = 2;
+template <int MP> struct Thin {
+    static constexpr int TILES = MP / 32;                    // of a side of A
+    static constexpr int SPLIT = kThinWaves / (TILES * TILES);       // waves that share a tile of the rows' Gram matrix, a part of the rows each
+    static constexpr int ROWS = kThinWaves / TILES * 32;     // of a run
+    static constexpr int KK = MP / 16, AB = MP * MP * 2, STAGE = ROWS * MP * 2, DIAG = 3 * MP * (int)sizeof(float),
+                         CARRY = SPLIT > 1 ? kThinWaves * 4096 : 0, LDS = AB + 2 * STAGE + DIAG + CARRY;     // CARRY: the waves' parts of A's tiles
+    typedef WaveStage<MP> ST;                    // (row, column) -> place in the A / B buffer and in the staged rows of X
+    static constexpr int PIECES = MP / 8, PER_THREAD = ROWS * PIECES / kThinThreads;         // 16-byte pieces of a row, of a run for each thread
+
+    // A run's rows straight to the stage: a wave's 64 pieces fill 1 KiB of consecutive LDS, so each lane fetches the piece whose
+    // place is its own.  Not waited for here.
+    static __device__ __forceinline__ void request_rows(const uint16_t *rows, char *stage, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < PER_THREAD; ++i) {
+            const int first = (i * kThinWaves + wave) * 64, r = (first + lane) / PIECES, piece = ((first + lane) ^ r) & (PIECES - 1);
+            load_lds16(rows + (size_t)r * MP + piece * 8, stage + first * 16);
+        }
+    }
+
+    static __device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16_t zero()
+    {
+        f32x16_t z;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) z[v] = 0.0f;
+        return z;
+    }
+    static __device__ __forceinline__ bf16x8_t frag(const char *ab, int row0, int kk, int lane)
+    {
+        return *reinterpret_cast<const bf16x8_t *>(ab + ST::acc_addr(row0 + (lane & 31), kk * 16 + (lane >> 5) * 8));
+    }
+    // rows contracted over: value k of column c0 + (lane & 31), k = kk * 16 + (lane / 32) * 8 .. + 7, by transposing LDS reads
+    static __device__ __forceinline__ bf16x8_t frag_across(const char *stage, int c0, int kk, int lane)
+    {
+        const int b = lane >> 4, i = lane & 15, c = c0 + (b & 1) * 16 + (i & 3) * 4, r = kk * 16 + (b >> 1) * 8 + (i >> 2);
+        const s16x4_t l = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(stage + ST::acc_addr(r, c)));
+        const s16x4_t h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(stage + ST::acc_addr(r + 4, c)));
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // g += this wave's tile of the staged rows' Gram matrix, over its part of the rows
+    static __device__ __forceinline__ f32x16_t gram(f32x16_t g, const char *stage, int wave, int lane)
+    {
+        const int tile = wave / SPLIT, a0 = tile / TILES * 32, b0 = tile % TILES * 32, k0 = wave % SPLIT * (ROWS / SPLIT / 16);
+#pragma unroll
+        for (int kk = 0; kk < ROWS / SPLIT / 16; ++kk) {
+            if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+            g = mfma(frag_across(stage, a0, k0 + kk, lane), frag_across(stage, b0, k0 + kk, lane), g);
+        }
+        return g;
+    }
+    // second halves lie in accumulator order: [32 x 32 tile of the run][4 registers of a lane][lane] of 4 values
+    static __device__ __forceinline__ int lo_at(int tile, int q, int lane) { return ((tile * 4 + q) * 64 + lane) * 4; }
+    // a partial A: [tile][part of the rows][4 registers of a lane][lane]
+    static __device__ __forceinline__ size_t part_at(size_t chunk, int tile_and_split, int q, int lane) { return ((chunk * kThinWaves + tile_and_split) * 4 + q) * 64 + lane; }
+    static __device__ __forceinline__ void store_part(const f32x16_t &g, float *part, size_t chunk, int wave, int lane)
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) reinterpret_cast<float4 *>(part)[part_at(chunk, wave, q, lane)] = make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]);
+    }
+};
+struct ThinShape {
+    int n, rows, cols;                           // as the caller gives them
+    int mp, run_rows, chunks, runs;              // short side padded to 64 or 128; rows of a run, workgroups of a matrix, runs of each
+    bool tall;
+    __host__ __device__ int longs() const { return tall ? rows : cols; }
+    __host__ __device__ int shorts() const { return tall ? cols : rows; }
+    __host__ __device__ size_t x_at(int mat) const { return (size_t)mat * chunks * runs * run_rows * mp; }
+};
+inline bool is_thin(int rows, int cols) { return std::min(rows, cols) <= kThinSide; }
+// One run to a workgroup as far as there are compute units (a workgroup fills one).  Every workgroup of a matrix reads all partial
+// A's (64 KiB apiece, two in flight, about 1.2 us each): of more than kThinDirect a kernel of its own makes one first.  us a call, without
+// it and the best number of workgroups -> with it: 4096 x 128 139 -> 91, 4 of 128 x 4096 149 -> 107, 16 of 3000 x 100 188 -> 155, 64 x 4096 101 -> 74.
+constexpr int kThinDirect = 4;
+inline ThinShape thin_shape(int n, int rows, int cols)
 {
-    const size_t per_matrix = (size_t)s.rows * s.cols;
-    const int parts = norm_parts(s);
-    const bool aligned = aligned16(g) && (mode == U_GRAD || (aligned16(m) && aligned16(m_out)));
-    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_NORM, stream, ortho_momentum_kernel<GT><<<dim3(parts, s.n), 256, 0, stream>>>(
-        g, m, mu, mode, per_matrix, aligned && per_matrix % 4 == 0, m_out, w.parts));
-    const size_t pieces = (size_t)s.rp * s.cp / 8;
-    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_LOAD, stream, ortho_load_kernel<GT><<<dim3((unsigned)std::min<size_t>((pieces + 255) / 256, 256), s.n), 256, 0, stream>>>(
-        g, m_out, mu, mode, s, aligned && s.cols % 8 == 0, w.parts, parts, w.x[0], w.lo));
+    ThinShape s{n, rows, cols, 128, Thin<128>::ROWS, 1, 1, rows > cols};
+    if (std::min(rows, cols) <= 64) s.mp = 64, s.run_rows = Thin<64>::ROWS;
+    const int all = (s.longs() + s.run_rows - 1) / s.run_rows;
+    const int chunks = std::max(1, std::min(kComputeUnits / n, all));
+    s.runs = (all + chunks - 1) / chunks;
+    s.chunks = (all + s.runs - 1) / s.runs;
+    return s;
+}
+struct ThinWs {
+    uint16_t *hi, *lo;
+    float *part[2], *sum;
+    double *parts;
+};
+inline size_t thin_x_bytes(const ThinShape &s) { return round256(s.x_at(s.n) * sizeof(uint16_t)); }
+inline size_t thin_part_bytes(const ThinShape &s) { return round256((size_t)s.n * s.chunks * kThinWaves * 1024 * sizeof(float)); }
+
+inline size_t thin_sum_bytes(const ThinShape &s) { return s.chunks > kThinDirect ? round256((size_t)s.n * kThinWaves * 1024 * sizeof(float)) : 0; }
+
+// Rows of a run, 8 values of the short side at a time, lanes along the memory of the caller's matrix: fn(row of the run, first value).
+template <int MP, int UNROLL, class Fn> __device__ __forceinline__ void thin_pieces(bool tall, int tid, const Fn &fn)
+{
+    constexpr int PIECES = Thin<MP>::PIECES, ROWS = Thin<MP>::ROWS;
+#pragma unroll UNROLL
+    for (int p = tid; p < ROWS * PIECES; p += kThinThreads) {
+        if (tall) fn(p / PIECES, p % PIECES * 8);
+        else fn(p % ROWS, p / ROWS * 8);
+    }
+}
+
+// First halves of a workgroup's rows and their partial A.
+template <class GT, int MP>
+__global__ void __launch_bounds__(kThinThreads)
+ortho_thin_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, float mu, int mode, ThinShape s, const double *__restrict__ parts, int n_parts,
+                       uint16_t *__restrict__ hi, uint16_t *__restrict__ lo, float *__restrict__ part)
+{
+    using TH = Thin<MP>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    __shared__ double scale_of;
+    int tid = threadIdx.x;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mat = blockIdx.y;
+    if (tid < 64) {
+        double sum = 0.0;
+        for (int i = tid; i < n_parts; i += 64) sum += parts[(size_t)mat * n_parts + i];
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+        if (tid == 0) scale_of = sum == 0.0 ? 0.0 : (double)kScale / sqrt(sum);
+    }
+    __syncthreads();
+    const double scale = scale_of;
+    const size_t from = (size_t)mat * s.rows * s.cols;
+    const int longs = s.longs(), shorts = s.shorts();
+    f32x16_t acc = TH::zero();
+    for (int run = 0; run < s.runs; ++run) {
+        const int row0 = (blockIdx.x * s.runs + run) * TH::ROWS;
+        asm volatile("" : "+v"(tid));                         // (opaque: else the addresses of a run are kept in registers from run to run)
+        thin_pieces<MP, 2>(s.tall, tid, [&](int i, int j0) __attribute__((always_inline)) {
+            const int li = row0 + i;
+            float gv[8] = {}, mv[8] = {};
+            if (s.tall && li < longs && j0 + 8 <= shorts) {
+                const size_t at = from + (size_t)li * s.cols + j0;
+                if (mode != U_MOMENTUM) unpack8(fetch8_any(g + at), gv);
+                if (mode != U_GRAD) unpack8(fetch8_any(m_new + at), mv);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (li < longs && j0 + j < shorts) {
+                        const size_t at = from + (s.tall ? (size_t)li * s.cols + j0 + j : (size_t)(j0 + j) * s.cols + li);
+                        if (mode != U_MOMENTUM) gv[j] = to_f32(g[at]);
+                        if (mode != U_GRAD) mv[j] = m_new[at];
+                    }
+            }
+            uint16_t h8[8], l8[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = li < longs && j0 + j < shorts;
+                const float u = in ? (float)((double)update_of(gv[j], mv[j], mu, mode) * scale) : 0.0f;
+                const _Float16 h = (_Float16)u;
+                h8[j] = __builtin_bit_cast(uint16_t, h);
+                l8[j] = __builtin_bit_cast(uint16_t, (_Float16)(u - (float)h));
+            }
+            *reinterpret_cast<uint4 *>(hi + s.x_at(mat) + (size_t)li * MP + j0) = *reinterpret_cast<const uint4 *>(h8);
+            uint16_t *l = lo + s.x_at(mat) + (size_t)row0 * MP + TH::lo_at(i / 32 * TH::TILES + j0 / 32, j0 % 32 / 8, i % 32);
+            *reinterpret_cast<uint2 *>(l) = *reinterpret_cast<const uint2 *>(l8);
+            *reinterpret_cast<uint2 *>(l + 32 * 4) = *reinterpret_cast<const uint2 *>(l8 + 4);
+            *reinterpret_cast<uint4 *>(lds + TH::ST::acc_addr(i, j0)) = *reinterpret_cast<const uint4 *>(h8);
+        });
+        __syncthreads();
+        acc = TH::gram(acc, lds, wave, lane);
+        __syncthreads();
+    }
+    TH::store_part(acc, part, (size_t)mat * s.chunks + blockIdx.x, wave, lane);
+}
+
+// One partial A of a matrix from those of its workgroups, in ascending order: blockIdx.x of kThinWaves blocks of 1024 values.
+__global__ void __launch_bounds__(256)
+ortho_thin_sum_kernel(const float4 *__restrict__ part, int chunks, float4 *__restrict__ sum)
+{
+    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x, base = (size_t)blockIdx.y * chunks * kThinWaves * 256 + at;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int c = 0; c < chunks; ++c) {
+        const float4 v = part[base + (size_t)c * kThinWaves * 256];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    sum[(size_t)blockIdx.y * kThinWaves * 256 + at] = s;
+}
+
+__device__ __forceinline__ void add4(f32x16_t &to, int q, const float4 &v)
+{
+    to[4 * q] += v.x;
+    to[4 * q + 1] += v.y;
+    to[4 * q + 2] += v.z;
+    to[4 * q + 3] += v.w;
+}
+
+// Steps first .. first + count - 1 of `steps` (count > 1 with one workgroup a matrix only).
+template <int MP>
+__global__ void __launch_bounds__(kThinThreads)
+ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *hi, uint16_t *lo, const float *__restrict__ part_in, int n_in,
+                       float *__restrict__ part_out, float out_scale, int vec,
+                       uint16_t *__restrict__ out)
+{
+    using TH = Thin<MP>;
+    using ST = typename TH::ST;
+    constexpr int KK = TH::KK, TILES = TH::TILES, SPLIT = TH::SPLIT;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    char *ab = lds;
+    float *da = reinterpret_cast<float *>(lds + TH::AB + 2 * TH::STAGE), *hi_by = da + MP, *lo_by = hi_by + MP;     // diagonal of A; a + d and a + w d, d that of B
+    float4 *carry = reinterpret_cast<float4 *>(lds + TH::AB + 2 * TH::STAGE + TH::DIAG);
+    f32x16_t acc = TH::zero();                                // this wave's tile of the next A over the workgroup's rows
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mat = blockIdx.y;
+    // this wave's tile of A (the first TILES^2 waves) and of a run's rows of X
+    const bool has_tile = wave < TILES * TILES;
+    const int a0 = wave / TILES * 32, b0 = wave % TILES * 32, x_col = wave % TILES * 32;
+    for (int step = first; step < first + count; ++step) {
+        const float w = step + 3 >= steps ? 1.0f : 0.0f;
+        const bool last = step + 1 == steps;
+        int lane = tid & 63, cols = s.cols;                   // (opaque: else every address of a step is kept in registers through all steps)
+        asm volatile("" : "+v"(lane), "+s"(cols));
+        const int r_ab = b0 + (lane & 31), half = (lane >> 5) * 4;
+        // the first run's rows are on their way while A and B are worked out, the next one's while a run is finished
+        uint2 lv[4];
+        auto fetch = [&](int run, int t) __attribute__((always_inline)) {
+            const size_t at_run = s.x_at(mat) + (size_t)(blockIdx.x * s.runs + run) * TH::ROWS * MP;
+            TH::request_rows(hi + at_run, lds + TH::AB + (run & 1) * TH::STAGE, wave, t & 63);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) lv[q] = *reinterpret_cast<const uint2 *>(lo + at_run + TH::lo_at(wave, q, t & 63));
+        };
+        fetch(0, tid);
+        // A: every wave adds up its part over the workgroups of the matrix, in ascending order, several at a time so that a memory
+        // round trip is paid once for all; the parts of a tile meet in LDS
+        if (step == first) {
+            const float4 *src = reinterpret_cast<const float4 *>(part_in);
+            acc = TH::zero();
+#pragma unroll 1
+            for (int c0 = 0; c0 < n_in; c0 += kThinBatch) {
+                float4 v[kThinBatch][4];
+#pragma unroll
+                for (int u = 0; u < kThinBatch; ++u)
+                    if (c0 + u < n_in)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) v[u][q] = src[TH::part_at((size_t)mat * n_in + c0 + u, wave, q, lane)];
+#pragma unroll
+                for (int u = 0; u < kThinBatch; ++u)
+                    if (c0 + u < n_in)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) add4(acc, q, v[u][q]);
+            }
+        }
+        if (SPLIT > 1) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) carry[TH::part_at(0, wave, q, lane)] = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+            __syncthreads();
+        }
+        uint2 at[4];
+        if (has_tile) {
+            f32x16_t sum = SPLIT > 1 ? TH::zero() : acc;
+            if (SPLIT > 1)
+#pragma unroll
+                for (int c = 0; c < SPLIT; ++c)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) add4(sum, q, carry[TH::part_at(0, wave * SPLIT + c, q, lane)]);
+            // A: its diagonal apart, the rest as halves
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = a0 + q * 8 + half;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = sum[4 * q + e] * (1.0f / kScale);
+                    if (a0 == b0 && r_ab == c + e) {
+                        da[r_ab] = v[e];
+                        v[e] = 0.0f;
+                    }
+                }
+                at[q] = pack4h(v);
+                ST::put(ab, r_ab, c, at[q]);
+            }
+        }
+        __syncthreads();
+        f32x16_t p = TH::zero();
+        if (has_tile) {
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                p = TH::mfma(TH::frag(ab, a0, kk, lane), TH::frag(ab, b0, kk, lane), p);
+            }
+        }
+        __syncthreads();                                      // A has been read: B takes its place
+        if (has_tile) {
+            const float d_r = da[r_ab];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = a0 + q * 8 + half;
+                const float4 d_c = *reinterpret_cast<const float4 *>(da + c);
+                const float dc[4] = {d_c.x, d_c.y, d_c.z, d_c.w};
+                float old[4], v[4];
+                unpack4h(at[q], old);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = kNsB * old[e] + (kNsC / kScale) * (p[4 * q + e] + (d_r + dc[e]) * old[e]);
+                    if (a0 == b0 && r_ab == c + e) {
+                        const float d = (kNsB * d_r + (kNsC / kScale) * (p[4 * q + e] + d_r * d_r)) * (1.0f / kScale);
+                        hi_by[r_ab] = kNsA + d;
+                        lo_by[r_ab] = kNsA + w * d;
+                        v[e] = 0.0f;
+                    }
+                }
+                ST::put(ab, r_ab, c, pack4h(v));
+            }
+        }
+        __syncthreads();
+        acc = TH::zero();
+        for (int run = 0; run < s.runs; ++run) {
+            const int row0 = (blockIdx.x * s.runs + run) * TH::ROWS;
+            int t = tid;
+            asm volatile("" : "+v"(t), "+s"(cols));
+            const int lane = t & 63, half = (lane >> 5) * 4, x_row = wave / TILES * 32 + (lane & 31);
+            const size_t at_run = s.x_at(mat) + (size_t)row0 * MP;
+            char *stage = lds + TH::AB + (run & 1) * TH::STAGE;
+            wait_vm_lgkm0<0>();                               // this wave's share of the rows is there
+            __syncthreads();
+            f32x16_t x = TH::zero();
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                x = TH::mfma(TH::frag(ab, x_col, kk, lane), TH::frag(stage, wave / TILES * 32, kk, lane), x);
+            }
+            uint2 h_now[4], l_now[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                h_now[q] = ST::get(stage, x_row, x_col + q * 8 + half);
+                l_now[q] = lv[q];
+            }
+            __syncthreads();                                  // the rows have been read: X' takes their place
+            if (run + 1 < s.runs) fetch(run + 1, t);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = x_col + q * 8 + half;
+                const float4 bh = *reinterpret_cast<const float4 *>(hi_by + c), bl = *reinterpret_cast<const float4 *>(lo_by + c);
+                const float by_h[4] = {bh.x, bh.y, bh.z, bh.w}, by_l[4] = {bl.x, bl.y, bl.z, bl.w};
+                float h[4], l[4], v[4];
+                unpack4h(h_now[q], h);
+                unpack4h(l_now[q], l);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = by_h[e] * h[e] + (by_l[e] * l[e] + x[4 * q + e] * (1.0f / kScale));
+                uint2 hp = pack4h(v);
+                if (!last) {
+                    unpack4h(hp, h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) l[e] = v[e] - h[e];
+                    *reinterpret_cast<uint2 *>(lo + at_run + TH::lo_at(wave, q, lane)) = pack4h(l);
+                } else {
+                    const float f = out_scale * (1.0f / kScale);
+                    hp = make_uint2(pack2bf(f * v[0], f * v[1]), pack2bf(f * v[2], f * v[3]));
+                }
+                ST::put(stage, x_row, c, hp);
+            }
+            __syncthreads();
+            if (!last) {
+#pragma unroll
+                for (int i = 0; i < TH::PER_THREAD; ++i) {
+                    const int p = i * kThinThreads + t;
+                    reinterpret_cast<uint4 *>(hi + at_run)[p] = *reinterpret_cast<const uint4 *>(stage + ST::acc_addr(p / TH::PIECES, p % TH::PIECES * 8));
+                }
+                acc = TH::gram(acc, stage, wave, lane);
+            } else {
+                uint16_t *o = out + (size_t)mat * s.rows * s.cols;
+                thin_pieces<MP, 1>(s.tall, t, [&](int i, int j0) __attribute__((always_inline)) {
+                    if (row0 + i >= s.longs() || j0 >= s.shorts()) return;
+                    uint16_t v[8];
+                    *reinterpret_cast<uint4 *>(v) = *reinterpret_cast<const uint4 *>(stage + ST::acc_addr(i, j0));
+                    if (s.tall && vec) *reinterpret_cast<uint4 *>(o + (size_t)(row0 + i) * cols + j0) = *reinterpret_cast<const uint4 *>(v);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j0 + j < s.shorts()) o[s.tall ? (size_t)(row0 + i) * cols + j0 + j : (size_t)(j0 + j) * cols + row0 + i] = v[j];
+                });
+            }
+            __syncthreads();                                  // the stage is free for the run after the next
+        }
+        if (step + 1 < first + count) {                       // one workgroup holds the matrix: the next A stays here
+            wait_vm_lgkm0<0>();
+            __syncthreads();                                  // the rows are where the next step finds them; B has been read
+        } else if (!last) TH::store_part(acc, part_out, (size_t)mat * s.chunks + blockIdx.x, wave, lane);
+    }
+}
+
+template <class GT, int MP>
+int thin_run(const ThinShape &s, const ThinWs &w, const GT *g, const float *m_new, float mu, int mode, int n_parts, int steps, float scale, uint16_t *out,
+             hipStream_t stream)
+{
+    using TH = Thin<MP>;
+    static const int limits = raise_lds_limits(TH::LDS, ortho_thin_load_kernel<GT, MP>, ortho_thin_step_kernel<MP>);
+    if (limits != RELIBRA_OK) return limits;
+    const dim3 grid(s.chunks, s.n);
+    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_LOAD, stream, (ortho_thin_load_kernel<GT, MP><<<grid, kThinThreads, TH::STAGE, stream>>>(
+        g, m_new, mu, mode, s, w.parts, n_parts, w.hi, w.lo, w.part[0])));
+    const int each = s.chunks == 1 ? steps : 1, vec = s.cols % 8 == 0 && aligned16(out);
+    for (int i = 0; i < steps; i += each) {
+        const bool summed = s.chunks > kThinDirect;
+        if (summed) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_POLY, stream, ortho_thin_sum_kernel<<<dim3(kThinWaves, s.n), 256, 0, stream>>>(
+            (const float4 *)w.part[i & 1], s.chunks, (float4 *)w.sum));
+        RELIBRA_LAUNCH(RELIBRA_K_ORTHO_THIN, stream, (ortho_thin_step_kernel<MP><<<grid, kThinThreads, TH::LDS, stream>>>(
+            s, i, each, steps, w.hi, w.lo, summed ? w.sum : w.part[i & 1], summed ? 1 : s.chunks, w.part[(i + 1) & 1], scale, vec, out)));
+    }
+    return RELIBRA_OK;
+}
+
+size_t ortho_ws_bytes(int n, int rows, int cols)
+{
+    const size_t parts = round256((size_t)n * norm_parts(n, rows, cols) * sizeof(double));
+    if (is_thin(rows, cols)) {
+        const ThinShape s = thin_shape(n, rows, cols);
+        return parts + 2 * thin_x_bytes(s) + 2 * thin_part_bytes(s) + thin_sum_bytes(s);
+    }
+    const OrthoShape s = ortho_shape(n, rows, cols);
+    return parts + 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + 2 * ortho_diag_bytes(s);
+}
+
+template <class GT>
+int ortho_run(int n, int rows, int cols, const GT *g, const float *m, float mu, float scale, int steps, int mode, float *m_out, uint16_t *out, char *ws, hipStream_t stream)
+{
+    const size_t per_matrix = (size_t)rows * cols;
+    const int n_parts = norm_parts(n, rows, cols);
+    double *parts = (double *)ws;
+    ws += round256((size_t)n * n_parts * sizeof(double));
+    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_NORM, stream, ortho_momentum_kernel<GT><<<dim3(n_parts, n), 256, 0, stream>>>(
+        g, m, mu, mode, per_matrix, m_out, parts));
+    if (is_thin(rows, cols)) {
+        const ThinShape s = thin_shape(n, rows, cols);
+        ThinWs w;
+        w.parts = parts;
+        w.hi = (uint16_t *)ws;
+        w.lo = (uint16_t *)(ws += thin_x_bytes(s));
+        w.part[0] = (float *)(ws += thin_x_bytes(s));
+        w.part[1] = (float *)(ws += thin_part_bytes(s));
+        w.sum = (float *)(ws + thin_part_bytes(s));
+        return s.mp == 64 ? thin_run<GT, 64>(s, w, g, m_out, mu, mode, n_parts, steps, scale, out, stream)
+                          : thin_run<GT, 128>(s, w, g, m_out, mu, mode, n_parts, steps, scale, out, stream);
+    }
+    const OrthoShape s = ortho_shape(n, rows, cols);
+    OrthoWs w;
+    w.x[0] = (uint16_t *)ws;
+    w.x[1] = (uint16_t *)(ws += ortho_x_bytes(s));
+    w.lo = (uint16_t *)(ws += ortho_x_bytes(s));
+    w.a = (uint16_t *)(ws += ortho_x_bytes(s));
+    w.b = (uint16_t *)(ws += ortho_gram_bytes(s));
+    w.da = (float *)(ws += ortho_gram_bytes(s));
+    w.db = (float *)(ws + ortho_diag_bytes(s));
+    const unsigned pieces = (unsigned)((size_t)s.rp * s.cp / 8), blocks = std::min((pieces + 255) / 256, std::max(32u, (4096u + n - 1) / n));
+    RELIBRA_LAUNCH(RELIBRA_K_ORTHO_LOAD, stream, ortho_load_kernel<GT><<<dim3(blocks, n), 256, 0, stream>>>(
+        g, m_out, mu, mode, s, parts, n_parts, w.x[0], w.lo));
+    return ortho_steps(s, w, steps, scale, out, stream);
 }
 
 }  // namespace relibra
@@ -488,25 +932,13 @@ extern "C" int relibra_orthogonalize(const void *grad, const float *momentum, in
     if ((momentum != nullptr) != (momentum_out != nullptr) || (!momentum && (flags & RELIBRA_ORTHO_NESTEROV))) return RELIBRA_EINVAL;
     if (n == 0 || rows == 0 || cols == 0) return RELIBRA_OK;
     if (!grad || !out || out == grad) return RELIBRA_EINVAL;
-    const OrthoShape s = ortho_shape(n, rows, cols);
-    const long long t = 128;
-    if ((long long)n * ((s.rp + t - 1) / t) * ((s.cp + t - 1) / t) > 0x3fffffff) return RELIBRA_EUNSUPPORTED;
+    if ((long long)n * ((rows + 63) / 64) * ((cols + 63) / 64) > 0x3fffffff) return RELIBRA_EUNSUPPORTED;
     if (!workspace || workspace_bytes < ortho_ws_bytes(n, rows, cols)) return RELIBRA_EWORKSPACE;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
-    OrthoWs w;
-    char *p = (char *)workspace;
-    w.x[0] = (uint16_t *)p;
-    w.x[1] = (uint16_t *)(p += ortho_x_bytes(s));
-    w.lo = (uint16_t *)(p += ortho_x_bytes(s));
-    w.a = (uint16_t *)(p += ortho_x_bytes(s));
-    w.b = (uint16_t *)(p += ortho_gram_bytes(s));
-    w.da = (float *)(p += ortho_gram_bytes(s));
-    w.db = (float *)(p += ortho_diag_bytes(s));
-    w.parts = (double *)(p + ortho_diag_bytes(s));
     const int mode = !momentum ? U_GRAD : flags & RELIBRA_ORTHO_NESTEROV ? U_NESTEROV : U_MOMENTUM;
-    if (flags & RELIBRA_ORTHO_BF16) ortho_load(s, w, (const bf16_t *)grad, momentum, mu, mode, momentum_out, stream);
-    else ortho_load(s, w, (const float *)grad, momentum, mu, mode, momentum_out, stream);
-    const int rc = ortho_steps(s, w, steps, scale, (uint16_t *)out, stream);
+    const int rc = flags & RELIBRA_ORTHO_BF16
+                       ? ortho_run(n, rows, cols, (const bf16_t *)grad, momentum, mu, scale, steps, mode, momentum_out, (uint16_t *)out, (char *)workspace, stream)
+                       : ortho_run(n, rows, cols, (const float *)grad, momentum, mu, scale, steps, mode, momentum_out, (uint16_t *)out, (char *)workspace, stream);
     if (rc != RELIBRA_OK) return rc;
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
