@@ -680,7 +680,7 @@ enum {
     RELIBRA_K_WGRAD_ORDER, RELIBRA_K_TRANSPOSE, RELIBRA_K_ROW_TOKENS, RELIBRA_K_ROW_GATES, RELIBRA_K_DGATE_REDUCE,
     RELIBRA_K_REPLICA_PULL, RELIBRA_K_WGRAD_PAIR, RELIBRA_K_PERM_SMALL,
     RELIBRA_K_ROUTER_FWD, RELIBRA_K_ROUTER_FINISH, RELIBRA_K_ROUTER_BWD, RELIBRA_K_NORM_FWD, RELIBRA_K_NORM_BWD, RELIBRA_K_NORM_REDUCE,
-    RELIBRA_K_ORTHO_NORM, RELIBRA_K_ORTHO_LOAD, RELIBRA_K_ORTHO_GRAM, RELIBRA_K_ORTHO_POLY, RELIBRA_K_ORTHO_UPDATE, RELIBRA_K_ORTHO_THIN, RELIBRA_K_COUNT
+    RELIBRA_K_ORTHO_NORM, RELIBRA_K_ORTHO_LOAD, RELIBRA_K_ORTHO_GRAM, RELIBRA_K_ORTHO_POLY, RELIBRA_K_ORTHO_UPDATE, RELIBRA_K_ORTHO_THIN, RELIBRA_K_ORTHO_JOIN, RELIBRA_K_COUNT
 };
 int relibra_prof_start(int level, int max_records);
 int relibra_prof_stop(double *ms_by_kernel_host, int64_t *launches_by_kernel_host);

@@ -43,7 +43,7 @@ KERNELS = ("hist", "perm_count", "perm_scan", "perm_rank", "gather", "combine_fw
            "wgrad_gate_up", "replica_sum", "replica_push", "wgrad_order", "transpose", "row_tokens", "row_gates",
            "dgate_reduce", "replica_pull", "wgrad_pair", "perm_small",
            "router_fwd", "router_finish", "router_bwd", "norm_fwd", "norm_bwd", "norm_reduce",
-           "ortho_norm", "ortho_load", "ortho_gram", "ortho_poly", "ortho_update", "ortho_thin")
+           "ortho_norm", "ortho_load", "ortho_gram", "ortho_poly", "ortho_update", "ortho_thin", "ortho_join")
 
 # Argument types of the calls that are short on the GPU: ctypes then takes plain integers and floats, which costs the host half
 # of what building an object for every argument does.

@@ -43,10 +43,11 @@ struct OrthoShape {
     int rp, cp;                                  // padded
     bool tall;                                   // rows > cols
 };
-// Workspace: two copies of X's first halves (a step reads one and writes the other), the second halves, A, B, their diagonals.
+// Workspace: two copies of X's first halves (a step reads one and writes the other), the second halves, A, B, their diagonals,
+// parts of A where its contraction is split.
 struct OrthoWs {
     uint16_t *x[2], *lo, *a, *b;
-    float *da, *db;
+    float *da, *db, *part;
 };
 inline size_t ortho_x_bytes(const OrthoShape &s) { return round256((size_t)s.n * s.rp * s.cp * 2); }
 inline size_t ortho_gram_bytes(const OrthoShape &s)
@@ -162,16 +163,18 @@ ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, flo
 }
 
 // ---------------------------------------------------------------- products
-// A tile has BB rows (on the lanes) and BA columns (in the accumulator registers); a wave owns 64 rows and BA / WA_ columns.
-template <int BA_, int BB_, int STAGES_, int OCC_, bool DEEP_ = false, int WA_ = 2> struct OrthoCfg {
-    static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = BB / 64, THREADS = WA * WB * 64, STAGES = STAGES_;
+// A tile has BB rows (on the lanes) and BA columns (in the accumulator registers); a wave owns 64 rows and COLS columns.  ADEPTH, BDEPTH: values
+// of the contraction in an LDS tile of the column and of the row operand.
+template <int BA_, int BB_, int STAGES_, int OCC_, int ADEPTH_ = BK, int BDEPTH_ = ADEPTH_> struct OrthoCfg {
+    static constexpr int BA = BA_, BB = BB_, WA = 2, WB = BB / 64, THREADS = WA * WB * 64, STAGES = STAGES_;
     static constexpr int COLS = BA / WA;                             // of a wave
-    static constexpr int BDEPTH = DEEP_ ? 2 * BK : BK;               // of the row operand's LDS tiles
+    static constexpr int ADEPTH = ADEPTH_, BDEPTH = BDEPTH_;
     static constexpr int WAVES_PER_SIMD = OCC_ * WA * WB / 4;        // OCC_: workgroups per compute unit
-    static constexpr int SLABS = STAGES * (BA + (DEEP_ ? 0 : BB)) * BK * 2 + (DEEP_ ? (STAGES + 3) / 2 * BB * BDEPTH * 2 : 0);
+    static constexpr bool DEEP = BDEPTH == 2 * ADEPTH;               // the row operand's tiles have a ring of their own
+    static constexpr int SLABS = STAGES * (BA + (DEEP ? 0 : BB)) * ADEPTH * 2 + (DEEP ? (STAGES + 3) / 2 * BB * BDEPTH * 2 : 0);
     static constexpr int STAGING = WA * WB * 2 * WaveStage<64>::BYTES;
     static constexpr int LDS = SLABS > STAGING ? SLABS : STAGING;
-    template <class AT> using Loop = KLoop<AT, KcTile<BB, BDEPTH>, 1, 1, BA, BB, WA, WB, 1, false, STAGES, true, false, false, true>;
+    template <class AT, class BT = KcTile<BB, BDEPTH>> using Loop = KLoop<AT, BT, 1, 1, BA, BB, WA, WB, 1, false, STAGES, true, false, false, true>;
 };
 
 __device__ __forceinline__ uint2 pack4h(const float (&v)[4])
@@ -200,88 +203,162 @@ __device__ __forceinline__ int xcd_tile(int block, int total)
 // Tiles that hold anything on or below the diagonal, row block after row block; of these the 64 x 64 blocks on or below it are
 // stored, those below a second time with rows and columns exchanged, read back from the staging area by transposing LDS reads.
 template <class CF> __host__ __device__ constexpr int gram_tiles_of_row(int i) { return ((i + 1) * CF::BB - 1) / CF::BA + 1; }
-template <class CF, bool ACROSS, bool POLY>
-__global__ void __launch_bounds__(CF::THREADS, CF::WAVES_PER_SIMD)
-ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag_in, int m, int k, int per_matrix, int total, uint16_t *__restrict__ out,
-                  float *__restrict__ diag_out)
+// Tile (i, j) of the triangle: which rows and columns.
+template <class CF> __device__ __forceinline__ void gram_tile(int tile, int &row0, int &col0)
 {
-    using KL = typename std::conditional<ACROSS, KLoop<KsTile<CF::BA>, KsTile<CF::BB>, 1, 1, CF::BA, CF::BB, CF::WA, CF::WB, 1, false, CF::STAGES, true, false, false, true>,
-                                         typename CF::template Loop<KcTile<CF::BA>>>::type;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int t = xcd_tile(blockIdx.x, total);
-    if (t < 0) return;
-    const int mat = t / per_matrix;
-    int i = 0, j = t % per_matrix;
-    while (j >= gram_tiles_of_row<CF>(i)) j -= gram_tiles_of_row<CF>(i++);
-    const uint16_t *src = p + (size_t)mat * m * k;
-    uint16_t *dst = out + (size_t)mat * m * m;
-    const int ld = ACROSS ? m : k, row0 = i * CF::BB, col0 = j * CF::BA;
-    const Operand A[1][1] = {{{src, ld, col0, m - 1}}}, B[1][1] = {{{src, ld, row0, m - 1}}};
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    typename KL::Acc acc;
-    KL::zero(acc);
-    KL::run(acc, A, B, k / BK, k, lds, tid);
-    __syncthreads();                                          // every wave is done with the operand slabs
+    int i = 0;
+    while (tile >= gram_tiles_of_row<CF>(i)) tile -= gram_tiles_of_row<CF>(i++);
+    row0 = i * CF::BB;
+    col0 = tile * CF::BA;
+}
+// A wave's 64 x 64 block of sums (rows wrow0.., columns wcol0.. at most as far) to halves, diagonal apart, stored in both triangles.  buf: two
+// staging areas.  src, din: P and its diagonal (POLY).
+template <bool POLY>
+__device__ __forceinline__ void gram_block(const f32x16_t (*sums)[2], char *buf, const uint16_t *src, const float *din, int m, int wrow0, int wcol0, uint16_t *dst,
+                                           float *dout, int lane)
+{
     using ST = WaveStage<64>;
-    char *buf = lds + wave * 2 * ST::BYTES;
+    float d_r[2] = {0.0f, 0.0f}, d_c[2][4][4];
+    if (POLY) {
+#pragma unroll
+        for (int ta = 0; ta < 2; ++ta)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4 *>(d_c[ta][q]) = *reinterpret_cast<const float4 *>(din + wcol0 + ta * 32 + q * 8 + (lane >> 5) * 4);
+        ST::fill(buf, src, m, wrow0, m, wcol0, m, lane);
+        d_r[0] = din[wrow0 + (lane & 31)];
+        d_r[1] = din[wrow0 + 32 + (lane & 31)];
+        wave_lds_fence();
+    }
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+        for (int ta = 0; ta < 2; ++ta)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = tb * 32 + (lane & 31), c = ta * 32 + q * 8 + (lane >> 5) * 4;
+                float v[4], old[4];
+                if (POLY) unpack4h(ST::get(buf, r, c), old);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float s = sums[ta][tb][q * 4 + e];
+                    v[e] = POLY ? kNsB * old[e] + (kNsC / kScale) * (s + (d_r[tb] + d_c[ta][q][e]) * old[e]) : s * (1.0f / kScale);
+                    if (wrow0 == wcol0 && r == c + e) {
+                        dout[wrow0 + r] = POLY ? kNsB * d_r[tb] + (kNsC / kScale) * (s + d_r[tb] * d_r[tb]) : v[e];
+                        v[e] = 0.0f;
+                    }
+                }
+                ST::put(buf, r, c, pack4h(v));
+            }
+    wave_lds_fence();
+    ST::flush(buf, dst, m, wrow0, m, wcol0, m, lane);
+    if (wrow0 != wcol0) {
+        char *turned = buf + ST::BYTES;
+#pragma unroll
+        for (int r0 = 0; r0 < 64; r0 += 32)               // rows of the exchanged block: columns r0 .. r0 + 31 of the staged one
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                const int bq = lane >> 4, iq = lane & 15;
+                const int c = r0 + (bq & 1) * 16 + (iq & 3) * 4, r = kk * 16 + (bq >> 1) * 8 + (iq >> 2);
+                const s16x4_t l = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(buf + ST::acc_addr(r, c)));
+                const s16x4_t h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(buf + ST::acc_addr(r + 4, c)));
+                const s16x8_t v = __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+                *reinterpret_cast<s16x8_t *>(turned + ST::acc_addr(r0 + (lane & 31), kk * 16 + (lane >> 5) * 8)) = v;
+            }
+        wave_lds_fence();
+        ST::flush(turned, dst, m, wcol0, m, wrow0, m, lane);
+    }
+    wave_lds_fence();
+}
+template <class CF, bool POLY, class Acc>
+__device__ __forceinline__ void gram_epilogue(const Acc &acc, char *lds, const uint16_t *src, const float *din, int m, int row0, int col0, uint16_t *dst, float *dout)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __syncthreads();                                          // every wave is done with the operand slabs
+    char *buf = lds + wave * 2 * WaveStage<64>::BYTES;
     const int wrow0 = row0 + (wave % CF::WB) * 64;
 #pragma unroll
     for (int half = 0; half < CF::COLS / 64; ++half) {
         const int wcol0 = col0 + (wave / CF::WB) * CF::COLS + half * 64;
         if (wrow0 >= m || wcol0 > wrow0) break;               // uniform in the wave; padding is in whole runs of 64
-        const float *din = diag_in + (size_t)mat * m;
-        float d_r[2] = {0.0f, 0.0f}, d_c[2][4][4];
-        if (POLY) {
+        gram_block<POLY>(&acc[0][half * 2], buf, src, din, m, wrow0, wcol0, dst, dout, lane);
+    }
+}
+template <class CF, bool ACROSS, bool POLY>
+__global__ void __launch_bounds__(CF::THREADS, CF::WAVES_PER_SIMD)
+ortho_gram_kernel(const uint16_t *__restrict__ p, const float *__restrict__ diag_in, int m, int k, int per_matrix, int total, int splits, int k_split,
+                  uint16_t *__restrict__ out, float *__restrict__ diag_out, float *__restrict__ part)
+{
+    using KL = typename std::conditional<ACROSS, typename CF::template Loop<KsTile<CF::BA, CF::ADEPTH>, KsTile<CF::BB, CF::ADEPTH>>,
+                                         typename CF::template Loop<KcTile<CF::BA, CF::ADEPTH>>>::type;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int t = xcd_tile(blockIdx.x, total);
+    if (t < 0) return;
+    const int tile = t / splits, split = t % splits, mat = tile / per_matrix;
+    int row0, col0;
+    gram_tile<CF>(tile % per_matrix, row0, col0);
+    const uint16_t *src = p + (size_t)mat * m * k;
+    const int ld = ACROSS ? m : k, k0 = split * k_split, depth = min(k - k0, k_split);
+    const uint16_t *from = src + (ACROSS ? (size_t)k0 * m : (size_t)k0);
+    const Operand A[1][1] = {{{from, ld, col0, m - 1}}}, B[1][1] = {{{from, ld, row0, m - 1}}};
+    typename KL::Acc acc;
+    KL::zero(acc);
+    KL::run(acc, A, B, depth / CF::ADEPTH, depth, lds, threadIdx.x);
+    if (!POLY && splits > 1) {
+        float4 *to = reinterpret_cast<float4 *>(part) + ((size_t)t * CF::THREADS / 64 + (threadIdx.x >> 6)) * CF::COLS / 32 * 2 * 4 * 64 + (threadIdx.x & 63);
 #pragma unroll
-            for (int ta = 0; ta < 2; ++ta)
+        for (int ta = 0; ta < CF::COLS / 32; ++ta)
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    *reinterpret_cast<float4 *>(d_c[ta][q]) = *reinterpret_cast<const float4 *>(din + wcol0 + ta * 32 + q * 8 + (lane >> 5) * 4);
-            ST::fill(buf, src, m, wrow0, m, wcol0, m, lane);
-            d_r[0] = din[wrow0 + (lane & 31)];
-            d_r[1] = din[wrow0 + 32 + (lane & 31)];
-            wave_lds_fence();
-        }
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-            for (int ta = 0; ta < 2; ++ta)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int r = tb * 32 + (lane & 31), c = ta * 32 + q * 8 + (lane >> 5) * 4;
-                    float v[4], old[4];
-                    if (POLY) unpack4h(ST::get(buf, r, c), old);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float s = acc[0][half * 2 + ta][tb][q * 4 + e];
-                        v[e] = POLY ? kNsB * old[e] + (kNsC / kScale) * (s + (d_r[tb] + d_c[ta][q][e]) * old[e]) : s * (1.0f / kScale);
-                        if (wrow0 == wcol0 && r == c + e) {
-                            diag_out[(size_t)mat * m + wrow0 + r] = POLY ? kNsB * d_r[tb] + (kNsC / kScale) * (s + d_r[tb] * d_r[tb]) : v[e];
-                            v[e] = 0.0f;
-                        }
-                    }
-                    ST::put(buf, r, c, pack4h(v));
-                }
-        wave_lds_fence();
-        ST::flush(buf, dst, m, wrow0, m, wcol0, m, lane);
-        if (wrow0 != wcol0) {
-            char *turned = buf + ST::BYTES;
-#pragma unroll
-            for (int r0 = 0; r0 < 64; r0 += 32)               // rows of the exchanged block: columns r0 .. r0 + 31 of the staged one
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    const int bq = lane >> 4, iq = lane & 15;
-                    const int c = r0 + (bq & 1) * 16 + (iq & 3) * 4, r = kk * 16 + (bq >> 1) * 8 + (iq >> 2);
-                    const s16x4_t l = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(buf + ST::acc_addr(r, c)));
-                    const s16x4_t h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(buf + ST::acc_addr(r + 4, c)));
-                    const s16x8_t v = __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
-                    *reinterpret_cast<s16x8_t *>(turned + ST::acc_addr(r0 + (lane & 31), kk * 16 + (lane >> 5) * 8)) = v;
-                }
-            wave_lds_fence();
-            ST::flush(turned, dst, m, wcol0, m, wrow0, m, lane);
-        }
-        wave_lds_fence();
+                    to[((ta * 2 + tb) * 4 + q) * 64] = make_float4(acc[0][ta][tb][4 * q], acc[0][ta][tb][4 * q + 1], acc[0][ta][tb][4 * q + 2], acc[0][ta][tb][4 * q + 3]);
+        return;
     }
+    gram_epilogue<CF, POLY>(acc, lds, src, POLY ? diag_in + (size_t)mat * m : nullptr, m, row0, col0, out + (size_t)mat * m * m, diag_out + (size_t)mat * m);
+}
+
+// A 64 x 64 block of A (one wave's of a tile) from the parts of a split contraction: wave w adds up parts w, w + 4, .., then the first
+// wave the four sums, always in this order.  (One workgroup a tile took 15 to 30 us: nothing but a wave's own loads in flight.)
+template <class CF>
+__global__ void __launch_bounds__(256)
+ortho_join_kernel(const float *__restrict__ part, int m, int per_matrix, int splits, uint16_t *__restrict__ out, float *__restrict__ diag_out)
+{
+    static_assert(CF::COLS == 64, "a wave's block");
+    constexpr int WAVES = CF::WA * CF::WB;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * 16 * 1024];
+    const int tile = blockIdx.x / WAVES, of = blockIdx.x % WAVES, mat = tile / per_matrix, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int row0, col0;
+    gram_tile<CF>(tile % per_matrix, row0, col0);
+    const int wrow0 = row0 + of % CF::WB * 64, wcol0 = col0 + of / CF::WB * 64;
+    if (wrow0 >= m || wcol0 > wrow0) return;
+    f32x16_t sums[2][2];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) sums[i >> 5][(i >> 4) & 1][i & 15] = 0.0f;
+    auto add = [&](const float4 *from) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float4 v = from[i * 64 + lane];
+            f32x16_t &to = sums[i >> 3][(i >> 2) & 1];
+            to[4 * (i & 3)] += v.x;
+            to[4 * (i & 3) + 1] += v.y;
+            to[4 * (i & 3) + 2] += v.z;
+            to[4 * (i & 3) + 3] += v.w;
+        }
+    };
+#pragma unroll 2
+    for (int s = wave; s < splits; s += 4) add(reinterpret_cast<const float4 *>(part) + (((size_t)tile * splits + s) * WAVES + of) * 16 * 64);
+    float4 *mine = reinterpret_cast<float4 *>(lds + wave * 16 * 1024);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const f32x16_t &v = sums[i >> 3][(i >> 2) & 1];
+        mine[i * 64 + lane] = make_float4(v[4 * (i & 3)], v[4 * (i & 3) + 1], v[4 * (i & 3) + 2], v[4 * (i & 3) + 3]);
+    }
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < 4; ++w) add(reinterpret_cast<const float4 *>(lds + w * 16 * 1024));
+    wave_lds_fence();
+    gram_block<false>(&sums[0], lds, nullptr, nullptr, m, wrow0, wcol0, out + (size_t)mat * m * m, diag_out + (size_t)mat * m, lane);
 }
 
 // X' = (a + d) hi + (a + w d) lo + B hi, d the diagonal of B kept apart.  Wide: X [m, n], B from the left, its rows on the lanes, X's
@@ -297,7 +374,7 @@ __global__ void __launch_bounds__(CF::THREADS, CF::WAVES_PER_SIMD)
 ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t *__restrict__ bmat, const float *__restrict__ diag, float w, OrthoShape s,
                     int tiles_r, int tiles_c, int total, uint16_t *__restrict__ x_out, OrthoLast last)
 {
-    using KL = typename CF::template Loop<typename std::conditional<TALL, KcTile<CF::BA>, KsTile<CF::BA>>::type>;
+    using KL = typename CF::template Loop<typename std::conditional<TALL, KcTile<CF::BA, CF::ADEPTH>, KsTile<CF::BA, CF::ADEPTH>>::type>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int t = xcd_tile(blockIdx.x, total);
     if (t < 0) return;
@@ -312,7 +389,7 @@ ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     typename KL::Acc acc;
     KL::zero(acc);
-    KL::run(acc, A, B, m / BK, m, lds, tid);
+    KL::run(acc, A, B, m / CF::ADEPTH, m, lds, tid);
     __syncthreads();                                          // every wave is done with the operand slabs
     using ST = WaveStage<64>;
     char *buf_h = lds + wave * 2 * ST::BYTES, *buf_l = buf_h + ST::BYTES;
@@ -389,14 +466,22 @@ template <class CF> int gram_tiles(int n, int m)
     for (int i = 0; i * CF::BB < m; ++i) per_matrix += gram_tiles_of_row<CF>(i);
     return n * per_matrix;
 }
-template <class CF, bool ACROSS, bool POLY>
-int launch_gram(const uint16_t *p, const float *diag_in, int n, int m, int k, uint16_t *out, float *diag_out, hipStream_t stream)
+struct GramSplit {
+    int splits, depth;                           // parts of the contraction, values of each but the last (whole LDS tiles)
+    float *part;
+};
+template <class CF, bool ACROSS, bool POLY, bool MAY_SPLIT = false>
+int launch_gram(const uint16_t *p, const float *diag_in, int n, int m, int k, const GramSplit &sp, uint16_t *out, float *diag_out, hipStream_t stream)
 {
     static const int limits = raise_lds_limits(CF::LDS, ortho_gram_kernel<CF, ACROSS, POLY>);
     if (limits != RELIBRA_OK) return limits;
-    const int per_matrix = gram_tiles<CF>(1, m);
+    const int per_matrix = gram_tiles<CF>(1, m), tiles = n * per_matrix, total = tiles * sp.splits;
     RELIBRA_LAUNCH(POLY ? RELIBRA_K_ORTHO_POLY : RELIBRA_K_ORTHO_GRAM, stream, (ortho_gram_kernel<CF, ACROSS, POLY>
-        <<<xcd_grid((long long)n * per_matrix), CF::THREADS, CF::LDS, stream>>>(p, diag_in, m, k, per_matrix, n * per_matrix, out, diag_out)));
+        <<<xcd_grid(total), CF::THREADS, CF::LDS, stream>>>(p, diag_in, m, k, per_matrix, total, sp.splits, sp.depth, out, diag_out, sp.part)));
+    if constexpr (MAY_SPLIT)
+        if (sp.splits > 1) {
+            RELIBRA_LAUNCH(RELIBRA_K_ORTHO_JOIN, stream, (ortho_join_kernel<CF><<<tiles * CF::WA * CF::WB, 256, 0, stream>>>(sp.part, m, per_matrix, sp.splits, out, diag_out)));
+        }
     return RELIBRA_OK;
 }
 template <class CF, bool TALL>
@@ -411,9 +496,10 @@ int launch_update(const OrthoShape &s, const OrthoWs &w, const uint16_t *x, uint
 }
 
 typedef OrthoCfg<256, 256, 4, 1> OrthoWide;
-typedef OrthoCfg<256, 256, 3, 1, true> OrthoWideDeep;
+typedef OrthoCfg<256, 256, 3, 1, BK, 2 * BK> OrthoWideDeep;
 typedef OrthoCfg<128, 128, 4, 2> OrthoNarrow;
-typedef OrthoCfg<128, 64, 4, 2> OrthoFlat;
+typedef OrthoCfg<128, 128, 3, 1, 2 * BK> OrthoFew;
+typedef OrthoCfg<128, 64, 3, 2, 2 * BK> OrthoFlat;
 
 template <class CF> int update_tiles(const OrthoShape &s) { return s.n * ((s.rp + CF::BB - 1) / CF::BB) * ((s.cp + CF::BA - 1) / CF::BA); }
 
@@ -424,15 +510,40 @@ template <class CF> int update_tiles(const OrthoShape &s) { return s.n * ((s.rp 
 // many rows again (128 x 64) where X' has few tiles: 5 of 1001 x 333 (120 of 128 x 128) 15.3 -> 13.2, 8 of 512 x 512 (128) 13.9 -> 12.7, 2048 x 2048
 // (256) 32.9 -> 34.4.
 constexpr int kEnoughWideTiles = 112, kFewNarrowTiles = 192;
+// Where even the small tiles are no more than the compute units, LDS tiles of twice the depth (half the barriers, a workgroup to
+// itself): us a call, 2048 x 2048 375 -> 322, 2 of 1000 x 3000 348 -> 324, 300 x 4000 278 -> 225, level at 8 of 512 x 512; with more tiles the second workgroup of a
+// unit is worth more, 16 of 768 x 2048 695 -> 716.  A long contraction of few tiles is split over the idle units besides, each part at
+// least kMinSplit deep, and joined by a second launch: 300 x 4000 222 -> 168, 4 of 3000 x 200 208 -> 177, 2 of 300 x 2000 176 -> 162, level at 2 of 1000 x
+// 3000 and 8 of 200 x 2048; contractions of 1024 that way: 8 of 256 x 1024 140 -> 155, 5 of 1001 x 333 166 -> 182.
+constexpr int kMinSplit = 512, kSplitFrom = 2048;
+inline GramSplit gram_split(int n, int m, int k)
+{
+    const int tiles = gram_tiles<OrthoFew>(n, m);
+    if (gram_tiles<OrthoWide>(n, m) >= kEnoughWideTiles || k < kSplitFrom || 2 * tiles > kComputeUnits) return GramSplit{1, k, nullptr};
+    const int splits = std::min(kComputeUnits / tiles, k / kMinSplit);
+    const int depth = ((k + splits - 1) / splits + OrthoFew::ADEPTH - 1) / OrthoFew::ADEPTH * OrthoFew::ADEPTH;
+    return GramSplit{(k + depth - 1) / depth, depth, nullptr};
+}
+inline size_t ortho_split_bytes(const OrthoShape &s)
+{
+    const int m = s.tall ? s.cp : s.rp, k = s.tall ? s.rp : s.cp;
+    const GramSplit sp = gram_split(s.n, m, k);
+    return sp.splits > 1 ? round256((size_t)gram_tiles<OrthoFew>(s.n, m) * sp.splits * OrthoFew::BA * OrthoFew::BB * sizeof(float)) : 0;
+}
 
 int ortho_steps(const OrthoShape &s, const OrthoWs &w, int steps, float scale, uint16_t *out, hipStream_t stream)
 {
     const int m = s.tall ? s.cp : s.rp, k = s.tall ? s.rp : s.cp;
     const bool wide_gram = gram_tiles<OrthoWide>(s.n, m) >= kEnoughWideTiles, wide_update = update_tiles<OrthoWideDeep>(s) >= kEnoughWideTiles;
-    const bool flat_update = update_tiles<OrthoNarrow>(s) <= kFewNarrowTiles;
-    auto gram = [&](auto across, auto poly, const uint16_t *p, const float *d, int depth, uint16_t *out_, float *d_out) {
-        return wide_gram ? launch_gram<OrthoWide, decltype(across)::value, decltype(poly)::value>(p, d, s.n, m, depth, out_, d_out, stream)
-                         : launch_gram<OrthoNarrow, decltype(across)::value, decltype(poly)::value>(p, d, s.n, m, depth, out_, d_out, stream);
+    const bool few_gram = gram_tiles<OrthoFew>(s.n, m) <= kComputeUnits, flat_update = update_tiles<OrthoNarrow>(s) <= kFewNarrowTiles;
+    const GramSplit whole{1, m, nullptr};
+    GramSplit split = gram_split(s.n, m, k);
+    split.part = w.part;
+    auto gram = [&](auto across, auto poly, const uint16_t *p, const float *d, int depth, const GramSplit &sp, uint16_t *out_, float *d_out) {
+        constexpr bool AC = decltype(across)::value, PO = decltype(poly)::value;
+        return wide_gram ? launch_gram<OrthoWide, AC, PO>(p, d, s.n, m, depth, sp, out_, d_out, stream)
+               : few_gram ? launch_gram<OrthoFew, AC, PO, !PO>(p, d, s.n, m, depth, sp, out_, d_out, stream)
+                          : launch_gram<OrthoNarrow, AC, PO>(p, d, s.n, m, depth, sp, out_, d_out, stream);
     };
     for (int i = 0; i < steps; ++i) {
         const uint16_t *x = w.x[i & 1];
@@ -445,8 +556,9 @@ int ortho_steps(const OrthoShape &s, const OrthoWs &w, int steps, float scale, u
                    : flat_update ? launch_update<OrthoFlat, T>(s, w, x, x_out, weight, last, stream)
                                  : launch_update<OrthoNarrow, T>(s, w, x, x_out, weight, last, stream);
         };
-        int rc = s.tall ? gram(std::true_type{}, std::false_type{}, x, nullptr, k, w.a, w.da) : gram(std::false_type{}, std::false_type{}, x, nullptr, k, w.a, w.da);
-        if (rc == RELIBRA_OK) rc = gram(std::false_type{}, std::true_type{}, w.a, w.da, m, w.b, w.db);
+        int rc = s.tall ? gram(std::true_type{}, std::false_type{}, x, nullptr, k, split, w.a, w.da)
+                        : gram(std::false_type{}, std::false_type{}, x, nullptr, k, split, w.a, w.da);
+        if (rc == RELIBRA_OK) rc = gram(std::false_type{}, std::true_type{}, w.a, w.da, m, whole, w.b, w.db);
         if (rc == RELIBRA_OK) rc = s.tall ? update(std::true_type{}) : update(std::false_type{});
         if (rc != RELIBRA_OK) return rc;
     }
@@ -880,7 +992,7 @@ size_t ortho_ws_bytes(int n, int rows, int cols)
         return parts + 2 * thin_x_bytes(s) + 2 * thin_part_bytes(s) + thin_sum_bytes(s);
     }
     const OrthoShape s = ortho_shape(n, rows, cols);
-    return parts + 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + 2 * ortho_diag_bytes(s);
+    return parts + 3 * ortho_x_bytes(s) + 2 * ortho_gram_bytes(s) + 2 * ortho_diag_bytes(s) + ortho_split_bytes(s);
 }
 
 template <class GT>
@@ -912,7 +1024,8 @@ int ortho_run(int n, int rows, int cols, const GT *g, const float *m, float mu, 
     w.a = (uint16_t *)(ws += ortho_x_bytes(s));
     w.b = (uint16_t *)(ws += ortho_gram_bytes(s));
     w.da = (float *)(ws += ortho_gram_bytes(s));
-    w.db = (float *)(ws + ortho_diag_bytes(s));
+    w.db = (float *)(ws += ortho_diag_bytes(s));
+    w.part = (float *)(ws + ortho_diag_bytes(s));
     const unsigned pieces = (unsigned)((size_t)s.rp * s.cp / 8), blocks = std::min((pieces + 255) / 256, std::max(32u, (4096u + n - 1) / n));
     RELIBRA_LAUNCH(RELIBRA_K_ORTHO_LOAD, stream, ortho_load_kernel<GT><<<dim3(blocks, n), 256, 0, stream>>>(
         g, m_out, mu, mode, s, parts, n_parts, w.x[0], w.lo));

@@ -49,7 +49,8 @@ def close(got, want, tol=TOL):
 
 SHAPES = [(1, 1, 1), (3, 1, 7), (2, 9, 1), (2, 64, 64), (1, 63, 65), (4, 128, 256), (3, 256, 128), (2, 257, 130), (1, 300, 1000), (1, 1001, 333), (2, 512, 520), (1, 640, 576),
           (9, 320, 257), (1, 40, 4100), (1, 4100, 24), (70, 33, 47), (1, 1100, 1030),
-          (3, 128, 1000), (2, 700, 127), (40, 128, 520), (200, 300, 64), (1, 65, 9000), (600, 16, 40), (5, 129, 128), (2, 128, 128)]
+          (3, 128, 1000), (2, 700, 127), (40, 128, 520), (200, 300, 64), (1, 65, 9000), (600, 16, 40), (5, 129, 128), (2, 128, 128),
+          (1, 200, 2500), (3, 2049, 150), (1, 260, 5000), (2, 8200, 140)]
 
 
 @gpu
