@@ -18,7 +18,7 @@
 
 namespace relibra {
 
-constexpr int kNormMaxWaves = 16;
+constexpr int kNormMaxWaves = 16, kComputeUnits = 256;
 constexpr int kNormMaxWidth = kNormMaxWaves * 64 * 8;      // 16 waves of one piece a lane, or 8 of two
 
 struct NormShape {
@@ -246,36 +246,66 @@ norm_bwd_kernel(NormShape sh, const XT *__restrict__ x_out, const XT *__restrict
             }
         }
     }
-    const size_t part = ((size_t)blockIdx.x * sh.rows_per_block + slot) * h;
+    // the block's row groups, in ascending order: one partial row a block
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    float *join = reinterpret_cast<float *>(smem);            // [rows_per_block - 1][h]
+    auto leave = [&](const float (&acc)[CH][8], float *to) __attribute__((always_inline)) {
+        if (!to) return;
+        __syncthreads();
+        if (slot > 0)
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int at = c * lanes + pos;
-        if (at < pieces) {
-            if (part_post) store8(part_post + part + at * 8, acc2[c]);
-            if (part_pre) store8(part_pre + part + at * 8, acc1[c]);
-        }
-    }
+            for (int c = 0; c < CH; ++c)
+                if (c * lanes + pos < pieces) store8(join + (size_t)(slot - 1) * h + (c * lanes + pos) * 8, acc[c]);
+        __syncthreads();
+        if (slot == 0)
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (c * lanes + pos < pieces) {
+                    float sum[8], v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] = acc[c][j];
+                    for (int r = 1; r < sh.rows_per_block; ++r) {
+                        load8(join + (size_t)(r - 1) * h + (c * lanes + pos) * 8, v);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum[j] += v[j];
+                    }
+                    store8(to + (size_t)blockIdx.x * h + (c * lanes + pos) * 8, sum);
+                }
+    };
+    leave(acc2, part_post);
+    leave(acc1, part_pre);
 }
 
-// dw (+)= the sum of P partial rows: 32 columns a block, 32 strips of rows, joined in ascending order.
-__global__ void __launch_bounds__(256)
+// dw (+)= the sum of P partial rows: 32 columns a block, 128 strips of rows, joined in ascending order.
+constexpr int kReduceStrips = 128;
+__global__ void __launch_bounds__(kReduceStrips * 8)
 norm_reduce_kernel(const float *__restrict__ part0, const float *__restrict__ part1, float *__restrict__ dw0, float *__restrict__ dw1, int P, int h, int add)
 {
-    __shared__ float4 join[32][8];
+    __shared__ float4 join[kReduceStrips][8];
     const float *part = blockIdx.y ? part1 : part0;
     float *dw = blockIdx.y ? dw1 : dw0;
     if (!dw) return;
     const int col = threadIdx.x & 7, strip = threadIdx.x >> 3, at = blockIdx.x * 32 + col * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (at < h)
-        for (int p = strip; p < P; p += 32) {
+#pragma unroll 4
+        for (int p = strip; p < P; p += kReduceStrips) {
             const float4 v = *reinterpret_cast<const float4 *>(part + (size_t)p * h + at);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
     join[strip][col] = s;
     __syncthreads();
+    // 128 strips to 8, then one thread a column the rest
+    if (strip < 8) {
+        for (int i = strip + 8; i < kReduceStrips; i += 8) {
+            const float4 v = join[i][col];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        join[strip][col] = s;
+    }
+    __syncthreads();
     if (strip == 0 && at < h) {
-        for (int i = 1; i < 32; ++i) {
+        for (int i = 1; i < 8; ++i) {
             const float4 v = join[i][col];
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
@@ -291,22 +321,31 @@ norm_reduce_kernel(const float *__restrict__ part0, const float *__restrict__ pa
 struct NormGrid {
     int chunks, waves, rows_per_block, blocks;
 };
+// Forward: two pieces a lane, four waves a block, 16 waves a unit, half of them where a block then still has 16 rounds; few rows are
+// latency and get twice the waves instead.  us, 16384 rows of 4096 in bf16 at 16 / 8 waves a unit 102 / 98, 4096 of 2048 12.2 / 13.4; 700 of
+// 8192 in fp32 with one / two pieces 16.3 / 14.5.
+// Backward: one piece a lane (two take 173 registers instead of 110: half the waves), eight waves a block, 16 a unit: 16384 rows of 4096
+// 157 us, with 8 waves a unit 200, 32 167; with two pieces and four waves a block 176.  The row groups of a block are joined in LDS: with a
+// partial row each the second kernel took longer than the first, 8000 rows of 512 56 -> 16 us, 4096 of 2048 48 -> 25.
 inline NormGrid norm_grid(int T, int h, bool bwd)
 {
     NormGrid g;
     const int pieces = h / 8;
-    g.chunks = pieces <= 64 || (T < 1024 && pieces <= 64 * kNormMaxWaves) ? 1 : 2;
+    g.chunks = bwd || pieces <= 64 || T < 256 ? 1 : 2;
     g.waves = (pieces + 64 * g.chunks - 1) / (64 * g.chunks);
-    g.rows_per_block = g.waves >= 4 ? 1 : 4 / g.waves;
-    const int want = 256 * std::max(1, 16 / (g.waves * g.rows_per_block));
-    g.blocks = std::max(1, std::min((T + g.rows_per_block - 1) / g.rows_per_block, want));
-    (void)bwd;
+    const int block_waves = bwd ? 8 : 4;
+    g.rows_per_block = g.waves >= block_waves ? 1 : block_waves / g.waves;
+    const int groups = (T + g.rows_per_block - 1) / g.rows_per_block;
+    int want = kComputeUnits * std::max(1, 16 / (g.waves * g.rows_per_block));
+    if (!bwd && groups >= 16 * want) want = std::max(kComputeUnits, want / 2);
+    g.blocks = std::max(1, std::min(groups, want));
     return g;
 }
+inline size_t norm_join_bytes(const NormGrid &g, int h) { return (size_t)(g.rows_per_block - 1) * h * sizeof(float); }
 size_t norm_ws_bytes(int T, int h)
 {
     const NormGrid g = norm_grid(T, h, true);
-    return 2 * round256((size_t)g.blocks * g.rows_per_block * h * sizeof(float));
+    return 2 * round256((size_t)g.blocks * h * sizeof(float));
 }
 
 inline int check_norm(int T, int h, int flags, int known, float eps)
@@ -318,21 +357,23 @@ inline int check_norm(int T, int h, int flags, int known, float eps)
 }
 inline int gate_kind(int flags) { return flags & RELIBRA_NORM_GATE_TOKEN ? GATE_TOKEN : flags & RELIBRA_NORM_GATE_ELEMENT ? GATE_ELEMENT : GATE_NONE; }
 
-template <class Fn> int norm_layout(int chunks, int gate, const Fn &fn)
+template <bool TWO, class Fn> int norm_layout(int chunks, int gate, const Fn &fn)
 {
     auto with_gate = [&](auto ch) {
         if (gate == GATE_TOKEN) return fn(ch, std::integral_constant<int, GATE_TOKEN>{});
         if (gate == GATE_ELEMENT) return fn(ch, std::integral_constant<int, GATE_ELEMENT>{});
         return fn(ch, std::integral_constant<int, GATE_NONE>{});
     };
-    return chunks == 1 ? with_gate(std::integral_constant<int, 1>{}) : with_gate(std::integral_constant<int, 2>{});
+    if constexpr (TWO)
+        if (chunks == 2) return with_gate(std::integral_constant<int, 2>{});
+    return with_gate(std::integral_constant<int, 1>{});
 }
 
 template <class XT>
 int norm_fwd_impl(const XT *x, const bf16_t *y, const bf16_t *w_post, const bf16_t *w_pre, const void *gate, int gkind, const NormShape &sh, const NormGrid &g,
                   XT *x_out, bf16_t *n, hipStream_t stream)
 {
-    return norm_layout(g.chunks, gkind, [&](auto ch, auto gk) {
+    return norm_layout<true>(g.chunks, gkind, [&](auto ch, auto gk) {
         RELIBRA_LAUNCH(RELIBRA_K_NORM_FWD, stream, (norm_fwd_kernel<XT, decltype(ch)::value, decltype(gk)::value>
             <<<g.blocks, g.waves * g.rows_per_block * 64, 0, stream>>>(sh, x, y, w_post, w_pre, gate, x_out, n)));
         return RELIBRA_OK;
@@ -342,9 +383,9 @@ template <class XT>
 int norm_bwd_impl(const XT *x_out, const XT *dx_out, const bf16_t *dn, const bf16_t *y, const bf16_t *w_post, const bf16_t *w_pre, const void *gate, int gkind,
                   const NormShape &sh, const NormGrid &g, XT *dx, bf16_t *dy, void *dgate, float *part_post, float *part_pre, hipStream_t stream)
 {
-    return norm_layout(g.chunks, gkind, [&](auto ch, auto gk) {
+    return norm_layout<false>(g.chunks, gkind, [&](auto ch, auto gk) {
         RELIBRA_LAUNCH(RELIBRA_K_NORM_BWD, stream, (norm_bwd_kernel<XT, decltype(ch)::value, decltype(gk)::value>
-            <<<g.blocks, g.waves * g.rows_per_block * 64, 0, stream>>>(sh, x_out, dx_out, dn, y, w_post, w_pre, gate, dx, dy, dgate, part_post, part_pre)));
+            <<<g.blocks, g.waves * g.rows_per_block * 64, norm_join_bytes(g, sh.h), stream>>>(sh, x_out, dx_out, dn, y, w_post, w_pre, gate, dx, dy, dgate, part_post, part_pre)));
         return RELIBRA_OK;
     });
 }
@@ -392,7 +433,7 @@ extern "C" int relibra_block_norm_bwd(const void *x_out, const void *dx_out, con
         if (!aligned16(p)) return RELIBRA_EINVAL;
     if (gkind == GATE_ELEMENT && (!aligned16(gate) || !aligned16(dgate))) return RELIBRA_EINVAL;
     const NormGrid g = norm_grid(T, h, true);
-    const int P = T > 0 ? g.blocks * g.rows_per_block : 0;
+    const int P = T > 0 ? g.blocks : 0;
     if ((w_post || w_pre) && (!workspace || workspace_bytes < norm_ws_bytes(T, h))) return RELIBRA_EWORKSPACE;
     float *part_post = w_post ? (float *)workspace : nullptr;
     float *part_pre = w_pre ? (float *)((char *)workspace + norm_ws_bytes(T, h) / 2) : nullptr;
@@ -406,7 +447,7 @@ extern "C" int relibra_block_norm_bwd(const void *x_out, const void *dx_out, con
                           sh, g, (bf16_t *)dx, (bf16_t *)dy, dgate, part_post, part_pre, stream);
     }
     if (w_post || w_pre)
-        RELIBRA_LAUNCH(RELIBRA_K_NORM_REDUCE, stream, norm_reduce_kernel<<<dim3((h + 31) / 32, 2), 256, 0, stream>>>(
+        RELIBRA_LAUNCH(RELIBRA_K_NORM_REDUCE, stream, norm_reduce_kernel<<<dim3((h + 31) / 32, 2), kReduceStrips * 8, 0, stream>>>(
             part_post, part_pre, w_post ? dw_post : nullptr, w_pre ? dw_pre : nullptr, P, h, flags & RELIBRA_NORM_ACCUMULATE ? 1 : 0));
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;

@@ -55,6 +55,7 @@ CASES = [
     dict(T=33, h=2048, post=False), dict(T=33, h=2048, pre=False), dict(T=33, h=1024, post=False, pre=False), dict(T=17, h=768, has_y=False),
     dict(T=1100, h=1032), dict(T=1030, h=4104, gate="element"), dict(T=1025, h=8192, gate="none"), dict(T=5000, h=64, gate="element"), dict(T=2000, h=256, has_y=False),
     dict(T=1500, h=640, post=False, gate="none"), dict(T=21, h=88, gate="element", post=False),
+    dict(T=300, h=8184, gate="element"), dict(T=4100, h=1536), dict(T=9000, h=200, gate="none"),
 ]
 IDS = lambda c: "-".join(f"{k}{v}" for k, v in c.items())
 
