@@ -52,8 +52,8 @@ enum { GATE_NONE = 0, GATE_TOKEN = 1, GATE_ELEMENT = 2 };
 
 template <class XT, int CH, int GATE>
 __global__ void __launch_bounds__(CH == 1 ? 1024 : 512)
-norm_fwd_kernel(NormShape sh, const XT *__restrict__ x, const bf16_t *__restrict__ y, const bf16_t *__restrict__ w_post, const bf16_t *__restrict__ w_pre,
-                const void *__restrict__ gate, XT *__restrict__ x_out, bf16_t *__restrict__ n)
+norm_fwd_kernel(NormShape sh, const XT *x, const bf16_t *y, const bf16_t *__restrict__ w_post, const bf16_t *__restrict__ w_pre,
+                const void *__restrict__ gate, XT *x_out, bf16_t *n)          // (x_out may be x, n may be y: a lane reads its pieces of a row first)
 {
     __shared__ float slots[2][3][kNormMaxWaves];
     int turn = 0;
@@ -139,9 +139,9 @@ norm_fwd_kernel(NormShape sh, const XT *__restrict__ x, const bf16_t *__restrict
 
 template <class XT, int CH, int GATE>
 __global__ void __launch_bounds__(CH == 1 ? 1024 : 512)
-norm_bwd_kernel(NormShape sh, const XT *__restrict__ x_out, const XT *__restrict__ dx_out, const bf16_t *__restrict__ dn, const bf16_t *__restrict__ y,
+norm_bwd_kernel(NormShape sh, const XT *__restrict__ x_out, const XT *dx_out, const bf16_t *dn, const bf16_t *y,
                 const bf16_t *__restrict__ w_post, const bf16_t *__restrict__ w_pre, const void *__restrict__ gate,
-                XT *__restrict__ dx, bf16_t *__restrict__ dy, void *__restrict__ dgate, float *__restrict__ part_post, float *__restrict__ part_pre)
+                XT *dx, bf16_t *dy, void *__restrict__ dgate, float *__restrict__ part_post, float *__restrict__ part_pre)
 {
     __shared__ float slots[2][3][kNormMaxWaves];
     int turn = 0;

@@ -215,9 +215,11 @@ template <int CH> constexpr bool router_ahead() { return CH <= 2; }
 
 template <int CH> constexpr int router_waves() { return CH == 8 ? 2 : 4; }
 
-// grid (blocks, n_mb); a block takes `per_block` tokens of its micro-batch, with SOLO all of them: it finishes the sums itself.  The next round's row, ids and mask are requested before
-// the present round is worked on: a round is a chain of LDS round trips, and with the loads in front of it the chain took 3.5
-// us (524288 tokens, 128 experts, bf16).
+// grid (blocks, n_mb); a block takes `per_block` tokens of its micro-batch, with SOLO all of them: it finishes the sums itself.  Bound by
+// the vector units and the latency of a round, not by memory: a round is a chain of LDS round trips and exponentials, so the
+// next round's row, ids and mask are requested before the present one is worked on, and a selection has a lane of its
+// own.  524288 tokens, 128 experts, 8 selected, bf16, 32 micro-batches: 50 us (168 MB at 3.4 TB/s); without the loads ahead, with a loop over the
+// selections and expf 93.
 template <class ZT, bool SIGMOID, int LT, int CH, int NS, bool SOLO>
 __global__ void __launch_bounds__(router_waves<CH>() * 64)
 router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids, const uint8_t *__restrict__ valid, RouterShape sh, int per_block,
@@ -322,18 +324,46 @@ router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
     } else if (tid == 0) part_out.tokens[at] = n;
 }
 
-// One block per micro-batch adds up the blocks' sums in ascending order and finishes the loss.
+// Many blocks' sums to kFoldRows (one block alone took 235 us for those of 8192 tokens of 1000 experts, with the fold both launches take 11): grid (64 experts, fold, n_mb), a fold's rows dealt to four waves, which join in ascending order.
+constexpr int kFoldRows = 16;
+__global__ void __launch_bounds__(256)
+router_fold_kernel(RouterPartials part, int blocks, int per_fold, int E, float *__restrict__ prob, int32_t *__restrict__ count)
+{
+    __shared__ float s_prob[4][64];
+    __shared__ int32_t s_count[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.x * 64 + lane, fold = blockIdx.y, mb = blockIdx.z;
+    const size_t base = (size_t)mb * blocks;
+    const int end = min(blocks, (fold + 1) * per_fold);
+    float p = 0.0f;
+    int32_t c = 0;
+    if (e < E)
+#pragma unroll 8
+        for (int b = fold * per_fold + wave; b < end; b += 4) {
+            p += part.prob[(base + b) * E + e];
+            c += part.count[(base + b) * E + e];
+        }
+    s_prob[wave][lane] = p;
+    s_count[wave][lane] = c;
+    __syncthreads();
+    if (wave == 0 && e < E) {
+        const size_t at = ((size_t)mb * kFoldRows + fold) * E + e;
+        prob[at] = ((p + s_prob[1][lane]) + s_prob[2][lane]) + s_prob[3][lane];
+        count[at] = c + s_count[1][lane] + s_count[2][lane] + s_count[3][lane];
+    }
+}
+
+// One block per micro-batch adds up `rows` rows of sums in ascending order and finishes the loss.
 constexpr int kFinishThreads = 1024;
 __global__ void __launch_bounds__(kFinishThreads)
-router_finish_kernel(RouterPartials part, int blocks, int k, int E, int lanes_e, float coef, RouterSums out)
+router_finish_kernel(RouterPartials part, int blocks, int rows, int k, int E, int lanes_e, float coef, RouterSums out)
 {
     __shared__ double red[kFinishThreads];
     __shared__ float s_prob[kFinishThreads];
     __shared__ int32_t s_count[kFinishThreads];
     const int tid = threadIdx.x, mb = blockIdx.x;
-    const size_t base = (size_t)mb * blocks;
+    const size_t base = (size_t)mb * rows;
     double tokens = 0.0;
-    for (int b = tid; b < blocks; b += kFinishThreads) tokens += part.tokens[base + b];
+    for (int b = tid; b < blocks; b += kFinishThreads) tokens += part.tokens[(size_t)mb * blocks + b];
     const double n = block_sum(tokens, red, kFinishThreads);
     const float inv_n = n > 0.0 ? (float)(1.0 / n) : 0.0f;
     const int el = tid % lanes_e, strip = tid / lanes_e, strips = kFinishThreads / lanes_e;
@@ -343,8 +373,8 @@ router_finish_kernel(RouterPartials part, int blocks, int k, int E, int lanes_e,
         float p = 0.0f;
         int32_t c = 0;
         if (e < E)
-#pragma unroll 4
-            for (int b = strip; b < blocks; b += strips) {
+#pragma unroll 8
+            for (int b = strip; b < rows; b += strips) {
                 p += part.prob[(base + b) * E + e];
                 c += part.count[(base + b) * E + e];
             }
@@ -509,23 +539,37 @@ inline RouterGrid router_grid(int n_mb, int T, int E, bool fwd)
     const int rounds = (T + round - 1) / round;
     g.solo = fwd && rounds <= kSoloRounds;
     const int want = g.solo ? 1 : (kRouterBlocks + n_mb - 1) / n_mb;
-    const int each = rounds > want ? (rounds + want - 1) / want : 1;
+    // forward: every block leaves E sums that are read again, so up to 4 rounds a block while the blocks fill the units
+    const int least = fwd ? (int)std::min(4LL, std::max(1LL, (long long)n_mb * rounds / 256)) : 1;
+    const int each = std::max(least, (rounds + want - 1) / want);
     g.per_block = each * round;
     g.blocks = std::max(1, (T + g.per_block - 1) / g.per_block);
     return g;
 }
-size_t router_ws_bytes(int n_mb, int T, int E)
+// Rows of sums are folded first where the one block would have more than 64 of them for each of its threads' experts.
+inline bool router_folds(const RouterGrid &g, int E) { return !g.solo && (size_t)g.blocks * E > 32 * kFinishThreads; }
+struct RouterWs {
+    size_t prob, count, tokens, fold_prob, fold_count, bytes;
+};
+inline RouterWs router_ws(int n_mb, const RouterGrid &g, int E)
 {
-    const RouterGrid g = router_grid(n_mb, T, E, true);
-    const size_t cells = (size_t)n_mb * g.blocks;
-    return round256(cells * E * sizeof(float)) + round256(cells * E * sizeof(int32_t)) + round256(cells * sizeof(int32_t));
+    const size_t cells = (size_t)n_mb * g.blocks, folded = router_folds(g, E) ? (size_t)n_mb * kFoldRows * E : 0;
+    RouterWs w;
+    w.prob = 0;
+    w.count = w.prob + round256(cells * E * sizeof(float));
+    w.tokens = w.count + round256(cells * E * sizeof(int32_t));
+    w.fold_prob = w.tokens + round256(cells * sizeof(int32_t));
+    w.fold_count = w.fold_prob + round256(folded * sizeof(float));
+    w.bytes = w.fold_count + round256(folded * sizeof(int32_t));
+    return w;
 }
+size_t router_ws_bytes(int n_mb, int T, int E) { return router_ws(n_mb, router_grid(n_mb, T, E, true), E).bytes; }
 
 inline int check_router(int n_mb, int T, int k, int E, int flags, const void *logits, const void *ids)
 {
     const int known = RELIBRA_ROUTER_SIGMOID | RELIBRA_ROUTER_NORMALIZE | RELIBRA_ROUTER_FP32;
     if (n_mb < 0 || T < 0 || E < 1 || k < 1 || k > E || (flags & ~known)) return RELIBRA_EINVAL;
-    if (E > kRouterMaxExperts || k > 64 || n_mb > 65535 || (long long)n_mb * T > 1 << 30) return RELIBRA_EUNSUPPORTED;
+    if (E > kRouterMaxExperts || k > 64 || n_mb > 65535 || (long long)n_mb * T > 1 << 30 || (long long)T * k > INT32_MAX) return RELIBRA_EUNSUPPORTED;
     if ((size_t)n_mb * T > 0 && (!logits || !ids || !aligned16(logits))) return RELIBRA_EINVAL;
     return RELIBRA_OK;
 }
@@ -594,14 +638,11 @@ extern "C" int relibra_router_fwd(const void *logits, const int32_t *ids, const 
     if (n_mb == 0) return RELIBRA_OK;
     if (!counts || !n_valid || !prob_mean || !loss || !err_flag || (T > 0 && !gates)) return RELIBRA_EINVAL;
     const RouterGrid g = router_grid(n_mb, T, E, true);
-    if (!workspace || workspace_bytes < router_ws_bytes(n_mb, T, E)) return RELIBRA_EWORKSPACE;
+    const RouterWs at = router_ws(n_mb, g, E);
+    if (!workspace || workspace_bytes < at.bytes) return RELIBRA_EWORKSPACE;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
-    const size_t cells = (size_t)n_mb * g.blocks;
     char *ws = (char *)workspace;
-    RouterPartials part;
-    part.prob = (float *)ws;
-    part.count = (int32_t *)(ws += round256(cells * E * sizeof(float)));
-    part.tokens = (int32_t *)(ws + round256(cells * E * sizeof(int32_t)));
+    RouterPartials part{(float *)(ws + at.prob), (int32_t *)(ws + at.count), (int32_t *)(ws + at.tokens)};
     const RouterShape sh{T, k, E, flags, scale};
     const RouterSums sums{counts, n_valid, prob_mean, loss};
     int rl;
@@ -615,7 +656,17 @@ extern "C" int relibra_router_fwd(const void *logits, const int32_t *ids, const 
     if (!g.solo) {
         int lanes_e = 1;
         while (lanes_e < kFinishThreads && lanes_e < E) lanes_e *= 2;
-        RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FINISH, stream, router_finish_kernel<<<n_mb, kFinishThreads, 0, stream>>>(part, g.blocks, k, E, lanes_e, balance_coef, sums));
+        int rows = g.blocks;
+        if (router_folds(g, E)) {
+            float *prob = (float *)(ws + at.fold_prob);
+            int32_t *count = (int32_t *)(ws + at.fold_count);
+            const int per_fold = (g.blocks + kFoldRows - 1) / kFoldRows;
+            RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FINISH, stream, router_fold_kernel<<<dim3((E + 63) / 64, kFoldRows, n_mb), 256, 0, stream>>>(part, g.blocks, per_fold, E, prob, count));
+            part.prob = prob;
+            part.count = count;
+            rows = kFoldRows;
+        }
+        RELIBRA_LAUNCH(RELIBRA_K_ROUTER_FINISH, stream, router_finish_kernel<<<n_mb, kFinishThreads, 0, stream>>>(part, g.blocks, rows, k, E, lanes_e, balance_coef, sums));
     }
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
