@@ -598,7 +598,8 @@ int relibra_unpermute_combine(int mode, const void *rows_dev, const void *tok_de
  *   [n_mb] int32 out; prob_mean_dev [n_mb, E], loss_dev [n_mb] fp32 out
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ROUTER, T, k, E, n_mb, 0, 0) bytes (G is n_mb)
  * Sums in fp32 and double in a fixed order: results are reproducible bit for bit.
- * Limits: E <= 4096, k <= min(E, 64), n_mb <= 65535, n_mb * T <= 2^30 (RELIBRA_EUNSUPPORTED beyond), 16-byte aligned logits.
+ * Limits: E <= 4096, k <= min(E, 64), n_mb <= 65535, n_mb * T <= 2^30, T * k <= 2^31 - 1 (RELIBRA_EUNSUPPORTED beyond), 16-byte aligned
+ * logits.  No output may overlap an input.
  */
 enum { RELIBRA_ROUTER_SIGMOID = 1, RELIBRA_ROUTER_NORMALIZE = 2, RELIBRA_ROUTER_FP32 = 4 };
 int relibra_router_fwd(const void *logits_dev, const int32_t *ids_dev, const uint8_t *valid_dev, int n_mb, int T, int k, int E, int flags,
@@ -653,7 +654,7 @@ int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const 
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ORTHOGONALIZE, 0, 1, n, 1, rows, cols) bytes (E, h, hff are n, rows, cols)
  * Products of half-precision operands with fp32 sums, the linear term in 22 bits: the result's error is that of its rounding to bf16
  * (about 2e-3 of its norm), for gradients of low rank too.  Fixed order, no atomics: results are reproducible bit for bit.
- * Limits: rows, cols <= 32768, n <= 65535, 1 <= steps <= 64.
+ * Limits: rows, cols <= 32768, n <= 65535, 1 <= steps <= 64.  No output but momentum_out overlaps an input.
  */
 enum { RELIBRA_ORTHO_BF16 = 1, RELIBRA_ORTHO_NESTEROV = 2 };
 int relibra_orthogonalize(const void *grad_dev, const float *momentum_dev, int n, int rows, int cols, float mu, float scale, int steps, int flags,
@@ -665,7 +666,8 @@ int relibra_orthogonalize(const void *grad_dev, const float *momentum_dev, int n
  * its launch stream: level 1 = the grouped-GEMM kernels, level 2 = every kernel, 0 = off.
  * Calls of few tiles do both weight gradients in one launch, recorded as RELIBRA_K_WGRAD_PAIR instead of
  * _WGRAD_DOWN and _WGRAD_GATE_UP; small permutations run as one kernel, RELIBRA_K_PERM_SMALL instead of
- * _PERM_COUNT, _SCAN and _RANK; calls whose row buffer holds few tiles work their schedule out in their first kernel and
+ * _PERM_COUNT, _SCAN and _RANK; what folds many blocks' router sums before RELIBRA_K_ROUTER_FINISH is recorded there, and what adds up
+ * the parts of A before RELIBRA_K_ORTHO_THIN as RELIBRA_K_ORTHO_POLY; calls whose row buffer holds few tiles work their schedule out in their first kernel and
  * launch no RELIBRA_K_SCHED.
  * At most max_records launches are recorded (events are created in relibra_prof_start, host
  * side only).  relibra_prof_stop waits for the recorded events and returns, per kernel id

@@ -118,7 +118,9 @@ def _ptr(t, dtype=None):
     """_dp as a plain integer, for calls with declared argument types."""
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous"
+    at = t.get_device()                          # (-1: host memory)
+    assert at >= 0 and t.is_contiguous(), "device tensors must be contiguous"
+    assert _device is None or at == _device(), f"tensor on device {at}: work goes to the current device's stream"
     assert dtype is None or t.dtype is dtype, f"expected {dtype}, got {t.dtype}"
     return t.data_ptr()
 
@@ -755,7 +757,7 @@ def relibra_router_bwd(logits, ids, dgates, counts=None, n_valid=None, dloss=Non
     [n_mb,T,E] in the logits' type."""
     n_mb, T, k, E, flags = _router_args(logits, ids, valid, sigmoid, normalize)
     assert dgates is None or dgates.shape == (n_mb, T, k), "dgates are [n_mb, T, k]"
-    assert dloss is None or (dloss.shape == (n_mb,) and counts.shape == (n_mb, E) and n_valid.shape == (n_mb,)), "dloss comes with counts and n_valid"
+    assert dloss is None or (dloss.shape == (n_mb,) and counts is not None and n_valid is not None and counts.shape == (n_mb, E) and n_valid.shape == (n_mb,)), "dloss comes with counts and n_valid"
     dlogits = _out(dlogits, logits.shape, logits.dtype, logits)
     if err_flag is None:
         err_flag = new_err_flag(logits.device)

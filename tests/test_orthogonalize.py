@@ -186,3 +186,26 @@ def test_orthogonalize_refusals():
     assert need > 0 and _call(ws_bytes=need - 1) == rl.EWORKSPACE and _call(ws=0) == rl.EWORKSPACE
     for none in (dict(n=0), dict(rows=0), dict(cols=0)):
         assert _call(**none) == rl.OK, none
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(40, 300, 520), (40, 520, 300), (28, 400, 527), (28, 527, 400), (16, 600, 600)], ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize_many_matrices(shape):
+    """Enough tiles for each of the tile sizes, of which the last of a matrix is not whole."""
+    g = 1e-3 * gauss(*shape, seed=sum(shape))
+    out, mom = rl.relibra_orthogonalize(g.to(DEV), momentum=torch.zeros(shape, device=DEV), nesterov=False)
+    assert torch.equal(mom.cpu(), g)
+    close(out, definition(g))
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(1, 32768, 136), (2, 140, 32768), (1, 32768, 24), (1, 1, 32768)], ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize_longest_sides(shape):
+    g = 1e-3 * gauss(*shape, seed=sum(shape))
+    out, _ = rl.relibra_orthogonalize(g.to(DEV))
+    close(out, definition(g))
+
+
+def test_orthogonalize_no_workspace_for_unusable_sizes():
+    for n, rows, cols in ((1, 32769, 8), (1, 8, 32769), (65536, 8, 8), (1, 2 ** 31 - 1, 2 ** 31 - 1)):
+        assert rl.workspace_bytes(rl.WS_ORTHOGONALIZE, 0, 1, n, 1, rows, cols) == 0

@@ -308,3 +308,41 @@ def test_router_refuses_missing_outputs_and_small_workspaces():
     assert need > 0 and _fwd(ws_bytes=need - 1) == rl.EWORKSPACE and _fwd(ws=0) == rl.EWORKSPACE and _fwd(ws=4104) == rl.EINVAL
     assert _bwd(dlogits=0) == rl.EINVAL and _bwd(counts=0) == rl.EINVAL and _bwd(n_valid=0) == rl.EINVAL and _bwd(T=0) == rl.OK
     assert rl.workspace_bytes(rl.WS_ROUTER, 1 << 29, 1, 8, 4, 0, 0) == 0
+
+
+@gpu
+@pytest.mark.parametrize("kw", [dict(n_mb=1, T=9000, E=1000, k=4), dict(n_mb=2, T=4099, E=256, k=8), dict(n_mb=1, T=1200, E=4096, k=16), dict(n_mb=1, T=20000, E=128, k=8)],
+                         ids=lambda c: "x".join(str(v) for v in c.values()))
+def test_router_few_long_micro_batches(kw):
+    """So many blocks that their sums are folded before they are finished.  A value passes at most 4 + 5 additions in a block, 9 in a
+    wave of a fold, 3 between the waves and 16 behind them: fewer than ROUNDINGS with the score's own."""
+    check(kw, False, True, torch.bfloat16, True, 0.1, seed=77)
+
+
+class _Elsewhere:
+    """A contiguous tensor of device 1."""
+    dtype = torch.float32
+
+    def get_device(self):
+        return 1
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 4096
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    monkeypatch.setattr(rl, "_device", lambda: 0)
+    with pytest.raises(AssertionError, match="current device"):
+        rl._ptr(_Elsewhere())
+    monkeypatch.setattr(rl, "_device", lambda: 1)
+    assert rl._ptr(_Elsewhere(), torch.float32) == 4096
+    with pytest.raises(AssertionError, match="contiguous"):
+        rl._ptr(torch.zeros(4))
+
+
+def test_router_refuses_more_selections_than_a_count_holds():
+    assert _fwd(T=1 << 28, k=8) == rl.EUNSUPPORTED and _bwd(T=1 << 28, k=8) == rl.EUNSUPPORTED
+    assert rl.workspace_bytes(rl.WS_ROUTER, 4, 2, 4097, 1, 0, 0) == 0 and rl.workspace_bytes(rl.WS_ROUTER, 4, 2, 8, 65536, 0, 0) == 0
