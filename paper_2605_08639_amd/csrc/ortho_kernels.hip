@@ -770,6 +770,21 @@ __device__ __forceinline__ void add4(f32x16_t &to, int q, const float4 &v)
     to[4 * q + 3] += v.w;
 }
 
+// Of a 32 x 32 accumulator tile on the diagonal: whether the lane holds one of its elements, and that element, with 0 left in its place.
+__device__ __forceinline__ bool holds_diagonal(int lane) { return ((lane >> 2) & 1) == lane >> 5; }
+__device__ __forceinline__ float take_diagonal(f32x16_t &v, int lane)
+{
+    const int at = (lane & 31) - (lane >> 5) * 4;
+    float d = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const bool here = at == i / 4 * 8 + i % 4;
+        d = here ? v[i] : d;
+        v[i] = here ? 0.0f : v[i];
+    }
+    return d;
+}
+
 // Steps first .. first + count - 1 of `steps` (count > 1 with one workgroup a matrix only).
 template <int MP>
 __global__ void __launch_bounds__(kThinThreads)
@@ -839,19 +854,16 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
                     for (int q = 0; q < 4; ++q) add4(sum, q, carry[TH::part_at(0, wave * SPLIT + c, q, lane)]);
             // A: its diagonal apart, the rest as halves
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = a0 + q * 8 + half;
-                float v[4];
+            for (int i = 0; i < 16; ++i) sum[i] *= 1.0f / kScale;
+            if (a0 == b0) {
+                const float d = take_diagonal(sum, lane);
+                if (holds_diagonal(lane)) da[r_ab] = d;
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = sum[4 * q + e] * (1.0f / kScale);
-                    if (a0 == b0 && r_ab == c + e) {
-                        da[r_ab] = v[e];
-                        v[e] = 0.0f;
-                    }
-                }
+            for (int q = 0; q < 4; ++q) {
+                const float v[4] = {sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
                 at[q] = pack4h(v);
-                ST::put(ab, r_ab, c, at[q]);
+                ST::put(ab, r_ab, a0 + q * 8 + half, at[q]);
             }
         }
         __syncthreads();
@@ -865,24 +877,23 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
         }
         __syncthreads();                                      // A has been read: B takes its place
         if (has_tile) {
-            const float d_r = da[r_ab];
+            const float d_r = da[r_ab], by_r = fmaf(kNsC / kScale, d_r, kNsB);
+            if (a0 == b0) {
+                const float d = (kNsB * d_r + (kNsC / kScale) * (take_diagonal(p, lane) + d_r * d_r)) * (1.0f / kScale);
+                if (holds_diagonal(lane)) {
+                    hi_by[r_ab] = kNsA + d;
+                    lo_by[r_ab] = kNsA + w * d;
+                }
+            }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 4; ++q) {                     // (on the diagonal both p and the half of A are 0 by now)
                 const int c = a0 + q * 8 + half;
                 const float4 d_c = *reinterpret_cast<const float4 *>(da + c);
                 const float dc[4] = {d_c.x, d_c.y, d_c.z, d_c.w};
                 float old[4], v[4];
                 unpack4h(at[q], old);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = kNsB * old[e] + (kNsC / kScale) * (p[4 * q + e] + (d_r + dc[e]) * old[e]);
-                    if (a0 == b0 && r_ab == c + e) {
-                        const float d = (kNsB * d_r + (kNsC / kScale) * (p[4 * q + e] + d_r * d_r)) * (1.0f / kScale);
-                        hi_by[r_ab] = kNsA + d;
-                        lo_by[r_ab] = kNsA + w * d;
-                        v[e] = 0.0f;
-                    }
-                }
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(fmaf(kNsC / kScale, dc[e], by_r), old[e], (kNsC / kScale) * p[4 * q + e]);
                 ST::put(ab, r_ab, c, pack4h(v));
             }
         }
@@ -920,7 +931,7 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
                 unpack4h(h_now[q], h);
                 unpack4h(l_now[q], l);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = by_h[e] * h[e] + (by_l[e] * l[e] + x[4 * q + e] * (1.0f / kScale));
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(by_h[e], h[e], fmaf(by_l[e], l[e], x[4 * q + e] * (1.0f / kScale)));
                 uint2 hp = pack4h(v);
                 if (!last) {
                     unpack4h(hp, h);
