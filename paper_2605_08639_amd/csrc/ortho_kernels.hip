@@ -619,23 +619,49 @@ template <int MP> struct Thin {
         const s16x4_t h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)RELIBRA_LDS(stage + ST::acc_addr(r + 4, c)));
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7));
     }
+    // Tile of a symmetric matrix -> its place: columns a0 .. in the registers, rows b0 .. on the lanes.  Only tiles with b0 <= a0 are
+    // worked out (half the LDS reads, which bound these products: those on the diagonal need one operand); the order of the first TILES leaves
+    // no SIMD with more than three of the ten.
+    static __device__ __forceinline__ int a_of(int tile) { return tile / TILES * 32; }
+    static __device__ __forceinline__ int b_of(int tile) { return (tile + (tile < TILES)) % TILES * 32; }
+    static __device__ __forceinline__ bool lower(int tile) { return b_of(tile) <= a_of(tile); }
     // g += this wave's tile of the staged rows' Gram matrix, over its part of the rows
     static __device__ __forceinline__ f32x16_t gram(f32x16_t g, const char *stage, int wave, int lane)
     {
-        const int tile = wave / SPLIT, a0 = tile / TILES * 32, b0 = tile % TILES * 32, k0 = wave % SPLIT * (ROWS / SPLIT / 16);
+        const int tile = wave / SPLIT, a0 = a_of(tile), b0 = b_of(tile), k0 = wave % SPLIT * (ROWS / SPLIT / 16);
+        if (a0 == b0) {
 #pragma unroll
-        for (int kk = 0; kk < ROWS / SPLIT / 16; ++kk) {
-            if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-            g = mfma(frag_across(stage, a0, k0 + kk, lane), frag_across(stage, b0, k0 + kk, lane), g);
+            for (int kk = 0; kk < ROWS / SPLIT / 16; ++kk) {
+                if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                const bf16x8_t f = frag_across(stage, a0, k0 + kk, lane);
+                g = mfma(f, f, g);
+            }
+        } else if (b0 < a0) {
+#pragma unroll
+            for (int kk = 0; kk < ROWS / SPLIT / 16; ++kk) {
+                if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                g = mfma(frag_across(stage, a0, k0 + kk, lane), frag_across(stage, b0, k0 + kk, lane), g);
+            }
         }
         return g;
     }
+    // four values of row r, columns c .. of a symmetric matrix, and (a tile below the diagonal) their images
+    static __device__ __forceinline__ void put_both(char *ab, int r, int c, uint2 v, bool image)
+    {
+        ST::put(ab, r, c, v);
+        if (image) {
+            const uint16_t h[4] = {(uint16_t)v.x, (uint16_t)(v.x >> 16), (uint16_t)v.y, (uint16_t)(v.y >> 16)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint16_t *>(ab + ST::acc_addr(c + e, r & ~3) + (r & 3) * 2) = h[e];
+        }
+    }
     // second halves lie in accumulator order: [32 x 32 tile of the run][4 registers of a lane][lane] of 4 values
     static __device__ __forceinline__ int lo_at(int tile, int q, int lane) { return ((tile * 4 + q) * 64 + lane) * 4; }
-    // a partial A: [tile][part of the rows][4 registers of a lane][lane]
+    // a partial A: [tile][part of the rows][4 registers of a lane][lane], of which tiles above the diagonal are left out
     static __device__ __forceinline__ size_t part_at(size_t chunk, int tile_and_split, int q, int lane) { return ((chunk * kThinWaves + tile_and_split) * 4 + q) * 64 + lane; }
     static __device__ __forceinline__ void store_part(const f32x16_t &g, float *part, size_t chunk, int wave, int lane)
     {
+        if (!lower(wave / SPLIT)) return;
 #pragma unroll
         for (int q = 0; q < 4; ++q) reinterpret_cast<float4 *>(part)[part_at(chunk, wave, q, lane)] = make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]);
     }
@@ -749,9 +775,11 @@ ortho_thin_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new
 }
 
 // One partial A of a matrix from those of its workgroups, in ascending order: blockIdx.x of kThinWaves blocks of 1024 values.
+template <int MP>
 __global__ void __launch_bounds__(256)
 ortho_thin_sum_kernel(const float4 *__restrict__ part, int chunks, float4 *__restrict__ sum)
 {
+    if (!Thin<MP>::lower(blockIdx.x / Thin<MP>::SPLIT)) return;
     const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x, base = (size_t)blockIdx.y * chunks * kThinWaves * 256 + at;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
@@ -801,9 +829,9 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
     float4 *carry = reinterpret_cast<float4 *>(lds + TH::AB + 2 * TH::STAGE + TH::DIAG);
     f32x16_t acc = TH::zero();                                // this wave's tile of the next A over the workgroup's rows
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mat = blockIdx.y;
-    // this wave's tile of A (the first TILES^2 waves) and of a run's rows of X
-    const bool has_tile = wave < TILES * TILES;
-    const int a0 = wave / TILES * 32, b0 = wave % TILES * 32, x_col = wave % TILES * 32;
+    // this wave's tile of A and B (those of the first TILES^2 waves that have one) and of a run's rows of X
+    const bool has_tile = wave < TILES * TILES && TH::lower(wave);
+    const int a0 = TH::a_of(wave), b0 = TH::b_of(wave), x_col = wave % TILES * 32;
     for (int step = first; step < first + count; ++step) {
         const float w = step + 3 >= steps ? 1.0f : 0.0f;
         const bool last = step + 1 == steps;
@@ -825,7 +853,7 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
             const float4 *src = reinterpret_cast<const float4 *>(part_in);
             acc = TH::zero();
 #pragma unroll 1
-            for (int c0 = 0; c0 < n_in; c0 += kThinBatch) {
+            for (int c0 = 0; TH::lower(wave / SPLIT) && c0 < n_in; c0 += kThinBatch) {
                 float4 v[kThinBatch][4];
 #pragma unroll
                 for (int u = 0; u < kThinBatch; ++u)
@@ -863,12 +891,19 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
             for (int q = 0; q < 4; ++q) {
                 const float v[4] = {sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
                 at[q] = pack4h(v);
-                ST::put(ab, r_ab, a0 + q * 8 + half, at[q]);
+                TH::put_both(ab, r_ab, a0 + q * 8 + half, at[q], b0 < a0);
             }
         }
         __syncthreads();
         f32x16_t p = TH::zero();
-        if (has_tile) {
+        if (has_tile && a0 == b0) {
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                const bf16x8_t f = TH::frag(ab, a0, kk, lane);
+                p = TH::mfma(f, f, p);
+            }
+        } else if (has_tile) {
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
                 if (kk % 4 == 0) __builtin_amdgcn_sched_barrier(0);
@@ -894,7 +929,7 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
                 unpack4h(at[q], old);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = fmaf(fmaf(kNsC / kScale, dc[e], by_r), old[e], (kNsC / kScale) * p[4 * q + e]);
-                ST::put(ab, r_ab, c, pack4h(v));
+                TH::put_both(ab, r_ab, c, pack4h(v), b0 < a0);
             }
         }
         __syncthreads();
@@ -987,7 +1022,7 @@ int thin_run(const ThinShape &s, const ThinWs &w, const GT *g, const float *m_ne
     const int each = s.chunks == 1 ? steps : 1, vec = s.cols % 8 == 0 && aligned16(out);
     for (int i = 0; i < steps; i += each) {
         const bool summed = s.chunks > kThinDirect;
-        if (summed) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_POLY, stream, ortho_thin_sum_kernel<<<dim3(kThinWaves, s.n), 256, 0, stream>>>(
+        if (summed) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_POLY, stream, ortho_thin_sum_kernel<MP><<<dim3(kThinWaves, s.n), 256, 0, stream>>>(
             (const float4 *)w.part[i & 1], s.chunks, (float4 *)w.sum));
         RELIBRA_LAUNCH(RELIBRA_K_ORTHO_THIN, stream, (ortho_thin_step_kernel<MP><<<grid, kThinThreads, TH::LDS, stream>>>(
             s, i, each, steps, w.hi, w.lo, summed ? w.sum : w.part[i & 1], summed ? 1 : s.chunks, w.part[(i + 1) & 1], scale, vec, out)));
