@@ -645,15 +645,13 @@ template <int MP> struct Thin {
         }
         return g;
     }
-    // four values of row r, columns c .. of a symmetric matrix, and (a tile below the diagonal) their images
-    static __device__ __forceinline__ void put_both(char *ab, int r, int c, uint2 v, bool image)
+    // The image of a tile below the diagonal that this wave has put into `ab`: read back transposed, 8 values of a column at a time.
+    static __device__ __forceinline__ void put_image(char *ab, int a0, int b0, int lane)
     {
-        ST::put(ab, r, c, v);
-        if (image) {
-            const uint16_t h[4] = {(uint16_t)v.x, (uint16_t)(v.x >> 16), (uint16_t)v.y, (uint16_t)(v.y >> 16)};
+        wave_lds_fence();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint16_t *>(ab + ST::acc_addr(c + e, r & ~3) + (r & 3) * 2) = h[e];
-        }
+        for (int kk = 0; kk < 2; ++kk)
+            *reinterpret_cast<bf16x8_t *>(ab + ST::acc_addr(a0 + (lane & 31), b0 + kk * 16 + (lane >> 5) * 8)) = frag_across(ab, a0, b0 / 16 + kk, lane);
     }
     // second halves lie in accumulator order: [32 x 32 tile of the run][4 registers of a lane][lane] of 4 values
     static __device__ __forceinline__ int lo_at(int tile, int q, int lane) { return ((tile * 4 + q) * 64 + lane) * 4; }
@@ -891,8 +889,9 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
             for (int q = 0; q < 4; ++q) {
                 const float v[4] = {sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
                 at[q] = pack4h(v);
-                TH::put_both(ab, r_ab, a0 + q * 8 + half, at[q], b0 < a0);
+                ST::put(ab, r_ab, a0 + q * 8 + half, at[q]);
             }
+            if (b0 < a0) TH::put_image(ab, a0, b0, lane);
         }
         __syncthreads();
         f32x16_t p = TH::zero();
@@ -929,8 +928,9 @@ ortho_thin_step_kernel(ThinShape s, int first, int count, int steps, uint16_t *h
                 unpack4h(at[q], old);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = fmaf(fmaf(kNsC / kScale, dc[e], by_r), old[e], (kNsC / kScale) * p[4 * q + e]);
-                TH::put_both(ab, r_ab, c, pack4h(v), b0 < a0);
+                ST::put(ab, r_ab, c, pack4h(v));
             }
+            if (b0 < a0) TH::put_image(ab, a0, b0, lane);
         }
         __syncthreads();
         acc = TH::zero();
