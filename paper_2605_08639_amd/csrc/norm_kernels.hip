@@ -141,7 +141,7 @@ template <class XT, int CH, int GATE>
 __global__ void __launch_bounds__(CH == 1 ? 1024 : 512)
 norm_bwd_kernel(NormShape sh, const XT *__restrict__ x_out, const XT *dx_out, const bf16_t *dn, const bf16_t *y,
                 const bf16_t *__restrict__ w_post, const bf16_t *__restrict__ w_pre, const void *__restrict__ gate,
-                XT *dx, bf16_t *dy, void *__restrict__ dgate, float *__restrict__ part_post, float *__restrict__ part_pre)
+                XT *dx, bf16_t *dy, void *__restrict__ dgate, float *__restrict__ part_post, float *__restrict__ part_pre, int add)
 {
     __shared__ float slots[2][3][kNormMaxWaves];
     int turn = 0;
@@ -246,7 +246,7 @@ norm_bwd_kernel(NormShape sh, const XT *__restrict__ x_out, const XT *dx_out, co
             }
         }
     }
-    // the block's row groups, in ascending order: one partial row a block
+    // the block's row groups, in ascending order: one partial row a block, or (one block, `add` with RELIBRA_NORM_ACCUMULATE) the gradient itself
     extern __shared__ __attribute__((aligned(16))) char smem[];
     float *join = reinterpret_cast<float *>(smem);            // [rows_per_block - 1][h]
     auto leave = [&](const float (&acc)[CH][8], float *to) __attribute__((always_inline)) {
@@ -266,6 +266,11 @@ norm_bwd_kernel(NormShape sh, const XT *__restrict__ x_out, const XT *dx_out, co
                     for (int j = 0; j < 8; ++j) sum[j] = acc[c][j];
                     for (int r = 1; r < sh.rows_per_block; ++r) {
                         load8(join + (size_t)(r - 1) * h + (c * lanes + pos) * 8, v);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum[j] += v[j];
+                    }
+                    if (add) {
+                        load8(to + (c * lanes + pos) * 8, v);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) sum[j] += v[j];
                     }
@@ -327,6 +332,7 @@ struct NormGrid {
 // Backward: one piece a lane (two take 173 registers instead of 110: half the waves), eight waves a block, 16 a unit: 16384 rows of 4096
 // 157 us, with 8 waves a unit 200, 32 167; with two pieces and four waves a block 176.  The row groups of a block are joined in LDS: with a
 // partial row each the second kernel took longer than the first, 8000 rows of 512 56 -> 16 us, 4096 of 2048 48 -> 25.
+constexpr int kOneBlockRounds = 4;
 inline NormGrid norm_grid(int T, int h, bool bwd)
 {
     NormGrid g;
@@ -338,6 +344,7 @@ inline NormGrid norm_grid(int T, int h, bool bwd)
     const int groups = (T + g.rows_per_block - 1) / g.rows_per_block;
     int want = kComputeUnits * std::max(1, 16 / (g.waves * g.rows_per_block));
     if (!bwd && groups >= 16 * want) want = std::max(kComputeUnits, want / 2);
+    if (bwd && groups <= kOneBlockRounds) want = 1;
     g.blocks = std::max(1, std::min(groups, want));
     return g;
 }
@@ -381,11 +388,11 @@ int norm_fwd_impl(const XT *x, const bf16_t *y, const bf16_t *w_post, const bf16
 }
 template <class XT>
 int norm_bwd_impl(const XT *x_out, const XT *dx_out, const bf16_t *dn, const bf16_t *y, const bf16_t *w_post, const bf16_t *w_pre, const void *gate, int gkind,
-                  const NormShape &sh, const NormGrid &g, XT *dx, bf16_t *dy, void *dgate, float *part_post, float *part_pre, hipStream_t stream)
+                  const NormShape &sh, const NormGrid &g, XT *dx, bf16_t *dy, void *dgate, float *part_post, float *part_pre, int add, hipStream_t stream)
 {
     return norm_layout<false>(g.chunks, gkind, [&](auto ch, auto gk) {
         RELIBRA_LAUNCH(RELIBRA_K_NORM_BWD, stream, (norm_bwd_kernel<XT, decltype(ch)::value, decltype(gk)::value>
-            <<<g.blocks, g.waves * g.rows_per_block * 64, norm_join_bytes(g, sh.h), stream>>>(sh, x_out, dx_out, dn, y, w_post, w_pre, gate, dx, dy, dgate, part_post, part_pre)));
+            <<<g.blocks, g.waves * g.rows_per_block * 64, norm_join_bytes(g, sh.h), stream>>>(sh, x_out, dx_out, dn, y, w_post, w_pre, gate, dx, dy, dgate, part_post, part_pre, add)));
         return RELIBRA_OK;
     });
 }
@@ -435,20 +442,22 @@ extern "C" int relibra_block_norm_bwd(const void *x_out, const void *dx_out, con
     const NormGrid g = norm_grid(T, h, true);
     const int P = T > 0 ? g.blocks : 0;
     if ((w_post || w_pre) && (!workspace || workspace_bytes < norm_ws_bytes(T, h))) return RELIBRA_EWORKSPACE;
-    float *part_post = w_post ? (float *)workspace : nullptr;
-    float *part_pre = w_pre ? (float *)((char *)workspace + norm_ws_bytes(T, h) / 2) : nullptr;
+    const bool one = P == 1;                                  // one block's sums are the gradients: no second launch
+    float *part_post = !w_post ? nullptr : one ? dw_post : (float *)workspace;
+    float *part_pre = !w_pre ? nullptr : one ? dw_pre : (float *)((char *)workspace + norm_ws_bytes(T, h) / 2);
+    const int add = flags & RELIBRA_NORM_ACCUMULATE ? 1 : 0;
     if (T > 0) {
         const NormShape sh{T, h, g.waves, g.rows_per_block, y ? res_scale : 1.0f, eps};
         if (flags & RELIBRA_NORM_STREAM_FP32)
             norm_bwd_impl((const float *)x_out, (const float *)dx_out, (const bf16_t *)dn, (const bf16_t *)y, (const bf16_t *)w_post, (const bf16_t *)w_pre, gate, gkind,
-                          sh, g, (float *)dx, (bf16_t *)dy, dgate, part_post, part_pre, stream);
+                          sh, g, (float *)dx, (bf16_t *)dy, dgate, part_post, part_pre, one && add, stream);
         else
             norm_bwd_impl((const bf16_t *)x_out, (const bf16_t *)dx_out, (const bf16_t *)dn, (const bf16_t *)y, (const bf16_t *)w_post, (const bf16_t *)w_pre, gate, gkind,
-                          sh, g, (bf16_t *)dx, (bf16_t *)dy, dgate, part_post, part_pre, stream);
+                          sh, g, (bf16_t *)dx, (bf16_t *)dy, dgate, part_post, part_pre, one && add, stream);
     }
-    if (w_post || w_pre)
+    if ((w_post || w_pre) && !one)
         RELIBRA_LAUNCH(RELIBRA_K_NORM_REDUCE, stream, norm_reduce_kernel<<<dim3((h + 31) / 32, 2), kReduceStrips * 8, 0, stream>>>(
-            part_post, part_pre, w_post ? dw_post : nullptr, w_pre ? dw_pre : nullptr, P, h, flags & RELIBRA_NORM_ACCUMULATE ? 1 : 0));
+            part_post, part_pre, w_post ? dw_post : nullptr, w_pre ? dw_pre : nullptr, P, h, add));
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
 }
