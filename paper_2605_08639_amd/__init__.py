@@ -114,15 +114,20 @@ def _dp(t, dtype=None):
     return C.c_void_p(t.data_ptr())
 
 
-def _ptr(t, dtype=None):
-    """_dp as a plain integer, for calls with declared argument types."""
-    if t is None:
-        return None
-    at = t.get_device()                          # (-1: host memory)
-    assert at >= 0 and t.is_contiguous(), "device tensors must be contiguous"
-    assert _device is None or at == _device(), f"tensor on device {at}: work goes to the current device's stream"
-    assert dtype is None or t.dtype is dtype, f"expected {dtype}, got {t.dtype}"
-    return t.data_ptr()
+def _ptrs(*tensors):
+    """Device pointers of contiguous tensors on the current device as plain integers (None: NULL), for calls with declared argument
+    types.  All at once: a call for each took a tenth of a small call's time."""
+    out, here = [], -1
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()                  # (-1: host memory)
+            assert at >= 0 and t.is_contiguous(), "device tensors must be contiguous"
+            if here < 0:
+                here = at if _device is None else _device()
+            assert at == here, f"tensor on device {at}: work goes to the current device's stream"
+            t = t.data_ptr()
+        out.append(t)
+    return out
 
 
 def _raw():
@@ -712,7 +717,7 @@ def _router_args(logits, ids, valid, sigmoid, normalize):
     n_mb, T, E = logits.shape
     k = ids.shape[2]
     assert logits.dtype in (torch.bfloat16, torch.float32), f"logits in bf16 or fp32, got {logits.dtype}"
-    assert ids.shape == (n_mb, T, k), "ids are [n_mb, T, k]"
+    assert ids.shape == (n_mb, T, k) and ids.dtype is torch.int32, "ids are [n_mb, T, k] int32"
     assert valid is None or (valid.shape == (n_mb, T) and valid.dtype in (torch.uint8, torch.bool)), "valid is [n_mb, T] of bytes"
     flags = (ROUTER_SIGMOID if sigmoid else 0) | (ROUTER_NORMALIZE if normalize else 0) | (ROUTER_FP32 if logits.dtype == torch.float32 else 0)
     return n_mb, T, k, E, flags
@@ -744,9 +749,9 @@ def relibra_router_fwd(logits, ids, sigmoid=False, normalize=True, scale=1.0, ba
         workspace = router_workspace(n_mb, T, k, E, logits.device)
     if err_flag is None:
         err_flag = new_err_flag(logits.device)
-    rc = lib().relibra_router_fwd(_ptr(logits), _ptr(ids, torch.int32), _ptr(valid), n_mb, T, k, E, flags, scale, balance_coef,
-                                  _ptr(gates), _ptr(counts), _ptr(n_valid), _ptr(prob_mean), _ptr(loss),
-                                  _ptr(workspace), workspace.numel(), _ptr(err_flag, torch.int32), _raw())
+    assert err_flag.dtype is torch.int32, "the error flag is int32"
+    at = _ptrs(logits, ids, valid, gates, counts, n_valid, prob_mean, loss, workspace, err_flag)
+    rc = lib().relibra_router_fwd(*at[:3], n_mb, T, k, E, flags, scale, balance_coef, *at[3:9], workspace.numel(), at[9], _raw())
     _check("relibra_router_fwd", rc)
     return gates, counts, n_valid, prob_mean, loss
 
@@ -756,14 +761,17 @@ def relibra_router_bwd(logits, ids, dgates, counts=None, n_valid=None, dloss=Non
     """dgates [n_mb,T,k] fp32 (or None) and dloss [n_mb] fp32 (or None; else with the forward call's counts and n_valid) -> dlogits
     [n_mb,T,E] in the logits' type."""
     n_mb, T, k, E, flags = _router_args(logits, ids, valid, sigmoid, normalize)
-    assert dgates is None or dgates.shape == (n_mb, T, k), "dgates are [n_mb, T, k]"
+    assert dgates is None or (dgates.shape == (n_mb, T, k) and dgates.dtype is torch.float32), "dgates are [n_mb, T, k] fp32"
+    assert counts is None or counts.dtype is torch.int32, "counts are int32"
+    assert n_valid is None or n_valid.dtype is torch.int32, "n_valid is int32"
+    assert dloss is None or dloss.dtype is torch.float32, "dloss is fp32"
     assert dloss is None or (dloss.shape == (n_mb,) and counts is not None and n_valid is not None and counts.shape == (n_mb, E) and n_valid.shape == (n_mb,)), "dloss comes with counts and n_valid"
     dlogits = _out(dlogits, logits.shape, logits.dtype, logits)
     if err_flag is None:
         err_flag = new_err_flag(logits.device)
-    rc = lib().relibra_router_bwd(_ptr(logits), _ptr(ids, torch.int32), _ptr(valid), _ptr(dgates, torch.float32), _ptr(counts, torch.int32),
-                                  _ptr(n_valid, torch.int32), _ptr(dloss, torch.float32), n_mb, T, k, E, flags, scale, balance_coef,
-                                  _ptr(dlogits), _ptr(err_flag, torch.int32), _raw())
+    assert err_flag.dtype is torch.int32, "the error flag is int32"
+    at = _ptrs(logits, ids, valid, dgates, counts, n_valid, dloss, dlogits, err_flag)
+    rc = lib().relibra_router_bwd(*at[:7], n_mb, T, k, E, flags, scale, balance_coef, *at[7:], _raw())
     _check("relibra_router_bwd", rc)
     return dlogits
 
@@ -771,14 +779,17 @@ def relibra_router_bwd(logits, ids, dgates, counts=None, n_valid=None, dloss=Non
 def _norm_args(x, y, w_post, w_pre, gate):
     T, h = x.shape
     assert x.dtype in (torch.bfloat16, torch.float32), f"the residual stream is bf16 or fp32, got {x.dtype}"
-    assert y is None or y.shape == (T, h), "y is [T, h]"
-    assert (w_post is None or w_post.shape == (h,)) and (w_pre is None or w_pre.shape == (h,)), "norm weights are [h]"
+    bf16 = torch.bfloat16
+    assert y is None or (y.shape == (T, h) and y.dtype is bf16), "y is [T, h] bf16"
+    assert w_post is None or (w_post.shape == (h,) and w_post.dtype is bf16), "norm weights are [h] bf16"
+    assert w_pre is None or (w_pre.shape == (h,) and w_pre.dtype is bf16), "norm weights are [h] bf16"
     flags = NORM_STREAM_FP32 if x.dtype == torch.float32 else 0
     gate_type = None
     if gate is not None:
         assert gate.shape in ((T,), (T, h)), "one gate a token or one an element"
         flags |= NORM_GATE_TOKEN if gate.dim() == 1 else NORM_GATE_ELEMENT
-        gate_type = torch.float32 if gate.dim() == 1 else torch.bfloat16
+        gate_type = torch.float32 if gate.dim() == 1 else bf16
+        assert gate.dtype is gate_type, f"expected {gate_type}, got {gate.dtype}"
     return T, h, flags, gate_type
 
 
@@ -788,8 +799,8 @@ def relibra_block_norm_fwd(x, y=None, w_post=None, w_pre=None, gate=None, res_sc
     T, h, flags, gate_type = _norm_args(x, y, w_post, w_pre, gate)
     x_out = x if y is None else _out(x_out, (T, h), x.dtype, x)
     n = None if w_pre is None else _out(n, (T, h), torch.bfloat16, x)
-    rc = lib().relibra_block_norm_fwd(_ptr(x), _ptr(y, torch.bfloat16), _ptr(w_post, torch.bfloat16), _ptr(w_pre, torch.bfloat16), _ptr(gate, gate_type),
-                                      T, h, res_scale, eps, flags, _ptr(None if y is None else x_out), _ptr(n), _raw())
+    at = _ptrs(x, y, w_post, w_pre, gate, None if y is None else x_out, n)
+    rc = lib().relibra_block_norm_fwd(*at[:5], T, h, res_scale, eps, flags, *at[5:], _raw())
     _check("relibra_block_norm_fwd", rc)
     return x_out, n
 
@@ -804,7 +815,7 @@ def relibra_block_norm_bwd(x_out, dx_out, dn, y=None, w_post=None, w_pre=None, g
     accumulate: dw_post and dw_pre (fp32 [h], given) are added to."""
     T, h, flags, gate_type = _norm_args(x_out, y, w_post, w_pre, gate)
     assert dx_out is None or (dx_out.shape == (T, h) and dx_out.dtype == x_out.dtype), "dx_out is like x_out"
-    assert (dn is None) == (w_pre is None) and (dn is None or dn.shape == (T, h)), "dn [T, h] goes with w_pre"
+    assert (dn is None) == (w_pre is None) and (dn is None or (dn.shape == (T, h) and dn.dtype is torch.bfloat16)), "dn [T, h] bf16 goes with w_pre"
     assert not accumulate or ((w_post is None or dw_post is not None) and (w_pre is None or dw_pre is not None)), "nothing to add to"
     dx = _out(dx, (T, h), x_out.dtype, x_out)
     dy = None if y is None else _out(dy, (T, h), torch.bfloat16, x_out)
@@ -813,10 +824,8 @@ def relibra_block_norm_bwd(x_out, dx_out, dn, y=None, w_post=None, w_pre=None, g
     dw_pre = None if w_pre is None else _out(dw_pre, (h,), torch.float32, x_out)
     if workspace is None:
         workspace = block_norm_workspace(T, h, x_out.device)
-    rc = lib().relibra_block_norm_bwd(_ptr(x_out), _ptr(dx_out), _ptr(dn, torch.bfloat16), _ptr(y, torch.bfloat16), _ptr(w_post, torch.bfloat16),
-                                      _ptr(w_pre, torch.bfloat16), _ptr(gate, gate_type), T, h, res_scale, eps,
-                                      flags | (NORM_ACCUMULATE if accumulate else 0), _ptr(dx), _ptr(dy), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre),
-                                      _ptr(workspace), workspace.numel(), _raw())
+    at = _ptrs(x_out, dx_out, dn, y, w_post, w_pre, gate, dx, dy, dgate, dw_post, dw_pre, workspace)
+    rc = lib().relibra_block_norm_bwd(*at[:7], T, h, res_scale, eps, flags | (NORM_ACCUMULATE if accumulate else 0), *at[7:], workspace.numel(), _raw())
     _check("relibra_block_norm_bwd", rc)
     return dx, dy, dgate, dw_post, dw_pre
 
@@ -830,7 +839,7 @@ def relibra_orthogonalize(grad, momentum=None, mu=0.95, nesterov=True, scale=1.0
     the new momentum (None without)).  momentum_out may be the momentum itself; nesterov counts with momentum only."""
     n, rows, cols = grad.shape
     assert grad.dtype in (torch.bfloat16, torch.float32), f"gradients in bf16 or fp32, got {grad.dtype}"
-    assert momentum is None or momentum.shape == grad.shape, "momentum is like grad"
+    assert momentum is None or (momentum.shape == grad.shape and momentum.dtype is torch.float32), "momentum is like grad, in fp32"
     assert momentum is not None or momentum_out is None, "no momentum to update"
     out = _out(out, grad.shape, torch.bfloat16, grad)
     if momentum is not None:
@@ -838,8 +847,8 @@ def relibra_orthogonalize(grad, momentum=None, mu=0.95, nesterov=True, scale=1.0
     if workspace is None:
         workspace = orthogonalize_workspace(n, rows, cols, grad.device)
     flags = (ORTHO_BF16 if grad.dtype == torch.bfloat16 else 0) | (ORTHO_NESTEROV if nesterov and momentum is not None else 0)
-    rc = lib().relibra_orthogonalize(_ptr(grad), _ptr(momentum, torch.float32), n, rows, cols, mu, scale, int(steps), flags,
-                                     _ptr(momentum_out), _ptr(out), _ptr(workspace), workspace.numel(), _raw())
+    at = _ptrs(grad, momentum, momentum_out, out, workspace)
+    rc = lib().relibra_orthogonalize(*at[:2], n, rows, cols, mu, scale, int(steps), flags, *at[2:], workspace.numel(), _raw())
     _check("relibra_orthogonalize", rc)
     return out, momentum_out
 

@@ -336,11 +336,11 @@ class _Elsewhere:
 def test_tensors_of_another_device_are_refused(monkeypatch):
     monkeypatch.setattr(rl, "_device", lambda: 0)
     with pytest.raises(AssertionError, match="current device"):
-        rl._ptr(_Elsewhere())
+        rl._ptrs(_Elsewhere())
     monkeypatch.setattr(rl, "_device", lambda: 1)
-    assert rl._ptr(_Elsewhere(), torch.float32) == 4096
+    assert rl._ptrs(None, _Elsewhere()) == [None, 4096]
     with pytest.raises(AssertionError, match="contiguous"):
-        rl._ptr(torch.zeros(4))
+        rl._ptrs(torch.zeros(4))
 
 
 def test_router_refuses_more_selections_than_a_count_holds():
