@@ -674,9 +674,10 @@ struct ThinShape {
 };
 inline bool is_thin(int rows, int cols) { return std::min(rows, cols) <= kThinSide; }
 // One run to a workgroup as far as there are compute units (a workgroup fills one).  Every workgroup of a matrix reads all partial
-// A's (64 KiB apiece, two in flight, about 1.2 us each): of more than kThinDirect a kernel of its own makes one first.  us a call, without
-// it and the best number of workgroups -> with it: 4096 x 128 139 -> 91, 4 of 128 x 4096 149 -> 107, 16 of 3000 x 100 188 -> 155, 64 x 4096 101 -> 74.
-constexpr int kThinDirect = 4;
+// A's (40 KiB apiece, two in flight, about 1 us each): of more than kThinDirect, or where the workgroups read more than kThinReads altogether, a
+// kernel of its own makes one first.  us a call, without / with it: 128 x 700 (6 workgroups) 67 / 73, 8 of 128 x 700 79 / 81, 32 of 100 x 700 104 / 97,
+// 128 x 1000 (8) 72 / 69, 32 of 128 x 500 (4) 79 / 90, 64 of 128 x 500 110 / 106, 16 of 100 x 1000 (8) 97 / 88.
+constexpr int kThinDirect = 6, kThinReads = 768;
 inline ThinShape thin_shape(int n, int rows, int cols)
 {
     ThinShape s{n, rows, cols, 128, Thin<128>::ROWS, 1, 1, rows > cols};
@@ -687,6 +688,7 @@ inline ThinShape thin_shape(int n, int rows, int cols)
     s.chunks = (all + s.runs - 1) / s.runs;
     return s;
 }
+inline bool thin_summed(const ThinShape &s) { return s.chunks > kThinDirect || (s.chunks > 1 && s.n * s.chunks * s.chunks > kThinReads); }
 struct ThinWs {
     uint16_t *hi, *lo;
     float *part[2], *sum;
@@ -695,7 +697,7 @@ struct ThinWs {
 inline size_t thin_x_bytes(const ThinShape &s) { return round256(s.x_at(s.n) * sizeof(uint16_t)); }
 inline size_t thin_part_bytes(const ThinShape &s) { return round256((size_t)s.n * s.chunks * kThinWaves * 1024 * sizeof(float)); }
 
-inline size_t thin_sum_bytes(const ThinShape &s) { return s.chunks > kThinDirect ? round256((size_t)s.n * kThinWaves * 1024 * sizeof(float)) : 0; }
+inline size_t thin_sum_bytes(const ThinShape &s) { return thin_summed(s) ? round256((size_t)s.n * kThinWaves * 1024 * sizeof(float)) : 0; }
 
 // Rows of a run, 8 values of the short side at a time, lanes along the memory of the caller's matrix: fn(row of the run, first value).
 template <int MP, int UNROLL, class Fn> __device__ __forceinline__ void thin_pieces(bool tall, int tid, const Fn &fn)
@@ -1021,7 +1023,7 @@ int thin_run(const ThinShape &s, const ThinWs &w, const GT *g, const float *m_ne
         g, m_new, mu, mode, s, w.parts, n_parts, w.hi, w.lo, w.part[0])));
     const int each = s.chunks == 1 ? steps : 1, vec = s.cols % 8 == 0 && aligned16(out);
     for (int i = 0; i < steps; i += each) {
-        const bool summed = s.chunks > kThinDirect;
+        const bool summed = thin_summed(s);
         if (summed) RELIBRA_LAUNCH(RELIBRA_K_ORTHO_POLY, stream, ortho_thin_sum_kernel<MP><<<dim3(kThinWaves, s.n), 256, 0, stream>>>(
             (const float4 *)w.part[i & 1], s.chunks, (float4 *)w.sum));
         RELIBRA_LAUNCH(RELIBRA_K_ORTHO_THIN, stream, (ortho_thin_step_kernel<MP><<<grid, kThinThreads, TH::LDS, stream>>>(
