@@ -20,6 +20,10 @@
 // Matrices are padded to multiples of 64 with zeros, which every step leaves zero.  X lies as the gradient does; the Gram matrix is
 // taken over the longer side, along memory (wide) or across it (tall), and X is multiplied from the left or the right.  A and B
 // are symmetric: only tiles on and below the diagonal are computed, and stored twice.
+//
+// Bound by the matrix units and, over a whole call, by power: 32 of 1536 x 4096 take 7.08 ms, of which 5 x (gram 345, poly 160, update 715 us) are
+// products: 0.90, 0.73 and 0.86 PFLOP/s of what the formulas need (a large library product of halves reaches 1.37), gram and poly with 21 tiles
+// of 256 x 256 for 18 tiles' worth, 2.6 rounds of the units paid as 3.
 #include "gemm_tile.h"
 #include "wave_ops.h"
 #include "wave_stage.h"
@@ -76,7 +80,7 @@ __device__ __forceinline__ float update_of(float g, float m_new, float mu, int m
 }
 
 // M' and the sum of U^2, part blockIdx.x of matrix blockIdx.y.  Squares in double: no gradient is too large or small.  Eight values at a
-// time, wherever the matrix starts.
+// time, wherever the matrix starts.  Bound by memory: 32 of 1536 x 4096 in fp32 450 us, 2.4 GB at 5.4 TB/s.
 template <class GT>
 __global__ void __launch_bounds__(256)
 ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mode, size_t per_matrix, float *m_out, double *__restrict__ parts)
@@ -111,7 +115,8 @@ ortho_momentum_kernel(const GT *__restrict__ g, const float *m, float mu, int mo
     if (threadIdx.x == 0) parts[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// X = kScale U / |U| as two halves, padding included.  A thread takes 8 consecutive padded columns of a row.
+// X = kScale U / |U| as two halves, padding included.  A thread takes 8 consecutive padded columns of a row.  A pass of its own over G
+// and M', since |U| is known only behind the first.  Bound by memory: 32 of 1536 x 4096 465 us, 2.4 GB at 5.2 TB/s.
 template <class GT>
 __global__ void __launch_bounds__(256)
 ortho_load_kernel(const GT *__restrict__ g, const float *__restrict__ m_new, float mu, int mode, OrthoShape s, const double *__restrict__ parts,
@@ -571,10 +576,13 @@ int ortho_steps(const OrthoShape &s, const OrthoWs &w, int steps, float scale, u
 // multiplies its own rows and takes their share of the next A while they are at hand.  X lies with the long side first whatever the
 // gradient's layout, so that every product finds what it needs along memory or through transposing LDS reads; a workgroup alone
 // reads and writes its rows, so they are updated in place.  Partial A's travel in accumulator order.  Where one workgroup holds a
-// matrix it does all the steps in one launch.  us a call, tiles and 17 launches -> this: 8 of 128 x 256 102 -> 70, 4096 x 128 200 -> 91, 64 x 4096 172 -> 74,
-// 128 of 128 x 2048 690 -> 470, 39 of 21 x 2499 238 -> 128.
+// matrix it does all the steps in one launch.  us a call, tiles and 17 launches -> this: 8 of 128 x 256 102 -> 58, 4096 x 128 200 -> 79, 64 x 4096 172 -> 70,
+// 128 of 128 x 2048 690 -> 433, 39 of 21 x 2499 238 -> 119.
 // 16 waves, one 32 x 32 tile each in every phase: the phases are short chains of LDS round trips and conversions, and with four waves
-// of four times the tiles a step of 128 x 128 took 16 us (nothing hides a wave's own latency) where this takes 10.
+// of four times the tiles a step of 128 x 128 took 16 us (nothing hides a wave's own latency) where 16 waves took 10.  Bound by LDS reads (products) and
+// vector instructions (conversions), 15300 cycles a step: A to halves 1900, A A^T 1400, B to halves 1900, B X 2050, X' 2650, its
+// Gram matrix and stores 3200, the rest waits.  Before images took the place of the tiles above the diagonal, and diagonals were taken out by the
+// waves that hold one, 19000.
 constexpr int kThinSide = 128, kThinWaves = 16, kThinThreads = kThinWaves * 64, kThinBatch = 2;
 template <int MP> struct Thin {
     static constexpr int TILES = MP / 32;                    // of a side of A

@@ -324,7 +324,8 @@ router_fwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids
     } else if (tid == 0) part_out.tokens[at] = n;
 }
 
-// Many blocks' sums to kFoldRows (one block alone took 235 us for those of 8192 tokens of 1000 experts, with the fold both launches take 11): grid (64 experts, fold, n_mb), a fold's rows dealt to four waves, which join in ascending order.
+// Many blocks' sums to kFoldRows: grid (64 experts, fold, n_mb), a fold's rows dealt to four waves, which join in ascending order.  (One
+// block alone took 235 us for the sums of 8192 tokens of 1000 experts; with the fold both launches take 11.)
 constexpr int kFoldRows = 16;
 __global__ void __launch_bounds__(256)
 router_fold_kernel(RouterPartials part, int blocks, int per_fold, int E, float *__restrict__ prob, int32_t *__restrict__ count)
@@ -404,7 +405,8 @@ router_finish_kernel(RouterPartials part, int blocks, int rows, int k, int E, in
 //   normalised gates: du_{id_s} += part_s (scale dg_s - sum part scale dg);  sigmoid scores as they are: du_{id_s} += part_s scale dg_s;
 //   dz = du (softmax), du sigmoid(-z) (sigmoid).
 // What falls on the selected experts goes through the token's LDS row, one selection after the other: the same expert twice adds
-// up in the order of the selections.
+// up in the order of the selections.  Probabilities are worked out again rather than saved: the row is read anyway.  524288 tokens, 128 experts, 8
+// selected, bf16: 74 us, 303 MB at 4.1 TB/s; 32768 tokens of 256 sigmoid scores in fp32 22 us, 69 MB at 3.1 TB/s.
 template <class ZT, bool SIGMOID, int LT, int CH, int NS>
 __global__ void __launch_bounds__(router_waves<CH>() * 64)
 router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids, const uint8_t *__restrict__ valid, const float *__restrict__ dgates,
