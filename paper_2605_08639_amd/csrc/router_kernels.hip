@@ -196,16 +196,15 @@ __device__ __forceinline__ float balance_loss(double dot, float coef, int E, int
     return n > 0.0 ? (float)((double)coef * E * dot / ((double)k * n * n)) : 0.0f;
 }
 
+// The block's sum for all of its threads: waves by shuffles, then the waves' sums in ascending order.
 __device__ __forceinline__ double block_sum(double v, double *red, int threads)
 {
-    const int tid = threadIdx.x;
-    red[tid] = v;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    for (int n = threads / 2; n > 0; n >>= 1) {
-        if (tid < n) red[tid] += red[tid + n];
-        __syncthreads();
-    }
-    const double total = red[0];
+    double total = 0.0;
+    for (int w = 0; w < threads / 64; ++w) total += red[w];
     __syncthreads();
     return total;
 }
@@ -358,15 +357,15 @@ constexpr int kFinishThreads = 1024;
 __global__ void __launch_bounds__(kFinishThreads)
 router_finish_kernel(RouterPartials part, int blocks, int rows, int k, int E, int lanes_e, float coef, RouterSums out)
 {
-    __shared__ double red[kFinishThreads];
+    __shared__ double red[kFinishThreads / 64];
     __shared__ float s_prob[kFinishThreads];
     __shared__ int32_t s_count[kFinishThreads];
     const int tid = threadIdx.x, mb = blockIdx.x;
     const size_t base = (size_t)mb * rows;
     double tokens = 0.0;
     for (int b = tid; b < blocks; b += kFinishThreads) tokens += part.tokens[(size_t)mb * blocks + b];
-    const double n = block_sum(tokens, red, kFinishThreads);
-    const float inv_n = n > 0.0 ? (float)(1.0 / n) : 0.0f;
+    double n = 0.0;
+    float inv_n = 0.0f;
     const int el = tid % lanes_e, strip = tid / lanes_e, strips = kFinishThreads / lanes_e;
     double dot = 0.0;
     for (int e0 = 0; e0 < E; e0 += lanes_e) {
@@ -381,6 +380,10 @@ router_finish_kernel(RouterPartials part, int blocks, int rows, int k, int E, in
             }
         s_prob[tid] = p;
         s_count[tid] = c;
+        if (e0 == 0) {                                        // (behind the first experts' loads: both are on their way together)
+            n = block_sum(tokens, red, kFinishThreads);
+            inv_n = n > 0.0 ? (float)(1.0 / n) : 0.0f;
+        }
         __syncthreads();
         if (strip == 0 && e < E) {
             for (int s = 1; s < strips; ++s) {
