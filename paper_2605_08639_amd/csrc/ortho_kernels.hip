@@ -448,9 +448,15 @@ ortho_update_kernel(const uint16_t *__restrict__ x, uint16_t *lo, const uint16_t
             uint16_t *O = last.out + (size_t)mat * s.rows * s.cols;
             if (last.vec) ST::flush(buf_h, O, s.cols, wrow0, s.rows, wcol0, s.cols, lane);
             else
-                for (int r = 0; r < 64 && wrow0 + r < s.rows; ++r)
-                    if (wcol0 + lane < s.cols)
-                        O[(size_t)(wrow0 + r) * s.cols + wcol0 + lane] = *reinterpret_cast<const uint16_t *>(buf_h + ST::acc_addr(r, lane & ~3) + (lane & 3) * 2);
+#pragma unroll 1
+                for (int r0 = 0; r0 < 64; r0 += 16) {         // 16 reads of LDS, then their stores
+                    uint16_t v[16];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) v[r] = *reinterpret_cast<const uint16_t *>(buf_h + ST::acc_addr(r0 + r, lane & ~3) + (lane & 3) * 2);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (wrow0 + r0 + r < s.rows && wcol0 + lane < s.cols) O[(size_t)(wrow0 + r0 + r) * s.cols + wcol0 + lane] = v[r];
+                }
         }
         wave_lds_fence();
     }
