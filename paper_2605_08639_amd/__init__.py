@@ -836,7 +836,7 @@ def orthogonalize_workspace(n, rows, cols, device="cuda"):
 
 def relibra_orthogonalize(grad, momentum=None, mu=0.95, nesterov=True, scale=1.0, steps=5, out=None, momentum_out=None, workspace=None):
     """grad [n,rows,cols] fp32 or bf16 (dWg, dWu, dWd of the experts) and momentum fp32 (or None) -> (the orthogonalised update [n,rows,cols] bf16,
-    the new momentum (None without)).  momentum_out may be the momentum itself; nesterov counts with momentum only."""
+    the new momentum (None without)).  momentum_out may be the momentum itself; nesterov counts with momentum only; 1 to 8 steps."""
     n, rows, cols = grad.shape
     assert grad.dtype in (torch.bfloat16, torch.float32), f"gradients in bf16 or fp32, got {grad.dtype}"
     assert momentum is None or (momentum.shape == grad.shape and momentum.dtype is torch.float32), "momentum is like grad, in fp32"

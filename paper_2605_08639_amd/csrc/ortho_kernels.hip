@@ -37,6 +37,7 @@ constexpr float kScale = 4096.0f;
 constexpr int kOrthoPad = 64;
 constexpr int kMinParts = 16, kMaxParts = 1024;  // partial sums of a matrix's squares
 constexpr int kOrthoMaxSide = 32768;
+constexpr int kOrthoMaxSteps = 8;                // rank 1 of 256 x 500, simulated: an error of 1.5e-3 of the norm (outside of its space, times 3.44 a step)
 constexpr int kComputeUnits = 256;
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
@@ -1103,7 +1104,7 @@ extern "C" int relibra_orthogonalize(const void *grad, const float *momentum, in
 {
     hipStream_t stream = (hipStream_t)stream_;
     if (n < 0 || rows < 0 || cols < 0 || steps < 1 || (flags & ~(RELIBRA_ORTHO_BF16 | RELIBRA_ORTHO_NESTEROV))) return RELIBRA_EINVAL;
-    if (n > 65535 || rows > kOrthoMaxSide || cols > kOrthoMaxSide || steps > 64) return RELIBRA_EUNSUPPORTED;
+    if (n > 65535 || rows > kOrthoMaxSide || cols > kOrthoMaxSide || steps > kOrthoMaxSteps) return RELIBRA_EUNSUPPORTED;
     if ((momentum != nullptr) != (momentum_out != nullptr) || (!momentum && (flags & RELIBRA_ORTHO_NESTEROV))) return RELIBRA_EINVAL;
     if (n == 0 || rows == 0 || cols == 0) return RELIBRA_OK;
     if (!grad || !out || out == grad) return RELIBRA_EINVAL;
