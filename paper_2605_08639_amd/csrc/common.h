@@ -58,8 +58,8 @@ inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Workspace sizes of the entry points in other translation units (relibra_workspace_bytes).
-size_t router_ws_bytes(int n_mb, int T, int E);
+// Workspace sizes of the entry points in other translation units (relibra_workspace_bytes); 0 where the call refuses the sizes.
+size_t router_ws_bytes(int n_mb, int T, int k, int E);
 size_t norm_ws_bytes(int T, int h);
 size_t ortho_ws_bytes(int n, int rows, int cols);
 

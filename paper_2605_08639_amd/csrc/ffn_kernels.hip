@@ -1200,9 +1200,9 @@ extern "C" size_t relibra_workspace_bytes(int which, int T, int k, int E, int G,
     case RELIBRA_WS_FFN_BWD: return ffn_ws_bytes(N, G, hff, true);
     case RELIBRA_WS_WGRAD_BATCHED: return round256(wgrad_plan_ints(E, G) * sizeof(int32_t));
     case RELIBRA_WS_DGATE: return dgate_scratch_bytes(N, hff);
-    case RELIBRA_WS_ROUTER: return (long long)G * T <= 1 << 30 && G <= 65535 && E <= 4096 ? router_ws_bytes(G, T, E) : 0;
-    case RELIBRA_WS_BLOCK_NORM: return h >= 8 && h <= 8192 && h % 8 == 0 && T <= 1 << 30 ? norm_ws_bytes(T, h) : 0;
-    case RELIBRA_WS_ORTHOGONALIZE: return h >= 1 && h <= 32768 && hff >= 1 && hff <= 32768 && E <= 65535 ? ortho_ws_bytes(E, h, hff) : 0;
+    case RELIBRA_WS_ROUTER: return router_ws_bytes(G, T, k, E);
+    case RELIBRA_WS_BLOCK_NORM: return norm_ws_bytes(T, h);
+    case RELIBRA_WS_ORTHOGONALIZE: return ortho_ws_bytes(E, h, hff);
     default: return 0;
     }
     (void)h;

@@ -354,8 +354,10 @@ inline NormGrid norm_grid(int T, int h, bool bwd)
     return g;
 }
 inline size_t norm_join_bytes(const NormGrid &g, int h) { return (size_t)(g.rows_per_block - 1) * h * sizeof(float); }
+inline bool norm_takes(int T, int h) { return h % 8 == 0 && h <= kNormMaxWidth && T <= 1 << 30; }
 size_t norm_ws_bytes(int T, int h)
 {
+    if (h < 8 || !norm_takes(T, h)) return 0;
     const NormGrid g = norm_grid(T, h, true);
     return 2 * round256((size_t)g.blocks * h * sizeof(float));
 }
@@ -363,7 +365,7 @@ size_t norm_ws_bytes(int T, int h)
 inline int check_norm(int T, int h, int flags, int known, float eps)
 {
     if (T < 0 || h < 8 || (flags & ~known) || !(eps > 0.0f)) return RELIBRA_EINVAL;
-    if (h % 8 || h > kNormMaxWidth || T > 1 << 30) return RELIBRA_EUNSUPPORTED;
+    if (!norm_takes(T, h)) return RELIBRA_EUNSUPPORTED;
     if ((flags & RELIBRA_NORM_GATE_TOKEN) && (flags & RELIBRA_NORM_GATE_ELEMENT)) return RELIBRA_EINVAL;
     return RELIBRA_OK;
 }

@@ -1047,8 +1047,14 @@ int thin_run(const ThinShape &s, const ThinWs &w, const GT *g, const float *m_ne
     return RELIBRA_OK;
 }
 
+// (2^30 tiles of 64 x 64: tile numbers are ints)
+inline bool ortho_takes(int n, int rows, int cols)
+{
+    return n <= 65535 && rows <= kOrthoMaxSide && cols <= kOrthoMaxSide && (long long)n * ((rows + 63) / 64) * ((cols + 63) / 64) < 1 << 30;
+}
 size_t ortho_ws_bytes(int n, int rows, int cols)
 {
+    if (rows < 1 || cols < 1 || !ortho_takes(n, rows, cols)) return 0;
     const size_t parts = round256((size_t)n * norm_parts(n, rows, cols) * sizeof(double));
     if (is_thin(rows, cols)) {
         const ThinShape s = thin_shape(n, rows, cols);
@@ -1104,11 +1110,10 @@ extern "C" int relibra_orthogonalize(const void *grad, const float *momentum, in
 {
     hipStream_t stream = (hipStream_t)stream_;
     if (n < 0 || rows < 0 || cols < 0 || steps < 1 || (flags & ~(RELIBRA_ORTHO_BF16 | RELIBRA_ORTHO_NESTEROV))) return RELIBRA_EINVAL;
-    if (n > 65535 || rows > kOrthoMaxSide || cols > kOrthoMaxSide || steps > kOrthoMaxSteps) return RELIBRA_EUNSUPPORTED;
+    if (!ortho_takes(n, rows, cols) || steps > kOrthoMaxSteps) return RELIBRA_EUNSUPPORTED;
     if ((momentum != nullptr) != (momentum_out != nullptr) || (!momentum && (flags & RELIBRA_ORTHO_NESTEROV))) return RELIBRA_EINVAL;
     if (n == 0 || rows == 0 || cols == 0) return RELIBRA_OK;
     if (!grad || !out || out == grad) return RELIBRA_EINVAL;
-    if ((long long)n * ((rows + 63) / 64) * ((cols + 63) / 64) > 0x3fffffff) return RELIBRA_EUNSUPPORTED;
     if (!workspace || workspace_bytes < ortho_ws_bytes(n, rows, cols)) return RELIBRA_EWORKSPACE;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     const int mode = !momentum ? U_GRAD : flags & RELIBRA_ORTHO_NESTEROV ? U_NESTEROV : U_MOMENTUM;

@@ -568,13 +568,20 @@ inline RouterWs router_ws(int n_mb, const RouterGrid &g, int E)
     w.bytes = w.fold_count + round256(folded * sizeof(int32_t));
     return w;
 }
-size_t router_ws_bytes(int n_mb, int T, int E) { return router_ws(n_mb, router_grid(n_mb, T, E, true), E).bytes; }
+inline bool router_takes(int n_mb, int T, int k, int E)
+{
+    return E <= kRouterMaxExperts && k <= 64 && n_mb <= 65535 && (long long)n_mb * T <= 1 << 30 && (long long)T * k <= INT32_MAX;
+}
+size_t router_ws_bytes(int n_mb, int T, int k, int E)
+{
+    return k <= E && router_takes(n_mb, T, k, E) ? router_ws(n_mb, router_grid(n_mb, T, E, true), E).bytes : 0;
+}
 
 inline int check_router(int n_mb, int T, int k, int E, int flags, const void *logits, const void *ids)
 {
     const int known = RELIBRA_ROUTER_SIGMOID | RELIBRA_ROUTER_NORMALIZE | RELIBRA_ROUTER_FP32;
     if (n_mb < 0 || T < 0 || E < 1 || k < 1 || k > E || (flags & ~known)) return RELIBRA_EINVAL;
-    if (E > kRouterMaxExperts || k > 64 || n_mb > 65535 || (long long)n_mb * T > 1 << 30 || (long long)T * k > INT32_MAX) return RELIBRA_EUNSUPPORTED;
+    if (!router_takes(n_mb, T, k, E)) return RELIBRA_EUNSUPPORTED;
     if ((size_t)n_mb * T > 0 && (!logits || !ids || !aligned16(logits))) return RELIBRA_EINVAL;
     return RELIBRA_OK;
 }

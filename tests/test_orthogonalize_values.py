@@ -140,3 +140,12 @@ def call(n=2, rows=64, cols=64, steps=5, flags=0, grad=1 << 20, mom=0, mom_out=0
 def test_orthogonalize_refuses_steps_whose_result_would_be_noise(steps):
     """Rank 1 of 256 x 500, simulated: 1.6e-2 of the norm after 10 steps, 0.2 after 12."""
     assert call(steps=steps) == rl.EUNSUPPORTED
+
+
+def test_no_workspace_for_sizes_that_the_calls_refuse():
+    for n, rows, cols in ((65535, 32768, 32768), (4096, 32768, 32768), (65535, 32768, 2049)):
+        assert call(n=n, rows=rows, cols=cols) == rl.EUNSUPPORTED
+        assert rl.workspace_bytes(rl.WS_ORTHOGONALIZE, 0, 1, n, 1, rows, cols) == 0
+    assert rl.workspace_bytes(rl.WS_ORTHOGONALIZE, 0, 1, 4095, 1, 32768, 32768) > 0
+    assert rl.workspace_bytes(rl.WS_ROUTER, 4, 65, 128, 1, 0, 0) == 0 and rl.workspace_bytes(rl.WS_ROUTER, 4, 9, 8, 1, 0, 0) == 0
+    assert rl.workspace_bytes(rl.WS_ROUTER, 4, 64, 128, 1, 0, 0) > 0 and rl.workspace_bytes(rl.WS_ROUTER, 4, 8, 8, 1, 0, 0) > 0
