@@ -588,8 +588,8 @@ int relibra_unpermute_combine(int mode, const void *rows_dev, const void *tok_de
  * Over a micro-batch's n valid tokens, f_e = counts_e / (k n) and P_e = mean p_e, the loss is
  *   loss = balance_coef * E * sum_e f_e P_e     (0 if n = 0).
  *   logits_dev [n_mb, T, E] bf16, or fp32 with RELIBRA_ROUTER_FP32, dev, in; -infinity takes an expert out of a token's reach
- *              (a set with nothing else in it has probabilities, parts and gates 0); +infinity and NaN make the token's p, and
- *              with them prob_mean and loss, NaN
+ *              (a set with nothing else in it has probabilities, parts and gates 0); NaN, and without RELIBRA_ROUTER_SIGMOID
+ *              +infinity, make the token's p, and with them prob_mean and loss, NaN (+infinity's sigmoid is 1, u 0)
  *   ids_dev    [n_mb, T, k] int32, dev, in: the replayed experts; an id outside [0, E) has gate 0, is not counted and raises
  *              RELIBRA_ERR_ID_RANGE; the same expert twice counts twice
  *   valid_dev  [n_mb, T] uint8, dev, in, or NULL: tokens with 0 (padding) have gates 0 and enter no sum; their logits and ids

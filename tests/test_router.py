@@ -346,3 +346,31 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
 def test_router_refuses_more_selections_than_a_count_holds():
     assert _fwd(T=1 << 28, k=8) == rl.EUNSUPPORTED and _bwd(T=1 << 28, k=8) == rl.EUNSUPPORTED
     assert rl.workspace_bytes(rl.WS_ROUTER, 4, 2, 4097, 1, 0, 0) == 0 and rl.workspace_bytes(rl.WS_ROUTER, 4, 2, 8, 65536, 0, 0) == 0
+
+
+@gpu
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+def test_router_positive_infinity(dtype, normalize):
+    """A sigmoid of +infinity is 1, as that of 200 in fp32: every result is the same bit for bit.  A softmax is NaN there, and stays with its token
+    and its micro-batch's means; gates normalised over other selections are not touched."""
+    E, k = 24, 3
+    z, ids, _ = make(2, 40, E, k, dtype, seed=41)
+    z[0, 4, 6] = z[0, 5, ids[0, 5, 1]] = 200.0
+    ids[0, 4] = torch.tensor([0, 1, 2], dtype=torch.int32)   # the infinite logit is not selected here
+    zi = z.clone()
+    zi[z == 200.0] = math.inf
+    dg, dl = torch.randn((2, 40, k), device=DEV), torch.full((2,), 30.0, device=DEV)
+
+    def both(zz, sigmoid):
+        how = dict(sigmoid=sigmoid, normalize=normalize, balance_coef=1.0)
+        f = rl.relibra_router_fwd(zz.to(DEV), ids.to(DEV), **how)
+        return (*f, rl.relibra_router_bwd(zz.to(DEV), ids.to(DEV), dg, f[1], f[2], dl, **how))
+    a, b = both(zi, True), both(z, True)
+    assert all(torch.isfinite(x.float()).all() and torch.equal(x, y) for x, y in zip(a, b))
+    a, b = both(zi, False), both(z, False)
+    hit = torch.zeros((2, 40), dtype=torch.bool)
+    hit[0, 4:6] = True
+    assert torch.isnan(a[3][0]).all() and torch.isnan(a[4][0]) and torch.equal(a[3][1], b[3][1]) and torch.equal(a[4][1], b[4][1])
+    assert torch.equal(a[0][~hit], b[0][~hit]) and torch.equal(a[5][~hit], b[5][~hit]) and torch.isnan(a[0][0, 5]).any()
+    assert torch.isnan(a[5][0, 4:6].float()).all() and (torch.equal(a[0][0, 4], b[0][0, 4]) if normalize else torch.isnan(a[0][0, 4]).all())
