@@ -658,7 +658,8 @@ int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const 
  * what rounding leaves outside of a low-rank gradient's space grows by 3.44 a step, to about (2^-24 + 2^-28 sqrt(m)) 3.44^steps of the norm, m the
  * shorter side: 2e-3 after 8 at m = 256, 1.4e-2 at 32768; more steps than 8 are refused.
  * Fixed order, no atomics: results are reproducible bit for bit.
- * Limits: rows, cols <= 32768, n <= 65535, 1 <= steps <= 8 (RELIBRA_EUNSUPPORTED beyond).  No output but momentum_out overlaps an input.
+ * Limits: rows, cols <= 32768, n <= 65535, 1 <= steps <= 8 (RELIBRA_EUNSUPPORTED beyond).  momentum_out may be momentum itself;
+ * beside that no output may overlap an input or the other output (RELIBRA_EINVAL).
  */
 enum { RELIBRA_ORTHO_BF16 = 1, RELIBRA_ORTHO_NESTEROV = 2 };
 int relibra_orthogonalize(const void *grad_dev, const float *momentum_dev, int n, int rows, int cols, float mu, float scale, int steps, int flags,

@@ -56,6 +56,13 @@ __device__ __forceinline__ int block_scan256(int v, int32_t *sums, int &total)
 
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Whether two pieces of memory share a byte.
+inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a), bt = reinterpret_cast<uintptr_t>(b);
+    return at < bt + b_bytes && bt < at + a_bytes;
+}
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Workspace sizes of the entry points in other translation units (relibra_workspace_bytes); 0 where the call refuses the sizes.

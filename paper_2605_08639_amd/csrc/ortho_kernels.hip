@@ -1113,9 +1113,14 @@ extern "C" int relibra_orthogonalize(const void *grad, const float *momentum, in
     if (!ortho_takes(n, rows, cols) || steps > kOrthoMaxSteps) return RELIBRA_EUNSUPPORTED;
     if ((momentum != nullptr) != (momentum_out != nullptr) || (!momentum && (flags & RELIBRA_ORTHO_NESTEROV))) return RELIBRA_EINVAL;
     if (n == 0 || rows == 0 || cols == 0) return RELIBRA_OK;
-    if (!grad || !out || out == grad) return RELIBRA_EINVAL;
+    if (!grad || !out) return RELIBRA_EINVAL;
     if (!workspace || workspace_bytes < ortho_ws_bytes(n, rows, cols)) return RELIBRA_EWORKSPACE;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
+    // a momentum written over the gradient would be read as the gradient by the pass that divides by the norm
+    const size_t halves = (size_t)n * rows * cols * 2, floats = 2 * halves, grad_bytes = flags & RELIBRA_ORTHO_BF16 ? halves : floats;
+    if (overlap(out, halves, grad, grad_bytes)) return RELIBRA_EINVAL;
+    if (momentum && (overlap(out, halves, momentum, floats) || overlap(out, halves, momentum_out, floats) || overlap(momentum_out, floats, grad, grad_bytes) ||
+                     (momentum_out != momentum && overlap(momentum_out, floats, momentum, floats)))) return RELIBRA_EINVAL;
     const int mode = !momentum ? U_GRAD : flags & RELIBRA_ORTHO_NESTEROV ? U_NESTEROV : U_MOMENTUM;
     const int rc = flags & RELIBRA_ORTHO_BF16
                        ? ortho_run(n, rows, cols, (const bf16_t *)grad, momentum, mu, scale, steps, mode, momentum_out, (uint16_t *)out, (char *)workspace, stream)

@@ -149,3 +149,17 @@ def test_no_workspace_for_sizes_that_the_calls_refuse():
     assert rl.workspace_bytes(rl.WS_ORTHOGONALIZE, 0, 1, 4095, 1, 32768, 32768) > 0
     assert rl.workspace_bytes(rl.WS_ROUTER, 4, 65, 128, 1, 0, 0) == 0 and rl.workspace_bytes(rl.WS_ROUTER, 4, 9, 8, 1, 0, 0) == 0
     assert rl.workspace_bytes(rl.WS_ROUTER, 4, 64, 128, 1, 0, 0) > 0 and rl.workspace_bytes(rl.WS_ROUTER, 4, 8, 8, 1, 0, 0) > 0
+
+
+def test_orthogonalize_refuses_outputs_over_inputs():
+    """2 matrices of 64 x 64: 32 KiB in fp32, 16 KiB in bf16.  A momentum written over the gradient would be read as the gradient."""
+    grad, mom, out, k = 1 << 20, 8 << 20, 2 << 20, 1 << 10
+    for flags in (0, rl.ORTHO_NESTEROV):
+        with_momentum = dict(mom=mom, flags=flags)
+        for at in (grad, grad + 4, grad + 32 * k - 4, grad - 32 * k + 4, mom + 4, mom - 4):
+            assert call(mom_out=at, **with_momentum) == rl.EINVAL, at
+        for at in (mom, mom + 32 * k - 2, mom - 16 * k + 2, grad + 2):
+            assert call(mom_out=mom, out=at, **with_momentum) == rl.EINVAL, at
+        assert call(mom_out=16 << 20, out=(16 << 20) + 8 * k, **with_momentum) == rl.EINVAL
+        assert call(mom_out=grad + 8 * k, grad=grad, mom=mom, flags=flags | rl.ORTHO_BF16) == rl.EINVAL
+    assert call(out=grad) == rl.EINVAL and call(out=grad - 16 * k + 2) == rl.EINVAL and call(out=grad + 16 * k - 2, flags=rl.ORTHO_BF16) == rl.EINVAL
