@@ -163,3 +163,85 @@ def test_orthogonalize_refuses_outputs_over_inputs():
         assert call(mom_out=16 << 20, out=(16 << 20) + 8 * k, **with_momentum) == rl.EINVAL
         assert call(mom_out=grad + 8 * k, grad=grad, mom=mom, flags=flags | rl.ORTHO_BF16) == rl.EINVAL
     assert call(out=grad) == rl.EINVAL and call(out=grad - 16 * k + 2) == rl.EINVAL and call(out=grad + 16 * k - 2, flags=rl.ORTHO_BF16) == rl.EINVAL
+
+
+# ------------------------------------------------------------------ every path, every value, nothing else
+def guarded(shape, dtype, odd=0):
+    """A tensor of NaN bits with 64 (+ odd) elements of them in front and 64 behind, and a check that those are as they were."""
+    count = math.prod(shape)
+    ints = {2: torch.int16, 4: torch.int32, 1: torch.uint8}[dtype.itemsize]
+    flat = torch.full((count + 128 + odd,), 255 if dtype.itemsize == 1 else -1, dtype=ints, device=DEV)
+    whole = flat.view(dtype)
+
+    def untouched():
+        edge = torch.cat([flat[:64 + odd], flat[64 + odd + count:]])
+        return bool((edge == (255 if dtype.itemsize == 1 else -1)).all())
+    return whole[64 + odd:64 + odd + count].view(shape), untouched
+
+
+PATHS = [
+    # a short side of at most 64 (runs of 256 rows): one workgroup a matrix; several runs each; several workgroups, their sums direct or summed first
+    (3, 1, 7), (2, 9, 1), (1, 1, 300), (9, 33, 47), (300, 16, 40), (130, 50, 600), (200, 300, 64), (2, 64, 700), (1, 24, 4100), (40, 2000, 60), (100, 2500, 33),
+    # at most 128 (runs of 128 rows): the same
+    (4, 128, 256), (5, 65, 66), (130, 100, 300), (130, 300, 100), (2, 127, 700), (1, 1000, 128), (100, 127, 700), (100, 700, 127), (40, 127, 1500), (40, 1500, 127),
+    # few tiles, wide and tall, contraction whole and split (2112: four parts; 4672: nine, the last of one LDS tile)
+    (2, 257, 130), (1, 300, 1000), (3, 1001, 333), (1, 300, 2112), (1, 2112, 300), (1, 260, 4672), (1, 4672, 140), (5, 129, 192),
+    # small tiles for X' where they are more: 216 of 128 x 128, 72 of 256 x 256
+    (6, 300, 1500), (6, 1500, 300),
+    # X' in large tiles, A and B in small ones of single depth (more than 256 of them) and in large ones
+    (28, 400, 527), (28, 527, 400), (40, 300, 520), (44, 500, 310),
+]
+
+
+@gpu
+@pytest.mark.parametrize("shape", PATHS, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("odd", [0, 1], ids=["aligned", "odd"])
+def test_orthogonalize_writes_every_value_and_nothing_else(shape, odd):
+    """Outputs and workspace full of NaN before the call, NaN around them; odd: outputs and inputs 2 or 4 bytes off 16."""
+    n, r, c = shape
+    dtype = torch.bfloat16 if odd else torch.float32
+    g, m = gauss(*shape, seed=sum(shape)).to(dtype), gauss(*shape, seed=r)
+    gd, md = guarded(shape, dtype, odd)[0].copy_(g), guarded(shape, torch.float32, odd)[0].copy_(m)
+    out, out_kept = guarded(shape, torch.bfloat16, odd)
+    mom, mom_kept = guarded(shape, torch.float32, odd)
+    ws, ws_kept = guarded((rl.workspace_bytes(rl.WS_ORTHOGONALIZE, 0, 1, n, 1, r, c),), torch.uint8)
+    rl.relibra_orthogonalize(gd, momentum=md, mu=0.5, nesterov=bool(odd), scale=0.3, out=out, momentum_out=mom, workspace=ws)
+    torch.cuda.synchronize()
+    assert out_kept() and mom_kept() and ws_kept()
+    assert torch.equal(md.cpu(), m) and torch.equal(gd.cpu(), g)
+    want_m = 0.5 * m.double() + g.double()
+    assert torch.equal(mom.cpu(), want_m.float())            # (0.5 m is exact: one rounding)
+    step = mom.cpu()
+    u = torch.addcmul(g.double(), step.double(), torch.tensor(0.5, dtype=torch.float64)) if odd else step.double()
+    some = [0, n // 2, n - 1] if n > 8 else range(n)
+    check_values(out[list(some)], u[list(some)], scale=0.3)
+    assert torch.isfinite(out.float()).all()
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(3, 70, 40), (3, 100, 300), (3, 1, 50), (2, 300, 140), (2, 130, 700), (100, 127, 700)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_orthogonalize_infinities_and_nan_fill_their_own_matrix(shape, value):
+    g = gauss(*shape, seed=9)
+    g[1, shape[1] // 2, shape[2] - 1] = value
+    out, _ = rl.relibra_orthogonalize(g.to(DEV))
+    assert torch.isnan(out[1].float()).all() and torch.isfinite(out[0].float()).all() and torch.isfinite(out[2:].float()).all()
+    check_values(out[:1], g[:1])
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(1, 32768, 136), (2, 140, 16384), (1, 1, 32768), (1, 32768, 90), (1, 4096, 700)], ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize_every_value_of_the_longest_sides(shape):
+    g = 1e-3 * gauss(*shape, seed=sum(shape))
+    check_values(rl.relibra_orthogonalize(g.to(DEV))[0], g)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(64, 1000), (1000, 64), (256, 256), (300, 700)], ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize_values_of_one_size(shape):
+    """Signs times signs: all values round alike, and their errors add up instead of averaging out."""
+    g = (gauss(1, shape[0], 1, 1).sign() * gauss(1, 1, shape[1], 2).sign()).expand(2, *shape).contiguous()
+    out, _ = rl.relibra_orthogonalize(g.to(DEV))
+    for o in out.cpu().double():
+        want = definition(wide(g[0]), 5)
+        assert (wide(o) - want).norm() <= 1.3e-2 * want.norm()
