@@ -630,7 +630,8 @@ int relibra_router_bwd(const void *logits_dev, const int32_t *ids_dev, const uin
  * x_out as the forward call left it (x where y is NULL).  dx, dx_out in the stream's type, dy bf16, dgate like the gate, dw_post,
  * dw_pre [h] fp32: overwritten, or added to with RELIBRA_NORM_ACCUMULATE.  dx may be dx_out, dy may be y or dn.
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_BLOCK_NORM, T, 1, 1, 1, h, 0) bytes
- * Row sums and weight gradients are added up in fp32 in a fixed order: results are reproducible bit for bit.
+ * Row sums and weight gradients are added up in fp32 in a fixed order: results are reproducible bit for bit.  A row whose squares add up to
+ * more than fp32 holds (h values of 2e19 / sqrt(h)) has an infinite rms, and norms of 0 as far as its values are finite.
  * Limits: eps > 0, h % 8 == 0, h <= 8192, T <= 2^30, 16-byte aligned tensors (one gate a row: 4 bytes).
  */
 enum { RELIBRA_NORM_STREAM_FP32 = 1, RELIBRA_NORM_GATE_TOKEN = 2, RELIBRA_NORM_GATE_ELEMENT = 4, RELIBRA_NORM_ACCUMULATE = 8 };

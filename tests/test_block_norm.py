@@ -271,3 +271,61 @@ def test_block_norm_refuses_missing_outputs_and_small_workspaces():
     assert _bwd(w_pre=0, dxo=0) == rl.EINVAL and _bwd(flags=4, dgate=4100) == rl.EINVAL and _bwd(ws=4104) == rl.EINVAL
     need = rl.workspace_bytes(rl.WS_BLOCK_NORM, 4, 1, 1, 1, 64, 0)
     assert need > 0 and _bwd(ws_bytes=need - 1) == rl.EWORKSPACE and _bwd(ws=0) == rl.EWORKSPACE
+
+
+@gpu
+@pytest.mark.parametrize("stream", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_block_norm_rows_whose_squares_pass_fp32(stream):
+    """sqrt(3.4e38 / 512) = 8e17: a row of 1e19 has an infinite rms and the norm 0, 1e17 is an ordinary row; no other row notices."""
+    d = make(40, 512, stream, gate="none", seed=15)
+    plain = rl.relibra_block_norm_fwd(dev(d["x"]), **{k: dev(d[k]) for k in ("y", "w_post", "w_pre")})
+    d["y"][3], d["x"][5], d["x"][6] = 1e19, 1e19, 1e17
+    x_out, n = rl.relibra_block_norm_fwd(dev(d["x"]), **{k: dev(d[k]) for k in ("y", "w_post", "w_pre")})
+    assert torch.equal(x_out[3], dev(d["x"][3]))             # x + 0
+    assert torch.all(n[5] == 0) and torch.all((n[6].float() / dev(d["w_pre"]).float() - 1).abs() <= 2 * HALF16)
+    rest = [i for i in range(40) if i not in (3, 5, 6)]
+    assert torch.equal(x_out[rest], plain[0][rest]) and torch.equal(n[rest], plain[1][rest])
+
+
+# ------------------------------------------------------------------ outputs of NaN before the call, NaN around them
+def guarded(shape, dtype):
+    """A tensor of NaN with 64 elements of it in front and behind, and a check that those are as they were."""
+    count = 1
+    for s in shape:
+        count *= s
+    flat = torch.full((count + 128,), -1, dtype=torch.int16 if dtype.itemsize == 2 else torch.int32, device=DEV)
+    return flat.view(dtype)[64:64 + count].view(shape), lambda: bool((torch.cat([flat[:64], flat[64 + count:]]) == -1).all())
+
+
+@gpu
+@pytest.mark.parametrize("kw", [dict(T=1, h=8), dict(T=601, h=200), dict(T=33, h=1032, gate="element"), dict(T=1027, h=4104), dict(T=7, h=8192, gate="none")], ids=IDS)
+@pytest.mark.parametrize("stream", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_block_norm_writes_every_value_and_nothing_else(kw, stream):
+    d = make(stream=stream, seed=18, **kw)
+    T, h, b16, f32 = kw["T"], kw["h"], torch.bfloat16, torch.float32
+    how = {k: dev(d[k]) for k in ("y", "w_post", "w_pre", "gate")}
+    want = rl.relibra_block_norm_fwd(dev(d["x"]), **how)
+    grads = rl.relibra_block_norm_bwd(want[0], dev(d["dx_out"]), dev(d["dn"]), **how)
+    out = [guarded((T, h), stream), guarded((T, h), b16)]
+    rl.relibra_block_norm_fwd(dev(d["x"]), **how, x_out=out[0][0], n=out[1][0])
+    ws = torch.full((rl.workspace_bytes(rl.WS_BLOCK_NORM, T, 1, 1, 1, h, 0) + 256,), 255, dtype=torch.uint8, device=DEV)
+    back = [guarded((T, h), stream), guarded((T, h), b16), None if d["gate"] is None else guarded(d["gate"].shape, d["gate"].dtype), guarded((h,), f32), guarded((h,), f32)]
+    names = ("dx", "dy", "dgate", "dw_post", "dw_pre")
+    rl.relibra_block_norm_bwd(want[0], dev(d["dx_out"]), dev(d["dn"]), **how, workspace=ws[:-256], **{k: v[0] for k, v in zip(names, back) if v})
+    for (got, kept), w in zip(out + [v for v in back if v], list(want) + [v for v in grads if v is not None]):
+        assert torch.equal(got, w) and kept() and torch.isfinite(got.float()).all()
+    assert torch.all(ws[-256:] == 255)
+
+
+@gpu
+@pytest.mark.parametrize("kw", [dict(T=601, h=200), dict(T=5, h=4096), dict(T=1027, h=1536, gate="element")], ids=IDS)
+def test_block_norm_gradient_over_its_upstream(kw):
+    """dx in the place of dx_out, dy in that of dn; the last rows of a block are not all there."""
+    d = make(stream=torch.float32, seed=19, **kw)
+    how = {k: dev(d[k]) for k in ("y", "w_post", "w_pre", "gate")}
+    x_out, _ = rl.relibra_block_norm_fwd(dev(d["x"]), **how)
+    want = rl.relibra_block_norm_bwd(x_out, dev(d["dx_out"]), dev(d["dn"]), **how)
+    dxo, dn = dev(d["dx_out"]), dev(d["dn"])
+    got = rl.relibra_block_norm_bwd(x_out, dxo, dn, **how, dx=dxo, dy=dn)
+    assert got[0] is dxo and got[1] is dn
+    assert all((a is None and b is None) or torch.equal(a, b) for a, b in zip(got, want))
