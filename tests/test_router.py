@@ -374,3 +374,31 @@ def test_router_positive_infinity(dtype, normalize):
     assert torch.isnan(a[3][0]).all() and torch.isnan(a[4][0]) and torch.equal(a[3][1], b[3][1]) and torch.equal(a[4][1], b[4][1])
     assert torch.equal(a[0][~hit], b[0][~hit]) and torch.equal(a[5][~hit], b[5][~hit]) and torch.isnan(a[0][0, 5]).any()
     assert torch.isnan(a[5][0, 4:6].float()).all() and (torch.equal(a[0][0, 4], b[0][0, 4]) if normalize else torch.isnan(a[0][0, 4]).all())
+
+
+@gpu
+@pytest.mark.parametrize("kw", [dict(n_mb=1, T=1, E=1, k=1), dict(n_mb=3, T=77, E=7, k=3), dict(n_mb=2, T=301, E=60, k=6), dict(n_mb=1, T=9000, E=1000, k=4), dict(n_mb=2, T=513, E=255, k=40)],
+                         ids=lambda c: "x".join(str(v) for v in c.values()))
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+def test_router_writes_every_value_and_nothing_else(kw, dtype):
+    """Outputs and workspace of NaN bits before the calls, NaN bits around them."""
+    n_mb, T, E, k = kw["n_mb"], kw["T"], kw["E"], kw["k"]
+    z, ids, valid = make(n_mb, T, E, k, dtype, seed=51, padded=T > 4)
+    how = dict(sigmoid=True, valid=None if valid is None else valid.to(DEV), balance_coef=0.5)
+    zd, idd, dg, dl = z.to(DEV), ids.to(DEV), torch.randn((n_mb, T, k), device=DEV), torch.full((n_mb,), 9.0, device=DEV)
+    want = rl.relibra_router_fwd(zd, idd, **how)
+    want_dz = rl.relibra_router_bwd(zd, idd, dg, want[1], want[2], dl, **how)
+    kept = []
+
+    def full(shape, t, pad=64):
+        count = math.prod(shape)
+        flat = torch.full((count + 2 * pad,), 255 if t.itemsize == 1 else -1, dtype={1: torch.uint8, 2: torch.int16, 4: torch.int32}[t.itemsize], device=DEV)
+        kept.append(lambda: bool((torch.cat([flat[:pad], flat[pad + count:]]) == (255 if t.itemsize == 1 else -1)).all()))
+        return flat.view(t)[pad:pad + count].view(shape)
+    out = dict(gates=full((n_mb, T, k), torch.float32), counts=full((n_mb, E), torch.int32), n_valid=full((n_mb,), torch.int32), prob_mean=full((n_mb, E), torch.float32),
+               loss=full((n_mb,), torch.float32))
+    ws = full((rl.workspace_bytes(rl.WS_ROUTER, T, k, E, n_mb, 0, 0),), torch.uint8, 256)
+    got = rl.relibra_router_fwd(zd, idd, **how, **out, workspace=ws)
+    dz = rl.relibra_router_bwd(zd, idd, dg, got[1], got[2], dl, **how, dlogits=full((n_mb, T, E), dtype))
+    assert all(torch.equal(a, b) for a, b in zip((*got, dz), (*want, want_dz))) and torch.isfinite(dz.float()).all()
+    assert all(k() for k in kept)
