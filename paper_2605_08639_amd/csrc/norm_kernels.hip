@@ -11,9 +11,10 @@
 // every tensor, so that all of a row's loads are in flight together and stay in registers across the row's sums; the weights
 // stay there from row to row.  Blocks walk the rows with a stride; weight gradients collect in registers, one partial
 // row per block goes to the workspace, and a second kernel adds the partial rows in a fixed order.  16384 rows of 4096 in bf16, one gate
-// a token: forward 98 us (537 MB at 5.5 TB/s), backward 152 us (805 MB at 5.3 TB/s); a plain copy moves 4.8 to 5.2 TB/s.  777 rows of 7168 in fp32 with
-// a gate an element 39 + 5 us (122 MB at 2.8 TB/s): a block a unit, so three rounds of rows and a fourth of nine rows.
-// Requesting the next row's tensors while a row is finished gained nothing (backward 152 -> 161 and 39 -> 39 us): 16 waves a unit hide the latency.
+// a token: forward 98 us (537 MB at 5.5 TB/s), backward 153 us (805 MB at 5.3 TB/s); a plain copy moves 4.8 to 5.2 TB/s.  777 rows of 7168 in fp32 with
+// a gate an element 47 us (122 MB at 2.6 TB/s; 40 + 5 in its kernels): a block a unit, so three rounds of rows and a fourth of nine rows, and a row's
+// loads, sums and stores one behind the other, with no register left for the next row's.
+// Requesting the next row's tensors while a row is finished gained nothing (backward 152 -> 161 and, in the kernel, 39 -> 39 us).
 #include "wave_ops.h"
 
 #include <algorithm>
@@ -332,8 +333,8 @@ struct NormGrid {
 // Forward: two pieces a lane, four waves a block, 16 waves a unit, half of them where a block then still has 16 rounds; few rows are
 // latency and get twice the waves instead.  us, 16384 rows of 4096 in bf16 at 16 / 8 waves a unit 102 / 98, 4096 of 2048 12.2 / 13.4; 700 of
 // 8192 in fp32 with one / two pieces 16.3 / 14.5.
-// Backward: one piece a lane (two take 173 registers instead of 110: half the waves), eight waves a block, 16 a unit: 16384 rows of 4096
-// 157 us, with 8 waves a unit 200, 32 167; with two pieces and four waves a block 176.  The row groups of a block are joined in LDS: with a
+// Backward: one piece a lane (two take 173 registers instead of 110: half the waves), eight waves a block, 16 a unit: 16384 rows of 4096 in one
+// session 157 us, with 8 waves a unit 200, 32 167; with two pieces and four waves a block 176.  The row groups of a block are joined in LDS: with a
 // partial row each the second kernel took longer than the first, 8000 rows of 512 56 -> 16 us, 4096 of 2048 48 -> 25.
 // Up to four rounds of rows are one block's, without a second launch: us a call, 4 rows of 4096 12.9 (two launches 15.7), 4 of 8192 15.0 (15.8), 8 of
 // 4096 18.0 (15.7).

@@ -21,9 +21,11 @@
 // taken over the longer side, along memory (wide) or across it (tall), and X is multiplied from the left or the right.  A and B
 // are symmetric: only tiles on and below the diagonal are computed, and stored twice.
 //
-// Bound by the matrix units and, over a whole call, by power: 32 of 1536 x 4096 take 7.08 ms, of which 5 x (gram 345, poly 160, update 715 us) are
-// products: 0.90, 0.73 and 0.86 PFLOP/s of what the formulas need (a large library product of halves reaches 1.37), gram and poly with 21 tiles
-// of 256 x 256 for 18 tiles' worth, 2.6 rounds of the units paid as 3.
+// 32 of 1536 x 4096 take 6.99 ms, of which 5 x (gram 343, poly 160, update 720 us) are products: 0.90, 0.73 and 0.86 PFLOP/s of what the
+// formulas need (a large library product of halves reaches 1.37).  Gram and poly are bound by the matrix units, with 21 tiles of 256 x 256 for 18 tiles' worth
+// and 2.6 rounds of the units paid as 3.  The update is bound by them and then by memory, one behind the other: its epilogue reads and writes hi and lo, 8 bytes a
+// value, 1.6 GB a launch or about 320 us at the copy rate, while a workgroup that has its unit to itself multiplies nothing, and tiles of one
+// length keep the units in step.  (The last step writes 2 bytes for 4: 655 us where the others take 735, traced.)
 #include "gemm_tile.h"
 #include "wave_ops.h"
 #include "wave_stage.h"
@@ -66,8 +68,8 @@ inline OrthoShape ortho_shape(int n, int rows, int cols)
     auto pad = [](int v) { return (v + kOrthoPad - 1) / kOrthoPad * kOrthoPad; };
     return OrthoShape{n, rows, cols, pad(rows), pad(cols), rows > cols};
 }
-// Blocks that share a matrix's squares: 2048 over all matrices, each with at least 4096 values.  With 64 a matrix one of
-// 4096 x 4096 took 197 us (0.25 of the copy rate).
+// Blocks that share a matrix's squares: about 2048 over all matrices, each with 4096 values or more, but 16 a matrix at least (of small ones
+// some have nothing to do) and 1024 at most.  With 64 a matrix one of 4096 x 4096 took 197 us (0.25 of the copy rate).
 inline int norm_parts(int n, int rows, int cols)
 {
     const size_t values = (size_t)rows * cols;
@@ -524,8 +526,8 @@ template <class CF> int update_tiles(const OrthoShape &s) { return s.n * ((s.rp 
 constexpr int kEnoughWideTiles = 112, kFewNarrowTiles = 192;
 // Where even the small tiles are no more than the compute units, LDS tiles of twice the depth (half the barriers, a workgroup to
 // itself): us a call, 2048 x 2048 375 -> 322, 2 of 1000 x 3000 348 -> 324, 300 x 4000 278 -> 225, level at 8 of 512 x 512; with more tiles the second workgroup of a
-// unit is worth more, 16 of 768 x 2048 695 -> 716.  A long contraction of few tiles is split over the idle units besides, each part at
-// least kMinSplit deep, and joined by a second launch: 300 x 4000 222 -> 168, 4 of 3000 x 200 208 -> 177, 2 of 300 x 2000 176 -> 162, level at 2 of 1000 x
+// unit is worth more, 16 of 768 x 2048 695 -> 716.  A long contraction of few tiles is split over the idle units besides, parts of
+// kMinSplit or a little more, in whole LDS tiles, the last one what is left (2112: three of 576 and one of 384), and joined by a second launch: 300 x 4000 222 -> 168, 4 of 3000 x 200 208 -> 177, 2 of 300 x 2000 176 -> 162, level at 2 of 1000 x
 // 3000 and 8 of 200 x 2048; contractions of 1024 that way: 8 of 256 x 1024 140 -> 155, 5 of 1001 x 333 166 -> 182.
 constexpr int kMinSplit = 512, kSplitFrom = 2048;
 inline GramSplit gram_split(int n, int m, int k)

@@ -27,7 +27,9 @@ struct RouterShape {
 
 // exp(x) for x <= 0, -infinity and NaN: 2^t with t = x log2(e) rounded once, and what that rounding left out put back to first
 // order.  (For x = -infinity that rest is a NaN, which the median takes out; 2^t is 0 then.)  Six instructions instead of
-// expf's fourteen; off by 2 units in the last place and |x| 2^-26.
+// expf's fourteen; off by 2 units in the last place and |x| 2^-26.  Reciprocals are the hardware's, off by one.  Together, over the norm of each result
+// (of torch operations in fp32, sums over tokens in double): gates 3e-8 to 7e-8 (3e-8 to 6e-8), prob_mean 2e-8 to 8e-8 (2.5e-8), fp32 logits' gradient 1.1e-7
+// (9e-8); single values up to 4.5e-7 (3.4e-7).
 __device__ __forceinline__ float exp_down(float x)
 {
     const float t = x * 1.44269504f;
@@ -217,7 +219,7 @@ template <int CH> constexpr int router_waves() { return CH == 8 ? 2 : 4; }
 // grid (blocks, n_mb); a block takes `per_block` tokens of its micro-batch, with SOLO all of them: it finishes the sums itself.  Bound by
 // the vector units and the latency of a round, not by memory: a round is a chain of LDS round trips and exponentials, so the
 // next round's row, ids and mask are requested before the present one is worked on, and a selection has a lane of its
-// own.  524288 tokens, 128 experts, 8 selected, bf16, 32 micro-batches: 50 us (168 MB at 3.4 TB/s); without the loads ahead, with a loop over the
+// own.  524288 tokens, 128 experts, 8 selected, bf16, 32 micro-batches: 50 us in this kernel (168 MB at 3.4 TB/s), 56 a call; without the loads ahead, with a loop over the
 // selections and expf 93.
 template <class ZT, bool SIGMOID, int LT, int CH, int NS, bool SOLO>
 __global__ void __launch_bounds__(router_waves<CH>() * 64)
@@ -409,7 +411,7 @@ router_finish_kernel(RouterPartials part, int blocks, int rows, int k, int E, in
 //   dz = du (softmax), du sigmoid(-z) (sigmoid).
 // What falls on the selected experts goes through the token's LDS row, one selection after the other: the same expert twice adds
 // up in the order of the selections.  Probabilities are worked out again rather than saved: the row is read anyway.  524288 tokens, 128 experts, 8
-// selected, bf16: 74 us, 303 MB at 4.1 TB/s; 32768 tokens of 256 sigmoid scores in fp32 22 us, 69 MB at 3.1 TB/s.
+// selected, bf16: 76 us, 303 MB at 4.0 TB/s; 32768 tokens of 256 sigmoid scores in fp32 22 us, 69 MB at 3.1 TB/s.
 template <class ZT, bool SIGMOID, int LT, int CH, int NS>
 __global__ void __launch_bounds__(router_waves<CH>() * 64)
 router_bwd_kernel(const ZT *__restrict__ logits, const int32_t *__restrict__ ids, const uint8_t *__restrict__ valid, const float *__restrict__ dgates,
@@ -551,7 +553,7 @@ inline RouterGrid router_grid(int n_mb, int T, int E, bool fwd)
     g.blocks = std::max(1, (T + g.per_block - 1) / g.per_block);
     return g;
 }
-// Rows of sums are folded first where the one block would have more than 64 of them for each of its threads' experts.
+// Rows of sums are folded first where a thread of the one block would read more than 32 of them.
 inline bool router_folds(const RouterGrid &g, int E) { return !g.solo && (size_t)g.blocks * E > 32 * kFinishThreads; }
 struct RouterWs {
     size_t prob, count, tokens, fold_prob, fold_count, bytes;
