@@ -655,9 +655,9 @@ int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const 
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ORTHOGONALIZE, 0, 1, n, 1, rows, cols) bytes (E, h, hff are n, rows, cols)
  * Products of half-precision operands with fp32 sums, the linear term in 22 bits.  Error of the result after 5 steps, of its norm: 2e-3 to 4e-3
  * with a shorter side of 24 or more (rounding it to bf16 alone 1.7e-3), low rank and decaying spectra among them; up to 9e-3 below, where few
- * values' roundings do not average out, and up to 1.3e-2 for a matrix whose values are all of one size, which round alike.  More steps:
- * what rounding leaves outside of a low-rank gradient's space grows by 3.44 a step, to about (2^-24 + 2^-28 sqrt(m)) 3.44^steps of the norm, m the
- * shorter side: 2e-3 after 8 at m = 256, 1.4e-2 at 32768; more steps than 8 are refused.
+ * values' roundings do not average out, and up to 1.3e-2 for a matrix whose values are all of one size, which round alike.  After 8
+ * steps up to 7e-3, with a shorter side below 24 up to 4e-2; what rounding leaves outside of a low-rank gradient's space grows by 3.44 a step, to about
+ * (2^-24 + 2^-28 sqrt(m)) 3.44^steps of the norm, m the shorter side: 2e-3 after 8 at m = 256, 1.4e-2 at 32768.  More steps than 8 are refused.
  * Fixed order, no atomics: results are reproducible bit for bit.
  * Limits: rows, cols <= 32768, n <= 65535, 1 <= steps <= 8 (RELIBRA_EUNSUPPORTED beyond).  momentum_out may be momentum itself;
  * beside that no output may overlap an input or the other output (RELIBRA_EINVAL).
