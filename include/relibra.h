@@ -50,13 +50,14 @@ enum {
 enum {
     RELIBRA_ERR_ID_RANGE = 1,    /* an expert id outside [0,E)                               */
     RELIBRA_ERR_PLAN_COVER = 2,  /* plan tables do not cover an assignment (permute)         */
-    RELIBRA_ERR_GROUP_TABLE = 4  /* group_offset / group_expert / dw_slot tables inconsistent */
+    RELIBRA_ERR_GROUP_TABLE = 4, /* group_offset / group_expert / dw_slot tables inconsistent */
+    RELIBRA_ERR_SEQ_TABLE = 8    /* seq_start / seq_len tables inconsistent (attention)      */
 };
 
 /* which = */
 enum { RELIBRA_WS_PERMUTE = 0, RELIBRA_WS_FFN_FWD = 1, RELIBRA_WS_FFN_BWD = 2, RELIBRA_WS_WGRAD_BATCHED = 3,
        RELIBRA_WS_DGATE = 4, RELIBRA_WS_ROUTER = 5, RELIBRA_WS_BLOCK_NORM = 6,
-       RELIBRA_WS_ORTHOGONALIZE = 7 };
+       RELIBRA_WS_ORTHOGONALIZE = 7, RELIBRA_WS_QK_NORM_ROPE = 8, RELIBRA_WS_ATTENTION_FWD = 9, RELIBRA_WS_ATTENTION_BWD = 10 };
 
 /* flags of relibra_moe_ffn_bwd */
 enum {
@@ -643,6 +644,63 @@ int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const 
                            void *workspace_dev, size_t workspace_bytes, relibra_stream stream);
 
 /*
+ * RMS norms of queries and keys for each head, and the rotation by their tokens' positions in the same pass: what stands between a
+ * block's fused projection and its attention.
+ *   u = x / sqrt(mean x^2 + eps) * w over the d values of a head (u = x with w = NULL), then the pairs (a, b) of the first `rot` values turn:
+ *   a' = a cos t - b sin t,  b' = b cos t + a sin t,   t_j = pos[axis[j]][token] * freq[j]  for pair j of rot / 2
+ * Pair j is (j, j + rot / 2), or with RELIBRA_ROPE_ADJACENT (2 j, 2 j + 1); values from rot on do not turn; rot = 0: norms only.
+ *   q_dev [T, Hq, d], k_dev [T, Hk, d] bf16, dev, in: a token's heads side by side, tokens q_stride, k_stride values apart (parts of the
+ *   projection's output as they lie; Hk = 0: no keys); q_out_dev, k_out_dev the same with strides of their own, out; q_out may be q, k_out k
+ *   w_q_dev, w_k_dev [d] bf16 or NULL (at least one of norm and rotation is there)
+ *   pos_dev [n_axes, T] int32, dev (any values); freq_dev [rot / 2] fp32, dev; axis_host [rot / 2] host, each below n_axes <= 4 (RELIBRA_ERANGE), or
+ *   NULL: all on the first axis (several: time, height and width of images and video)
+ * Angles in double, everything else in fp32 with one rounding at the end.
+ * Backward: dq, dk from dq_out, dk_out and the inputs q, k of the forward call (not read without their norm), and dw_q, dw_k [d] fp32: overwritten,
+ * or added to with RELIBRA_QK_ACCUMULATE.  dq may be dq_out or q, dk may be dk_out or k.  A fixed order: the same bits every call.
+ *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_QK_NORM_ROPE, T, 1, Hq, 1, Hk, d) bytes (E, h, hff are Hq, Hk, d); unused without norms
+ * Limits: d % 16 == 0, d <= 256, rot % 16 == 0, Hq, Hk <= 4096, T <= 2^30 (RELIBRA_EUNSUPPORTED beyond); eps > 0 with a norm; strides are multiples
+ * of 8 of at least H * d and at most 2^28, tensors 16-byte aligned.  Beside the pairs named no output may share memory with an input or the other
+ * output (RELIBRA_EINVAL; tensors of one stride may interleave).
+ */
+enum { RELIBRA_ROPE_ADJACENT = 1, RELIBRA_QK_ACCUMULATE = 2 };
+int relibra_qk_norm_rope_fwd(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *w_q_dev, const void *w_k_dev,
+                             const int32_t *pos_dev, const float *freq_dev, const uint8_t *axis_host, int n_axes, int T, int Hq, int Hk, int d, int rot,
+                             float eps, int flags, void *q_out_dev, int64_t q_out_stride, void *k_out_dev, int64_t k_out_stride, relibra_stream stream);
+int relibra_qk_norm_rope_bwd(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *dq_out_dev, int64_t dq_out_stride,
+                             const void *dk_out_dev, int64_t dk_out_stride, const void *w_q_dev, const void *w_k_dev, const int32_t *pos_dev,
+                             const float *freq_dev, const uint8_t *axis_host, int n_axes, int T, int Hq, int Hk, int d, int rot, float eps, int flags,
+                             void *dq_dev, int64_t dq_stride, void *dk_dev, int64_t dk_stride, float *dw_q_dev, float *dw_k_dev,
+                             void *workspace_dev, size_t workspace_bytes, relibra_stream stream);
+
+/*
+ * Causal attention of a micro-batch of packed sequences: each token over itself and the tokens before it in its sequence,
+ *   out_i = sum_j p_ij v_j,   p_ij = exp(scale q_i . k_j - lse_i),   lse_i = ln sum_j exp(scale q_i . k_j),   j <= i of i's sequence
+ * with Hq query heads in groups of Hq / Hk that share a key head (query head g belongs to key head g / (Hq / Hk)).
+ *   q_dev [T, Hq, d], k_dev, v_dev [T, Hk, d] bf16, dev, in, tokens at strides of their own as above; out_dev [T, Hq, d] bf16 out; lse_dev [T, Hq] fp32 out
+ *   seq_start_dev [n_seq + 1] int32, dev: sequence s has the rows from seq_start[s] on to seq_start[s + 1]; ascending, within [0, T]
+ *   seq_len_dev [n_seq] int32, dev, or NULL: tokens of sequence s at the start of its rows, the rest of them padding: out, lse (and the gradients)
+ *   become 0 there and its inputs are not read.  NULL: no padding.  Rows before the first and behind the last sequence are left as they are.
+ *   Tables with other values: nothing is computed, RELIBRA_ERR_SEQ_TABLE.
+ *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ATTENTION_FWD, T, 1, Hq, n_seq, Hk, d) bytes (E, G, h, hff are Hq, n_seq, Hk, d)
+ * Scores, their exponentials' sums and the result are added up in fp32; the exponentials are rounded to bf16 for their product with v, the result once.
+ * A NaN or infinity stays in its sequence, reaches the rows that see it, and may reach rows up to 127 tokens before it.
+ * Backward: dq, dk, dv from dout, with out and lse as the forward call left them; p and ds are rounded to bf16 for their products, the sums
+ * are fp32.  A key head's gradients are summed over its group.  No atomics on values, a fixed order: the same bits every call.
+ *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ATTENTION_BWD, T, 1, Hq, n_seq, Hk, d) bytes
+ * Limits: d % 8 == 0, d <= 128, Hq % Hk == 0 (RELIBRA_EINVAL), Hq / Hk <= 64, Hq <= 4096, n_seq <= 8192, T * Hq / Hk <= 2^26 (RELIBRA_EUNSUPPORTED
+ * beyond); scale > 0; strides and alignment as above.  No output may share memory with an input or another output (RELIBRA_EINVAL).
+ */
+int relibra_attention_fwd(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *v_dev, int64_t v_stride,
+                          const int32_t *seq_start_dev, const int32_t *seq_len_dev, int n_seq, int T, int Hq, int Hk, int d, float scale,
+                          void *out_dev, int64_t out_stride, float *lse_dev, void *workspace_dev, size_t workspace_bytes, int32_t *err_flag_dev,
+                          relibra_stream stream);
+int relibra_attention_bwd(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *v_dev, int64_t v_stride,
+                          const void *out_dev, int64_t out_stride, const float *lse_dev, const void *dout_dev, int64_t dout_stride,
+                          const int32_t *seq_start_dev, const int32_t *seq_len_dev, int n_seq, int T, int Hq, int Hk, int d, float scale,
+                          void *dq_dev, int64_t dq_stride, void *dk_dev, int64_t dk_stride, void *dv_dev, int64_t dv_stride,
+                          void *workspace_dev, size_t workspace_bytes, int32_t *err_flag_dev, relibra_stream stream);
+
+/*
  * Orthogonalised updates of n matrices (the experts' weight gradients) by Newton-Schulz products, as the Muon optimiser takes them:
  *   M' = mu M + G;   U = G + mu M' with RELIBRA_ORTHO_NESTEROV, else M';   without momentum U = G
  *   X = U / |U|_F, then `steps` times  A = X X^T,  X = a X + (b A + c A^2) X   with (a, b, c) = (3.4445, -4.7750, 2.0315)
@@ -688,7 +746,8 @@ enum {
     RELIBRA_K_WGRAD_ORDER, RELIBRA_K_TRANSPOSE, RELIBRA_K_ROW_TOKENS, RELIBRA_K_ROW_GATES, RELIBRA_K_DGATE_REDUCE,
     RELIBRA_K_REPLICA_PULL, RELIBRA_K_WGRAD_PAIR, RELIBRA_K_PERM_SMALL,
     RELIBRA_K_ROUTER_FWD, RELIBRA_K_ROUTER_FINISH, RELIBRA_K_ROUTER_BWD, RELIBRA_K_NORM_FWD, RELIBRA_K_NORM_BWD, RELIBRA_K_NORM_REDUCE,
-    RELIBRA_K_ORTHO_NORM, RELIBRA_K_ORTHO_LOAD, RELIBRA_K_ORTHO_GRAM, RELIBRA_K_ORTHO_POLY, RELIBRA_K_ORTHO_UPDATE, RELIBRA_K_ORTHO_THIN, RELIBRA_K_ORTHO_JOIN, RELIBRA_K_COUNT
+    RELIBRA_K_ORTHO_NORM, RELIBRA_K_ORTHO_LOAD, RELIBRA_K_ORTHO_GRAM, RELIBRA_K_ORTHO_POLY, RELIBRA_K_ORTHO_UPDATE, RELIBRA_K_ORTHO_THIN, RELIBRA_K_ORTHO_JOIN,
+    RELIBRA_K_QK_FWD, RELIBRA_K_QK_BWD, RELIBRA_K_QK_REDUCE, RELIBRA_K_ATTN_SCHED, RELIBRA_K_ATTN_FWD, RELIBRA_K_ATTN_DQ, RELIBRA_K_ATTN_DKV, RELIBRA_K_ATTN_JOIN, RELIBRA_K_COUNT
 };
 int relibra_prof_start(int level, int max_records);
 int relibra_prof_stop(double *ms_by_kernel_host, int64_t *launches_by_kernel_host);

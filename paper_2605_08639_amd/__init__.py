@@ -17,8 +17,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librelibra.so")
 
 OK, EINVAL, ERANGE, EWORKSPACE, EHIP, EUNSUPPORTED, ENOMEM = 0, -1, -2, -3, -4, -5, -6
-ERR_ID_RANGE, ERR_PLAN_COVER, ERR_GROUP_TABLE = 1, 2, 4
+ERR_ID_RANGE, ERR_PLAN_COVER, ERR_GROUP_TABLE, ERR_SEQ_TABLE = 1, 2, 4, 8
 WS_PERMUTE, WS_FFN_FWD, WS_FFN_BWD, WS_WGRAD_BATCHED, WS_DGATE, WS_ROUTER, WS_BLOCK_NORM, WS_ORTHOGONALIZE = 0, 1, 2, 3, 4, 5, 6, 7
+WS_QK_NORM_ROPE, WS_ATTENTION_FWD, WS_ATTENTION_BWD = 8, 9, 10
 BWD_ACCUMULATE, BWD_NO_REPLICA_SUM, BWD_REPLICA_WEIGHTS, BWD_DEFER_WGRAD, BWD_TRANSPOSED_WEIGHTS = 1, 2, 4, 8, 16
 FWD_TRANSPOSED_WEIGHTS = 1
 WGRAD_ACCUMULATE, WGRAD_TILE_NARROW, WGRAD_TILE_WIDE = 1, 2, 4
@@ -27,6 +28,7 @@ COMBINE_FWD, COMBINE_BWD, COMBINE_SUM = 0, 1, 2
 ROUTER_SIGMOID, ROUTER_NORMALIZE, ROUTER_FP32 = 1, 2, 4
 NORM_STREAM_FP32, NORM_GATE_TOKEN, NORM_GATE_ELEMENT, NORM_ACCUMULATE = 1, 2, 4, 8
 ORTHO_BF16, ORTHO_NESTEROV = 1, 2
+ROPE_ADJACENT, QK_ACCUMULATE = 1, 2
 
 EXPORTS = ("relibra_route_hist", "relibra_plan", "relibra_plan_placed", "relibra_moe_time", "relibra_reorder_sa", "relibra_load_stats",
            "relibra_cost_model_init", "relibra_reorder_sa_trace",
@@ -35,6 +37,7 @@ EXPORTS = ("relibra_route_hist", "relibra_plan", "relibra_plan_placed", "relibra
            "relibra_moe_ffn_bwd_gated", "relibra_moe_ffn_fwd",
            "relibra_moe_ffn_bwd", "relibra_moe_ffn_wgrad_batched", "relibra_transpose_experts", "relibra_unpermute_combine", "relibra_replica_push", "relibra_replica_pull",
            "relibra_router_fwd", "relibra_router_bwd", "relibra_block_norm_fwd", "relibra_block_norm_bwd", "relibra_orthogonalize",
+           "relibra_qk_norm_rope_fwd", "relibra_qk_norm_rope_bwd", "relibra_attention_fwd", "relibra_attention_bwd",
            "relibra_workspace_bytes",
            "relibra_status_string", "relibra_prof_start", "relibra_prof_stop")
 
@@ -43,16 +46,21 @@ KERNELS = ("hist", "perm_count", "perm_scan", "perm_rank", "gather", "combine_fw
            "wgrad_gate_up", "replica_sum", "replica_push", "wgrad_order", "transpose", "row_tokens", "row_gates",
            "dgate_reduce", "replica_pull", "wgrad_pair", "perm_small",
            "router_fwd", "router_finish", "router_bwd", "norm_fwd", "norm_bwd", "norm_reduce",
-           "ortho_norm", "ortho_load", "ortho_gram", "ortho_poly", "ortho_update", "ortho_thin", "ortho_join")
+           "ortho_norm", "ortho_load", "ortho_gram", "ortho_poly", "ortho_update", "ortho_thin", "ortho_join",
+           "qk_fwd", "qk_bwd", "qk_reduce", "attn_sched", "attn_fwd", "attn_dq", "attn_dkv", "attn_join")
 
 # Argument types of the calls that are short on the GPU: ctypes then takes plain integers and floats, which costs the host half
 # of what building an object for every argument does.
-_P, _I, _F, _Z = C.c_void_p, C.c_int, C.c_float, C.c_size_t
+_P, _I, _F, _Z, _L = C.c_void_p, C.c_int, C.c_float, C.c_size_t, C.c_int64
 _ARGTYPES = {
     "relibra_router_fwd": [_P] * 3 + [_I] * 5 + [_F] * 2 + [_P] * 6 + [_Z] + [_P] * 2,
     "relibra_router_bwd": [_P] * 7 + [_I] * 5 + [_F] * 2 + [_P] * 3,
     "relibra_block_norm_fwd": [_P] * 5 + [_I] * 2 + [_F] * 2 + [_I] + [_P] * 3,
     "relibra_block_norm_bwd": [_P] * 7 + [_I] * 2 + [_F] * 2 + [_I] + [_P] * 6 + [_Z, _P],
+    "relibra_qk_norm_rope_fwd": [_P, _L] * 2 + [_P] * 5 + [_I] * 6 + [_F, _I] + [_P, _L] * 2 + [_P],
+    "relibra_qk_norm_rope_bwd": [_P, _L] * 4 + [_P] * 5 + [_I] * 6 + [_F, _I] + [_P, _L] * 2 + [_P] * 3 + [_Z, _P],
+    "relibra_attention_fwd": [_P, _L] * 3 + [_P] * 2 + [_I] * 5 + [_F] + [_P, _L] + [_P] * 2 + [_Z] + [_P] * 2,
+    "relibra_attention_bwd": [_P, _L] * 4 + [_P] + [_P, _L] + [_P] * 2 + [_I] * 5 + [_F] + [_P, _L] * 3 + [_P, _Z] + [_P] * 2,
     "relibra_orthogonalize": [_P] * 2 + [_I] * 3 + [_F] * 2 + [_I] * 2 + [_P] * 3 + [_Z, _P],
 }
 
@@ -851,6 +859,134 @@ def relibra_orthogonalize(grad, momentum=None, mu=0.95, nesterov=True, scale=1.0
     rc = lib().relibra_orthogonalize(*at[:2], n, rows, cols, mu, scale, int(steps), flags, *at[2:], workspace.numel(), _raw())
     _check("relibra_orthogonalize", rc)
     return out, momentum_out
+
+
+def _heads(t, shape, what):
+    """Pointer and token stride of a tensor [T, H, d] of bf16 whose heads lie side by side, on the current device (None: NULL, 0)."""
+    if t is None:
+        return None, 0
+    assert t.shape == shape and t.dtype is torch.bfloat16, f"{what}: expected bf16 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
+    T, H, d = shape
+    strides = t.stride()
+    assert (strides[2] == 1 or d == 1) and (strides[1] == d or H == 1), f"{what}: a token's heads lie side by side"
+    at = t.get_device()
+    assert at >= 0, "device tensors, not host memory"
+    here = at if _device is None else _device()
+    assert at == here, f"tensor on device {at}: work goes to the current device's stream"
+    return t.data_ptr(), strides[0] if T > 1 else H * d
+
+
+def _heads_out(t, shape, like):
+    return torch.empty(shape, dtype=torch.bfloat16, device=like.device) if t is None else t
+
+
+def qk_norm_rope_workspace(T, Hq, Hk, d, device="cuda"):
+    return torch.empty(max(workspace_bytes(WS_QK_NORM_ROPE, T, 1, Hq, 1, Hk, d), 1), dtype=torch.uint8, device=device)
+
+
+def _qk_args(q, k, pos, freq, w_q, w_k, axis):
+    T, Hq, d = q.shape
+    Hk = 0 if k is None else k.shape[1]
+    rot = 0 if freq is None else 2 * freq.shape[0]
+    n_axes = 0 if pos is None else 1 if pos.dim() == 1 else pos.shape[0]
+    assert (pos is None) == (freq is None), "positions come with frequencies"
+    assert pos is None or (pos.shape[-1] == T and pos.dim() <= 2 and pos.dtype is torch.int32), "pos is [T] or [n_axes, T] int32"
+    assert freq is None or (freq.dim() == 1 and freq.dtype is torch.float32), "freq is [rot / 2] fp32"
+    for w in (w_q, w_k):
+        assert w is None or (w.shape == (d,) and w.dtype is torch.bfloat16), "norm weights are [d] bf16"
+    if axis is not None:
+        assert len(axis) == rot // 2, "one axis a pair"
+        axis = bytes(axis)
+    return T, Hq, Hk, d, rot, n_axes, axis
+
+
+def relibra_qk_norm_rope_fwd(q, k, pos=None, freq=None, w_q=None, w_k=None, axis=None, adjacent=False, eps=1e-6, q_out=None, k_out=None):
+    """q [T,Hq,d], k [T,Hk,d] (or None) bf16, parts of a fused projection as they lie or tensors of their own -> (q', k'): each head's RMS norm
+    (w_q, w_k [d] bf16 or None) and rotation: pos [T] or [n_axes,T] int32, freq [rot/2] fp32, axis: each pair's axis (None: the first).
+    Pairs (j, j + rot/2), or neighbours with `adjacent`.  q_out, k_out may be q, k."""
+    T, Hq, Hk, d, rot, n_axes, axis = _qk_args(q, k, pos, freq, w_q, w_k, axis)
+    q_out = _heads_out(q_out, (T, Hq, d), q)
+    k_out = None if k is None else _heads_out(k_out, (T, Hk, d), k)
+    at = _ptrs(w_q, w_k, pos, freq)
+    rc = lib().relibra_qk_norm_rope_fwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *at, axis, n_axes, T, Hq, Hk, d, rot, eps,
+                                        ROPE_ADJACENT if adjacent else 0, *_heads(q_out, (T, Hq, d), "q_out"), *_heads(k_out, (T, Hk, d), "k_out"), _raw())
+    _check("relibra_qk_norm_rope_fwd", rc)
+    return q_out, k_out
+
+
+def relibra_qk_norm_rope_bwd(q, k, dq_out, dk_out, pos=None, freq=None, w_q=None, w_k=None, axis=None, adjacent=False, eps=1e-6, accumulate=False,
+                             dq=None, dk=None, dw_q=None, dw_k=None, workspace=None):
+    """The forward call's inputs q, k and the gradients of its outputs -> (dq, dk, dw_q, dw_k), None where there is no such input.
+    accumulate: dw_q and dw_k (fp32 [d], given) are added to.  dq may be dq_out or q, dk may be dk_out or k."""
+    T, Hq, Hk, d, rot, n_axes, axis = _qk_args(q, k, pos, freq, w_q, w_k, axis)
+    assert (dk_out is None) == (k is None), "dk_out goes with k"
+    assert not accumulate or ((w_q is None or dw_q is not None) and (w_k is None or dw_k is not None)), "nothing to add to"
+    dq = _heads_out(dq, (T, Hq, d), q)
+    dk = None if k is None else _heads_out(dk, (T, Hk, d), k)
+    dw_q = None if w_q is None else _out(dw_q, (d,), torch.float32, q)
+    dw_k = None if w_k is None else _out(dw_k, (d,), torch.float32, q)
+    if workspace is None:
+        workspace = qk_norm_rope_workspace(T, Hq, Hk, d, q.device)
+    at = _ptrs(w_q, w_k, pos, freq, dw_q, dw_k, workspace)
+    rc = lib().relibra_qk_norm_rope_bwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *_heads(dq_out, (T, Hq, d), "dq_out"),
+                                        *_heads(dk_out, (T, Hk, d), "dk_out"), *at[:4], axis, n_axes, T, Hq, Hk, d, rot, eps,
+                                        (ROPE_ADJACENT if adjacent else 0) | (QK_ACCUMULATE if accumulate else 0), *_heads(dq, (T, Hq, d), "dq"),
+                                        *_heads(dk, (T, Hk, d), "dk"), *at[4:], workspace.numel(), _raw())
+    _check("relibra_qk_norm_rope_bwd", rc)
+    return dq, dk, dw_q, dw_k
+
+
+def attention_fwd_workspace(T, n_seq, Hq, Hk, d, device="cuda"):
+    return torch.empty(max(workspace_bytes(WS_ATTENTION_FWD, T, 1, Hq, max(n_seq, 1), Hk, d), 1), dtype=torch.uint8, device=device)
+
+
+def attention_bwd_workspace(T, n_seq, Hq, Hk, d, device="cuda"):
+    return torch.empty(max(workspace_bytes(WS_ATTENTION_BWD, T, 1, Hq, max(n_seq, 1), Hk, d), 1), dtype=torch.uint8, device=device)
+
+
+def _attention_args(q, k, seq_start, seq_len, scale):
+    T, Hq, d = q.shape
+    n_seq = seq_start.shape[0] - 1
+    assert n_seq >= 0 and seq_start.dim() == 1 and seq_start.dtype is torch.int32, "seq_start is [n_seq + 1] int32"
+    assert seq_len is None or (seq_len.shape == (n_seq,) and seq_len.dtype is torch.int32), "seq_len is [n_seq] int32"
+    return T, Hq, k.shape[1], d, n_seq, d ** -0.5 if scale is None else scale
+
+
+def relibra_attention_fwd(q, k, v, seq_start, seq_len=None, scale=None, out=None, lse=None, workspace=None, err_flag=None):
+    """Causal attention of packed sequences: q [T,Hq,d], k, v [T,Hk,d] bf16 (parts of a fused projection as they lie, or tensors of their own), sequence s
+    in rows seq_start[s] .. seq_start[s+1] (int32), its first seq_len[s] (None: all) of them tokens -> out [T,Hq,d] bf16, lse [T,Hq] fp32.
+    scale: d^-1/2 unless given."""
+    T, Hq, Hk, d, n_seq, scale = _attention_args(q, k, seq_start, seq_len, scale)
+    out = _heads_out(out, (T, Hq, d), q)
+    lse = _out(lse, (T, Hq), torch.float32, q)
+    if workspace is None:
+        workspace = attention_fwd_workspace(T, n_seq, Hq, Hk, d, q.device)
+    if err_flag is None:
+        err_flag = new_err_flag(q.device)
+    assert err_flag.dtype is torch.int32, "the error flag is int32"
+    at = _ptrs(seq_start, seq_len, lse, workspace, err_flag)
+    rc = lib().relibra_attention_fwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *_heads(v, (T, Hk, d), "v"), *at[:2], n_seq, T, Hq, Hk, d,
+                                     scale, *_heads(out, (T, Hq, d), "out"), *at[2:4], workspace.numel(), at[4], _raw())
+    _check("relibra_attention_fwd", rc)
+    return out, lse
+
+
+def relibra_attention_bwd(q, k, v, out, lse, dout, seq_start, seq_len=None, scale=None, dq=None, dk=None, dv=None, workspace=None, err_flag=None):
+    """dout [T,Hq,d] bf16 and the forward call's inputs and outputs -> (dq [T,Hq,d], dk, dv [T,Hk,d]) bf16; they may be parts of one tensor [T, (Hq+2Hk) d]."""
+    T, Hq, Hk, d, n_seq, scale = _attention_args(q, k, seq_start, seq_len, scale)
+    assert lse.shape == (T, Hq) and lse.dtype is torch.float32, "lse is [T, Hq] fp32"
+    dq, dk, dv = _heads_out(dq, (T, Hq, d), q), _heads_out(dk, (T, Hk, d), q), _heads_out(dv, (T, Hk, d), q)
+    if workspace is None:
+        workspace = attention_bwd_workspace(T, n_seq, Hq, Hk, d, q.device)
+    if err_flag is None:
+        err_flag = new_err_flag(q.device)
+    assert err_flag.dtype is torch.int32, "the error flag is int32"
+    at = _ptrs(lse, seq_start, seq_len, workspace, err_flag)
+    rc = lib().relibra_attention_bwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *_heads(v, (T, Hk, d), "v"), *_heads(out, (T, Hq, d), "out"),
+                                     at[0], *_heads(dout, (T, Hq, d), "dout"), *at[1:3], n_seq, T, Hq, Hk, d, scale, *_heads(dq, (T, Hq, d), "dq"),
+                                     *_heads(dk, (T, Hk, d), "dk"), *_heads(dv, (T, Hk, d), "dv"), at[3], workspace.numel(), at[4], _raw())
+    _check("relibra_attention_bwd", rc)
+    return dq, dk, dv
 
 
 def prof_start(level=1, max_records=4096):

@@ -1,0 +1,796 @@
+// Causal attention of packed sequences with grouped heads, and its gradients.
+//
+//   z_ij = scale q_i . k_j for the keys j <= i of row i's sequence;  lse_i = ln sum_j exp z_ij;  p_ij = exp(z_ij - lse_i);  o_i = sum_j p_ij v_j
+//   D_i = do_i . o_i;  ds_ij = p_ij (do_i . v_j - D_i);  dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij do_i
+//
+// The G query heads of a key head are rows of one matrix: packed row r of a sequence is token r / G, head r % G of the group.  A block takes
+// 128 packed rows (forward, dq) or 128 keys (dk, dv) of one key head, 32 a wave, and walks the other side in tiles of 64 through LDS, two
+// tiles in turn, filled by direct loads.  Products are MFMA 32x32x16 with the block's own side on the lanes: a lane then holds one row's
+// (one key's) scores in its registers, so that softmax statistics and rescaling are a lane's own work, and the exponentials, rounded
+// to bf16, are the next product's operand as they lie: MFMA does not care for the order of the contracted index as long as both sides
+// agree, so the other side is read (by transposing LDS reads) in the order that the registers have.  Everything else is fp32.  Gradients
+// are computed from the scores again in two kernels, seven products where five would do with atomics: fixed order, the same bits every call.
+#include "gemm_tile.h"
+#include "head_rows.h"
+#include "wave_ops.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace relibra {
+
+constexpr int kAttnThreads = 256, kAttnWaves = 4;
+constexpr int kRowTile = 128;                                // packed rows (or keys) of a block
+constexpr int kKeyTile = 64;                                 // keys of a step
+constexpr int kRowStep = 32;                                 // packed rows of a step of keys' gradients
+constexpr int kAttnMaxDim = 128, kAttnMaxSeq = 8192, kAttnMaxGroup = 64;
+constexpr int kAttnMaxRows = 1 << 26;                        // packed rows of a key head
+constexpr int kAttnSlots = 512;                              // blocks that run at once: two a unit
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttnShape {
+    int T, Hq, Hk, G, d;
+    float scale;
+};
+// A tensor of heads: element (token, head * d + c) at p[token * ld + head * d + c].
+struct HeadsIn {
+    const bf16_t *p;
+    long long ld;
+};
+struct HeadsOut {
+    bf16_t *p;
+    long long ld;
+};
+// One block's work: rows (or keys) tile * 128 .. of the sequence that starts at row0; tile < 0: rows row0 .. row0 + len - 1 are padding.
+// Keys: steps from .. to - 1 of 32 packed rows, into slot `slot` of the partial sums (-1: all there are).
+struct AttnUnit {
+    int row0, len, tile, from, to, slot, chunks, pad;
+};
+struct AttnList {
+    int count, joins, pad[6];
+};
+
+// ---------------------------------------------------------------- LDS tiles: [R][W] of 16-bit values, W = 64 or 128
+template <int ND, int R = kKeyTile> struct AttnTile {
+    static constexpr int W = ND <= 2 ? 64 : 128;             // ND blocks of 32 columns are used
+    static constexpr int ROW = W * 2, SPR = W / 8;            // bytes and 16-byte pieces of a row
+    static constexpr int RPB = 64 / SPR;                      // rows of a 1 KiB load
+    static constexpr int BYTES = R * ROW, LOADS = BYTES / 1024 / kAttnWaves;
+    // Piece c of row r lies at piece c ^ swz(r).  16 consecutive rows at one piece fall into distinct 16-byte bank groups (row reads), and so
+    // do 4 consecutive rows at 4 pieces (transposing reads).
+    static __device__ __forceinline__ int swz(int r) { return W == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3); }
+    // Fragment reads from an LDS address plus the lane's part of it; what is left is an exclusive or and an offset, both constants (a piece's
+    // number is bits 4 to 7 of an address, tiles start at multiples of 1 KiB).
+    // rows r0 + lane % 32, columns kk * 16 + lane / 32 * 8 .. + 7
+    static __device__ __forceinline__ uint32_t row_lane(int lane)
+    {
+        const int r = lane & 31;
+        return r * ROW + (((lane >> 5) ^ swz(r)) << 4);
+    }
+    static __device__ __forceinline__ bf16x8_t rows(uint32_t at, int r0, int kk)
+    {
+        return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8_t *>((at ^ (kk << 5)) + r0 * ROW);
+    }
+    // columns c0 + lane % 32 of rows k0 + 4 (lane / 32) + {0..3, 8..11}: the order in which a lane holds 16 rows of an accumulator
+    static __device__ __forceinline__ uint32_t col_lane(int lane)
+    {
+        const int b = lane >> 4, i = lane & 15, c = (b & 1) * 16 + (i & 3) * 4, k = (b >> 1) * 4 + (i >> 2);
+        return k * ROW + (((c >> 3) ^ swz(k)) << 4) + (c >> 2 & 1) * 8;
+    }
+    static __device__ __forceinline__ bf16x8_t cols(uint32_t at, int c0, int k0)
+    {
+        typedef __attribute__((address_space(3))) s16x4_t *lds_ptr;
+        const s16x4_t l = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)((at ^ (c0 << 1)) + k0 * ROW));
+        const s16x4_t h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)((at ^ (c0 << 1) ^ 32) + (k0 + 8) * ROW));   // (8 rows on: 2 in the swizzle)
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+// A lane's LDS address, opaque to the compiler: kept as one register instead of one for every constant it is combined with.
+__device__ __forceinline__ uint32_t lds_at(const char *tile, uint32_t lane_part)
+{
+    uint32_t at = (uint32_t)(uintptr_t)RELIBRA_LDS(tile) + lane_part;
+    asm volatile("" : "+v"(at));
+    return at;
+}
+
+__device__ __forceinline__ f32x16_t mfma16(bf16x8_t a, bf16x8_t b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ f32x16_t zero16()
+{
+    f32x16_t z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    return z;
+}
+
+// Registers 8 j .. 8 j + 7 of an accumulator as bf16: the operand of the 16 contracted values they are (rounded once, half a step).
+__device__ __forceinline__ bf16x8_t pack_half(const f32x16_t &v, int j)
+{
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(bf16x8_t, u32x4_t{pack2bf(v[8 * j], v[8 * j + 1]), pack2bf(v[8 * j + 2], v[8 * j + 3]), pack2bf(v[8 * j + 4], v[8 * j + 5]),
+                                                pack2bf(v[8 * j + 6], v[8 * j + 7])});
+}
+
+// A lane's own row as a product's operand: values kk * 16 + lane / 32 * 8 .. + 7 of `row`, zeros from d on.
+template <int ND> __device__ __forceinline__ void load_row(bf16x8_t (&f)[2 * ND], const bf16_t *row, int d, int lane)
+{
+#pragma unroll
+    for (int kk = 0; kk < 2 * ND; ++kk) {
+        const int c = kk * 16 + (lane >> 5) * 8;
+        const uint4 v = c < d ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0, 0, 0, 0);
+        f[kk] = __builtin_bit_cast(bf16x8_t, v);
+    }
+}
+
+// An accumulator [d][row on the lanes] to the lanes' rows: the halves of a wave trade 8-byte pieces, so that a lane stores 16 bytes.
+template <int ND> __device__ __forceinline__ void store_row(const f32x16_t (&acc)[ND], float by, bf16_t *row, int d, int lane, bool live)
+{
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const f32x16_t &v = acc[n];
+            uint32_t a0 = pack2bf(v[8 * p] * by, v[8 * p + 1] * by), a1 = pack2bf(v[8 * p + 2] * by, v[8 * p + 3] * by);
+            uint32_t b0 = pack2bf(v[8 * p + 4] * by, v[8 * p + 5] * by), b1 = pack2bf(v[8 * p + 6] * by, v[8 * p + 7] * by);
+            const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+            const int c = n * 32 + p * 16 + (lane >> 5) * 8;
+            if (live && c < d) *reinterpret_cast<uint4 *>(row + c) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
+        }
+}
+
+__device__ __forceinline__ float halves_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+__device__ __forceinline__ float halves_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+
+// This wave's loads have landed, and everyone's: the tile is there, and nobody reads the one before it any more.
+__device__ __forceinline__ void tile_barrier()
+{
+    wait_vm_lgkm0<0>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Loads of tiles of 64 consecutive tokens of one head (keys, values).  Rows behind the sequence are its last row again and pieces
+// behind d the last piece: nothing outside of the sequence is read, and what lands there is masked or never stored.
+template <int ND> struct TokenTiles {
+    typedef AttnTile<ND> Tile;
+    const bf16_t *base;                                       // the sequence's first row
+    long long ld;
+    int len, wave, sub, col;
+    uint32_t lane_off;
+    __device__ __forceinline__ TokenTiles(const HeadsIn &x, const AttnUnit &u, int head, int d, int wave_, int lane) : ld(x.ld), len(u.len), wave(wave_)
+    {
+        base = x.p + (long long)u.row0 * x.ld + (long long)head * d;
+        sub = lane / Tile::SPR;
+        const int r = wave * Tile::RPB + sub;                 // the swizzle is the same in all of a wave's loads
+        col = min((lane % Tile::SPR) ^ Tile::swz(r), d / 8 - 1) * 8;
+        lane_off = (uint32_t)(sub * ld + col) * 2u;
+    }
+    __device__ __forceinline__ void load(char *lds, int t) const
+    {
+        const int first = t * kKeyTile;
+#pragma unroll
+        for (int i = 0; i < Tile::LOADS; ++i) {
+            const int blk = wave + i * kAttnWaves, r = first + blk * Tile::RPB;
+            if (first + kKeyTile <= len) load_lds16_sv(base + (long long)r * ld, lane_off, lds + blk * 1024);
+            else load_lds16(base + (long long)min(r + sub, len - 1) * ld + col, lds + blk * 1024);
+        }
+    }
+};
+
+// ---------------------------------------------------------------- schedule
+// Lists the blocks' work, heaviest first.  One block: sequences are counted (their rows' or keys' tiles, and the tiles of padding behind
+// them), every thread finds the sequence of its share of the tiles by bisection, and a counting sort by work puts them in order (within a
+// bin in any order: results do not depend on it).  A table that does not ascend within [0, T], or lengths beyond their places: nothing is listed.
+constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinChunk = 32;
+
+__device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // inclusive; two barriers
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int below = __shfl_up(v, off);
+        if (lane >= off) v += below;
+    }
+    if (lane == 63) sums[wave] = v;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kSchedThreads / 64; ++w) {
+        if (w < wave) v += sums[w];
+        total += sums[w];
+    }
+    __syncthreads();
+    return v;
+}
+
+__host__ __device__ inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile); }
+
+template <bool KEYS>
+__global__ void __launch_bounds__(kSchedThreads)
+attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, int Hk, int max_units, int max_slots,
+                  AttnList *head, AttnUnit *units, AttnUnit *joins, int32_t *err_flag)
+{
+    __shared__ int before[kAttnMaxSeq + 1];                   // tiles of the sequences before
+    __shared__ int bins[kSchedBins], sums[kSchedThreads / 64], n_slots, n_joins;
+    __shared__ unsigned long long steps;
+    const int tid = threadIdx.x;
+    if (tid == 0) steps = 0, n_slots = 0, n_joins = 0, before[0] = 0;
+    bins[tid] = 0;
+    __syncthreads();
+    bool bad = false;
+    int carry = 0;
+    for (int s0 = 0; s0 < n_seq; s0 += kSchedThreads) {
+        const int s = s0 + tid;
+        int tiles = 0;
+        if (s < n_seq) {
+            const int a = seq_start[s], b = seq_start[s + 1], len = seq_len ? seq_len[s] : b - a;
+            if (a < 0 || b < a || b > T || len < 0 || len > b - a) bad = true;
+            else {
+                const int own = tiles_of(KEYS ? (long long)len : (long long)len * G, kRowTile);
+                tiles = own + tiles_of(b - a - len, kRowTile);
+                if (KEYS && own) {                             // sum of ceil(len G / 32) - 4 G t over the tiles t
+                    const long long end = tiles_of((long long)len * G, kRowStep);
+                    atomicAdd(&steps, (unsigned long long)(end * own - (long long)(kRowTile / kRowStep) * G * own * (own - 1) / 2));
+                }
+            }
+        }
+        int total;
+        const int incl = scan1024(tiles, sums, total);
+        if (s < n_seq) before[s + 1] = carry + incl;
+        carry += total;
+    }
+    if (__syncthreads_or(bad)) {
+        if (tid == 0) {
+            head->count = 0, head->joins = 0;
+            atomicOr(err_flag, RELIBRA_ERR_SEQ_TABLE);
+        }
+        return;
+    }
+    const int chunk = KEYS ? (int)max((unsigned long long)kMinChunk, (steps * Hk + 2 * kAttnSlots - 1) / (2 * kAttnSlots)) : 0;
+    const int most = KEYS ? chunk : tiles_of(T, kKeyTile);    // the largest work of a unit
+    int shift = 0;
+    while ((most >> shift) >= kSchedBins) ++shift;
+    // a tile's unit(s) and their work: fn(unit, work)
+    auto each = [&](int f, bool place, auto fn) __attribute__((always_inline)) {
+        int lo = 0, hi = n_seq;                               // the last sequence with before[s] <= f
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (before[mid] <= f) lo = mid;
+            else hi = mid;
+        }
+        const int a = seq_start[lo], b = seq_start[lo + 1], len = seq_len ? seq_len[lo] : b - a;
+        int t = f - before[lo];
+        const int own = tiles_of(KEYS ? (long long)len : (long long)len * G, kRowTile);
+        AttnUnit u{a, len, t, 0, 0, -1, 1, 0};
+        if (t >= own) {
+            u.row0 = a + len + (t - own) * kRowTile;
+            u.len = min(kRowTile, b - u.row0);
+            u.tile = -1;
+            fn(u, 0);
+        } else if (!KEYS) {
+            fn(u, tiles_of(min(((long long)t * kRowTile + kRowTile - 1) / G + 1, (long long)len), kKeyTile));
+        } else {
+            const int first = kRowTile / kRowStep * G * t, end = tiles_of((long long)len * G, kRowStep), n = end - first;
+            int chunks = tiles_of(n, chunk), slot = -1;
+            if (chunks > 1 && place) {
+                slot = atomicAdd(&n_slots, chunks);
+                if (slot + chunks > max_slots) slot = -1, chunks = 1;      // (cannot be: max_slots covers the most there are)
+            }
+            if (chunks > 1 && place) {
+                u.slot = slot, u.chunks = chunks;
+                joins[atomicAdd(&n_joins, 1)] = u;
+            }
+            for (int c = 0; c < chunks; ++c) {
+                u.from = first + c * chunk;
+                u.to = chunks == 1 ? end : min(u.from + chunk, end);
+                u.slot = chunks > 1 ? slot + c : -1;
+                fn(u, min(u.to - u.from, chunk));
+            }
+        }
+    };
+    const int flat = before[n_seq];
+    for (int f = tid; f < flat; f += kSchedThreads) each(f, false, [&](const AttnUnit &, int work) { atomicAdd(&bins[work >> shift], 1); });
+    __syncthreads();
+    int total;
+    const int mine = bins[kSchedBins - 1 - tid], upto = scan1024(mine, sums, total);
+    bins[kSchedBins - 1 - tid] = upto - mine;                  // heaviest first
+    __syncthreads();
+    for (int f = tid; f < flat; f += kSchedThreads)
+        each(f, true, [&](const AttnUnit &u, int work) {
+            const int at = atomicAdd(&bins[work >> shift], 1);
+            if (at < max_units) units[at] = u;
+        });
+    __syncthreads();
+    if (tid == 0) head->count = min(total, max_units), head->joins = n_joins;
+}
+
+// ---------------------------------------------------------------- forward
+template <int ND>
+__global__ void __launch_bounds__(kAttnThreads, 2)
+attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut out, float *__restrict__ lse)
+{
+    typedef AttnTile<ND> Tile;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];      // keys and values, two tiles each
+    const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
+    if (at >= list->count) return;
+    const AttnUnit u = units[at];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
+    if (u.tile < 0) {                                         // padding: zeros
+        const int pieces = G * d / 8;
+        for (int i = threadIdx.x; i < u.len * pieces; i += kAttnThreads)
+            *reinterpret_cast<uint4 *>(out.p + (u.row0 + i / pieces) * out.ld + (long long)hk * G * d + i % pieces * 8) = make_uint4(0, 0, 0, 0);
+        for (int i = threadIdx.x; i < u.len * G; i += kAttnThreads) lse[(long long)(u.row0 + i / G) * sh.Hq + hk * G + i % G] = 0.0f;
+        return;
+    }
+    const int rows = u.len * G, first = u.tile * kRowTile + wave * 32;         // (this wave's first packed row)
+    const int r = min(first + (lane & 31), rows - 1), tok = r / G, head = hk * G + r - tok * G;
+    const int wave_lo = min(first, rows - 1) / G, wave_hi = min(first + 31, rows - 1) / G;
+    const int steps = tiles_of(min((u.tile * kRowTile + kRowTile - 1) / G, u.len - 1) + 1, kKeyTile);
+
+    const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
+    TokenTiles<ND> kt(k, u, hk, d, wave, lane), vt(v, u, hk, d, wave, lane);
+    kt.load(lds, 0);
+    vt.load(lds + 2 * Tile::BYTES, 0);
+    bf16x8_t qf[2 * ND];
+    load_row<ND>(qf, q.p + (long long)(u.row0 + tok) * q.ld + head * d, d, lane);
+
+    const float c = sh.scale * kLog2e;
+    float m = -INFINITY, l = 0.0f;
+    f32x16_t o[ND];
+#pragma unroll
+    for (int n = 0; n < ND; ++n) o[n] = zero16();
+    for (int t = 0; t < steps; ++t) {
+        tile_barrier();
+        const char *keys = lds + (t & 1) * Tile::BYTES, *vals = lds + (2 + (t & 1)) * Tile::BYTES;
+        if (t + 1 < steps) {
+            kt.load(lds + (~t & 1) * Tile::BYTES, t + 1);
+            vt.load(lds + (2 + (~t & 1)) * Tile::BYTES, t + 1);
+        }
+        if (t * kKeyTile > wave_hi) continue;                 // all of this wave's rows come before these keys
+        const uint32_t key_rows = lds_at(keys, row_lane), val_cols = lds_at(vals, col_lane);
+        f32x16_t s[2] = {zero16(), zero16()};
+#pragma unroll
+        for (int kk = 0; kk < 2 * ND; ++kk)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[b] = mfma16(Tile::rows(key_rows, b * 32, kk), qf[kk], s[b]);
+        if (t * kKeyTile + kKeyTile - 1 > wave_lo) {          // keys behind a row's token
+            const int seen = tok - t * kKeyTile - (lane >> 5) * 4;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) s[b][i] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        top = halves_max(top);
+        // The reference value of the exponentials follows the maximum only where it has risen by more than 2^8: the sums then stay below
+        // 2^8 times their count, and most steps need no rescaling.
+        if (__any((top - m) * c > 8.0f)) {
+            const float m_new = fmaxf(m, top), by = __builtin_amdgcn_exp2f((m - m_new) * c);
+            m = m_new;
+            l *= by;
+#pragma unroll
+            for (int n = 0; n < ND; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[n][i] *= by;
+        }
+        const float mc = m * c;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -mc));
+                l += s[b][i];
+            }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8_t p = pack_half(s[b], j);
+#pragma unroll
+                for (int n = 0; n < ND; ++n) o[n] = mfma16(Tile::cols(val_cols, n * 32, b * 32 + j * 16), p, o[n]);
+            }
+    }
+    l = halves_sum(l);
+    const bool live = first + (lane & 31) < rows;
+    store_row<ND>(o, 1.0f / l, out.p + (long long)(u.row0 + tok) * out.ld + head * d, d, lane, live);
+    if (live && lane < 32) lse[(long long)(u.row0 + tok) * sh.Hq + head] = (m * c + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ---------------------------------------------------------------- backward: queries
+// dq of 128 packed rows, and for the other kernel each row's lse in powers of two and D.
+template <int ND>
+__global__ void __launch_bounds__(kAttnThreads, 2)
+attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, const AttnList *__restrict__ list,
+               const AttnUnit *__restrict__ units, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ delta)
+{
+    typedef AttnTile<ND> Tile;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
+    const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
+    if (at >= list->count) return;
+    const AttnUnit u = units[at];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
+    if (u.tile < 0) {
+        const int pieces = G * d / 8;
+        for (int i = threadIdx.x; i < u.len * pieces; i += kAttnThreads)
+            *reinterpret_cast<uint4 *>(dq.p + (u.row0 + i / pieces) * dq.ld + (long long)hk * G * d + i % pieces * 8) = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const int rows = u.len * G, first = u.tile * kRowTile + wave * 32;
+    const int r = min(first + (lane & 31), rows - 1), tok = r / G, head = hk * G + r - tok * G;
+    const int wave_lo = min(first, rows - 1) / G, wave_hi = min(first + 31, rows - 1) / G;
+    const int steps = tiles_of(min((u.tile * kRowTile + kRowTile - 1) / G, u.len - 1) + 1, kKeyTile);
+    const bool live = first + (lane & 31) < rows;
+
+    const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
+    TokenTiles<ND> kt(k, u, hk, d, wave, lane), vt(v, u, hk, d, wave, lane);
+    kt.load(lds, 0);
+    vt.load(lds + 2 * Tile::BYTES, 0);
+    bf16x8_t qf[2 * ND], df[2 * ND];
+    load_row<ND>(qf, q.p + (long long)(u.row0 + tok) * q.ld + head * d, d, lane);
+    load_row<ND>(df, dout.p + (long long)(u.row0 + tok) * dout.ld + head * d, d, lane);
+    float D = 0.0f;
+    {
+        bf16x8_t of[2 * ND];
+        load_row<ND>(of, out.p + (long long)(u.row0 + tok) * out.ld + head * d, d, lane);
+#pragma unroll
+        for (int kk = 0; kk < 2 * ND; ++kk)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) D = fmaf((float)of[kk][i], (float)df[kk][i], D);
+        D = halves_sum(D);
+    }
+    const long long place = (long long)(u.row0 + tok) * sh.Hq + head;
+    const float l2 = lse[place] * kLog2e, c = sh.scale * kLog2e;
+    if (live && lane < 32) lse2[place] = l2, delta[place] = D;
+
+    f32x16_t acc[ND];
+#pragma unroll
+    for (int n = 0; n < ND; ++n) acc[n] = zero16();
+    for (int t = 0; t < steps; ++t) {
+        tile_barrier();
+        const char *keys = lds + (t & 1) * Tile::BYTES, *vals = lds + (2 + (t & 1)) * Tile::BYTES;
+        if (t + 1 < steps) {
+            kt.load(lds + (~t & 1) * Tile::BYTES, t + 1);
+            vt.load(lds + (2 + (~t & 1)) * Tile::BYTES, t + 1);
+        }
+        if (t * kKeyTile > wave_hi) continue;
+        const bool masked = t * kKeyTile + kKeyTile - 1 > wave_lo;
+        const uint32_t key_rows = lds_at(keys, row_lane), val_rows = lds_at(vals, row_lane), key_cols = lds_at(keys, col_lane);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            f32x16_t s = zero16(), dp = zero16();
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; ++kk) {
+                s = mfma16(Tile::rows(key_rows, b * 32, kk), qf[kk], s);
+                dp = mfma16(Tile::rows(val_rows, b * 32, kk), df[kk], dp);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)) * (dp[i] - D);
+            if (masked) {
+                // a sequence's first row has one key and a constant softmax: its scores have no gradient (what rounding would leave is not stored)
+                const int seen = (tok > 0 ? tok : -1) - t * kKeyTile - (lane >> 5) * 4;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) s[i] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8_t ds = pack_half(s, j);
+#pragma unroll
+                for (int n = 0; n < ND; ++n) acc[n] = mfma16(Tile::cols(key_cols, n * 32, b * 32 + j * 16), ds, acc[n]);
+            }
+        }
+    }
+    store_row<ND>(acc, sh.scale, dq.p + (long long)(u.row0 + tok) * dq.ld + head * d, d, lane, live);
+}
+
+// ---------------------------------------------------------------- backward: keys and values
+// Partial sums of a unit: registers as they lie, 16 bytes a lane, so that stores are whole lines.
+template <int ND> struct KeyPart {
+    static constexpr size_t FLOATS = (size_t)kAttnWaves * 2 * ND * 16 * 64;
+    static __device__ __forceinline__ float *at(float *parts, int slot, int wave, int which, int n, int quad, int lane)
+    {
+        return parts + (size_t)slot * FLOATS + ((((wave * 2 + which) * ND + n) * 4 + quad) * 64 + lane) * 4;
+    }
+};
+
+// r / G: for r < 2^26 and G <= 64 the upper half of r * ceil(2^32 / G), whose excess over r / G, below r / 2^32 < 1 / G, never reaches the next integer.
+inline unsigned token_magic(int G) { return G == 1 ? 0u : (unsigned)(((1ull << 32) + G - 1) / G); }
+__device__ __forceinline__ int token_of(int r, unsigned magic) { return magic ? (int)__umulhi((unsigned)r, magic) : r; }
+
+// dk and dv of 128 keys over some of the packed rows behind the first of them.
+template <int ND>
+__global__ void __launch_bounds__(kAttnThreads, ND > 2 ? 1 : 2)
+attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ delta, unsigned magic,
+                const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut dk, HeadsOut dv, float *__restrict__ parts)
+{
+    typedef AttnTile<ND, kRowStep> Tile;
+    typedef AttnTile<ND, kRowTile> Vals;
+    constexpr int STATS = Vals::BYTES + 4 * Tile::BYTES;
+    // the block's values; queries and their upstream, two steps each; the rows' lse and D, two steps each
+    __shared__ __attribute__((aligned(1024))) char lds[STATS + 4 * kRowStep * 4];
+    const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
+    if (at >= list->count) return;
+    const AttnUnit u = units[at];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
+    if (u.tile < 0) {
+        const int pieces = d / 8;
+        for (int i = threadIdx.x; i < u.len * pieces; i += kAttnThreads) {
+            *reinterpret_cast<uint4 *>(dk.p + (u.row0 + i / pieces) * dk.ld + (long long)hk * d + i % pieces * 8) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>(dv.p + (u.row0 + i / pieces) * dv.ld + (long long)hk * d + i % pieces * 8) = make_uint4(0, 0, 0, 0);
+        }
+        return;
+    }
+    const int rows = u.len * G, first = u.tile * kRowTile + wave * 32, key = min(first + (lane & 31), u.len - 1);
+    const int need = key * G;                                 // this key's first packed row; keys behind the sequence see what its last one sees
+    const int wave_first = min(first, u.len - 1) * G, wave_last = min(first + 31, u.len - 1) * G;
+
+    // the block's values, with zeros behind d: there the upstream's LDS rows hold other columns
+    const int sub = lane / Tile::SPR, piece = (lane % Tile::SPR) ^ Tile::swz(wave * Tile::RPB + sub), col = min(piece, d / 8 - 1) * 8;
+#pragma unroll
+    for (int i = 0; i < Vals::LOADS; ++i) {
+        const int blk = wave + i * kAttnWaves, r = min(u.tile * kRowTile + blk * Vals::RPB + sub, u.len - 1);
+        const uint4 x = *reinterpret_cast<const uint4 *>(v.p + (long long)(u.row0 + r) * v.ld + hk * d + col);
+        *reinterpret_cast<uint4 *>(lds + blk * 1024 + lane * 16) = piece < d / 8 ? x : make_uint4(0, 0, 0, 0);
+    }
+    // this wave's loads of a step's packed rows
+    const bf16_t *q0 = q.p + (long long)u.row0 * q.ld + (long long)hk * G * d + col, *d0 = dout.p + (long long)u.row0 * dout.ld + (long long)hk * G * d + col;
+    const float *stat = (lane < 32 ? lse2 : delta) + (long long)u.row0 * sh.Hq + hk * G;
+    auto load = [&](int t, int slot) __attribute__((always_inline)) {
+        char *to = lds + Vals::BYTES + slot * Tile::BYTES;
+#pragma unroll
+        for (int i = 0; i < Tile::LOADS; ++i) {
+            const int blk = wave + i * kAttnWaves, r = min(t * kRowStep + blk * Tile::RPB + sub, rows - 1), tok = token_of(r, magic), g = r - tok * G;
+            load_lds16(q0 + (long long)tok * q.ld + g * d, to + blk * 1024);
+            load_lds16(d0 + (long long)tok * dout.ld + g * d, to + 2 * Tile::BYTES + blk * 1024);
+        }
+        if (wave == 0) {
+            const int r = min(t * kRowStep + (lane & 31), rows - 1), tok = token_of(r, magic);
+            load_lds4(stat + (long long)tok * sh.Hq + (r - tok * G), lds + STATS + slot * 2 * kRowStep * 4);
+        }
+    };
+    const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
+    load(u.from, u.from & 1);
+    bf16x8_t kf[2 * ND];
+    load_row<ND>(kf, k.p + (long long)(u.row0 + key) * k.ld + hk * d, d, lane);
+
+    const float c = sh.scale * kLog2e;
+    f32x16_t ak[ND], av[ND];
+#pragma unroll
+    for (int n = 0; n < ND; ++n) ak[n] = av[n] = zero16();
+    for (int t = u.from; t < u.to; ++t) {
+        tile_barrier();
+        const int slot = t & 1;
+        const char *qs = lds + Vals::BYTES + slot * Tile::BYTES, *ds = qs + 2 * Tile::BYTES;
+        const float *ls = reinterpret_cast<const float *>(lds + STATS + slot * 2 * kRowStep * 4), *Ds = ls + kRowStep;
+        if (t + 1 < u.to) load(t + 1, slot ^ 1);
+        const int r0 = t * kRowStep;
+        if (r0 + kRowStep - 1 < wave_first) continue;         // all of these rows come before this wave's keys
+        const uint32_t q_rows = lds_at(qs, row_lane), d_rows = lds_at(ds, row_lane), v_rows = lds_at(lds + wave * 32 * Vals::ROW, row_lane);
+        f32x16_t s = zero16(), dp = zero16();
+#pragma unroll
+        for (int kk = 0; kk < 2 * ND; ++kk) {
+            s = mfma16(Tile::rows(q_rows, 0, kk), kf[kk], s);
+            dp = mfma16(Tile::rows(d_rows, 0, kk), Vals::rows(v_rows, 0, kk), dp);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 l4 = *reinterpret_cast<const float4 *>(ls + g * 8 + (lane >> 5) * 4);
+            const float4 D4 = *reinterpret_cast<const float4 *>(Ds + g * 8 + (lane >> 5) * 4);
+            const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, Dv[4] = {D4.x, D4.y, D4.z, D4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c, -lv[i]));
+                dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - Dv[i]);
+            }
+        }
+        if (r0 < max(wave_last, G) || r0 + kRowStep > rows) {
+            const int base = r0 + (lane >> 5) * 4;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = base + (i >> 2) * 8 + (i & 3);
+                if (r < need || r >= rows) s[i] = dp[i] = 0.0f;
+                if (r < G) dp[i] = 0.0f;                      // the sequence's first token: one key, no gradient of its scores
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t q_cols = lds_at(qs, col_lane), d_cols = lds_at(ds, col_lane);
+            const bf16x8_t p = pack_half(s, j), e = pack_half(dp, j);
+#pragma unroll
+            for (int n = 0; n < ND; ++n) {
+                av[n] = mfma16(Tile::cols(d_cols, n * 32, j * 16), p, av[n]);
+                ak[n] = mfma16(Tile::cols(q_cols, n * 32, j * 16), e, ak[n]);
+            }
+        }
+    }
+    if (u.slot >= 0) {
+#pragma unroll
+        for (int n = 0; n < ND; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                *reinterpret_cast<float4 *>(KeyPart<ND>::at(parts, u.slot * sh.Hk + hk, wave, 0, n, g, lane)) = make_float4(ak[n][4 * g], ak[n][4 * g + 1], ak[n][4 * g + 2], ak[n][4 * g + 3]);
+                *reinterpret_cast<float4 *>(KeyPart<ND>::at(parts, u.slot * sh.Hk + hk, wave, 1, n, g, lane)) = make_float4(av[n][4 * g], av[n][4 * g + 1], av[n][4 * g + 2], av[n][4 * g + 3]);
+            }
+        return;
+    }
+    const bool live = first + (lane & 31) < u.len;
+    store_row<ND>(ak, sh.scale, dk.p + (long long)(u.row0 + key) * dk.ld + hk * d, d, lane, live);
+    store_row<ND>(av, 1.0f, dv.p + (long long)(u.row0 + key) * dv.ld + hk * d, d, lane, live);
+}
+
+// Adds up the partial sums of the tiles whose rows several blocks shared, in ascending order.
+template <int ND>
+__global__ void __launch_bounds__(kAttnThreads)
+attn_join_kernel(AttnShape sh, const AttnList *__restrict__ list, const AttnUnit *__restrict__ joins, float *__restrict__ parts, HeadsOut dk, HeadsOut dv)
+{
+    const int at = blockIdx.x / (2 * sh.Hk), rest = blockIdx.x - at * 2 * sh.Hk, hk = rest >> 1, which = rest & 1;
+    if (at >= list->joins) return;
+    const AttnUnit u = joins[at];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = u.tile * kRowTile + wave * 32, key = min(first + (lane & 31), u.len - 1);
+    f32x16_t acc[ND];
+#pragma unroll
+    for (int n = 0; n < ND; ++n) acc[n] = zero16();
+    for (int c = 0; c < u.chunks; ++c)
+#pragma unroll
+        for (int n = 0; n < ND; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 v = *reinterpret_cast<const float4 *>(KeyPart<ND>::at(parts, (u.slot + c) * sh.Hk + hk, wave, which, n, g, lane));
+                acc[n][4 * g] += v.x, acc[n][4 * g + 1] += v.y, acc[n][4 * g + 2] += v.z, acc[n][4 * g + 3] += v.w;
+            }
+    const HeadsOut &to = which ? dv : dk;
+    store_row<ND>(acc, which ? 1.0f : sh.scale, to.p + (long long)(u.row0 + key) * to.ld + hk * sh.d, sh.d, lane, first + (lane & 31) < u.len);
+}
+
+// ---------------------------------------------------------------- host
+inline bool attn_takes(int T, int n_seq, int Hq, int Hk, int d)
+{
+    return d % 8 == 0 && d <= kAttnMaxDim && n_seq <= kAttnMaxSeq && Hq / Hk <= kAttnMaxGroup && Hq <= 4096 && (long long)T * (Hq / Hk) <= kAttnMaxRows;
+}
+inline int attn_nd(int d) { return (d + 31) / 32; }
+// Lists: at most so many units of rows, units of keys, joined tiles and partial sums a key head; places of padding are at most a tile a sequence more
+// than the rows they take.
+struct AttnSizes {
+    int row_units, key_units, joins, slots;
+    size_t part_bytes;
+};
+inline AttnSizes attn_sizes(int T, int n_seq, int Hq, int Hk, int d)
+{
+    const int G = Hq / Hk;
+    AttnSizes s;
+    s.row_units = (int)((long long)T * G / kRowTile + T / kRowTile) + 2 * n_seq;
+    const long long key_tiles = T / kRowTile + n_seq, most = tiles_of((long long)T * G, kRowStep);
+    // a chunk has at least a 1024th of all heads' steps, and 32: tiles of two or more chunks have at most twice as many as their steps make whole ones
+    const long long whole = std::min<long long>(2 * kAttnSlots / Hk + 1, key_tiles * most / kMinChunk);
+    s.slots = (int)(2 * whole);
+    s.joins = (int)std::min<long long>(whole, key_tiles);
+    s.key_units = (int)(2 * key_tiles + 2 * whole);
+    s.part_bytes = round256((size_t)s.slots * Hk * kAttnWaves * 2 * attn_nd(d) * 16 * 64 * sizeof(float));
+    return s;
+}
+inline size_t attn_list_bytes(int units) { return round256(sizeof(AttnList) + (size_t)units * sizeof(AttnUnit)); }
+size_t attn_fwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
+{
+    if (T < 0 || n_seq < 0 || Hk < 1 || Hq < 1 || Hq % Hk || d < 8 || !attn_takes(T, n_seq, Hq, Hk, d)) return 0;
+    return attn_list_bytes(attn_sizes(T, n_seq, Hq, Hk, d).row_units);
+}
+size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
+{
+    const size_t fwd = attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d);
+    if (!fwd) return 0;
+    const AttnSizes s = attn_sizes(T, n_seq, Hq, Hk, d);
+    return fwd + attn_list_bytes(s.key_units + s.joins) + 2 * round256((size_t)T * Hq * sizeof(float)) + s.part_bytes;
+}
+inline int check_attn(const int32_t *seq_start, int n_seq, int T, int Hq, int Hk, int d, float scale, const int32_t *err_flag)
+{
+    if (T < 0 || n_seq < 0 || Hq < 1 || Hk < 1 || Hq % Hk || d < 8 || !(scale > 0.0f) || scale > 3e38f) return RELIBRA_EINVAL;
+    if (!attn_takes(T, n_seq, Hq, Hk, d)) return RELIBRA_EUNSUPPORTED;
+    if (T > 0 && n_seq > 0 && (!seq_start || !err_flag)) return RELIBRA_EINVAL;
+    return RELIBRA_OK;
+}
+template <class Fn> void attn_layout(int d, const Fn &fn)
+{
+    switch (attn_nd(d)) {
+    case 1: fn(std::integral_constant<int, 1>{}); break;
+    case 2: fn(std::integral_constant<int, 2>{}); break;
+    case 3: fn(std::integral_constant<int, 3>{}); break;
+    default: fn(std::integral_constant<int, 4>{}); break;
+    }
+}
+
+}  // namespace relibra
+
+using namespace relibra;
+
+extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *seq_start,
+                                     const int32_t *seq_len, int n_seq, int T, int Hq, int Hk, int d, float scale, void *out, int64_t out_stride, float *lse,
+                                     void *workspace, size_t workspace_bytes, int32_t *err_flag, relibra_stream stream_)
+{
+    hipStream_t stream = (hipStream_t)stream_;
+    const int rc = check_attn(seq_start, n_seq, T, Hq, Hk, d, scale, err_flag);
+    if (rc != RELIBRA_OK) return rc;
+    if (T == 0 || n_seq == 0) return RELIBRA_OK;
+    const HeadRows in[3] = {{q, q_stride, Hq * d}, {k, k_stride, Hk * d}, {v, v_stride, Hk * d}}, to{out, out_stride, Hq * d};
+    if (!to.usable() || !lse) return RELIBRA_EINVAL;
+    for (const HeadRows &x : in)
+        if (!x.usable() || x.overlaps(to, T)) return RELIBRA_EINVAL;
+    if (!aligned16(workspace)) return RELIBRA_EINVAL;
+    if (!workspace || workspace_bytes < attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
+    const AttnSizes sz = attn_sizes(T, n_seq, Hq, Hk, d);
+    AttnList *list = (AttnList *)workspace;
+    AttnUnit *units = (AttnUnit *)(list + 1);
+    const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
+    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<false><<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, sz.row_units, 0, list, units,
+                                                                                                           nullptr, err_flag));
+    attn_layout(d, [&](auto nd) {
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_FWD, stream, (attn_fwd_kernel<decltype(nd)::value><<<sz.row_units * Hk, kAttnThreads, 0, stream>>>(
+            sh, HeadsIn{(const bf16_t *)q, q_stride}, HeadsIn{(const bf16_t *)k, k_stride}, HeadsIn{(const bf16_t *)v, v_stride}, list, units,
+            HeadsOut{(bf16_t *)out, out_stride}, lse)));
+    });
+    RELIBRA_HIP_TRY(launch_check());
+    return RELIBRA_OK;
+}
+
+extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *out,
+                                     int64_t out_stride, const float *lse, const void *dout, int64_t dout_stride, const int32_t *seq_start, const int32_t *seq_len,
+                                     int n_seq, int T, int Hq, int Hk, int d, float scale, void *dq, int64_t dq_stride, void *dk, int64_t dk_stride, void *dv,
+                                     int64_t dv_stride, void *workspace, size_t workspace_bytes, int32_t *err_flag, relibra_stream stream_)
+{
+    hipStream_t stream = (hipStream_t)stream_;
+    const int rc = check_attn(seq_start, n_seq, T, Hq, Hk, d, scale, err_flag);
+    if (rc != RELIBRA_OK) return rc;
+    if (T == 0 || n_seq == 0) return RELIBRA_OK;
+    const HeadRows in[5] = {{q, q_stride, Hq * d}, {k, k_stride, Hk * d}, {v, v_stride, Hk * d}, {out, out_stride, Hq * d}, {dout, dout_stride, Hq * d}};
+    const HeadRows to[3] = {{dq, dq_stride, Hq * d}, {dk, dk_stride, Hk * d}, {dv, dv_stride, Hk * d}};
+    if (!lse) return RELIBRA_EINVAL;
+    for (const HeadRows &x : in)
+        if (!x.usable()) return RELIBRA_EINVAL;
+    for (int i = 0; i < 3; ++i) {
+        if (!to[i].usable()) return RELIBRA_EINVAL;
+        for (const HeadRows &x : in)
+            if (x.overlaps(to[i], T)) return RELIBRA_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (to[j].overlaps(to[i], T)) return RELIBRA_EINVAL;
+    }
+    if (!aligned16(workspace)) return RELIBRA_EINVAL;
+    if (!workspace || workspace_bytes < attn_bwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
+    const AttnSizes sz = attn_sizes(T, n_seq, Hq, Hk, d);
+    char *ws = (char *)workspace;
+    AttnList *rows = (AttnList *)ws, *keys = (AttnList *)(ws += attn_list_bytes(sz.row_units));
+    float *lse2 = (float *)(ws += attn_list_bytes(sz.key_units + sz.joins));
+    float *delta = (float *)(ws += round256((size_t)T * Hq * sizeof(float)));
+    float *parts = (float *)(ws += round256((size_t)T * Hq * sizeof(float)));
+    AttnUnit *row_units = (AttnUnit *)(rows + 1), *key_units = (AttnUnit *)(keys + 1), *joins = key_units + sz.key_units;
+    const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
+    const HeadsIn qi{(const bf16_t *)q, q_stride}, ki{(const bf16_t *)k, k_stride}, vi{(const bf16_t *)v, v_stride}, oi{(const bf16_t *)out, out_stride},
+        di{(const bf16_t *)dout, dout_stride};
+    const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
+    const unsigned magic = token_magic(sh.G);
+    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<false><<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, sz.row_units, 0, rows,
+                                                                                                           row_units, nullptr, err_flag));
+    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<true><<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, sz.key_units, sz.slots, keys,
+                                                                                                          key_units, joins, err_flag));
+    attn_layout(d, [&](auto nd) {
+        constexpr int ND = decltype(nd)::value;
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<sz.row_units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, rows, row_units, dqo, lse2, delta)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<sz.key_units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, magic, keys, key_units, dko, dvo, parts)));
+        if (sz.joins > 0)
+            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<sz.joins * Hk * 2, kAttnThreads, 0, stream>>>(sh, keys, joins, parts, dko, dvo)));
+    });
+    RELIBRA_HIP_TRY(launch_check());
+    return RELIBRA_OK;
+}

@@ -69,6 +69,9 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 size_t router_ws_bytes(int n_mb, int T, int k, int E);
 size_t norm_ws_bytes(int T, int h);
 size_t ortho_ws_bytes(int n, int rows, int cols);
+size_t qk_ws_bytes(int T, int Hq, int Hk, int d);
+size_t attn_fwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d);
+size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d);
 
 inline hipError_t launch_check() { return hipGetLastError(); }
 

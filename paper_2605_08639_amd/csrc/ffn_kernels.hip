@@ -1203,6 +1203,9 @@ extern "C" size_t relibra_workspace_bytes(int which, int T, int k, int E, int G,
     case RELIBRA_WS_ROUTER: return router_ws_bytes(G, T, k, E);
     case RELIBRA_WS_BLOCK_NORM: return norm_ws_bytes(T, h);
     case RELIBRA_WS_ORTHOGONALIZE: return ortho_ws_bytes(E, h, hff);
+    case RELIBRA_WS_QK_NORM_ROPE: return qk_ws_bytes(T, E, h, hff);
+    case RELIBRA_WS_ATTENTION_FWD: return attn_fwd_ws_bytes(T, G, E, h, hff);
+    case RELIBRA_WS_ATTENTION_BWD: return attn_bwd_ws_bytes(T, G, E, h, hff);
     default: return 0;
     }
     (void)h;

@@ -70,6 +70,12 @@ __device__ __forceinline__ void load_lds16_sv(const bf16_t *uniform_base, uint32
     const uint32_t m = (uint32_t)(uintptr_t)RELIBRA_LDS(block);
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_byte_off), "s"(uniform_base), "s"(m) : "memory", "m0");
 }
+// 64 lanes x 4 bytes to 256 bytes at block.
+__device__ __forceinline__ void load_lds4(const float *g, char *block)
+{
+    const uint32_t m = (uint32_t)(uintptr_t)RELIBRA_LDS(block);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(m) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 struct Operand {

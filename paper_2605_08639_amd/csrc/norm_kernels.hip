@@ -15,6 +15,7 @@
 // a gate an element 47 us (122 MB at 2.6 TB/s; 40 + 5 in its kernels): a block a unit, so three rounds of rows and a fourth of nine rows, and a row's
 // loads, sums and stores one behind the other, with no register left for the next row's.
 // Requesting the next row's tensors while a row is finished gained nothing (backward 152 -> 161 and, in the kernel, 39 -> 39 us).
+#include "row_reduce.h"
 #include "wave_ops.h"
 
 #include <algorithm>
@@ -285,48 +286,6 @@ norm_bwd_kernel(NormShape sh, const XT *__restrict__ x_out, const XT *dx_out, co
     leave(acc1, part_pre);
 }
 
-// dw (+)= the sum of P partial rows: 32 columns a block, 128 strips of rows, joined in ascending order.
-constexpr int kReduceStrips = 128;
-__global__ void __launch_bounds__(kReduceStrips * 8)
-norm_reduce_kernel(const float *__restrict__ part0, const float *__restrict__ part1, float *__restrict__ dw0, float *__restrict__ dw1, int P, int h, int add)
-{
-    __shared__ float4 join[kReduceStrips][8];
-    const float *part = blockIdx.y ? part1 : part0;
-    float *dw = blockIdx.y ? dw1 : dw0;
-    if (!dw) return;
-    const int col = threadIdx.x & 7, strip = threadIdx.x >> 3, at = blockIdx.x * 32 + col * 4;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (at < h)
-#pragma unroll 4
-        for (int p = strip; p < P; p += kReduceStrips) {
-            const float4 v = *reinterpret_cast<const float4 *>(part + (size_t)p * h + at);
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-    join[strip][col] = s;
-    __syncthreads();
-    // 128 strips to 8, then one thread a column the rest
-    if (strip < 8) {
-        for (int i = strip + 8; i < kReduceStrips; i += 8) {
-            const float4 v = join[i][col];
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        join[strip][col] = s;
-    }
-    __syncthreads();
-    if (strip == 0 && at < h) {
-        for (int i = 1; i < 8; ++i) {
-            const float4 v = join[i][col];
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        float4 *to = reinterpret_cast<float4 *>(dw + at);
-        if (add) {
-            const float4 o = *to;
-            s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
-        }
-        *to = s;
-    }
-}
-
 struct NormGrid {
     int chunks, waves, rows_per_block, blocks;
 };
@@ -464,7 +423,7 @@ extern "C" int relibra_block_norm_bwd(const void *x_out, const void *dx_out, con
                           sh, g, (bf16_t *)dx, (bf16_t *)dy, dgate, part_post, part_pre, one && add, stream);
     }
     if ((w_post || w_pre) && !one)
-        RELIBRA_LAUNCH(RELIBRA_K_NORM_REDUCE, stream, norm_reduce_kernel<<<dim3((h + 31) / 32, 2), kReduceStrips * 8, 0, stream>>>(
+        RELIBRA_LAUNCH(RELIBRA_K_NORM_REDUCE, stream, row_reduce_kernel<<<dim3((h + 31) / 32, 2), kReduceStrips * 8, 0, stream>>>(
             part_post, part_pre, w_post ? dw_post : nullptr, w_pre ? dw_pre : nullptr, P, h, add));
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
