@@ -20,9 +20,10 @@
 namespace relibra {
 
 constexpr int kAttnThreads = 256, kAttnWaves = 4;
-constexpr int kRowTile = 128;                                // packed rows (or keys) of a block
-constexpr int kKeyTile = 64;                                 // keys of a step
-constexpr int kRowStep = 32;                                 // packed rows of a step of keys' gradients
+constexpr int kRowTile = 128;                                // packed rows of a block, keys of a step
+constexpr int kKeyTile = 64;
+constexpr int kKeyRows = 64;                                 // keys' gradients: keys of a block, packed rows of a step
+constexpr int kRowStep = 64;
 constexpr int kAttnMaxDim = 128, kAttnMaxSeq = 8192, kAttnMaxGroup = 64;
 constexpr int kAttnMaxRows = 1 << 26;                        // packed rows of a key head
 constexpr int kAttnSlots = 512;                              // blocks that run at once: two a unit
@@ -42,7 +43,7 @@ struct HeadsOut {
     long long ld;
 };
 // One block's work: rows (or keys) tile * 128 .. of the sequence that starts at row0; tile < 0: rows row0 .. row0 + len - 1 are padding.
-// Keys: steps from .. to - 1 of 32 packed rows, into slot `slot` of the partial sums (-1: all there are).
+// Keys: steps from .. to - 1 of 64 packed rows, into slot `slot` of the partial sums (-1: all there are).
 struct AttnUnit {
     int row0, len, tile, from, to, slot, chunks, pad;
 };
@@ -190,7 +191,7 @@ template <int ND> struct TokenTiles {
 // Lists the blocks' work, heaviest first.  One block: sequences are counted (their rows' or keys' tiles, and the tiles of padding behind
 // them), every thread finds the sequence of its share of the tiles by bisection, and a counting sort by work puts them in order (within a
 // bin in any order: results do not depend on it).  A table that does not ascend within [0, T], or lengths beyond their places: nothing is listed.
-constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinChunk = 32;
+constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinChunk = 16;
 
 __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // inclusive; two barriers
 {
@@ -235,11 +236,11 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
             const int a = seq_start[s], b = seq_start[s + 1], len = seq_len ? seq_len[s] : b - a;
             if (a < 0 || b < a || b > T || len < 0 || len > b - a) bad = true;
             else {
-                const int own = tiles_of(KEYS ? (long long)len : (long long)len * G, kRowTile);
+                const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile);
                 tiles = own + tiles_of(b - a - len, kRowTile);
-                if (KEYS && own) {                             // sum of ceil(len G / 32) - 4 G t over the tiles t
+                if (KEYS && own) {                             // sum of ceil(len G / 64) - G t over the tiles t
                     const long long end = tiles_of((long long)len * G, kRowStep);
-                    atomicAdd(&steps, (unsigned long long)(end * own - (long long)(kRowTile / kRowStep) * G * own * (own - 1) / 2));
+                    atomicAdd(&steps, (unsigned long long)(end * own - (long long)(kKeyRows / kRowStep) * G * own * (own - 1) / 2));
                 }
             }
         }
@@ -269,7 +270,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
         }
         const int a = seq_start[lo], b = seq_start[lo + 1], len = seq_len ? seq_len[lo] : b - a;
         int t = f - before[lo];
-        const int own = tiles_of(KEYS ? (long long)len : (long long)len * G, kRowTile);
+        const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile);
         AttnUnit u{a, len, t, 0, 0, -1, 1, 0};
         if (t >= own) {
             u.row0 = a + len + (t - own) * kRowTile;
@@ -279,7 +280,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
         } else if (!KEYS) {
             fn(u, tiles_of(min(((long long)t * kRowTile + kRowTile - 1) / G + 1, (long long)len), kKeyTile));
         } else {
-            const int first = kRowTile / kRowStep * G * t, end = tiles_of((long long)len * G, kRowStep), n = end - first;
+            const int first = kKeyRows / kRowStep * G * t, end = tiles_of((long long)len * G, kRowStep), n = end - first;
             int chunks = tiles_of(n, chunk), slot = -1;
             if (chunks > 1 && place) {
                 slot = atomicAdd(&n_slots, chunks);
@@ -500,10 +501,10 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
 // ---------------------------------------------------------------- backward: keys and values
 // Partial sums of a unit: registers as they lie, 16 bytes a lane, so that stores are whole lines.
 template <int ND> struct KeyPart {
-    static constexpr size_t FLOATS = (size_t)kAttnWaves * 2 * ND * 16 * 64;
-    static __device__ __forceinline__ float *at(float *parts, int slot, int wave, int which, int n, int quad, int lane)
+    static constexpr size_t FLOATS = (size_t)kAttnWaves * ND * 16 * 64;
+    static __device__ __forceinline__ float *at(float *parts, int slot, int wave, int n, int quad, int lane)
     {
-        return parts + (size_t)slot * FLOATS + ((((wave * 2 + which) * ND + n) * 4 + quad) * 64 + lane) * 4;
+        return parts + (size_t)slot * FLOATS + (((wave * ND + n) * 4 + quad) * 64 + lane) * 4;
     }
 };
 
@@ -511,21 +512,22 @@ template <int ND> struct KeyPart {
 inline unsigned token_magic(int G) { return G == 1 ? 0u : (unsigned)(((1ull << 32) + G - 1) / G); }
 __device__ __forceinline__ int token_of(int r, unsigned magic) { return magic ? (int)__umulhi((unsigned)r, magic) : r; }
 
-// dk and dv of 128 keys over some of the packed rows behind the first of them.
+// dk and dv of 64 keys over some of the packed rows behind the first of them.  Two waves share 32 keys: each works out p and ds for 32 of a step's
+// 64 rows, hands the other the half that it needs, and adds up one of the two gradients over all 64 rows.  A wave for itself would hold both sums,
+// 128 registers beside the operands' 64 and the scores' 32, and leave no room for a second wave on its SIMD.
 template <int ND>
-__global__ void __launch_bounds__(kAttnThreads, ND > 2 ? 1 : 2)
+__global__ void __launch_bounds__(kAttnThreads, 2)
 attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ delta, unsigned magic,
                 const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut dk, HeadsOut dv, float *__restrict__ parts)
 {
     typedef AttnTile<ND, kRowStep> Tile;
-    typedef AttnTile<ND, kRowTile> Vals;
-    constexpr int STATS = Vals::BYTES + 4 * Tile::BYTES;
-    // the block's values; queries and their upstream, two steps each; the rows' lse and D, two steps each
-    __shared__ __attribute__((aligned(1024))) char lds[STATS + 4 * kRowStep * 4];
+    constexpr int STATS = 4 * Tile::BYTES, TRADE = STATS + 4 * kRowStep * 4;
+    // queries and their upstream, two steps each; the rows' lse and D, two steps each; what the waves of a pair hand each other
+    __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves * 2048];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     if (at >= list->count) return;
     const AttnUnit u = units[at];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), role = wave & 1, G = sh.G, d = sh.d;   // role 0: dv, 1: dk
     if (u.tile < 0) {
         const int pieces = d / 8;
         for (int i = threadIdx.x; i < u.len * pieces; i += kAttnThreads) {
@@ -534,102 +536,107 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
         }
         return;
     }
-    const int rows = u.len * G, first = u.tile * kRowTile + wave * 32, key = min(first + (lane & 31), u.len - 1);
+    const int rows = u.len * G, first = u.tile * kKeyRows + (wave >> 1) * 32, key = min(first + (lane & 31), u.len - 1);
     const int need = key * G;                                 // this key's first packed row; keys behind the sequence see what its last one sees
-    const int wave_first = min(first, u.len - 1) * G, wave_last = min(first + 31, u.len - 1) * G;
+    const int pair_first = min(first, u.len - 1) * G, pair_last = min(first + 31, u.len - 1) * G;
 
-    // the block's values, with zeros behind d: there the upstream's LDS rows hold other columns
-    const int sub = lane / Tile::SPR, piece = (lane % Tile::SPR) ^ Tile::swz(wave * Tile::RPB + sub), col = min(piece, d / 8 - 1) * 8;
-#pragma unroll
-    for (int i = 0; i < Vals::LOADS; ++i) {
-        const int blk = wave + i * kAttnWaves, r = min(u.tile * kRowTile + blk * Vals::RPB + sub, u.len - 1);
-        const uint4 x = *reinterpret_cast<const uint4 *>(v.p + (long long)(u.row0 + r) * v.ld + hk * d + col);
-        *reinterpret_cast<uint4 *>(lds + blk * 1024 + lane * 16) = piece < d / 8 ? x : make_uint4(0, 0, 0, 0);
-    }
     // this wave's loads of a step's packed rows
+    const int sub = lane / Tile::SPR, col = min((lane % Tile::SPR) ^ Tile::swz(wave * Tile::RPB + sub), d / 8 - 1) * 8;
     const bf16_t *q0 = q.p + (long long)u.row0 * q.ld + (long long)hk * G * d + col, *d0 = dout.p + (long long)u.row0 * dout.ld + (long long)hk * G * d + col;
-    const float *stat = (lane < 32 ? lse2 : delta) + (long long)u.row0 * sh.Hq + hk * G;
+    const float *stat = (wave == 0 ? lse2 : delta) + (long long)u.row0 * sh.Hq + hk * G;
     auto load = [&](int t, int slot) __attribute__((always_inline)) {
-        char *to = lds + Vals::BYTES + slot * Tile::BYTES;
+        char *to = lds + slot * Tile::BYTES;
 #pragma unroll
         for (int i = 0; i < Tile::LOADS; ++i) {
             const int blk = wave + i * kAttnWaves, r = min(t * kRowStep + blk * Tile::RPB + sub, rows - 1), tok = token_of(r, magic), g = r - tok * G;
             load_lds16(q0 + (long long)tok * q.ld + g * d, to + blk * 1024);
             load_lds16(d0 + (long long)tok * dout.ld + g * d, to + 2 * Tile::BYTES + blk * 1024);
         }
-        if (wave == 0) {
-            const int r = min(t * kRowStep + (lane & 31), rows - 1), tok = token_of(r, magic);
-            load_lds4(stat + (long long)tok * sh.Hq + (r - tok * G), lds + STATS + slot * 2 * kRowStep * 4);
+        if (wave < 2) {
+            const int r = min(t * kRowStep + lane, rows - 1), tok = token_of(r, magic);
+            load_lds4(stat + (long long)tok * sh.Hq + (r - tok * G), lds + STATS + (slot * 2 + wave) * kRowStep * 4);
         }
     };
-    const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
+    const uint32_t row_lane = Tile::row_lane(lane) + role * 32 * Tile::ROW, col_lane = Tile::col_lane(lane);
     load(u.from, u.from & 1);
-    bf16x8_t kf[2 * ND];
+    bf16x8_t kf[2 * ND], vf[2 * ND];
     load_row<ND>(kf, k.p + (long long)(u.row0 + key) * k.ld + hk * d, d, lane);
+    load_row<ND>(vf, v.p + (long long)(u.row0 + key) * v.ld + hk * d, d, lane);
 
     const float c = sh.scale * kLog2e;
-    f32x16_t ak[ND], av[ND];
+    f32x16_t acc[ND];
 #pragma unroll
-    for (int n = 0; n < ND; ++n) ak[n] = av[n] = zero16();
+    for (int n = 0; n < ND; ++n) acc[n] = zero16();
+    char *give = lds + TRADE + wave * 2048 + lane * 16;
+    const char *take = lds + TRADE + (wave ^ 1) * 2048 + lane * 16;
     for (int t = u.from; t < u.to; ++t) {
         tile_barrier();
-        const int slot = t & 1;
-        const char *qs = lds + Vals::BYTES + slot * Tile::BYTES, *ds = qs + 2 * Tile::BYTES;
-        const float *ls = reinterpret_cast<const float *>(lds + STATS + slot * 2 * kRowStep * 4), *Ds = ls + kRowStep;
+        const int slot = t & 1, r0 = t * kRowStep;
+        const char *qs = lds + slot * Tile::BYTES, *ds = qs + 2 * Tile::BYTES;
+        const float *ls = reinterpret_cast<const float *>(lds + STATS + slot * 2 * kRowStep * 4) + role * 32, *Ds = ls + kRowStep;
         if (t + 1 < u.to) load(t + 1, slot ^ 1);
-        const int r0 = t * kRowStep;
-        if (r0 + kRowStep - 1 < wave_first) continue;         // all of these rows come before this wave's keys
-        const uint32_t q_rows = lds_at(qs, row_lane), d_rows = lds_at(ds, row_lane), v_rows = lds_at(lds + wave * 32 * Vals::ROW, row_lane);
-        f32x16_t s = zero16(), dp = zero16();
+        const bool dead = r0 + kRowStep - 1 < pair_first;     // all of these rows come before this pair's keys
+        bf16x8_t mine[2];
+        if (!dead) {
+            const uint32_t q_rows = lds_at(qs, row_lane), d_rows = lds_at(ds, row_lane);
+            f32x16_t s = zero16(), dp = zero16();
 #pragma unroll
-        for (int kk = 0; kk < 2 * ND; ++kk) {
-            s = mfma16(Tile::rows(q_rows, 0, kk), kf[kk], s);
-            dp = mfma16(Tile::rows(d_rows, 0, kk), Vals::rows(v_rows, 0, kk), dp);
-        }
+            for (int kk = 0; kk < 2 * ND; ++kk) {
+                s = mfma16(Tile::rows(q_rows, 0, kk), kf[kk], s);
+                dp = mfma16(Tile::rows(d_rows, 0, kk), vf[kk], dp);
+            }
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const float4 l4 = *reinterpret_cast<const float4 *>(ls + g * 8 + (lane >> 5) * 4);
-            const float4 D4 = *reinterpret_cast<const float4 *>(Ds + g * 8 + (lane >> 5) * 4);
-            const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, Dv[4] = {D4.x, D4.y, D4.z, D4.w};
+            for (int g = 0; g < 4; ++g) {
+                const float4 l4 = *reinterpret_cast<const float4 *>(ls + g * 8 + (lane >> 5) * 4);
+                const float4 D4 = *reinterpret_cast<const float4 *>(Ds + g * 8 + (lane >> 5) * 4);
+                const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, Dv[4] = {D4.x, D4.y, D4.z, D4.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c, -lv[i]));
-                dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - Dv[i]);
+                for (int i = 0; i < 4; ++i) {
+                    s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c, -lv[i]));
+                    dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - Dv[i]);
+                }
+            }
+            if (r0 < max(pair_last, G) || r0 + kRowStep > rows) {
+                const int base = r0 + role * 32 + (lane >> 5) * 4;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int r = base + (i >> 2) * 8 + (i & 3);
+                    if (r < need || r >= rows) s[i] = dp[i] = 0.0f;
+                    if (r < G) dp[i] = 0.0f;                  // the sequence's first token: one key, no gradient of its scores
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8_t p = pack_half(s, j), e = pack_half(dp, j);
+                mine[j] = role ? e : p;
+                *reinterpret_cast<bf16x8_t *>(give + j * 1024) = role ? p : e;
             }
         }
-        if (r0 < max(wave_last, G) || r0 + kRowStep > rows) {
-            const int base = r0 + (lane >> 5) * 4;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = base + (i >> 2) * 8 + (i & 3);
-                if (r < need || r >= rows) s[i] = dp[i] = 0.0f;
-                if (r < G) dp[i] = 0.0f;                      // the sequence's first token: one key, no gradient of its scores
-            }
-        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (dead) continue;
+        const uint32_t cols = lds_at(role ? qs : ds, col_lane);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint32_t q_cols = lds_at(qs, col_lane), d_cols = lds_at(ds, col_lane);
-            const bf16x8_t p = pack_half(s, j), e = pack_half(dp, j);
+            const bf16x8_t theirs = *reinterpret_cast<const bf16x8_t *>(take + j * 1024);
+            const bf16x8_t lo = role ? theirs : mine[j], hi = role ? mine[j] : theirs;
 #pragma unroll
-            for (int n = 0; n < ND; ++n) {
-                av[n] = mfma16(Tile::cols(d_cols, n * 32, j * 16), p, av[n]);
-                ak[n] = mfma16(Tile::cols(q_cols, n * 32, j * 16), e, ak[n]);
-            }
+            for (int n = 0; n < ND; ++n) acc[n] = mfma16(Tile::cols(cols, n * 32, j * 16), lo, acc[n]);
+#pragma unroll
+            for (int n = 0; n < ND; ++n) acc[n] = mfma16(Tile::cols(cols, n * 32, 32 + j * 16), hi, acc[n]);
         }
     }
     if (u.slot >= 0) {
 #pragma unroll
         for (int n = 0; n < ND; ++n)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                *reinterpret_cast<float4 *>(KeyPart<ND>::at(parts, u.slot * sh.Hk + hk, wave, 0, n, g, lane)) = make_float4(ak[n][4 * g], ak[n][4 * g + 1], ak[n][4 * g + 2], ak[n][4 * g + 3]);
-                *reinterpret_cast<float4 *>(KeyPart<ND>::at(parts, u.slot * sh.Hk + hk, wave, 1, n, g, lane)) = make_float4(av[n][4 * g], av[n][4 * g + 1], av[n][4 * g + 2], av[n][4 * g + 3]);
-            }
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4 *>(KeyPart<ND>::at(parts, u.slot * sh.Hk + hk, wave, n, g, lane)) = make_float4(acc[n][4 * g], acc[n][4 * g + 1], acc[n][4 * g + 2], acc[n][4 * g + 3]);
         return;
     }
-    const bool live = first + (lane & 31) < u.len;
-    store_row<ND>(ak, sh.scale, dk.p + (long long)(u.row0 + key) * dk.ld + hk * d, d, lane, live);
-    store_row<ND>(av, 1.0f, dv.p + (long long)(u.row0 + key) * dv.ld + hk * d, d, lane, live);
+    const HeadsOut &to = role ? dk : dv;
+    store_row<ND>(acc, role ? sh.scale : 1.0f, to.p + (long long)(u.row0 + key) * to.ld + hk * d, d, lane, first + (lane & 31) < u.len);
 }
 
 // Adds up the partial sums of the tiles whose rows several blocks shared, in ascending order.
@@ -637,10 +644,10 @@ template <int ND>
 __global__ void __launch_bounds__(kAttnThreads)
 attn_join_kernel(AttnShape sh, const AttnList *__restrict__ list, const AttnUnit *__restrict__ joins, float *__restrict__ parts, HeadsOut dk, HeadsOut dv)
 {
-    const int at = blockIdx.x / (2 * sh.Hk), rest = blockIdx.x - at * 2 * sh.Hk, hk = rest >> 1, which = rest & 1;
+    const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     if (at >= list->joins) return;
     const AttnUnit u = joins[at];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = u.tile * kRowTile + wave * 32, key = min(first + (lane & 31), u.len - 1);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = u.tile * kKeyRows + (wave >> 1) * 32, key = min(first + (lane & 31), u.len - 1);
     f32x16_t acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; ++n) acc[n] = zero16();
@@ -649,11 +656,11 @@ attn_join_kernel(AttnShape sh, const AttnList *__restrict__ list, const AttnUnit
         for (int n = 0; n < ND; ++n)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float4 v = *reinterpret_cast<const float4 *>(KeyPart<ND>::at(parts, (u.slot + c) * sh.Hk + hk, wave, which, n, g, lane));
+                const float4 v = *reinterpret_cast<const float4 *>(KeyPart<ND>::at(parts, (u.slot + c) * sh.Hk + hk, wave, n, g, lane));
                 acc[n][4 * g] += v.x, acc[n][4 * g + 1] += v.y, acc[n][4 * g + 2] += v.z, acc[n][4 * g + 3] += v.w;
             }
-    const HeadsOut &to = which ? dv : dk;
-    store_row<ND>(acc, which ? 1.0f : sh.scale, to.p + (long long)(u.row0 + key) * to.ld + hk * sh.d, sh.d, lane, first + (lane & 31) < u.len);
+    const HeadsOut &to = wave & 1 ? dk : dv;
+    store_row<ND>(acc, wave & 1 ? sh.scale : 1.0f, to.p + (long long)(u.row0 + key) * to.ld + hk * sh.d, sh.d, lane, first + (lane & 31) < u.len);
 }
 
 // ---------------------------------------------------------------- host
@@ -673,13 +680,13 @@ inline AttnSizes attn_sizes(int T, int n_seq, int Hq, int Hk, int d)
     const int G = Hq / Hk;
     AttnSizes s;
     s.row_units = (int)((long long)T * G / kRowTile + T / kRowTile) + 2 * n_seq;
-    const long long key_tiles = T / kRowTile + n_seq, most = tiles_of((long long)T * G, kRowStep);
-    // a chunk has at least a 1024th of all heads' steps, and 32: tiles of two or more chunks have at most twice as many as their steps make whole ones
+    const long long key_tiles = T / kKeyRows + n_seq, most = tiles_of((long long)T * G, kRowStep);
+    // a chunk has at least a 1024th of all heads' steps, and 16: tiles of two or more chunks have at most twice as many as their steps make whole ones
     const long long whole = std::min<long long>(2 * kAttnSlots / Hk + 1, key_tiles * most / kMinChunk);
     s.slots = (int)(2 * whole);
     s.joins = (int)std::min<long long>(whole, key_tiles);
-    s.key_units = (int)(2 * key_tiles + 2 * whole);
-    s.part_bytes = round256((size_t)s.slots * Hk * kAttnWaves * 2 * attn_nd(d) * 16 * 64 * sizeof(float));
+    s.key_units = (int)(key_tiles + T / kRowTile + n_seq + 2 * whole);
+    s.part_bytes = round256((size_t)s.slots * Hk * kAttnWaves * attn_nd(d) * 16 * 64 * sizeof(float));
     return s;
 }
 inline size_t attn_list_bytes(int units) { return round256(sizeof(AttnList) + (size_t)units * sizeof(AttnUnit)); }
@@ -789,7 +796,7 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<sz.row_units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, rows, row_units, dqo, lse2, delta)));
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<sz.key_units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, magic, keys, key_units, dko, dvo, parts)));
         if (sz.joins > 0)
-            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<sz.joins * Hk * 2, kAttnThreads, 0, stream>>>(sh, keys, joins, parts, dko, dvo)));
+            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<sz.joins * Hk, kAttnThreads, 0, stream>>>(sh, keys, joins, parts, dko, dvo)));
     });
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
