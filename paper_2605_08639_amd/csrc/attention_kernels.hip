@@ -51,6 +51,13 @@ struct AttnList {
     int count, joins, pad[6];
 };
 
+// At the start of a rare branch: keeps the compiler from turning it into selects that every step pays for.
+__device__ __forceinline__ void rare() { asm volatile(""); }
+
+// Nothing moves across: the order of a step's instructions is written out, fragment reads some products ahead of their use and vector
+// instructions in the shadow of the products before them (left to itself the compiler reads a fragment, waits for it and multiplies).
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // ---------------------------------------------------------------- LDS tiles: [R][W] of 16-bit values, W = 64 or 128
 template <int ND, int R = kKeyTile> struct AttnTile {
     static constexpr int W = ND <= 2 ? 64 : 128;             // ND blocks of 32 columns are used
@@ -159,31 +166,44 @@ __device__ __forceinline__ void tile_barrier()
     asm volatile("" ::: "memory");
 }
 
-// Loads of tiles of 64 consecutive tokens of one head (keys, values).  Rows behind the sequence are its last row again and pieces
-// behind d the last piece: nothing outside of the sequence is read, and what lands there is masked or never stored.
+// Loads of tiles of 64 consecutive tokens of one head (keys, values), one after the other.  Rows behind the sequence are its last row again and
+// pieces behind d the last piece: nothing outside of the sequence is read, and what lands there is masked or never stored.
 template <int ND> struct TokenTiles {
     typedef AttnTile<ND> Tile;
-    const bf16_t *base;                                       // the sequence's first row
-    long long ld;
-    int len, wave, sub, col;
+    const bf16_t *base, *at;                                  // the sequence's first row; (uniform) where this wave's next load starts
+    long long ld, step;                                       // elements to the next row, to the wave's next load
+    int left, sub, col, row;                                  // rows from the next tile on; the lane's row in a load, its column, its row in the first tile
     uint32_t lane_off;
-    __device__ __forceinline__ TokenTiles(const HeadsIn &x, const AttnUnit &u, int head, int d, int wave_, int lane) : ld(x.ld), len(u.len), wave(wave_)
+    __device__ __forceinline__ TokenTiles(const HeadsIn &x, const AttnUnit &u, int head, int d, int wave, int lane) : ld(x.ld), left(u.len)
     {
         base = x.p + (long long)u.row0 * x.ld + (long long)head * d;
+        at = base + (long long)(wave * Tile::RPB) * ld;
+        step = (long long)(kAttnWaves * Tile::RPB) * ld;
         sub = lane / Tile::SPR;
-        const int r = wave * Tile::RPB + sub;                 // the swizzle is the same in all of a wave's loads
-        col = min((lane % Tile::SPR) ^ Tile::swz(r), d / 8 - 1) * 8;
+        row = wave * Tile::RPB + sub;                         // the swizzle is the same in all of a wave's loads
+        col = min((lane % Tile::SPR) ^ Tile::swz(row), d / 8 - 1) * 8;
         lane_off = (uint32_t)(sub * ld + col) * 2u;
     }
-    __device__ __forceinline__ void load(char *lds, int t) const
+    __device__ __forceinline__ void load_next(char *lds, int wave)
     {
-        const int first = t * kKeyTile;
+        lds += wave * 1024;
+        if (left >= kKeyTile) {
 #pragma unroll
-        for (int i = 0; i < Tile::LOADS; ++i) {
-            const int blk = wave + i * kAttnWaves, r = first + blk * Tile::RPB;
-            if (first + kKeyTile <= len) load_lds16_sv(base + (long long)r * ld, lane_off, lds + blk * 1024);
-            else load_lds16(base + (long long)min(r + sub, len - 1) * ld + col, lds + blk * 1024);
+            for (int i = 0; i < Tile::LOADS; ++i) {
+                load_lds16_sv(at, lane_off, lds + i * kAttnWaves * 1024);
+                at += step;
+            }
+        } else {
+            rare();
+#pragma unroll
+            for (int i = 0; i < Tile::LOADS; ++i) {
+                const int over = max(row + i * kAttnWaves * Tile::RPB - (left - 1), 0);      // rows behind the last one
+                const bf16_t *lane_at = at + (long long)(sub - over) * ld + col;
+                load_lds16(lane_at, lds + i * kAttnWaves * 1024);
+                at += step;
+            }
         }
+        left -= kKeyTile;
     }
 };
 
@@ -339,47 +359,60 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *_
 
     const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
     TokenTiles<ND> kt(k, u, hk, d, wave, lane), vt(v, u, hk, d, wave, lane);
-    kt.load(lds, 0);
-    vt.load(lds + 2 * Tile::BYTES, 0);
+    kt.load_next(lds, wave);
     bf16x8_t qf[2 * ND];
     load_row<ND>(qf, q.p + (long long)(u.row0 + tok) * q.ld + head * d, d, lane);
 
     const float c = sh.scale * kLog2e;
     float m = -INFINITY, l = 0.0f;
-    f32x16_t o[ND];
+    f32x16_t o[ND], s[2];
 #pragma unroll
     for (int n = 0; n < ND; ++n) o[n] = zero16();
-    for (int t = 0; t < steps; ++t) {
+    // A step's scores are computed beside the exponentials of the step before: matrix and vector instructions of one wave, independent of each other.
+    // Keys are therefore one step ahead of values.
+    auto step_in = [&](int t) __attribute__((always_inline)) {       // keys of step t + 1 and values of step t are there; the next ones go out
         tile_barrier();
-        const char *keys = lds + (t & 1) * Tile::BYTES, *vals = lds + (2 + (t & 1)) * Tile::BYTES;
-        if (t + 1 < steps) {
-            kt.load(lds + (~t & 1) * Tile::BYTES, t + 1);
-            vt.load(lds + (2 + (~t & 1)) * Tile::BYTES, t + 1);
+        if (t + 2 < steps) kt.load_next(lds + (t & 1) * Tile::BYTES, wave);
+        if (t + 1 < steps) vt.load_next(lds + (2 + (~t & 1)) * Tile::BYTES, wave);
+    };
+    // scores of step t, and beside(kk) vector work for each of the 2 ND pairs of products
+    auto scores = [&](int t, f32x16_t (&to)[2], auto beside) __attribute__((always_inline)) {
+        const uint32_t key_rows = lds_at(lds + (t & 1) * Tile::BYTES, row_lane);
+        constexpr int N = 2 * ND, AHEAD = 2;
+        bf16x8_t f[N][2];
+        auto fetch = [&](int kk) __attribute__((always_inline)) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) f[kk][b] = Tile::rows(key_rows, b * 32, kk);
+        };
+        to[0] = to[1] = zero16();
+#pragma unroll
+        for (int kk = 0; kk < AHEAD; ++kk) fetch(kk);
+#pragma unroll
+        for (int kk = 0; kk < N; ++kk) {
+            if (kk + AHEAD < N) fetch(kk + AHEAD);
+            in_order();
+#pragma unroll
+            for (int b = 0; b < 2; ++b) to[b] = mfma16(f[kk][b], qf[kk], to[b]);
+            beside(kk);
+            in_order();
         }
-        if (t * kKeyTile > wave_hi) continue;                 // all of this wave's rows come before these keys
-        const uint32_t key_rows = lds_at(keys, row_lane), val_cols = lds_at(vals, col_lane);
-        f32x16_t s[2] = {zero16(), zero16()};
-#pragma unroll
-        for (int kk = 0; kk < 2 * ND; ++kk)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = mfma16(Tile::rows(key_rows, b * 32, kk), qf[kk], s[b]);
+    };
+    auto mask = [&](int t, f32x16_t (&x)[2]) __attribute__((always_inline)) {
         if (t * kKeyTile + kKeyTile - 1 > wave_lo) {          // keys behind a row's token
+            rare();
             const int seen = tok - t * kKeyTile - (lane >> 5) * 4;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) s[b][i] = -INFINITY;
+                    if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) x[b][i] = -INFINITY;
         }
-        float top = s[0][0];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = halves_max(top);
-        // The reference value of the exponentials follows the maximum only where it has risen by more than 2^8: the sums then stay below
-        // 2^8 times their count, and most steps need no rescaling.
+    };
+    // The reference value of the exponentials follows the maximum only where it has risen by more than 2^8: the sums then stay below
+    // 2^8 times their count, and most steps need no rescaling.
+    auto follow = [&](float top) __attribute__((always_inline)) {
         if (__any((top - m) * c > 8.0f)) {
+            rare();
             const float m_new = fmaxf(m, top), by = __builtin_amdgcn_exp2f((m - m_new) * c);
             m = m_new;
             l *= by;
@@ -388,23 +421,86 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *_
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[n][i] *= by;
         }
-        const float mc = m * c;
+    };
+    // exponentials number from .. to - 1 of a lane's 32, their sum, and every eight of them as an operand
+    float sum[4];
+    auto exponentials = [&](f32x16_t (&x)[2], bf16x8_t (&p)[4], float mc, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -mc));
-                l += s[b][i];
+        for (int i = from; i < to; ++i) {
+            float &e = reinterpret_cast<float(&)[32]>(x)[i];
+            e = __builtin_amdgcn_exp2f(fmaf(e, c, -mc));
+            sum[i & 3] += e;
+            if ((i & 7) == 7) {
+                p[i >> 3] = pack_half(x[i >> 4], i >> 3 & 1);
+                asm volatile("" : "+v"(p[i >> 3]));           // (here, not put off until the next products)
             }
+        }
+        asm volatile("" : "+v"(sum[0]), "+v"(sum[1]), "+v"(sum[2]), "+v"(sum[3]));
+    };
+    auto weigh = [&](int t, const bf16x8_t (&p)[4], auto beside) __attribute__((always_inline)) {
+        const uint32_t val_cols = lds_at(lds + (2 + (t & 1)) * Tile::BYTES, col_lane);
+        constexpr int N = 4 * ND, AHEAD = 3;
+        bf16x8_t f[N];
+        auto fetch = [&](int i) __attribute__((always_inline)) { f[i] = Tile::cols(val_cols, i % ND * 32, i / ND * 16); };
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int i = 0; i < AHEAD; ++i) fetch(i);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bf16x8_t p = pack_half(s[b], j);
+        for (int i = 0; i < N; ++i) {
+            if (i + AHEAD < N) fetch(i + AHEAD);
+            in_order();
+            o[i % ND] = mfma16(f[i], p[i / ND], o[i % ND]);
+            beside(i);
+            in_order();
+        }
+    };
+    auto nothing = [](int) {};
+
+    tile_barrier();                                           // the first keys
+    if (steps > 1) kt.load_next(lds + Tile::BYTES, wave);
+    vt.load_next(lds + 2 * Tile::BYTES, wave);
+    scores(0, s, nothing);
+    mask(0, s);
+    {
+        float top = s[0][0];
 #pragma unroll
-                for (int n = 0; n < ND; ++n) o[n] = mfma16(Tile::cols(val_cols, n * 32, b * 32 + j * 16), p, o[n]);
-            }
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+        follow(halves_max(top));
     }
+    const int own = wave_hi / kKeyTile;                       // this wave's last step; the block's other waves may have more
+    auto step = [&](int t, f32x16_t (&now)[2], f32x16_t (&next)[2]) __attribute__((always_inline)) {
+        step_in(t);
+        bf16x8_t p[4];
+        const float mc = m * c;
+        sum[0] = l, sum[1] = sum[2] = sum[3] = 0.0f;
+        scores(t + 1, next, [&](int kk) __attribute__((always_inline)) { exponentials(now, p, mc, kk * 16 / ND, (kk + 1) * 16 / ND); });
+        l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        mask(t + 1, next);
+        float top = next[0][0];
+        weigh(t, p, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = i * 8 / ND; e < (i + 1) * 8 / ND; ++e) top = fmaxf(top, next[e >> 4][e & 15]);
+        });
+        follow(halves_max(top));
+    };
+    f32x16_t other[2];
+    int t = 0;
+    for (; t + 1 < own; t += 2) {
+        step(t, s, other);
+        step(t + 1, other, s);
+    }
+    if (t < own) {
+        step(t, s, other);
+        s[0] = other[0], s[1] = other[1];
+    }
+    step_in(own);
+    {
+        bf16x8_t p[4];
+        sum[0] = l, sum[1] = sum[2] = sum[3] = 0.0f;
+        exponentials(s, p, m * c, 0, 32);
+        l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        weigh(own, p, nothing);
+    }
+    for (t = own + 1; t < steps; ++t) step_in(t);
     l = halves_sum(l);
     const bool live = first + (lane & 31) < rows;
     store_row<ND>(o, 1.0f / l, out.p + (long long)(u.row0 + tok) * out.ld + head * d, d, lane, live);
@@ -438,8 +534,8 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
 
     const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
     TokenTiles<ND> kt(k, u, hk, d, wave, lane), vt(v, u, hk, d, wave, lane);
-    kt.load(lds, 0);
-    vt.load(lds + 2 * Tile::BYTES, 0);
+    kt.load_next(lds, wave);
+    vt.load_next(lds + 2 * Tile::BYTES, wave);
     bf16x8_t qf[2 * ND], df[2 * ND];
     load_row<ND>(qf, q.p + (long long)(u.row0 + tok) * q.ld + head * d, d, lane);
     load_row<ND>(df, dout.p + (long long)(u.row0 + tok) * dout.ld + head * d, d, lane);
@@ -464,8 +560,8 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
         tile_barrier();
         const char *keys = lds + (t & 1) * Tile::BYTES, *vals = lds + (2 + (t & 1)) * Tile::BYTES;
         if (t + 1 < steps) {
-            kt.load(lds + (~t & 1) * Tile::BYTES, t + 1);
-            vt.load(lds + (2 + (~t & 1)) * Tile::BYTES, t + 1);
+            kt.load_next(lds + (~t & 1) * Tile::BYTES, wave);
+            vt.load_next(lds + (2 + (~t & 1)) * Tile::BYTES, wave);
         }
         if (t * kKeyTile > wave_hi) continue;
         const bool masked = t * kKeyTile + kKeyTile - 1 > wave_lo;
@@ -481,6 +577,7 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)) * (dp[i] - D);
             if (masked) {
+                rare();
                 // a sequence's first row has one key and a constant softmax: its scores have no gradient (what rounding would leave is not stored)
                 const int seen = (tok > 0 ? tok : -1) - t * kKeyTile - (lane >> 5) * 4;
 #pragma unroll
@@ -597,6 +694,7 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
                 }
             }
             if (r0 < max(pair_last, G) || r0 + kRowStep > rows) {
+                rare();
                 const int base = r0 + role * 32 + (lane >> 5) * 4;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
