@@ -311,8 +311,8 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
                 joins[atomicAdd(&n_joins, 1)] = u;
             }
             for (int c = 0; c < chunks; ++c) {
-                u.from = first + c * chunk;
-                u.to = chunks == 1 ? end : min(u.from + chunk, end);
+                u.to = end - c * chunk;
+                u.from = chunks == 1 ? first : max(u.to - chunk, first);
                 u.slot = chunks > 1 ? slot + c : -1;
                 fn(u, min(u.to - u.from, chunk));
             }
@@ -507,6 +507,27 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *_
     if (live && lane < 32) lse[(long long)(u.row0 + tok) * sh.Hq + head] = (m * c + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// s = rows of x0 times the lanes' f0, dp = rows of x1 times f1; fragments are read two products ahead.
+template <int ND>
+__device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x8_t (&f0)[2 * ND], const bf16x8_t (&f1)[2 * ND], f32x16_t &s, f32x16_t &dp)
+{
+    typedef AttnTile<ND> Tile;                                // (rows lie alike in tiles of any height)
+    constexpr int N = 2 * ND, AHEAD = 2;
+    bf16x8_t a[N][2];
+    auto fetch = [&](int kk) __attribute__((always_inline)) { a[kk][0] = Tile::rows(x0, 0, kk), a[kk][1] = Tile::rows(x1, 0, kk); };
+    s = dp = zero16();
+#pragma unroll
+    for (int kk = 0; kk < AHEAD; ++kk) fetch(kk);
+#pragma unroll
+    for (int kk = 0; kk < N; ++kk) {
+        if (kk + AHEAD < N) fetch(kk + AHEAD);
+        in_order();
+        s = mfma16(a[kk][0], f0[kk], s);
+        dp = mfma16(a[kk][1], f1[kk], dp);
+        in_order();
+    }
+}
+
 // ---------------------------------------------------------------- backward: queries
 // dq of 128 packed rows, and for the other kernel each row's lse in powers of two and D.
 template <int ND>
@@ -568,28 +589,36 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
         const uint32_t key_rows = lds_at(keys, row_lane), val_rows = lds_at(vals, row_lane), key_cols = lds_at(keys, col_lane);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            f32x16_t s = zero16(), dp = zero16();
-#pragma unroll
-            for (int kk = 0; kk < 2 * ND; ++kk) {
-                s = mfma16(Tile::rows(key_rows, b * 32, kk), qf[kk], s);
-                dp = mfma16(Tile::rows(val_rows, b * 32, kk), df[kk], dp);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)) * (dp[i] - D);
+            f32x16_t s, dp;
+            score_pair<ND>(key_rows + b * 32 * Tile::ROW, val_rows + b * 32 * Tile::ROW, qf, df, s, dp);
             if (masked) {
                 rare();
                 // a sequence's first row has one key and a constant softmax: its scores have no gradient (what rounding would leave is not stored)
                 const int seen = (tok > 0 ? tok : -1) - t * kKeyTile - (lane >> 5) * 4;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) s[i] = 0.0f;
+                    if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) s[i] = -INFINITY;
             }
+            bf16x8_t f[ND];
+            auto fetch = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bf16x8_t ds = pack_half(s, j);
+                for (int n = 0; n < ND; ++n) f[n] = Tile::cols(key_cols, n * 32, b * 32 + j * 16);
+            };
+            auto gradients = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-                for (int n = 0; n < ND; ++n) acc[n] = mfma16(Tile::cols(key_cols, n * 32, b * 32 + j * 16), ds, acc[n]);
-            }
+                for (int i = 8 * j; i < 8 * j + 8; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)) * (dp[i] - D);
+                return pack_half(s, j);
+            };
+            fetch(0);
+            const bf16x8_t ds0 = gradients(0);
+            in_order();
+#pragma unroll
+            for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], ds0, acc[n]);
+            const bf16x8_t ds1 = gradients(1);
+            in_order();
+            fetch(1);
+#pragma unroll
+            for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], ds1, acc[n]);
         }
     }
     store_row<ND>(acc, sh.scale, dq.p + (long long)(u.row0 + tok) * dq.ld + head * d, d, lane, live);
@@ -637,25 +666,49 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     const int need = key * G;                                 // this key's first packed row; keys behind the sequence see what its last one sees
     const int pair_first = min(first, u.len - 1) * G, pair_last = min(first + 31, u.len - 1) * G;
 
-    // this wave's loads of a step's packed rows
+    // This wave's loads of a step's packed rows, step after step downwards.  Where groups divide the rows between two loads, every load's rows lie as
+    // those of the load before, so many tokens on: a lane's constant beside a uniform base that moves by a constant.  (Divisions for every load took a
+    // quarter of a step's time.)  Other groups' and the last rows' are worked out lane by lane.
+    constexpr int APART = kAttnWaves * Tile::RPB;
     const int sub = lane / Tile::SPR, col = min((lane % Tile::SPR) ^ Tile::swz(wave * Tile::RPB + sub), d / 8 - 1) * 8;
-    const bf16_t *q0 = q.p + (long long)u.row0 * q.ld + (long long)hk * G * d + col, *d0 = dout.p + (long long)u.row0 * dout.ld + (long long)hk * G * d + col;
-    const float *stat = (wave == 0 ? lse2 : delta) + (long long)u.row0 * sh.Hq + hk * G;
+    const bool alike = APART % G == 0;
+    const int top = u.to * kRowStep - APART + wave * Tile::RPB, top_tok = u.row0 + top / G, col0 = (hk * G + top % G) * d;
+    const bf16_t *q_at = q.p + (long long)top_tok * q.ld + col0, *d_at = dout.p + (long long)top_tok * dout.ld + col0;
+    const long long q_apart = (long long)(APART / G) * q.ld, d_apart = (long long)(APART / G) * dout.ld;
+    const float *stat = wave == 0 ? lse2 : delta, *stat_at = stat + (long long)(u.row0 + ((u.to - 1) * kRowStep + lane) / G) * sh.Hq + hk * G + lane % G;
+    const uint32_t q_off = (uint32_t)((sub / G) * q.ld + sub % G * d + col) * 2u, d_off = (uint32_t)((sub / G) * dout.ld + sub % G * d + col) * 2u;
     auto load = [&](int t, int slot) __attribute__((always_inline)) {
-        char *to = lds + slot * Tile::BYTES;
+        char *to = lds + slot * Tile::BYTES + wave * 1024, *stat_to = lds + STATS + (slot * 2 + wave) * kRowStep * 4;
+        if (alike && t * kRowStep + kRowStep <= rows) {
 #pragma unroll
-        for (int i = 0; i < Tile::LOADS; ++i) {
-            const int blk = wave + i * kAttnWaves, r = min(t * kRowStep + blk * Tile::RPB + sub, rows - 1), tok = token_of(r, magic), g = r - tok * G;
-            load_lds16(q0 + (long long)tok * q.ld + g * d, to + blk * 1024);
-            load_lds16(d0 + (long long)tok * dout.ld + g * d, to + 2 * Tile::BYTES + blk * 1024);
+            for (int i = Tile::LOADS - 1; i >= 0; --i) {
+                load_lds16_sv(q_at, q_off, to + i * kAttnWaves * 1024);
+                load_lds16_sv(d_at, d_off, to + 2 * Tile::BYTES + i * kAttnWaves * 1024);
+                q_at -= q_apart;
+                d_at -= d_apart;
+            }
+            if (wave < 2) load_lds4(stat_at, stat_to);
+        } else {
+            rare();
+            int row0 = u.row0;
+            asm volatile("" : "+s"(row0));                    // (nothing of this branch is kept in registers for it)
+#pragma unroll
+            for (int i = 0; i < Tile::LOADS; ++i) {
+                const int r = min(t * kRowStep + (wave + i * kAttnWaves) * Tile::RPB + sub, rows - 1), tok = token_of(r, magic), c0 = (hk * G + r - tok * G) * d + col;
+                load_lds16(q.p + (long long)(row0 + tok) * q.ld + c0, to + i * kAttnWaves * 1024);
+                load_lds16(dout.p + (long long)(row0 + tok) * dout.ld + c0, to + 2 * Tile::BYTES + i * kAttnWaves * 1024);
+                q_at -= q_apart;
+                d_at -= d_apart;
+            }
+            if (wave < 2) {
+                const int r = min(t * kRowStep + lane, rows - 1), tok = token_of(r, magic);
+                load_lds4(stat + (long long)(row0 + tok) * sh.Hq + hk * G + r - tok * G, stat_to);
+            }
         }
-        if (wave < 2) {
-            const int r = min(t * kRowStep + lane, rows - 1), tok = token_of(r, magic);
-            load_lds4(stat + (long long)tok * sh.Hq + (r - tok * G), lds + STATS + (slot * 2 + wave) * kRowStep * 4);
-        }
+        stat_at -= (long long)(kRowStep / G) * sh.Hq;
     };
     const uint32_t row_lane = Tile::row_lane(lane) + role * 32 * Tile::ROW, col_lane = Tile::col_lane(lane);
-    load(u.from, u.from & 1);
+    load(u.to - 1, (u.to - 1) & 1);
     bf16x8_t kf[2 * ND], vf[2 * ND];
     load_row<ND>(kf, k.p + (long long)(u.row0 + key) * k.ld + hk * d, d, lane);
     load_row<ND>(vf, v.p + (long long)(u.row0 + key) * v.ld + hk * d, d, lane);
@@ -666,64 +719,72 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     for (int n = 0; n < ND; ++n) acc[n] = zero16();
     char *give = lds + TRADE + wave * 2048 + lane * 16;
     const char *take = lds + TRADE + (wave ^ 1) * 2048 + lane * 16;
-    for (int t = u.from; t < u.to; ++t) {
+    // From the last rows to the first: the blocks of a head, which begin at different rows, then read the same ones at about the same time, out of L2.
+    for (int t = u.to - 1; t >= u.from; --t) {
         tile_barrier();
         const int slot = t & 1, r0 = t * kRowStep;
         const char *qs = lds + slot * Tile::BYTES, *ds = qs + 2 * Tile::BYTES;
         const float *ls = reinterpret_cast<const float *>(lds + STATS + slot * 2 * kRowStep * 4) + role * 32, *Ds = ls + kRowStep;
-        if (t + 1 < u.to) load(t + 1, slot ^ 1);
+        if (t > u.from) load(t - 1, slot ^ 1);
         const bool dead = r0 + kRowStep - 1 < pair_first;     // all of these rows come before this pair's keys
-        bf16x8_t mine[2];
+        const uint32_t cols = lds_at(role ? qs : ds, col_lane);
+        bf16x8_t f[ND];
+        auto fetch = [&](int half, int j) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < ND; ++n) f[n] = Tile::cols(cols + half * 32 * Tile::ROW, n * 32, j * 16);
+        };
+        auto add = [&](const bf16x8_t &x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], x, acc[n]);
+        };
         if (!dead) {
-            const uint32_t q_rows = lds_at(qs, row_lane), d_rows = lds_at(ds, row_lane);
-            f32x16_t s = zero16(), dp = zero16();
-#pragma unroll
-            for (int kk = 0; kk < 2 * ND; ++kk) {
-                s = mfma16(Tile::rows(q_rows, 0, kk), kf[kk], s);
-                dp = mfma16(Tile::rows(d_rows, 0, kk), vf[kk], dp);
-            }
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 l4 = *reinterpret_cast<const float4 *>(ls + g * 8 + (lane >> 5) * 4);
-                const float4 D4 = *reinterpret_cast<const float4 *>(Ds + g * 8 + (lane >> 5) * 4);
-                const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, Dv[4] = {D4.x, D4.y, D4.z, D4.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c, -lv[i]));
-                    dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - Dv[i]);
-                }
-            }
+            f32x16_t s, dp;
+            score_pair<ND>(lds_at(qs, row_lane), lds_at(ds, row_lane), kf, vf, s, dp);
             if (r0 < max(pair_last, G) || r0 + kRowStep > rows) {
                 rare();
                 const int base = r0 + role * 32 + (lane >> 5) * 4;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int r = base + (i >> 2) * 8 + (i & 3);
-                    if (r < need || r >= rows) s[i] = dp[i] = 0.0f;
-                    if (r < G) dp[i] = 0.0f;                  // the sequence's first token: one key, no gradient of its scores
+                    if (r < need || r >= rows) s[i] = -INFINITY;
+                    if (r < G) dp[i] = Ds[r - r0 - role * 32];    // the sequence's first token: one key, no gradient of its scores
                 }
             }
+            // exponentials and gradients of 16 rows; the half that this wave adds up, and the other wave's to LDS
+            auto gradients = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+                for (int g = 2 * j; g < 2 * j + 2; ++g) {
+                    const float4 l4 = *reinterpret_cast<const float4 *>(ls + g * 8 + (lane >> 5) * 4);
+                    const float4 D4 = *reinterpret_cast<const float4 *>(Ds + g * 8 + (lane >> 5) * 4);
+                    const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, Dv[4] = {D4.x, D4.y, D4.z, D4.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c, -lv[i]));
+                        dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - Dv[i]);
+                    }
+                }
                 const bf16x8_t p = pack_half(s, j), e = pack_half(dp, j);
-                mine[j] = role ? e : p;
                 *reinterpret_cast<bf16x8_t *>(give + j * 1024) = role ? p : e;
-            }
+                return role ? e : p;
+            };
+            fetch(role, 0);
+            const bf16x8_t x0 = gradients(0);
+            in_order();
+            add(x0);
+            const bf16x8_t x1 = gradients(1);
+            in_order();
+            fetch(role, 1);
+            add(x1);
+            fetch(role ^ 1, 0);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (dead) continue;
-        const uint32_t cols = lds_at(role ? qs : ds, col_lane);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const bf16x8_t theirs = *reinterpret_cast<const bf16x8_t *>(take + j * 1024);
-            const bf16x8_t lo = role ? theirs : mine[j], hi = role ? mine[j] : theirs;
-#pragma unroll
-            for (int n = 0; n < ND; ++n) acc[n] = mfma16(Tile::cols(cols, n * 32, j * 16), lo, acc[n]);
-#pragma unroll
-            for (int n = 0; n < ND; ++n) acc[n] = mfma16(Tile::cols(cols, n * 32, 32 + j * 16), hi, acc[n]);
-        }
+        const bf16x8_t y0 = *reinterpret_cast<const bf16x8_t *>(take), y1 = *reinterpret_cast<const bf16x8_t *>(take + 1024);
+        add(y0);
+        fetch(role ^ 1, 1);
+        add(y1);
     }
     if (u.slot >= 0) {
 #pragma unroll
