@@ -42,8 +42,8 @@ struct HeadsOut {
     bf16_t *p;
     long long ld;
 };
-// One block's work: rows (or keys) tile * 128 .. of the sequence that starts at row0; tile < 0: rows row0 .. row0 + len - 1 are padding.
-// Keys: steps from .. to - 1 of 64 packed rows, into slot `slot` of the partial sums (-1: all there are).
+// One block's work: rows (or keys) tile * 128 (64) .. of the sequence that starts at row0, over steps from .. to - 1 of the keys (of the packed rows), 64
+// each; into slot `slot` of the partial sums, or all there are (-1).  tile < 0: rows row0 .. row0 + len - 1 are padding.
 struct AttnUnit {
     int row0, len, tile, from, to, slot, chunks, pad;
 };
@@ -170,14 +170,13 @@ __device__ __forceinline__ void tile_barrier()
 // pieces behind d the last piece: nothing outside of the sequence is read, and what lands there is masked or never stored.
 template <int ND> struct TokenTiles {
     typedef AttnTile<ND> Tile;
-    const bf16_t *base, *at;                                  // the sequence's first row; (uniform) where this wave's next load starts
+    const bf16_t *at;                                         // (uniform) where this wave's next load starts
     long long ld, step;                                       // elements to the next row, to the wave's next load
     int left, sub, col, row;                                  // rows from the next tile on; the lane's row in a load, its column, its row in the first tile
     uint32_t lane_off;
-    __device__ __forceinline__ TokenTiles(const HeadsIn &x, const AttnUnit &u, int head, int d, int wave, int lane) : ld(x.ld), left(u.len)
+    __device__ __forceinline__ TokenTiles(const HeadsIn &x, const AttnUnit &u, int head, int d, int wave, int lane) : ld(x.ld), left(u.len - u.from * kKeyTile)
     {
-        base = x.p + (long long)u.row0 * x.ld + (long long)head * d;
-        at = base + (long long)(wave * Tile::RPB) * ld;
+        at = x.p + (long long)(u.row0 + u.from * kKeyTile + wave * Tile::RPB) * ld + (long long)head * d;
         step = (long long)(kAttnWaves * Tile::RPB) * ld;
         sub = lane / Tile::SPR;
         row = wave * Tile::RPB + sub;                         // the swizzle is the same in all of a wave's loads
@@ -208,10 +207,13 @@ template <int ND> struct TokenTiles {
 };
 
 // ---------------------------------------------------------------- schedule
-// Lists the blocks' work, heaviest first.  One block: sequences are counted (their rows' or keys' tiles, and the tiles of padding behind
+// Lists the blocks' work, heaviest first: one block for the rows, one for the keys.  Sequences are counted (their tiles, and those of the padding behind
 // them), every thread finds the sequence of its share of the tiles by bisection, and a counting sort by work puts them in order (within a
 // bin in any order: results do not depend on it).  A table that does not ascend within [0, T], or lengths beyond their places: nothing is listed.
-constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinChunk = 16;
+// A tile with more than `chunk` steps is several blocks', whose partial sums a second kernel joins.  Rows: where a fair share of all steps is less than
+// the longest tile's, so that one long tile does not outlast the rest (8 steps at least: a join costs what four do).  Keys: two chunks to each of
+// the blocks that run at once, or one where that leaves few steps.
+constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinRowChunk = 8, kMinKeyChunk = 4, kFullKeyChunk = 16;
 
 __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // inclusive; two barriers
 {
@@ -235,11 +237,18 @@ __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // in
 
 __host__ __device__ inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile); }
 
-template <bool KEYS>
+struct SchedOut {
+    AttnList *head;
+    AttnUnit *units, *joins;
+    int max_units, max_slots;                                 // (max_slots 0: no tile is shared)
+};
+
 __global__ void __launch_bounds__(kSchedThreads)
-attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, int Hk, int max_units, int max_slots,
-                  AttnList *head, AttnUnit *units, AttnUnit *joins, int32_t *err_flag)
+attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, int Hk, SchedOut row_out, SchedOut key_out,
+                  int32_t *err_flag)
 {
+    const bool KEYS = blockIdx.x == 1;
+    const SchedOut to = KEYS ? key_out : row_out;
     __shared__ int before[kAttnMaxSeq + 1];                   // tiles of the sequences before
     __shared__ int bins[kSchedBins], sums[kSchedThreads / 64], n_slots, n_joins;
     __shared__ unsigned long long steps;
@@ -258,10 +267,9 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
             else {
                 const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile);
                 tiles = own + tiles_of(b - a - len, kRowTile);
-                if (KEYS && own) {                             // sum of ceil(len G / 64) - G t over the tiles t
-                    const long long end = tiles_of((long long)len * G, kRowStep);
-                    atomicAdd(&steps, (unsigned long long)(end * own - (long long)(kKeyRows / kRowStep) * G * own * (own - 1) / 2));
-                }
+                // keys: the sum of ceil(len G / 64) - G t over the tiles t;  rows: no less than that of (128 t + 127) / (64 G) + 1
+                const long long n = own;
+                if (own) atomicAdd(&steps, (unsigned long long)(KEYS ? n * tiles_of((long long)len * G, kRowStep) - (long long)G * n * (n - 1) / 2 : n * (n + 1) / G + 1 + n));
             }
         }
         int total;
@@ -271,13 +279,20 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
     }
     if (__syncthreads_or(bad)) {
         if (tid == 0) {
-            head->count = 0, head->joins = 0;
+            to.head->count = 0, to.head->joins = 0;
             atomicOr(err_flag, RELIBRA_ERR_SEQ_TABLE);
         }
         return;
     }
-    const int chunk = KEYS ? (int)max((unsigned long long)kMinChunk, (steps * Hk + 2 * kAttnSlots - 1) / (2 * kAttnSlots)) : 0;
-    const int most = KEYS ? chunk : tiles_of(T, kKeyTile);    // the largest work of a unit
+    const unsigned long long share = (steps * Hk + kAttnSlots - 1) / kAttnSlots;
+    const int longest = KEYS ? tiles_of((long long)T * G, kRowStep) : tiles_of(T, kKeyTile);
+    int chunk = longest;
+    if (to.max_slots > 0) {
+        const unsigned long long want = !KEYS ? max(share, (unsigned long long)kMinRowChunk)
+                                        : share < kFullKeyChunk ? max(share, (unsigned long long)kMinKeyChunk) : max((share + 1) / 2, (unsigned long long)kFullKeyChunk);
+        chunk = (int)min(want, (unsigned long long)longest);
+    }
+    const int most = chunk;                                   // the largest work of a unit
     int shift = 0;
     while ((most >> shift) >= kSchedBins) ++shift;
     // a tile's unit(s) and their work: fn(unit, work)
@@ -297,24 +312,29 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
             u.len = min(kRowTile, b - u.row0);
             u.tile = -1;
             fn(u, 0);
-        } else if (!KEYS) {
-            fn(u, tiles_of(min(((long long)t * kRowTile + kRowTile - 1) / G + 1, (long long)len), kKeyTile));
         } else {
-            const int first = kKeyRows / kRowStep * G * t, end = tiles_of((long long)len * G, kRowStep), n = end - first;
-            int chunks = tiles_of(n, chunk), slot = -1;
+            const int first = KEYS ? G * t : 0;
+            const int end = KEYS ? tiles_of((long long)len * G, kRowStep) : tiles_of(min(((long long)t * kRowTile + kRowTile - 1) / G + 1, (long long)len), kKeyTile);
+            const int chunks = tiles_of(end - first, chunk), per = tiles_of(end - first, chunks);
+            int slot = -1;
             if (chunks > 1 && place) {
                 slot = atomicAdd(&n_slots, chunks);
-                if (slot + chunks > max_slots) slot = -1, chunks = 1;      // (cannot be: max_slots covers the most there are)
-            }
-            if (chunks > 1 && place) {
-                u.slot = slot, u.chunks = chunks;
-                joins[atomicAdd(&n_joins, 1)] = u;
+                if (slot + chunks > to.max_slots) slot = -1;  // (cannot be: max_slots covers the most there are)
+                else {
+                    u.slot = slot, u.chunks = chunks;
+                    to.joins[atomicAdd(&n_joins, 1)] = u;
+                }
             }
             for (int c = 0; c < chunks; ++c) {
-                u.to = end - c * chunk;
-                u.from = chunks == 1 ? first : max(u.to - chunk, first);
-                u.slot = chunks > 1 ? slot + c : -1;
-                fn(u, min(u.to - u.from, chunk));
+                // keys: from the last rows on, so that chunks of one number begin at the same rows
+                u.from = KEYS ? max(end - (c + 1) * per, first) : c * per;
+                u.to = KEYS ? end - c * per : min(u.from + per, end);
+                u.slot = slot < 0 ? -1 : slot + c;
+                if (slot < 0 && place && chunks > 1) {
+                    if (c == 0) u.from = first, u.to = end;
+                    else u.tile = -1, u.len = 0;
+                }
+                fn(u, per);
             }
         }
     };
@@ -328,16 +348,43 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
     for (int f = tid; f < flat; f += kSchedThreads)
         each(f, true, [&](const AttnUnit &u, int work) {
             const int at = atomicAdd(&bins[work >> shift], 1);
-            if (at < max_units) units[at] = u;
+            if (at < to.max_units) to.units[at] = u;
         });
     __syncthreads();
-    if (tid == 0) head->count = min(total, max_units), head->joins = n_joins;
+    if (tid == 0) to.head->count = min(total, to.max_units), to.head->joins = n_joins;
 }
+
+// Partial sums of a unit: registers as they lie, 16 bytes a lane, so that stores are whole lines; and in the forward pass two values a row, behind them.
+template <int ND> struct Part {
+    static constexpr size_t FLOATS = (size_t)kAttnWaves * ND * 16 * 64;
+    static __device__ __forceinline__ float *at(float *parts, int slot, int wave, int n, int quad, int lane)
+    {
+        return parts + (size_t)slot * FLOATS + (((wave * ND + n) * 4 + quad) * 64 + lane) * 4;
+    }
+    static __device__ __forceinline__ void put(float *parts, int slot, int wave, int lane, const f32x16_t (&acc)[ND])
+    {
+#pragma unroll
+        for (int n = 0; n < ND; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4 *>(at(parts, slot, wave, n, g, lane)) = make_float4(acc[n][4 * g], acc[n][4 * g + 1], acc[n][4 * g + 2], acc[n][4 * g + 3]);
+    }
+    // acc += by * the part's columns 32 n ..
+    static __device__ __forceinline__ void add(float *parts, int slot, int wave, int lane, int n, float by, f32x16_t &acc)
+    {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 v = *reinterpret_cast<const float4 *>(at(parts, slot, wave, n, g, lane));
+            acc[4 * g] += by * v.x, acc[4 * g + 1] += by * v.y, acc[4 * g + 2] += by * v.z, acc[4 * g + 3] += by * v.w;
+        }
+    }
+};
 
 // ---------------------------------------------------------------- forward
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
-attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut out, float *__restrict__ lse)
+attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut out, float *__restrict__ lse,
+                float *__restrict__ parts, float2 *__restrict__ sums)
 {
     typedef AttnTile<ND> Tile;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];      // keys and values, two tiles each
@@ -355,11 +402,10 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *_
     const int rows = u.len * G, first = u.tile * kRowTile + wave * 32;         // (this wave's first packed row)
     const int r = min(first + (lane & 31), rows - 1), tok = r / G, head = hk * G + r - tok * G;
     const int wave_lo = min(first, rows - 1) / G, wave_hi = min(first + 31, rows - 1) / G;
-    const int steps = tiles_of(min((u.tile * kRowTile + kRowTile - 1) / G, u.len - 1) + 1, kKeyTile);
 
     const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
     TokenTiles<ND> kt(k, u, hk, d, wave, lane), vt(v, u, hk, d, wave, lane);
-    kt.load_next(lds, wave);
+    kt.load_next(lds + (u.from & 1) * Tile::BYTES, wave);
     bf16x8_t qf[2 * ND];
     load_row<ND>(qf, q.p + (long long)(u.row0 + tok) * q.ld + head * d, d, lane);
 
@@ -372,8 +418,8 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *_
     // Keys are therefore one step ahead of values.
     auto step_in = [&](int t) __attribute__((always_inline)) {       // keys of step t + 1 and values of step t are there; the next ones go out
         tile_barrier();
-        if (t + 2 < steps) kt.load_next(lds + (t & 1) * Tile::BYTES, wave);
-        if (t + 1 < steps) vt.load_next(lds + (2 + (~t & 1)) * Tile::BYTES, wave);
+        if (t + 2 < u.to) kt.load_next(lds + (t & 1) * Tile::BYTES, wave);
+        if (t + 1 < u.to) vt.load_next(lds + (2 + (~t & 1)) * Tile::BYTES, wave);
     };
     // scores of step t, and beside(kk) vector work for each of the 2 ND pairs of products
     auto scores = [&](int t, f32x16_t (&to)[2], auto beside) __attribute__((always_inline)) {
@@ -455,18 +501,6 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *_
     };
     auto nothing = [](int) {};
 
-    tile_barrier();                                           // the first keys
-    if (steps > 1) kt.load_next(lds + Tile::BYTES, wave);
-    vt.load_next(lds + 2 * Tile::BYTES, wave);
-    scores(0, s, nothing);
-    mask(0, s);
-    {
-        float top = s[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-        follow(halves_max(top));
-    }
-    const int own = wave_hi / kKeyTile;                       // this wave's last step; the block's other waves may have more
     auto step = [&](int t, f32x16_t (&now)[2], f32x16_t (&next)[2]) __attribute__((always_inline)) {
         step_in(t);
         bf16x8_t p[4];
@@ -482,29 +516,74 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *_
         });
         follow(halves_max(top));
     };
-    f32x16_t other[2];
-    int t = 0;
-    for (; t + 1 < own; t += 2) {
-        step(t, s, other);
-        step(t + 1, other, s);
-    }
-    if (t < own) {
-        step(t, s, other);
-        s[0] = other[0], s[1] = other[1];
-    }
-    step_in(own);
-    {
+    tile_barrier();                                           // the first keys
+    if (u.from + 1 < u.to) kt.load_next(lds + (~u.from & 1) * Tile::BYTES, wave);
+    vt.load_next(lds + (2 + (u.from & 1)) * Tile::BYTES, wave);
+    const int own = min(wave_hi / kKeyTile, u.to - 1);        // this wave's last step; the block's other waves may have more
+    int t = u.from;
+    if (t <= own) {
+        scores(t, s, nothing);
+        mask(t, s);
+        float top = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+        follow(halves_max(top));
+        f32x16_t other[2];
+        for (; t + 1 < own; t += 2) {
+            step(t, s, other);
+            step(t + 1, other, s);
+        }
+        if (t < own) {
+            step(t, s, other);
+            s[0] = other[0], s[1] = other[1];
+        }
+        step_in(own);
         bf16x8_t p[4];
         sum[0] = l, sum[1] = sum[2] = sum[3] = 0.0f;
         exponentials(s, p, m * c, 0, 32);
         l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
         weigh(own, p, nothing);
+        t = own + 1;
     }
-    for (t = own + 1; t < steps; ++t) step_in(t);
+    for (; t < u.to; ++t) step_in(t);
     l = halves_sum(l);
+    if (u.slot >= 0) {
+        Part<ND>::put(parts, u.slot * sh.Hk + hk, wave, lane, o);
+        if (lane < 32) sums[(u.slot * sh.Hk + hk) * kRowTile + wave * 32 + lane] = make_float2(m * c, l);
+        return;
+    }
     const bool live = first + (lane & 31) < rows;
     store_row<ND>(o, 1.0f / l, out.p + (long long)(u.row0 + tok) * out.ld + head * d, d, lane, live);
     if (live && lane < 32) lse[(long long)(u.row0 + tok) * sh.Hq + head] = (m * c + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Joins the rows whose keys several blocks shared: their sums at one reference value, in ascending order.  A part without keys has the sum 0 at -infinity.
+// 32 columns a block and four parts' loads together: reading one part after the other took longer than the attention (11 us for 4999 rows of 12 heads).
+template <int ND>
+__global__ void __launch_bounds__(kAttnThreads)
+attn_join_out_kernel(AttnShape sh, const AttnList *__restrict__ list, const AttnUnit *__restrict__ joins, float *__restrict__ parts, const float2 *__restrict__ sums, HeadsOut out,
+                     float *__restrict__ lse)
+{
+    const int n = blockIdx.x % ND, tile = blockIdx.x / ND, at = tile / sh.Hk, hk = tile - at * sh.Hk;
+    if (at >= list->joins) return;
+    const AttnUnit u = joins[at];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = u.len * sh.G, first = u.tile * kRowTile + wave * 32;
+    const int r = min(first + (lane & 31), rows - 1), tok = r / sh.G, head = hk * sh.G + r - tok * sh.G;
+    const float2 *mine = sums + (u.slot * sh.Hk + hk) * kRowTile + wave * 32 + (lane & 31);
+    float top = -INFINITY, l = 0.0f;
+#pragma unroll 4
+    for (int c = 0; c < u.chunks; ++c) top = fmaxf(top, mine[c * sh.Hk * kRowTile].x);
+    f32x16_t o[1] = {zero16()};
+#pragma unroll 4
+    for (int c = 0; c < u.chunks; ++c) {
+        const float2 part = mine[c * sh.Hk * kRowTile];
+        const float by = __builtin_amdgcn_exp2f(part.x - top);
+        l += by * part.y;
+        Part<ND>::add(parts, (u.slot + c) * sh.Hk + hk, wave, lane, n, by, o[0]);
+    }
+    const bool live = first + (lane & 31) < rows;
+    store_row<1>(o, 1.0f / l, out.p + (long long)(u.row0 + tok) * out.ld + head * sh.d + n * 32, sh.d - n * 32, lane, live);
+    if (n == 0 && live && lane < 32) lse[(long long)(u.row0 + tok) * sh.Hq + head] = (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // s = rows of x0 times the lanes' f0, dp = rows of x1 times f1; fragments are read two products ahead.
@@ -533,7 +612,7 @@ __device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, const AttnList *__restrict__ list,
-               const AttnUnit *__restrict__ units, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ delta)
+               const AttnUnit *__restrict__ units, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ delta, float *__restrict__ parts)
 {
     typedef AttnTile<ND> Tile;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
@@ -550,13 +629,12 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
     const int rows = u.len * G, first = u.tile * kRowTile + wave * 32;
     const int r = min(first + (lane & 31), rows - 1), tok = r / G, head = hk * G + r - tok * G;
     const int wave_lo = min(first, rows - 1) / G, wave_hi = min(first + 31, rows - 1) / G;
-    const int steps = tiles_of(min((u.tile * kRowTile + kRowTile - 1) / G, u.len - 1) + 1, kKeyTile);
     const bool live = first + (lane & 31) < rows;
 
     const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
     TokenTiles<ND> kt(k, u, hk, d, wave, lane), vt(v, u, hk, d, wave, lane);
-    kt.load_next(lds, wave);
-    vt.load_next(lds + 2 * Tile::BYTES, wave);
+    kt.load_next(lds + (u.from & 1) * Tile::BYTES, wave);
+    vt.load_next(lds + (2 + (u.from & 1)) * Tile::BYTES, wave);
     bf16x8_t qf[2 * ND], df[2 * ND];
     load_row<ND>(qf, q.p + (long long)(u.row0 + tok) * q.ld + head * d, d, lane);
     load_row<ND>(df, dout.p + (long long)(u.row0 + tok) * dout.ld + head * d, d, lane);
@@ -572,15 +650,15 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
     }
     const long long place = (long long)(u.row0 + tok) * sh.Hq + head;
     const float l2 = lse[place] * kLog2e, c = sh.scale * kLog2e;
-    if (live && lane < 32) lse2[place] = l2, delta[place] = D;
+    if (live && lane < 32 && u.from == 0) lse2[place] = l2, delta[place] = D;
 
     f32x16_t acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; ++n) acc[n] = zero16();
-    for (int t = 0; t < steps; ++t) {
+    for (int t = u.from; t < u.to; ++t) {
         tile_barrier();
         const char *keys = lds + (t & 1) * Tile::BYTES, *vals = lds + (2 + (t & 1)) * Tile::BYTES;
-        if (t + 1 < steps) {
+        if (t + 1 < u.to) {
             kt.load_next(lds + (~t & 1) * Tile::BYTES, wave);
             vt.load_next(lds + (2 + (~t & 1)) * Tile::BYTES, wave);
         }
@@ -621,19 +699,14 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
             for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], ds1, acc[n]);
         }
     }
+    if (u.slot >= 0) {
+        Part<ND>::put(parts, u.slot * sh.Hk + hk, wave, lane, acc);
+        return;
+    }
     store_row<ND>(acc, sh.scale, dq.p + (long long)(u.row0 + tok) * dq.ld + head * d, d, lane, live);
 }
 
 // ---------------------------------------------------------------- backward: keys and values
-// Partial sums of a unit: registers as they lie, 16 bytes a lane, so that stores are whole lines.
-template <int ND> struct KeyPart {
-    static constexpr size_t FLOATS = (size_t)kAttnWaves * ND * 16 * 64;
-    static __device__ __forceinline__ float *at(float *parts, int slot, int wave, int n, int quad, int lane)
-    {
-        return parts + (size_t)slot * FLOATS + (((wave * ND + n) * 4 + quad) * 64 + lane) * 4;
-    }
-};
-
 // r / G: for r < 2^26 and G <= 64 the upper half of r * ceil(2^32 / G), whose excess over r / G, below r / 2^32 < 1 / G, never reaches the next integer.
 inline unsigned token_magic(int G) { return G == 1 ? 0u : (unsigned)(((1ull << 32) + G - 1) / G); }
 __device__ __forceinline__ int token_of(int r, unsigned magic) { return magic ? (int)__umulhi((unsigned)r, magic) : r; }
@@ -787,39 +860,31 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
         add(y1);
     }
     if (u.slot >= 0) {
-#pragma unroll
-        for (int n = 0; n < ND; ++n)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<float4 *>(KeyPart<ND>::at(parts, u.slot * sh.Hk + hk, wave, n, g, lane)) = make_float4(acc[n][4 * g], acc[n][4 * g + 1], acc[n][4 * g + 2], acc[n][4 * g + 3]);
+        Part<ND>::put(parts, u.slot * sh.Hk + hk, wave, lane, acc);
         return;
     }
     const HeadsOut &to = role ? dk : dv;
     store_row<ND>(acc, role ? sh.scale : 1.0f, to.p + (long long)(u.row0 + key) * to.ld + hk * d, d, lane, first + (lane & 31) < u.len);
 }
 
-// Adds up the partial sums of the tiles whose rows several blocks shared, in ascending order.
+// Adds up the partial sums of the tiles that several blocks shared, in ascending order: those of rows, behind row_joins tiles' those of keys.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads)
-attn_join_kernel(AttnShape sh, const AttnList *__restrict__ list, const AttnUnit *__restrict__ joins, float *__restrict__ parts, HeadsOut dk, HeadsOut dv)
+attn_join_kernel(AttnShape sh, int row_joins, const AttnList *__restrict__ rows, const AttnUnit *__restrict__ row_units, float *__restrict__ row_parts, HeadsOut dq,
+                 const AttnList *__restrict__ keys, const AttnUnit *__restrict__ key_units, float *__restrict__ key_parts, HeadsOut dk, HeadsOut dv)
 {
-    const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
-    if (at >= list->joins) return;
-    const AttnUnit u = joins[at];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = u.tile * kKeyRows + (wave >> 1) * 32, key = min(first + (lane & 31), u.len - 1);
-    f32x16_t acc[ND];
-#pragma unroll
-    for (int n = 0; n < ND; ++n) acc[n] = zero16();
-    for (int c = 0; c < u.chunks; ++c)
-#pragma unroll
-        for (int n = 0; n < ND; ++n)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 v = *reinterpret_cast<const float4 *>(KeyPart<ND>::at(parts, (u.slot + c) * sh.Hk + hk, wave, n, g, lane));
-                acc[n][4 * g] += v.x, acc[n][4 * g + 1] += v.y, acc[n][4 * g + 2] += v.z, acc[n][4 * g + 3] += v.w;
-            }
-    const HeadsOut &to = wave & 1 ? dk : dv;
-    store_row<ND>(acc, wave & 1 ? sh.scale : 1.0f, to.p + (long long)(u.row0 + key) * to.ld + hk * sh.d, sh.d, lane, first + (lane & 31) < u.len);
+    const int n = blockIdx.x % ND, block = blockIdx.x / ND, tile = block / sh.Hk, hk = block - tile * sh.Hk, of_keys = tile >= row_joins, at = of_keys ? tile - row_joins : tile;
+    if (at >= (of_keys ? keys : rows)->joins) return;
+    const AttnUnit u = (of_keys ? key_units : row_units)[at];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float *parts = of_keys ? key_parts : row_parts;
+    f32x16_t acc[1] = {zero16()};
+#pragma unroll 4
+    for (int c = 0; c < u.chunks; ++c) Part<ND>::add(parts, (u.slot + c) * sh.Hk + hk, wave, lane, n, 1.0f, acc[0]);
+    const int first = of_keys ? u.tile * kKeyRows + (wave >> 1) * 32 : u.tile * kRowTile + wave * 32, count = of_keys ? u.len : u.len * sh.G;
+    const int mine = min(first + (lane & 31), count - 1), tok = of_keys ? mine : mine / sh.G, head = of_keys ? hk : hk * sh.G + mine - tok * sh.G;
+    const HeadsOut &to = !of_keys ? dq : wave & 1 ? dk : dv;
+    store_row<1>(acc, of_keys && !(wave & 1) ? 1.0f : sh.scale, to.p + (long long)(u.row0 + tok) * to.ld + head * sh.d + n * 32, sh.d - n * 32, lane, first + (lane & 31) < count);
 }
 
 // ---------------------------------------------------------------- host
@@ -828,38 +893,55 @@ inline bool attn_takes(int T, int n_seq, int Hq, int Hk, int d)
     return d % 8 == 0 && d <= kAttnMaxDim && n_seq <= kAttnMaxSeq && Hq / Hk <= kAttnMaxGroup && Hq <= 4096 && (long long)T * (Hq / Hk) <= kAttnMaxRows;
 }
 inline int attn_nd(int d) { return (d + 31) / 32; }
-// Lists: at most so many units of rows, units of keys, joined tiles and partial sums a key head; places of padding are at most a tile a sequence more
-// than the rows they take.
+// Lists: at most so many units, joined tiles and partial sums a key head, for rows and for keys; places of padding are at most a tile a sequence more than
+// the rows they take.  A chunk has at least a fair share's worth (half of it: keys) of all heads' steps, and a least number of them; tiles of two or
+// more chunks have at most twice as many as their steps make whole ones.
 struct AttnSizes {
-    int row_units, key_units, joins, slots;
+    int units, joins, slots;
     size_t part_bytes;
+    size_t list_bytes() const { return round256(sizeof(AttnList) + (size_t)(units + joins) * sizeof(AttnUnit)); }
 };
-inline AttnSizes attn_sizes(int T, int n_seq, int Hq, int Hk, int d)
+inline AttnSizes attn_sizes(long long tiles, long long most, long long whole, int min_chunk, int T, int n_seq, int Hk, int d)
 {
-    const int G = Hq / Hk;
     AttnSizes s;
-    s.row_units = (int)((long long)T * G / kRowTile + T / kRowTile) + 2 * n_seq;
-    const long long key_tiles = T / kKeyRows + n_seq, most = tiles_of((long long)T * G, kRowStep);
-    // a chunk has at least a 1024th of all heads' steps, and 16: tiles of two or more chunks have at most twice as many as their steps make whole ones
-    const long long whole = std::min<long long>(2 * kAttnSlots / Hk + 1, key_tiles * most / kMinChunk);
+    whole = std::min(whole, tiles * most / min_chunk);
+    s.joins = (int)std::min(whole, tiles);
     s.slots = (int)(2 * whole);
-    s.joins = (int)std::min<long long>(whole, key_tiles);
-    s.key_units = (int)(key_tiles + T / kRowTile + n_seq + 2 * whole);
+    s.units = (int)(tiles + T / kRowTile + n_seq + 2 * whole);
     s.part_bytes = round256((size_t)s.slots * Hk * kAttnWaves * attn_nd(d) * 16 * 64 * sizeof(float));
     return s;
 }
-inline size_t attn_list_bytes(int units) { return round256(sizeof(AttnList) + (size_t)units * sizeof(AttnUnit)); }
+// Rows of more than 2^18 heads and tokens have several times the tiles that run at once: none is shared.
+inline AttnSizes row_sizes(int T, int n_seq, int Hq, int Hk, int d)
+{
+    const int G = Hq / Hk, most = tiles_of(T, kKeyTile);
+    const bool share = most > kMinRowChunk && (long long)T * Hq < 1 << 18;
+    return attn_sizes((long long)T * G / kRowTile + n_seq, most, share ? kAttnSlots / Hk + 1 : 0, kMinRowChunk, T, n_seq, Hk, d);
+}
+inline AttnSizes key_sizes(int T, int n_seq, int Hq, int Hk, int d)
+{
+    return attn_sizes(T / kKeyRows + n_seq, tiles_of((long long)T * (Hq / Hk), kRowStep), 2 * kAttnSlots / Hk + 1, kMinKeyChunk, T, n_seq, Hk, d);
+}
+inline size_t row_sum_bytes(const AttnSizes &s, int Hk) { return round256((size_t)s.slots * Hk * kRowTile * sizeof(float2)); }
 size_t attn_fwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
 {
     if (T < 0 || n_seq < 0 || Hk < 1 || Hq < 1 || Hq % Hk || d < 8 || !attn_takes(T, n_seq, Hq, Hk, d)) return 0;
-    return attn_list_bytes(attn_sizes(T, n_seq, Hq, Hk, d).row_units);
+    const AttnSizes s = row_sizes(T, n_seq, Hq, Hk, d);
+    return s.list_bytes() + s.part_bytes + row_sum_bytes(s, Hk);
 }
 size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
 {
-    const size_t fwd = attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d);
-    if (!fwd) return 0;
-    const AttnSizes s = attn_sizes(T, n_seq, Hq, Hk, d);
-    return fwd + attn_list_bytes(s.key_units + s.joins) + 2 * round256((size_t)T * Hq * sizeof(float)) + s.part_bytes;
+    if (!attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return 0;
+    const AttnSizes r = row_sizes(T, n_seq, Hq, Hk, d), k = key_sizes(T, n_seq, Hq, Hk, d);
+    return r.list_bytes() + r.part_bytes + k.list_bytes() + k.part_bytes + 2 * round256((size_t)T * Hq * sizeof(float));
+}
+// A list in the workspace, and the next free byte behind it.
+inline SchedOut sched_out(char *&ws, const AttnSizes &s)
+{
+    AttnList *head = (AttnList *)ws;
+    AttnUnit *units = (AttnUnit *)(head + 1);
+    ws += s.list_bytes();
+    return SchedOut{head, units, units + s.units, s.units, s.slots};
 }
 inline int check_attn(const int32_t *seq_start, int n_seq, int T, int Hq, int Hk, int d, float scale, const int32_t *err_flag)
 {
@@ -896,16 +978,20 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
         if (!x.usable() || x.overlaps(to, T)) return RELIBRA_EINVAL;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     if (!workspace || workspace_bytes < attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
-    const AttnSizes sz = attn_sizes(T, n_seq, Hq, Hk, d);
-    AttnList *list = (AttnList *)workspace;
-    AttnUnit *units = (AttnUnit *)(list + 1);
+    const AttnSizes sz = row_sizes(T, n_seq, Hq, Hk, d);
+    char *ws = (char *)workspace;
+    const SchedOut rows = sched_out(ws, sz);
+    float *parts = (float *)ws;
+    float2 *sums = (float2 *)(ws + sz.part_bytes);
     const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
-    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<false><<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, sz.row_units, 0, list, units,
-                                                                                                           nullptr, err_flag));
+    const HeadsOut oo{(bf16_t *)out, out_stride};
+    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, rows, err_flag));
     attn_layout(d, [&](auto nd) {
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_FWD, stream, (attn_fwd_kernel<decltype(nd)::value><<<sz.row_units * Hk, kAttnThreads, 0, stream>>>(
-            sh, HeadsIn{(const bf16_t *)q, q_stride}, HeadsIn{(const bf16_t *)k, k_stride}, HeadsIn{(const bf16_t *)v, v_stride}, list, units,
-            HeadsOut{(bf16_t *)out, out_stride}, lse)));
+        constexpr int ND = decltype(nd)::value;
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_FWD, stream, (attn_fwd_kernel<ND><<<sz.units * Hk, kAttnThreads, 0, stream>>>(
+            sh, HeadsIn{(const bf16_t *)q, q_stride}, HeadsIn{(const bf16_t *)k, k_stride}, HeadsIn{(const bf16_t *)v, v_stride}, rows.head, rows.units, oo, lse, parts, sums)));
+        if (sz.joins > 0)
+            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_out_kernel<ND><<<sz.joins * Hk * ND, kAttnThreads, 0, stream>>>(sh, rows.head, rows.joins, parts, sums, oo, lse)));
     });
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
@@ -934,28 +1020,24 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
     }
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     if (!workspace || workspace_bytes < attn_bwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
-    const AttnSizes sz = attn_sizes(T, n_seq, Hq, Hk, d);
+    const AttnSizes rs = row_sizes(T, n_seq, Hq, Hk, d), ks = key_sizes(T, n_seq, Hq, Hk, d);
     char *ws = (char *)workspace;
-    AttnList *rows = (AttnList *)ws, *keys = (AttnList *)(ws += attn_list_bytes(sz.row_units));
-    float *lse2 = (float *)(ws += attn_list_bytes(sz.key_units + sz.joins));
-    float *delta = (float *)(ws += round256((size_t)T * Hq * sizeof(float)));
-    float *parts = (float *)(ws += round256((size_t)T * Hq * sizeof(float)));
-    AttnUnit *row_units = (AttnUnit *)(rows + 1), *key_units = (AttnUnit *)(keys + 1), *joins = key_units + sz.key_units;
+    const SchedOut rows = sched_out(ws, rs), keys = sched_out(ws, ks);
+    float *row_parts = (float *)ws, *key_parts = (float *)(ws += rs.part_bytes);
+    float *lse2 = (float *)(ws += ks.part_bytes), *delta = (float *)(ws + round256((size_t)T * Hq * sizeof(float)));
     const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
     const HeadsIn qi{(const bf16_t *)q, q_stride}, ki{(const bf16_t *)k, k_stride}, vi{(const bf16_t *)v, v_stride}, oi{(const bf16_t *)out, out_stride},
         di{(const bf16_t *)dout, dout_stride};
     const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
     const unsigned magic = token_magic(sh.G);
-    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<false><<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, sz.row_units, 0, rows,
-                                                                                                           row_units, nullptr, err_flag));
-    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<true><<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, sz.key_units, sz.slots, keys,
-                                                                                                          key_units, joins, err_flag));
+    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<2, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, keys, err_flag));
     attn_layout(d, [&](auto nd) {
         constexpr int ND = decltype(nd)::value;
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<sz.row_units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, rows, row_units, dqo, lse2, delta)));
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<sz.key_units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, magic, keys, key_units, dko, dvo, parts)));
-        if (sz.joins > 0)
-            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<sz.joins * Hk, kAttnThreads, 0, stream>>>(sh, keys, joins, parts, dko, dvo)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, rows.head, rows.units, dqo, lse2, delta, row_parts)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, magic, keys.head, keys.units, dko, dvo, key_parts)));
+        if (rs.joins + ks.joins > 0)
+            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<(rs.joins + ks.joins) * Hk * ND, kAttnThreads, 0, stream>>>(
+                sh, rs.joins, rows.head, rows.joins, row_parts, dqo, keys.head, keys.joins, key_parts, dko, dvo)));
     });
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
