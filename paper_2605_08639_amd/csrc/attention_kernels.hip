@@ -249,7 +249,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
 {
     const bool KEYS = blockIdx.x == 1;
     const SchedOut to = KEYS ? key_out : row_out;
-    __shared__ int before[kAttnMaxSeq + 1];                   // tiles of the sequences before
+    __shared__ int before[kAttnMaxSeq + 1], starts[kAttnMaxSeq + 1], lens[kAttnMaxSeq];       // tiles of the sequences before; the tables
     __shared__ int bins[kSchedBins], sums[kSchedThreads / 64], n_slots, n_joins;
     __shared__ unsigned long long steps;
     const int tid = threadIdx.x;
@@ -263,6 +263,8 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
         int tiles = 0;
         if (s < n_seq) {
             const int a = seq_start[s], b = seq_start[s + 1], len = seq_len ? seq_len[s] : b - a;
+            starts[s] = a, lens[s] = len;
+            if (s == n_seq - 1) starts[n_seq] = b;
             if (a < 0 || b < a || b > T || len < 0 || len > b - a) bad = true;
             else {
                 const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile);
@@ -303,7 +305,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
             if (before[mid] <= f) lo = mid;
             else hi = mid;
         }
-        const int a = seq_start[lo], b = seq_start[lo + 1], len = seq_len ? seq_len[lo] : b - a;
+        const int a = starts[lo], b = starts[lo + 1], len = lens[lo];
         int t = f - before[lo];
         const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile);
         AttnUnit u{a, len, t, 0, 0, -1, 1, 0};
@@ -586,15 +588,15 @@ attn_join_out_kernel(AttnShape sh, const AttnList *__restrict__ list, const Attn
     if (n == 0 && live && lane < 32) lse[(long long)(u.row0 + tok) * sh.Hq + head] = (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// s = rows of x0 times the lanes' f0, dp = rows of x1 times f1; fragments are read two products ahead.
+// s = rows of x0 times the lanes' f0, dp = rows of x1 times f1 plus what `start` has (-D: a subtraction a value less); fragments are read two products ahead.
 template <int ND>
-__device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x8_t (&f0)[2 * ND], const bf16x8_t (&f1)[2 * ND], f32x16_t &s, f32x16_t &dp)
+__device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x8_t (&f0)[2 * ND], const bf16x8_t (&f1)[2 * ND], const f32x16_t &start, f32x16_t &s, f32x16_t &dp)
 {
     typedef AttnTile<ND> Tile;                                // (rows lie alike in tiles of any height)
     constexpr int N = 2 * ND, AHEAD = 2;
     bf16x8_t a[N][2];
     auto fetch = [&](int kk) __attribute__((always_inline)) { a[kk][0] = Tile::rows(x0, 0, kk), a[kk][1] = Tile::rows(x1, 0, kk); };
-    s = dp = zero16();
+    s = zero16();
 #pragma unroll
     for (int kk = 0; kk < AHEAD; ++kk) fetch(kk);
 #pragma unroll
@@ -602,17 +604,17 @@ __device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x
         if (kk + AHEAD < N) fetch(kk + AHEAD);
         in_order();
         s = mfma16(a[kk][0], f0[kk], s);
-        dp = mfma16(a[kk][1], f1[kk], dp);
+        dp = mfma16(a[kk][1], f1[kk], kk ? dp : start);
         in_order();
     }
 }
 
 // ---------------------------------------------------------------- backward: queries
-// dq of 128 packed rows, and for the other kernel each row's lse in powers of two and D.
+// dq of 128 packed rows, and for the other kernel each row's lse in powers of two and -D.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, const AttnList *__restrict__ list,
-               const AttnUnit *__restrict__ units, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ delta, float *__restrict__ parts)
+               const AttnUnit *__restrict__ units, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ minus_delta, float *__restrict__ parts)
 {
     typedef AttnTile<ND> Tile;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
@@ -650,7 +652,10 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
     }
     const long long place = (long long)(u.row0 + tok) * sh.Hq + head;
     const float l2 = lse[place] * kLog2e, c = sh.scale * kLog2e;
-    if (live && lane < 32 && u.from == 0) lse2[place] = l2, delta[place] = D;
+    if (live && lane < 32 && u.from == 0) lse2[place] = l2, minus_delta[place] = -D;
+    f32x16_t minus_D;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) minus_D[i] = -D;
 
     f32x16_t acc[ND];
 #pragma unroll
@@ -668,7 +673,7 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             f32x16_t s, dp;
-            score_pair<ND>(key_rows + b * 32 * Tile::ROW, val_rows + b * 32 * Tile::ROW, qf, df, s, dp);
+            score_pair<ND>(key_rows + b * 32 * Tile::ROW, val_rows + b * 32 * Tile::ROW, qf, df, minus_D, s, dp);
             if (masked) {
                 rare();
                 // a sequence's first row has one key and a constant softmax: its scores have no gradient (what rounding would leave is not stored)
@@ -684,7 +689,7 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
             };
             auto gradients = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 8 * j; i < 8 * j + 8; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)) * (dp[i] - D);
+                for (int i = 8 * j; i < 8 * j + 8; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)) * dp[i];
                 return pack_half(s, j);
             };
             fetch(0);
@@ -716,12 +721,12 @@ __device__ __forceinline__ int token_of(int r, unsigned magic) { return magic ? 
 // 128 registers beside the operands' 64 and the scores' 32, and leave no room for a second wave on its SIMD.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
-attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ delta, unsigned magic,
+attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ minus_delta, unsigned magic,
                 const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut dk, HeadsOut dv, float *__restrict__ parts)
 {
     typedef AttnTile<ND, kRowStep> Tile;
     constexpr int STATS = 4 * Tile::BYTES, TRADE = STATS + 4 * kRowStep * 4;
-    // queries and their upstream, two steps each; the rows' lse and D, two steps each; what the waves of a pair hand each other
+    // queries and their upstream, two steps each; the rows' lse and -D, two steps each; what the waves of a pair hand each other
     __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves * 2048];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     if (at >= list->count) return;
@@ -748,7 +753,7 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     const int top = u.to * kRowStep - APART + wave * Tile::RPB, top_tok = u.row0 + top / G, col0 = (hk * G + top % G) * d;
     const bf16_t *q_at = q.p + (long long)top_tok * q.ld + col0, *d_at = dout.p + (long long)top_tok * dout.ld + col0;
     const long long q_apart = (long long)(APART / G) * q.ld, d_apart = (long long)(APART / G) * dout.ld;
-    const float *stat = wave == 0 ? lse2 : delta, *stat_at = stat + (long long)(u.row0 + ((u.to - 1) * kRowStep + lane) / G) * sh.Hq + hk * G + lane % G;
+    const float *stat = wave == 0 ? lse2 : minus_delta, *stat_at = stat + (long long)(u.row0 + ((u.to - 1) * kRowStep + lane) / G) * sh.Hq + hk * G + lane % G;
     const uint32_t q_off = (uint32_t)((sub / G) * q.ld + sub % G * d + col) * 2u, d_off = (uint32_t)((sub / G) * dout.ld + sub % G * d + col) * 2u;
     auto load = [&](int t, int slot) __attribute__((always_inline)) {
         char *to = lds + slot * Tile::BYTES + wave * 1024, *stat_to = lds + STATS + (slot * 2 + wave) * kRowStep * 4;
@@ -793,72 +798,81 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     char *give = lds + TRADE + wave * 2048 + lane * 16;
     const char *take = lds + TRADE + (wave ^ 1) * 2048 + lane * 16;
     // From the last rows to the first: the blocks of a head, which begin at different rows, then read the same ones at about the same time, out of L2.
-    for (int t = u.to - 1; t >= u.from; --t) {
-        tile_barrier();
-        const int slot = t & 1, r0 = t * kRowStep;
-        const char *qs = lds + slot * Tile::BYTES, *ds = qs + 2 * Tile::BYTES;
-        const float *ls = reinterpret_cast<const float *>(lds + STATS + slot * 2 * kRowStep * 4) + role * 32, *Ds = ls + kRowStep;
-        if (t > u.from) load(t - 1, slot ^ 1);
-        const bool dead = r0 + kRowStep - 1 < pair_first;     // all of these rows come before this pair's keys
-        const uint32_t cols = lds_at(role ? qs : ds, col_lane);
-        bf16x8_t f[ND];
-        auto fetch = [&](int half, int j) __attribute__((always_inline)) {
+    auto walk = [&](auto which) __attribute__((always_inline)) {
+        constexpr int ROLE = decltype(which)::value;
+        for (int t = u.to - 1; t >= u.from; --t) {
+            tile_barrier();
+            const int slot = t & 1, r0 = t * kRowStep;
+            const char *qs = lds + slot * Tile::BYTES, *ds = qs + 2 * Tile::BYTES;
+            const float *ls = reinterpret_cast<const float *>(lds + STATS + slot * 2 * kRowStep * 4) + ROLE * 32 + (lane >> 5) * 4, *Ds = ls + kRowStep;
+            if (t > u.from) load(t - 1, slot ^ 1);
+            const bool dead = r0 + kRowStep - 1 < pair_first; // all of these rows come before this pair's keys
+            const uint32_t cols = lds_at(ROLE ? qs : ds, col_lane);
+            bf16x8_t f[ND];
+            auto fetch = [&](int half, int j) __attribute__((always_inline)) {
 #pragma unroll
-            for (int n = 0; n < ND; ++n) f[n] = Tile::cols(cols + half * 32 * Tile::ROW, n * 32, j * 16);
-        };
-        auto add = [&](const bf16x8_t &x) __attribute__((always_inline)) {
+                for (int n = 0; n < ND; ++n) f[n] = Tile::cols(cols + half * 32 * Tile::ROW, n * 32, j * 16);
+            };
+            auto add = [&](const bf16x8_t &x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], x, acc[n]);
-        };
-        if (!dead) {
-            f32x16_t s, dp;
-            score_pair<ND>(lds_at(qs, row_lane), lds_at(ds, row_lane), kf, vf, s, dp);
-            if (r0 < max(pair_last, G) || r0 + kRowStep > rows) {
-                rare();
-                const int base = r0 + role * 32 + (lane >> 5) * 4;
+                for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], x, acc[n]);
+            };
+            if (!dead) {
+                f32x16_t s, dp, minus_D;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int r = base + (i >> 2) * 8 + (i & 3);
-                    if (r < need || r >= rows) s[i] = -INFINITY;
-                    if (r < G) dp[i] = Ds[r - r0 - role * 32];    // the sequence's first token: one key, no gradient of its scores
+                for (int g = 0; g < 4; ++g) {
+                    const float4 D4 = *reinterpret_cast<const float4 *>(Ds + g * 8);
+                    minus_D[4 * g] = D4.x, minus_D[4 * g + 1] = D4.y, minus_D[4 * g + 2] = D4.z, minus_D[4 * g + 3] = D4.w;
                 }
-            }
-            // exponentials and gradients of 16 rows; the half that this wave adds up, and the other wave's to LDS
-            auto gradients = [&](int j) __attribute__((always_inline)) {
+                score_pair<ND>(lds_at(qs, row_lane), lds_at(ds, row_lane), kf, vf, minus_D, s, dp);
+                if (r0 < max(pair_last, G) || r0 + kRowStep > rows) {
+                    rare();
+                    const int base = r0 + ROLE * 32 + (lane >> 5) * 4;
 #pragma unroll
-                for (int g = 2 * j; g < 2 * j + 2; ++g) {
-                    const float4 l4 = *reinterpret_cast<const float4 *>(ls + g * 8 + (lane >> 5) * 4);
-                    const float4 D4 = *reinterpret_cast<const float4 *>(Ds + g * 8 + (lane >> 5) * 4);
-                    const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, Dv[4] = {D4.x, D4.y, D4.z, D4.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c, -lv[i]));
-                        dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - Dv[i]);
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = base + (i >> 2) * 8 + (i & 3);
+                        if (r < need || r >= rows) s[i] = -INFINITY;
+                        if (r < G) dp[i] = 0.0f;              // the sequence's first token: one key, no gradient of its scores
                     }
                 }
-                const bf16x8_t p = pack_half(s, j), e = pack_half(dp, j);
-                *reinterpret_cast<bf16x8_t *>(give + j * 1024) = role ? p : e;
-                return role ? e : p;
-            };
-            fetch(role, 0);
-            const bf16x8_t x0 = gradients(0);
-            in_order();
-            add(x0);
-            const bf16x8_t x1 = gradients(1);
-            in_order();
-            fetch(role, 1);
-            add(x1);
-            fetch(role ^ 1, 0);
+                // exponentials and gradients of 16 rows; the half that this wave adds up, and the other wave's to LDS
+                auto gradients = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int g = 2 * j; g < 2 * j + 2; ++g) {
+                        const float4 l4 = *reinterpret_cast<const float4 *>(ls + g * 8);
+                        const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c, -lv[i]));
+                            dp[4 * g + i] *= s[4 * g + i];
+                        }
+                    }
+                    const bf16x8_t p = pack_half(s, j), e = pack_half(dp, j);
+                    *reinterpret_cast<bf16x8_t *>(give + j * 1024) = ROLE ? p : e;
+                    return ROLE ? e : p;
+                };
+                fetch(ROLE, 0);
+                const bf16x8_t x0 = gradients(0);
+                in_order();
+                add(x0);
+                const bf16x8_t x1 = gradients(1);
+                in_order();
+                fetch(ROLE, 1);
+                add(x1);
+                fetch(ROLE ^ 1, 0);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (dead) continue;
+            const bf16x8_t y0 = *reinterpret_cast<const bf16x8_t *>(take), y1 = *reinterpret_cast<const bf16x8_t *>(take + 1024);
+            add(y0);
+            fetch(ROLE ^ 1, 1);
+            add(y1);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (dead) continue;
-        const bf16x8_t y0 = *reinterpret_cast<const bf16x8_t *>(take), y1 = *reinterpret_cast<const bf16x8_t *>(take + 1024);
-        add(y0);
-        fetch(role ^ 1, 1);
-        add(y1);
-    }
+    };
+    if (role) walk(std::integral_constant<int, 1>{});
+    else walk(std::integral_constant<int, 0>{});
     if (u.slot >= 0) {
         Part<ND>::put(parts, u.slot * sh.Hk + hk, wave, lane, acc);
         return;
