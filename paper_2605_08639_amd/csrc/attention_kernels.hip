@@ -46,6 +46,10 @@ struct HeadsOut {
 // each; into slot `slot` of the partial sums, or all there are (-1).  tile < 0: rows row0 .. row0 + len - 1 are padding.
 struct AttnUnit {
     int row0, len, tile, from, to, slot, chunks, pad;
+    __device__ __forceinline__ void make_uniform()            // (the same in every lane: scalars from here on)
+    {
+        for (int *x : {&row0, &len, &tile, &from, &to, &slot, &chunks}) *x = __builtin_amdgcn_readfirstlane(*x);
+    }
 };
 struct AttnList {
     int count, joins, pad[6];
@@ -237,6 +241,9 @@ __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // in
 
 __host__ __device__ inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile); }
 
+// Steps of 64 keys of tile t: up to the token of its last row.
+__device__ __forceinline__ int row_steps(int t, int G, int len) { return tiles_of(min(((long long)t * kRowTile + kRowTile - 1) / G + 1, (long long)len), kKeyTile); }
+
 struct SchedOut {
     AttnList *head;
     AttnUnit *units, *joins;
@@ -316,7 +323,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
             fn(u, 0);
         } else {
             const int first = KEYS ? G * t : 0;
-            const int end = KEYS ? tiles_of((long long)len * G, kRowStep) : tiles_of(min(((long long)t * kRowTile + kRowTile - 1) / G + 1, (long long)len), kKeyTile);
+            const int end = KEYS ? tiles_of((long long)len * G, kRowStep) : row_steps(t, G, len);
             const int chunks = tiles_of(end - first, chunk), per = tiles_of(end - first, chunks);
             int slot = -1;
             if (chunks > 1 && place) {
@@ -356,6 +363,44 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
     if (tid == 0) to.head->count = min(total, to.max_units), to.head->joins = n_joins;
 }
 
+// Where a block finds its unit: in the list, or, for calls of at most 64 sequences whose tiles all run at once and are shared by nobody, from the tables
+// itself, a sequence a lane: no scheduling launch (one prompt of 33 tokens, 32 heads: 12.5 -> 9 us).
+struct UnitSource {
+    const AttnList *list;                                     // NULL: from the tables
+    const AttnUnit *units;
+    const int32_t *seq_start, *seq_len;
+    int n_seq, T;
+    int32_t *err_flag;
+    template <bool KEYS> __device__ __forceinline__ bool find(int at, int G, AttnUnit &u) const
+    {
+        if (list) {
+            if (at >= list->count) return false;
+            u = units[at];
+            return true;
+        }
+        const int lane = threadIdx.x & 63, s = min(lane, n_seq - 1);
+        const int a = seq_start[s], b = seq_start[s + 1], len = seq_len ? seq_len[s] : b - a;
+        if (__any(a < 0 || b < a || b > T || len < 0 || len > b - a)) {
+            if (at == 0 && threadIdx.x == 0) atomicOr(err_flag, RELIBRA_ERR_SEQ_TABLE);
+            return false;
+        }
+        const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile), tiles = lane < n_seq ? own + tiles_of(b - a - len, kRowTile) : 0;
+        int upto = tiles;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int below = __shfl_up(upto, off);
+            if (lane >= off) upto += below;
+        }
+        const unsigned long long behind = __ballot(upto > at);
+        if (!behind) return false;
+        const int mine = __builtin_ctzll(behind), t = at - __shfl(upto - tiles, mine), row0 = __shfl(a, mine), end = __shfl(b, mine), n = __shfl(len, mine), n_own = __shfl(own, mine);
+        u.slot = -1, u.chunks = 1, u.from = 0, u.to = 0, u.row0 = row0, u.len = n, u.tile = t;
+        if (t >= n_own) u.row0 = row0 + n + (t - n_own) * kRowTile, u.len = min(kRowTile, end - u.row0), u.tile = -1;
+        else u.from = KEYS ? G * t : 0, u.to = KEYS ? tiles_of((long long)n * G, kRowStep) : row_steps(t, G, n);
+        return true;
+    }
+};
+
 // Partial sums of a unit: registers as they lie, 16 bytes a lane, so that stores are whole lines; and in the forward pass two values a row, behind them.
 template <int ND> struct Part {
     static constexpr size_t FLOATS = (size_t)kAttnWaves * ND * 16 * 64;
@@ -385,14 +430,15 @@ template <int ND> struct Part {
 // ---------------------------------------------------------------- forward
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
-attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut out, float *__restrict__ lse,
+attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source, HeadsOut out, float *__restrict__ lse,
                 float *__restrict__ parts, float2 *__restrict__ sums)
 {
     typedef AttnTile<ND> Tile;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];      // keys and values, two tiles each
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
-    if (at >= list->count) return;
-    const AttnUnit u = units[at];
+    AttnUnit u;
+    if (!source.find<false>(at, sh.G, u)) return;
+    u.make_uniform();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
     if (u.tile < 0) {                                         // padding: zeros
         const int pieces = G * d / 8;
@@ -613,14 +659,14 @@ __device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x
 // dq of 128 packed rows, and for the other kernel each row's lse in powers of two and -D.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
-attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, const AttnList *__restrict__ list,
-               const AttnUnit *__restrict__ units, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ minus_delta, float *__restrict__ parts)
+attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, UnitSource source, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ minus_delta, float *__restrict__ parts)
 {
     typedef AttnTile<ND> Tile;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
-    if (at >= list->count) return;
-    const AttnUnit u = units[at];
+    AttnUnit u;
+    if (!source.find<false>(at, sh.G, u)) return;
+    u.make_uniform();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
     if (u.tile < 0) {
         const int pieces = G * d / 8;
@@ -722,15 +768,16 @@ __device__ __forceinline__ int token_of(int r, unsigned magic) { return magic ? 
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ minus_delta, unsigned magic,
-                const AttnList *__restrict__ list, const AttnUnit *__restrict__ units, HeadsOut dk, HeadsOut dv, float *__restrict__ parts)
+                UnitSource source, HeadsOut dk, HeadsOut dv, float *__restrict__ parts)
 {
     typedef AttnTile<ND, kRowStep> Tile;
     constexpr int STATS = 4 * Tile::BYTES, TRADE = STATS + 4 * kRowStep * 4;
     // queries and their upstream, two steps each; the rows' lse and -D, two steps each; what the waves of a pair hand each other
     __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves * 2048];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
-    if (at >= list->count) return;
-    const AttnUnit u = units[at];
+    AttnUnit u;
+    if (!source.find<true>(at, sh.G, u)) return;
+    u.make_uniform();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), role = wave & 1, G = sh.G, d = sh.d;   // role 0: dv, 1: dk
     if (u.tile < 0) {
         const int pieces = d / 8;
@@ -949,6 +996,8 @@ size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
     const AttnSizes r = row_sizes(T, n_seq, Hq, Hk, d), k = key_sizes(T, n_seq, Hq, Hk, d);
     return r.list_bytes() + r.part_bytes + k.list_bytes() + k.part_bytes + 2 * round256((size_t)T * Hq * sizeof(float));
 }
+// Whether blocks find their units themselves.
+inline bool unlisted(const AttnSizes &s, int n_seq, int Hk, int most, int min_chunk) { return n_seq <= 64 && most <= min_chunk && (long long)s.units * Hk <= 2 * kAttnSlots; }
 // A list in the workspace, and the next free byte behind it.
 inline SchedOut sched_out(char *&ws, const AttnSizes &s)
 {
@@ -999,12 +1048,15 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
     float2 *sums = (float2 *)(ws + sz.part_bytes);
     const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
     const HeadsOut oo{(bf16_t *)out, out_stride};
-    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, rows, err_flag));
+    const bool listed = !unlisted(sz, n_seq, Hk, tiles_of(T, kKeyTile), kMinRowChunk);
+    const UnitSource source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
+    if (listed)
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, rows, err_flag));
     attn_layout(d, [&](auto nd) {
         constexpr int ND = decltype(nd)::value;
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_FWD, stream, (attn_fwd_kernel<ND><<<sz.units * Hk, kAttnThreads, 0, stream>>>(
-            sh, HeadsIn{(const bf16_t *)q, q_stride}, HeadsIn{(const bf16_t *)k, k_stride}, HeadsIn{(const bf16_t *)v, v_stride}, rows.head, rows.units, oo, lse, parts, sums)));
-        if (sz.joins > 0)
+            sh, HeadsIn{(const bf16_t *)q, q_stride}, HeadsIn{(const bf16_t *)k, k_stride}, HeadsIn{(const bf16_t *)v, v_stride}, source, oo, lse, parts, sums)));
+        if (listed && sz.joins > 0)
             RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_out_kernel<ND><<<sz.joins * Hk * ND, kAttnThreads, 0, stream>>>(sh, rows.head, rows.joins, parts, sums, oo, lse)));
     });
     RELIBRA_HIP_TRY(launch_check());
@@ -1044,12 +1096,16 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
         di{(const bf16_t *)dout, dout_stride};
     const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
     const unsigned magic = token_magic(sh.G);
-    RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<2, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, keys, err_flag));
+    const bool listed = !unlisted(rs, n_seq, Hk, tiles_of(T, kKeyTile), kMinRowChunk) || !unlisted(ks, n_seq, Hk, tiles_of((long long)T * sh.G, kRowStep), 2 * kMinKeyChunk);
+    const UnitSource row_source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
+    const UnitSource key_source{listed ? keys.head : nullptr, keys.units, seq_start, seq_len, n_seq, T, err_flag};
+    if (listed)
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<2, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, keys, err_flag));
     attn_layout(d, [&](auto nd) {
         constexpr int ND = decltype(nd)::value;
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, rows.head, rows.units, dqo, lse2, delta, row_parts)));
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, magic, keys.head, keys.units, dko, dvo, key_parts)));
-        if (rs.joins + ks.joins > 0)
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, row_source, dqo, lse2, delta, row_parts)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, magic, key_source, dko, dvo, key_parts)));
+        if (listed && rs.joins + ks.joins > 0)
             RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<(rs.joins + ks.joins) * Hk * ND, kAttnThreads, 0, stream>>>(
                 sh, rs.joins, rows.head, rows.joins, row_parts, dqo, keys.head, keys.joins, key_parts, dko, dvo)));
     });
