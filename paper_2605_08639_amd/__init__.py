@@ -861,19 +861,24 @@ def relibra_orthogonalize(grad, momentum=None, mu=0.95, nesterov=True, scale=1.0
     return out, momentum_out
 
 
-def _heads(t, shape, what):
-    """Pointer and token stride of a tensor [T, H, d] of bf16 whose heads lie side by side, on the current device (None: NULL, 0)."""
-    if t is None:
-        return None, 0
-    assert t.shape == shape and t.dtype is torch.bfloat16, f"{what}: expected bf16 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}"
-    T, H, d = shape
-    strides = t.stride()
-    assert (strides[2] == 1 or d == 1) and (strides[1] == d or H == 1), f"{what}: a token's heads lie side by side"
-    at = t.get_device()
-    assert at >= 0, "device tensors, not host memory"
-    here = at if _device is None else _device()
-    assert at == here, f"tensor on device {at}: work goes to the current device's stream"
-    return t.data_ptr(), strides[0] if T > 1 else H * d
+def _heads(T, d, *heads):
+    """Pointers and token strides, one after the other, of tensors [T, H, d] of bf16 given as (tensor, H, name), whose heads lie side by side, on the
+    current device (None: NULL, 0).  All at once, as _ptrs: small calls are bound by what the host spends on them."""
+    out, here = [], -1
+    for t, H, name in heads:
+        if t is None:
+            out += (None, 0)
+            continue
+        strides = t.stride()
+        assert t.dtype is torch.bfloat16 and t.shape == (T, H, d), f"{name}: expected bf16 {(T, H, d)}, got {t.dtype} {tuple(t.shape)}"
+        assert (strides[2] == 1 or d == 1) and (strides[1] == d or H == 1), f"{name}: a token's heads lie side by side"
+        at = t.get_device()
+        assert at >= 0, "device tensors, not host memory"
+        if here < 0:
+            here = at if _device is None else _device()
+        assert at == here, f"tensor on device {at}: work goes to the current device's stream"
+        out += (t.data_ptr(), strides[0] if T > 1 else H * d)
+    return out
 
 
 def _heads_out(t, shape, like):
@@ -892,8 +897,7 @@ def _qk_args(q, k, pos, freq, w_q, w_k, axis):
     assert (pos is None) == (freq is None), "positions come with frequencies"
     assert pos is None or (pos.shape[-1] == T and pos.dim() <= 2 and pos.dtype is torch.int32), "pos is [T] or [n_axes, T] int32"
     assert freq is None or (freq.dim() == 1 and freq.dtype is torch.float32), "freq is [rot / 2] fp32"
-    for w in (w_q, w_k):
-        assert w is None or (w.shape == (d,) and w.dtype is torch.bfloat16), "norm weights are [d] bf16"
+    assert (w_q is None or (w_q.shape == (d,) and w_q.dtype is torch.bfloat16)) and (w_k is None or (w_k.shape == (d,) and w_k.dtype is torch.bfloat16)), "norm weights are [d] bf16"
     if axis is not None:
         assert len(axis) == rot // 2, "one axis a pair"
         axis = bytes(axis)
@@ -908,8 +912,8 @@ def relibra_qk_norm_rope_fwd(q, k, pos=None, freq=None, w_q=None, w_k=None, axis
     q_out = _heads_out(q_out, (T, Hq, d), q)
     k_out = None if k is None else _heads_out(k_out, (T, Hk, d), k)
     at = _ptrs(w_q, w_k, pos, freq)
-    rc = lib().relibra_qk_norm_rope_fwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *at, axis, n_axes, T, Hq, Hk, d, rot, eps,
-                                        ROPE_ADJACENT if adjacent else 0, *_heads(q_out, (T, Hq, d), "q_out"), *_heads(k_out, (T, Hk, d), "k_out"), _raw())
+    x = _heads(T, d, (q, Hq, "q"), (k, Hk, "k"), (q_out, Hq, "q_out"), (k_out, Hk, "k_out"))
+    rc = lib().relibra_qk_norm_rope_fwd(*x[:4], *at, axis, n_axes, T, Hq, Hk, d, rot, eps, ROPE_ADJACENT if adjacent else 0, *x[4:], _raw())
     _check("relibra_qk_norm_rope_fwd", rc)
     return q_out, k_out
 
@@ -928,10 +932,9 @@ def relibra_qk_norm_rope_bwd(q, k, dq_out, dk_out, pos=None, freq=None, w_q=None
     if workspace is None:
         workspace = qk_norm_rope_workspace(T, Hq, Hk, d, q.device)
     at = _ptrs(w_q, w_k, pos, freq, dw_q, dw_k, workspace)
-    rc = lib().relibra_qk_norm_rope_bwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *_heads(dq_out, (T, Hq, d), "dq_out"),
-                                        *_heads(dk_out, (T, Hk, d), "dk_out"), *at[:4], axis, n_axes, T, Hq, Hk, d, rot, eps,
-                                        (ROPE_ADJACENT if adjacent else 0) | (QK_ACCUMULATE if accumulate else 0), *_heads(dq, (T, Hq, d), "dq"),
-                                        *_heads(dk, (T, Hk, d), "dk"), *at[4:], workspace.numel(), _raw())
+    x = _heads(T, d, (q, Hq, "q"), (k, Hk, "k"), (dq_out, Hq, "dq_out"), (dk_out, Hk, "dk_out"), (dq, Hq, "dq"), (dk, Hk, "dk"))
+    rc = lib().relibra_qk_norm_rope_bwd(*x[:8], *at[:4], axis, n_axes, T, Hq, Hk, d, rot, eps,
+                                        (ROPE_ADJACENT if adjacent else 0) | (QK_ACCUMULATE if accumulate else 0), *x[8:], *at[4:], workspace.numel(), _raw())
     _check("relibra_qk_norm_rope_bwd", rc)
     return dq, dk, dw_q, dw_k
 
@@ -965,8 +968,8 @@ def relibra_attention_fwd(q, k, v, seq_start, seq_len=None, scale=None, out=None
         err_flag = new_err_flag(q.device)
     assert err_flag.dtype is torch.int32, "the error flag is int32"
     at = _ptrs(seq_start, seq_len, lse, workspace, err_flag)
-    rc = lib().relibra_attention_fwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *_heads(v, (T, Hk, d), "v"), *at[:2], n_seq, T, Hq, Hk, d,
-                                     scale, *_heads(out, (T, Hq, d), "out"), *at[2:4], workspace.numel(), at[4], _raw())
+    x = _heads(T, d, (q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v"), (out, Hq, "out"))
+    rc = lib().relibra_attention_fwd(*x[:6], *at[:2], n_seq, T, Hq, Hk, d, scale, *x[6:], *at[2:4], workspace.numel(), at[4], _raw())
     _check("relibra_attention_fwd", rc)
     return out, lse
 
@@ -982,9 +985,8 @@ def relibra_attention_bwd(q, k, v, out, lse, dout, seq_start, seq_len=None, scal
         err_flag = new_err_flag(q.device)
     assert err_flag.dtype is torch.int32, "the error flag is int32"
     at = _ptrs(lse, seq_start, seq_len, workspace, err_flag)
-    rc = lib().relibra_attention_bwd(*_heads(q, (T, Hq, d), "q"), *_heads(k, (T, Hk, d), "k"), *_heads(v, (T, Hk, d), "v"), *_heads(out, (T, Hq, d), "out"),
-                                     at[0], *_heads(dout, (T, Hq, d), "dout"), *at[1:3], n_seq, T, Hq, Hk, d, scale, *_heads(dq, (T, Hq, d), "dq"),
-                                     *_heads(dk, (T, Hk, d), "dk"), *_heads(dv, (T, Hk, d), "dv"), at[3], workspace.numel(), at[4], _raw())
+    x = _heads(T, d, (q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v"), (out, Hq, "out"), (dout, Hq, "dout"), (dq, Hq, "dq"), (dk, Hk, "dk"), (dv, Hk, "dv"))
+    rc = lib().relibra_attention_bwd(*x[:8], at[0], *x[8:10], *at[1:3], n_seq, T, Hq, Hk, d, scale, *x[10:], at[3], workspace.numel(), at[4], _raw())
     _check("relibra_attention_bwd", rc)
     return dq, dk, dv
 

@@ -47,14 +47,15 @@ template <bool ADJ> struct QkLane {
         at1 = split ? (pos + quarter) * 8 : pos * 16 + 8;
     }
     // (values of the two pieces) -> turned, by +theta or, with s = -1, by -theta
-    static __device__ __forceinline__ void turn(float (&v0)[8], float (&v1)[8], const float (&c)[8], const float (&s)[8], float sign)
+    static __device__ __forceinline__ void turn(float (&v0)[8], float (&v1)[8], const float2 *angles, float sign)
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            const float2 at = angles[i];
             float &a = ADJ ? (i < 4 ? v0[2 * (i & 3)] : v1[2 * (i & 3)]) : v0[i];
             float &b = ADJ ? (i < 4 ? v0[2 * (i & 3) + 1] : v1[2 * (i & 3) + 1]) : v1[i];
-            const float sn = sign * s[i], x = a * c[i] - b * sn;
-            b = b * c[i] + a * sn;
+            const float sn = sign * at.y, x = a * at.x - b * sn;
+            b = b * at.x + a * sn;
             a = x;
         }
     }
@@ -73,6 +74,13 @@ __device__ __forceinline__ void qk_angles(const QkShape &sh, const QkTables &tab
     }
 }
 
+// Weights as loaded to fp32, at every use: left to itself the compiler keeps them unpacked, 32 registers more.
+__device__ __forceinline__ void unpack_weights(Raw8<bf16_t> r, float (&w)[8])
+{
+    asm volatile("" : "+v"(r.q.x), "+v"(r.q.y), "+v"(r.q.z), "+v"(r.q.w));
+    unpack8(r, w);
+}
+
 template <int LANES, bool ADJ>
 __global__ void __launch_bounds__(kQkThreads)
 qk_fwd_kernel(QkShape sh, QkTables tab, const bf16_t *q, size_t q_ld, const bf16_t *k, size_t k_ld, bf16_t *q_out, size_t qo_ld, bf16_t *k_out, size_t ko_ld)
@@ -88,19 +96,13 @@ qk_fwd_kernel(QkShape sh, QkTables tab, const bf16_t *q, size_t q_ld, const bf16
         wq[i] = tab.w_q && me.in ? fetch8(tab.w_q + (i ? me.at1 : me.at0)) : zero8<bf16_t>();
         wk[i] = tab.w_k && me.in ? fetch8(tab.w_k + (i ? me.at1 : me.at0)) : zero8<bf16_t>();
     }
-    const long long items = (long long)sh.T * sh.groups;
+    const long long items = (long long)sh.T * sh.groups;      // (below 2^31: groups are few tokens')
     for (long long item = (long long)blockIdx.x * kQkWaves + wave; item < items; item += (long long)gridDim.x * kQkWaves) {
-        const int token = (int)(item / sh.groups), group = (int)(item - (long long)token * sh.groups);
-        float c[8], s[8];
+        const int token = (int)(sh.groups == 1 ? (unsigned)item : (unsigned)item / (unsigned)sh.groups), group = (int)(item - (long long)token * sh.groups);
         if (sh.rot) {
             wave_lds_fence();                                 // the last token's are read
             qk_angles(sh, tab, token, lane, angles[wave]);
             wave_lds_fence();
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 a = me.turns ? angles[wave][pos * 8 + i] : make_float2(1.0f, 0.0f);
-            c[i] = a.x, s[i] = a.y;
         }
         auto pass = [&](auto is_q, int head) __attribute__((always_inline)) {
             constexpr bool Q = decltype(is_q)::value;
@@ -115,12 +117,12 @@ qk_fwd_kernel(QkShape sh, QkTables tab, const bf16_t *q, size_t q_ld, const bf16
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += v0[i] * v0[i] + v1[i] * v1[i];
                 const float r = 1.0f / sqrtf(group_sum<LANES>(sum) * inv_d + sh.eps);
-                unpack8(Q ? wq[0] : wk[0], w0);
-                unpack8(Q ? wq[1] : wk[1], w1);
+                unpack_weights(Q ? wq[0] : wk[0], w0);
+                unpack_weights(Q ? wq[1] : wk[1], w1);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v0[i] = v0[i] * r * w0[i], v1[i] = v1[i] * r * w1[i];
             }
-            if (me.turns) me.turn(v0, v1, c, s, 1.0f);
+            if (me.turns) me.turn(v0, v1, angles[wave] + pos * 8, 1.0f);
             if (in) {
                 bf16_t *y = Q ? q_out + token * qo_ld + col : k_out + token * ko_ld + col;
                 store8(y + me.at0, v0);
@@ -157,17 +159,11 @@ qk_bwd_kernel(QkShape sh, QkTables tab, const bf16_t *q, size_t q_ld, const bf16
     for (int i = 0; i < 16; ++i) acc_q[i] = acc_k[i] = 0.0f;
     const long long items = (long long)sh.T * sh.groups;
     for (long long item = (long long)blockIdx.x * kQkWaves + wave; item < items; item += (long long)gridDim.x * kQkWaves) {
-        const int token = (int)(item / sh.groups), group = (int)(item - (long long)token * sh.groups);
-        float c[8], s[8];
+        const int token = (int)(sh.groups == 1 ? (unsigned)item : (unsigned)item / (unsigned)sh.groups), group = (int)(item - (long long)token * sh.groups);
         if (sh.rot) {
             wave_lds_fence();
             qk_angles(sh, tab, token, lane, angles[wave]);
             wave_lds_fence();
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 a = me.turns ? angles[wave][pos * 8 + i] : make_float2(1.0f, 0.0f);
-            c[i] = a.x, s[i] = a.y;
         }
         auto pass = [&](auto is_q, int head) __attribute__((always_inline)) {
             constexpr bool Q = decltype(is_q)::value;
@@ -179,13 +175,13 @@ qk_bwd_kernel(QkShape sh, QkTables tab, const bf16_t *q, size_t q_ld, const bf16
             float g0[8], g1[8];
             unpack8(in ? fetch8(up + me.at0) : zero8<bf16_t>(), g0);
             unpack8(in ? fetch8(up + me.at1) : zero8<bf16_t>(), g1);
-            if (me.turns) me.turn(g0, g1, c, s, -1.0f);
+            if (me.turns) me.turn(g0, g1, angles[wave] + pos * 8, -1.0f);
             if (norm) {
                 float v0[8], v1[8], w0[8], w1[8], sum = 0.0f, dot = 0.0f;
                 unpack8(x0, v0);
                 unpack8(x1, v1);
-                unpack8(Q ? wq[0] : wk[0], w0);
-                unpack8(Q ? wq[1] : wk[1], w1);
+                unpack_weights(Q ? wq[0] : wk[0], w0);
+                unpack_weights(Q ? wq[1] : wk[1], w1);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     sum += v0[i] * v0[i] + v1[i] * v1[i];
@@ -218,9 +214,7 @@ qk_bwd_kernel(QkShape sh, QkTables tab, const bf16_t *q, size_t q_ld, const bf16
     auto leave = [&](float (&acc)[16], float *to) __attribute__((always_inline)) {
         if (!to) return;
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-#pragma unroll
-            for (int off = LANES; off < 64; off <<= 1) acc[i] += __shfl_xor(acc[i], off);
+        for (int i = 0; i < 16; ++i) acc[i] = place_sum<LANES>(acc[i]);
         __syncthreads();
         if (lane < LANES && me.in)
 #pragma unroll

@@ -39,6 +39,18 @@ template <int LANES, class Op> __device__ __forceinline__ float group_reduce(flo
 template <int LANES> __device__ __forceinline__ float group_sum(float v) { return group_reduce<LANES, SumOp>(v); }
 template <int LANES> __device__ __forceinline__ float group_max(float v) { return group_reduce<LANES, MaxOp>(v); }
 
+// Sum over the lanes of a wave that have the same place in their group of LANES (4, 8, 16); every lane gets its place's.
+template <int LANES> __device__ __forceinline__ float place_sum(float v)
+{
+    static_assert(LANES == 4 || LANES == 8 || LANES == 16, "group size");
+    if constexpr (LANES <= 8) v += dpp<0x128>(v);                  // row_ror 8
+    if constexpr (LANES <= 4) v += dpp<0x124>(v);                  // row_ror 4
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    v = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+    const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    return __builtin_bit_cast(float, (unsigned)s[0]) + __builtin_bit_cast(float, (unsigned)s[1]);
+}
+
 // Eight consecutive values of memory (16-byte aligned) as loaded, as fp32, and back (one rounding to bf16).
 template <class T> struct Raw8;
 template <> struct Raw8<bf16_t> {
