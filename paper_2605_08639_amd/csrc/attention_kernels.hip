@@ -1036,9 +1036,10 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
     if (rc != RELIBRA_OK) return rc;
     if (T == 0 || n_seq == 0) return RELIBRA_OK;
     const HeadRows in[3] = {{q, q_stride, Hq * d}, {k, k_stride, Hk * d}, {v, v_stride, Hk * d}}, to{out, out_stride, Hq * d};
-    if (!to.usable() || !lse) return RELIBRA_EINVAL;
+    const size_t lse_bytes = (size_t)T * Hq * sizeof(float);
+    if (!to.usable() || !lse || to.overlaps(lse, lse_bytes, T)) return RELIBRA_EINVAL;
     for (const HeadRows &x : in)
-        if (!x.usable() || x.overlaps(to, T)) return RELIBRA_EINVAL;
+        if (!x.usable() || x.overlaps(to, T) || x.overlaps(lse, lse_bytes, T)) return RELIBRA_EINVAL;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     if (!workspace || workspace_bytes < attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
     const AttnSizes sz = row_sizes(T, n_seq, Hq, Hk, d);
@@ -1078,7 +1079,7 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
     for (const HeadRows &x : in)
         if (!x.usable()) return RELIBRA_EINVAL;
     for (int i = 0; i < 3; ++i) {
-        if (!to[i].usable()) return RELIBRA_EINVAL;
+        if (!to[i].usable() || to[i].overlaps(lse, (size_t)T * Hq * sizeof(float), T)) return RELIBRA_EINVAL;
         for (const HeadRows &x : in)
             if (x.overlaps(to[i], T)) return RELIBRA_EINVAL;
         for (int j = 0; j < i; ++j)

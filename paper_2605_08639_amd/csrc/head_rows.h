@@ -5,7 +5,7 @@
 
 namespace relibra {
 
-constexpr int64_t kMaxHeadStride = 1 << 28;                   // a few rows' distance stays within a lane's 32-bit byte offset
+constexpr int64_t kMaxHeadStride = 1 << 27;                   // eight rows' distance stays within 31 bits of bytes, a lane's offset
 
 struct HeadRows {
     const void *p;
@@ -13,6 +13,7 @@ struct HeadRows {
     int width;                                                // H * d; 0: no such tensor
     bool usable() const { return width == 0 || (p && aligned16(p) && stride >= width && stride % 8 == 0 && stride <= kMaxHeadStride); }
     bool same(const HeadRows &o) const { return p == o.p && stride == o.stride && width == o.width; }
+    bool overlaps(const void *other, size_t bytes, int64_t T) const { return width > 0 && T > 0 && overlap(p, (size_t)((T - 1) * stride + width) * 2, other, bytes); }
     // Whether the two share a byte over T tokens.  Rows of one stride may interleave; of unlike strides only whole ranges are compared.
     bool overlaps(const HeadRows &o, int64_t T) const
     {

@@ -273,6 +273,29 @@ def test_attention_of_many_sequences():
 
 
 @gpu
+def test_attention_of_as_many_sequences_as_there_may_be():
+    """8192 of one token each, and one more token's place of padding behind every second: a token's attention is its value."""
+    n, d = 8192, 64
+    g = torch.Generator().manual_seed(14)
+    places = torch.tensor([1, 2] * (n // 2))
+    start = torch.cat([torch.zeros(1, dtype=torch.long), places.cumsum(0)]).to(torch.int32)
+    T = int(start[-1])
+    q, k, v, do = (torch.randn(T, h, d, generator=g).to(BF16).to(DEV) for h in (2, 1, 1, 2))
+    length = torch.ones(n, dtype=torch.int32, device=DEV)
+    out, lse = rl.relibra_attention_fwd(q, k, v, start.to(DEV), seq_len=length)
+    real = torch.zeros(T, dtype=torch.bool)
+    real[start[:-1].long()] = True
+    real = real.to(DEV)
+    assert torch.equal(out[real], v[real].expand(-1, 2, -1)) and torch.all(out[~real] == 0) and torch.all(lse[~real] == 0)
+    z = (q[real].double() * k[real].double()).sum(2) / 8
+    assert torch.all((lse[real].double() - z).abs() <= (d + 12) * U * ((q[real].double() * k[real].double()).abs().sum(2) / 8 + z.abs()))
+    dq, dk, dv = rl.relibra_attention_bwd(q, k, v, out, lse, do, start.to(DEV), seq_len=length)
+    both = do[real].double().sum(1, keepdim=True)
+    assert torch.all(dq == 0) and torch.all(dk == 0) and torch.all(dv[~real] == 0)
+    assert torch.all((dv[real].double() - both).abs() <= H * both.abs() + 16 * U * do[real].double().abs().sum(1, keepdim=True))
+
+
+@gpu
 def test_attention_in_a_graph_beside_eager_calls():
     c = make([300, 129, 500], 2, 4, 128, lens=[300, 100, 481], seed=10)
     start, length = tables(c)
@@ -388,9 +411,9 @@ def test_attention_refusals(call):
 
 
 def test_attention_refuses_overlaps_and_small_workspaces():
-    for bad in (dict(out=M), dict(out=2 * M, ol=256), dict(out=3 * M + 16), dict(out=M + 256)):
+    for bad in (dict(out=M), dict(out=2 * M, ol=256), dict(out=3 * M + 16), dict(out=M + 256), dict(lse=4 * M + 64), dict(lse=M), dict(lse=3 * M - 64)):
         assert _fwd(**bad) == rl.EINVAL, bad
-    for bad in (dict(do=0), dict(dq=0), dict(dk=0), dict(dv=0), dict(dol=255), dict(dq=M), dict(dq=4 * M), dict(dq=5 * M), dict(dk=2 * M), dict(dv=3 * M), dict(dk=8 * M), dict(dk=6 * M + 128)):
+    for bad in (dict(do=0), dict(dq=0), dict(dk=0), dict(dv=0), dict(dol=255), dict(dq=M), dict(dq=4 * M), dict(dq=5 * M), dict(dk=2 * M), dict(dv=3 * M), dict(dk=8 * M), dict(dk=6 * M + 128), dict(lse=6 * M), dict(lse=8 * M - 4)):
         assert _bwd(**bad) == rl.EINVAL, bad
     for call, which in ((_fwd, rl.WS_ATTENTION_FWD), (_bwd, rl.WS_ATTENTION_BWD)):
         need = rl.workspace_bytes(which, 8, 1, 4, 2, 2, 64)

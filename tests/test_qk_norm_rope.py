@@ -257,6 +257,23 @@ def test_qk_norm_rope_in_a_graph_beside_eager_calls():
         assert all(torch.equal(a, b) for a, b in zip(again, want)), i
 
 
+@gpu
+def test_qk_norm_rope_past_32_bits_of_offset():
+    """Tokens 2^20 values apart: the last ones lie beyond 2^31 values from the first."""
+    T, stride = 2300, 1 << 20
+    c = make(T, 3, 2, 64, seed=11)
+    want = rl.relibra_qk_norm_rope_fwd(dev(c["q"]), dev(c["k"]), **how(c))
+    back = rl.relibra_qk_norm_rope_bwd(dev(c["q"]), dev(c["k"]), dev(c["up_q"]), dev(c["up_k"]), **how(c))
+    whole = torch.empty((T, stride), dtype=BF16, device=DEV)
+    q, k, uq, uk, oq, ok = (whole[:, a:a + h * 64].unflatten(1, (h, 64)) for a, h in ((0, 3), (192, 2), (1 << 19, 3), ((1 << 19) + 192, 2), (1024, 3), (1216, 2)))
+    for to, name in ((q, "q"), (k, "k"), (uq, "up_q"), (uk, "up_k")):
+        to.copy_(dev(c[name]))
+    got = rl.relibra_qk_norm_rope_fwd(q, k, **how(c), q_out=oq, k_out=ok)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = rl.relibra_qk_norm_rope_bwd(q, k, uq, uk, **how(c), dq=oq, dk=uk)
+    assert all(torch.equal(a, b) for a, b in zip(got, back))
+
+
 # ------------------------------------------------------------------ refusals (no GPU needed: nothing is launched)
 P, F, L = C.c_void_p, C.c_float, C.c_int64
 M = 1 << 24                                                  # pretended tensors lie far apart
