@@ -949,26 +949,22 @@ attn_join_kernel(AttnShape sh, int row_joins, const AttnList *__restrict__ rows,
 }
 
 // ---------------------------------------------------------------- host
-inline bool attn_takes(int T, int n_seq, int Hq, int Hk, int d)
-{
-    return d % 8 == 0 && d <= kAttnMaxDim && n_seq <= kAttnMaxSeq && Hq / Hk <= kAttnMaxGroup && Hq <= 4096 && (long long)T * (Hq / Hk) <= kAttnMaxRows;
-}
 inline int attn_nd(int d) { return (d + 31) / 32; }
-// Lists: at most so many units, joined tiles and partial sums a key head, for rows and for keys; places of padding are at most a tile a sequence more than
-// the rows they take.  A chunk has at least a fair share's worth (half of it: keys) of all heads' steps, and a least number of them; tiles of two or
+// Lists: at most so many units, joined tiles and partial sums a key head, for rows and for keys.  A token is a sequence's or padding's, and padding
+// takes no more places than it would as rows or keys, but for a tile a sequence.  A chunk has at least a fair share's worth (half of it: keys) of all heads' steps, and a least number of them; tiles of two or
 // more chunks have at most twice as many as their steps make whole ones.
 struct AttnSizes {
     int units, joins, slots;
     size_t part_bytes;
     size_t list_bytes() const { return round256(sizeof(AttnList) + (size_t)(units + joins) * sizeof(AttnUnit)); }
 };
-inline AttnSizes attn_sizes(long long tiles, long long most, long long whole, int min_chunk, int T, int n_seq, int Hk, int d)
+inline AttnSizes attn_sizes(long long tiles, long long most, long long whole, int min_chunk, int n_seq, int Hk, int d)
 {
     AttnSizes s;
     whole = std::min(whole, tiles * most / min_chunk);
     s.joins = (int)std::min(whole, tiles);
     s.slots = (int)(2 * whole);
-    s.units = (int)(tiles + T / kRowTile + n_seq + 2 * whole);
+    s.units = (int)(tiles + n_seq + 2 * whole);
     s.part_bytes = round256((size_t)s.slots * Hk * kAttnWaves * attn_nd(d) * 16 * 64 * sizeof(float));
     return s;
 }
@@ -977,11 +973,17 @@ inline AttnSizes row_sizes(int T, int n_seq, int Hq, int Hk, int d)
 {
     const int G = Hq / Hk, most = tiles_of(T, kKeyTile);
     const bool share = most > kMinRowChunk && (long long)T * Hq < 1 << 18;
-    return attn_sizes((long long)T * G / kRowTile + n_seq, most, share ? kAttnSlots / Hk + 1 : 0, kMinRowChunk, T, n_seq, Hk, d);
+    return attn_sizes((long long)T * G / kRowTile + n_seq, most, share ? kAttnSlots / Hk + 1 : 0, kMinRowChunk, n_seq, Hk, d);
 }
 inline AttnSizes key_sizes(int T, int n_seq, int Hq, int Hk, int d)
 {
-    return attn_sizes(T / kKeyRows + n_seq, tiles_of((long long)T * (Hq / Hk), kRowStep), 2 * kAttnSlots / Hk + 1, kMinKeyChunk, T, n_seq, Hk, d);
+    return attn_sizes(T / kKeyRows + n_seq, tiles_of((long long)T * (Hq / Hk), kRowStep), 2 * kAttnSlots / Hk + 1, kMinKeyChunk, n_seq, Hk, d);
+}
+// (a launch has fewer than 2^32 threads)
+inline bool attn_takes(int T, int n_seq, int Hq, int Hk, int d)
+{
+    if (d % 8 || d > kAttnMaxDim || n_seq > kAttnMaxSeq || Hq / Hk > kAttnMaxGroup || Hq > 4096 || (long long)T * (Hq / Hk) > kAttnMaxRows) return false;
+    return (long long)std::max(row_sizes(T, n_seq, Hq, Hk, d).units, key_sizes(T, n_seq, Hq, Hk, d).units) * Hk < (1ll << 32) / kAttnThreads;
 }
 inline size_t row_sum_bytes(const AttnSizes &s, int Hk) { return round256((size_t)s.slots * Hk * kRowTile * sizeof(float2)); }
 size_t attn_fwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)

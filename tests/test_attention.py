@@ -410,6 +410,15 @@ def test_attention_refusals(call):
     assert call(T=0, q=0, k=0, v=0, out=0) == rl.OK and call(n_seq=0, start=0) == rl.OK
 
 
+@pytest.mark.parametrize("call", [_fwd, _bwd])
+def test_attention_refuses_more_blocks_than_a_launch_has(call):
+    """A launch has fewer than 2^32 threads, 256 a block; a block has 64 keys of a key head."""
+    big = dict(Hq=64, Hk=64, d=8, ql=512, kl=512, vl=512, ol=512, n_seq=8192)
+    assert call(T=1 << 24, **big) == rl.EUNSUPPORTED
+    for which in (rl.WS_ATTENTION_FWD, rl.WS_ATTENTION_BWD):
+        assert rl.workspace_bytes(which, 1 << 24, 1, 64, 8192, 64, 8) == 0 and rl.workspace_bytes(which, 1 << 23, 1, 64, 8192, 64, 8) > 0
+
+
 def test_attention_refuses_overlaps_and_small_workspaces():
     for bad in (dict(out=M), dict(out=2 * M, ol=256), dict(out=3 * M + 16), dict(out=M + 256), dict(lse=4 * M + 64), dict(lse=M), dict(lse=3 * M - 64)):
         assert _fwd(**bad) == rl.EINVAL, bad
