@@ -218,6 +218,7 @@ template <int ND> struct TokenTiles {
 // the longest tile's, so that one long tile does not outlast the rest (8 steps at least: a join costs what four do).  Keys: two chunks to each of
 // the blocks that run at once, or one where that leaves few steps.
 constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinRowChunk = 8, kMinKeyChunk = 4, kFullKeyChunk = 16;
+constexpr int kShareTiles = 768, kFwdShareSteps = 24, kBwdShareSteps = 12;
 
 __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // inclusive; two barriers
 {
@@ -394,9 +395,10 @@ struct UnitSource {
         const unsigned long long behind = __ballot(upto > at);
         if (!behind) return false;
         const int mine = __builtin_ctzll(behind), t = at - __shfl(upto - tiles, mine), row0 = __shfl(a, mine), end = __shfl(b, mine), n = __shfl(len, mine), n_own = __shfl(own, mine);
-        u.slot = -1, u.chunks = 1, u.from = 0, u.to = 0, u.row0 = row0, u.len = n, u.tile = t;
+        u.slot = -1, u.chunks = 1, u.from = 0, u.to = 0, u.row0 = row0, u.len = n;
         if (t >= n_own) u.row0 = row0 + n + (t - n_own) * kRowTile, u.len = min(kRowTile, end - u.row0), u.tile = -1;
-        else u.from = KEYS ? G * t : 0, u.to = KEYS ? tiles_of((long long)n * G, kRowStep) : row_steps(t, G, n);
+        else if (KEYS) u.tile = t, u.from = G * t, u.to = tiles_of((long long)n * G, kRowStep);
+        else u.tile = n_own - 1 - t, u.to = row_steps(u.tile, G, n);       // the longest first here, too
         return true;
     }
 };
@@ -968,11 +970,13 @@ inline AttnSizes attn_sizes(long long tiles, long long most, long long whole, in
     s.part_bytes = round256((size_t)s.slots * Hk * kAttnWaves * attn_nd(d) * 16 * 64 * sizeof(float));
     return s;
 }
-// Rows of more than 2^18 heads and tokens have several times the tiles that run at once: none is shared.
-inline AttnSizes row_sizes(int T, int n_seq, int Hq, int Hk, int d)
+// Rows are shared where the longest tile can outlast the rest by enough steps to pay for partial sums and the join's launch, which is there
+// anyway for the keys in the backward pass.
+inline AttnSizes row_sizes(int T, int n_seq, int Hq, int Hk, int d, bool bwd)
 {
     const int G = Hq / Hk, most = tiles_of(T, kKeyTile);
-    const bool share = most > kMinRowChunk && (long long)T * Hq < 1 << 18;
+    const long long rest = (long long)most * T * Hq / (kShareTiles * kRowTile);
+    const bool share = most - rest >= (bwd ? kBwdShareSteps : kFwdShareSteps);
     return attn_sizes((long long)T * G / kRowTile + n_seq, most, share ? kAttnSlots / Hk + 1 : 0, kMinRowChunk, n_seq, Hk, d);
 }
 inline AttnSizes key_sizes(int T, int n_seq, int Hq, int Hk, int d)
@@ -983,23 +987,24 @@ inline AttnSizes key_sizes(int T, int n_seq, int Hq, int Hk, int d)
 inline bool attn_takes(int T, int n_seq, int Hq, int Hk, int d)
 {
     if (d % 8 || d > kAttnMaxDim || n_seq > kAttnMaxSeq || Hq / Hk > kAttnMaxGroup || Hq > 4096 || (long long)T * (Hq / Hk) > kAttnMaxRows) return false;
-    return (long long)std::max(row_sizes(T, n_seq, Hq, Hk, d).units, key_sizes(T, n_seq, Hq, Hk, d).units) * Hk < (1ll << 32) / kAttnThreads;
+    return (long long)std::max(row_sizes(T, n_seq, Hq, Hk, d, true).units, key_sizes(T, n_seq, Hq, Hk, d).units) * Hk < (1ll << 32) / kAttnThreads;
 }
 inline size_t row_sum_bytes(const AttnSizes &s, int Hk) { return round256((size_t)s.slots * Hk * kRowTile * sizeof(float2)); }
 size_t attn_fwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
 {
     if (T < 0 || n_seq < 0 || Hk < 1 || Hq < 1 || Hq % Hk || d < 8 || !attn_takes(T, n_seq, Hq, Hk, d)) return 0;
-    const AttnSizes s = row_sizes(T, n_seq, Hq, Hk, d);
+    const AttnSizes s = row_sizes(T, n_seq, Hq, Hk, d, false);
     return s.list_bytes() + s.part_bytes + row_sum_bytes(s, Hk);
 }
 size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
 {
     if (!attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return 0;
-    const AttnSizes r = row_sizes(T, n_seq, Hq, Hk, d), k = key_sizes(T, n_seq, Hq, Hk, d);
+    const AttnSizes r = row_sizes(T, n_seq, Hq, Hk, d, true), k = key_sizes(T, n_seq, Hq, Hk, d);
     return r.list_bytes() + r.part_bytes + k.list_bytes() + k.part_bytes + 2 * round256((size_t)T * Hq * sizeof(float));
 }
-// Whether blocks find their units themselves.
-inline bool unlisted(const AttnSizes &s, int n_seq, int Hk, int most, int min_chunk) { return n_seq <= 64 && most <= min_chunk && (long long)s.units * Hk <= 2 * kAttnSlots; }
+// Whether blocks may find their units themselves.
+constexpr int kUnlisted = 4096;
+inline bool unlisted(const AttnSizes &s, int n_seq, int Hk) { return n_seq == 1 || (n_seq <= 64 && (long long)s.units * Hk <= kUnlisted); }
 // A list in the workspace, and the next free byte behind it.
 inline SchedOut sched_out(char *&ws, const AttnSizes &s)
 {
@@ -1044,14 +1049,14 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
         if (!x.usable() || x.overlaps(to, T) || x.overlaps(lse, lse_bytes, T)) return RELIBRA_EINVAL;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     if (!workspace || workspace_bytes < attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
-    const AttnSizes sz = row_sizes(T, n_seq, Hq, Hk, d);
+    const AttnSizes sz = row_sizes(T, n_seq, Hq, Hk, d, false);
     char *ws = (char *)workspace;
     const SchedOut rows = sched_out(ws, sz);
     float *parts = (float *)ws;
     float2 *sums = (float2 *)(ws + sz.part_bytes);
     const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
     const HeadsOut oo{(bf16_t *)out, out_stride};
-    const bool listed = !unlisted(sz, n_seq, Hk, tiles_of(T, kKeyTile), kMinRowChunk);
+    const bool listed = sz.joins > 0 || !unlisted(sz, n_seq, Hk);
     const UnitSource source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
     if (listed)
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, rows, err_flag));
@@ -1089,7 +1094,7 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
     }
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     if (!workspace || workspace_bytes < attn_bwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
-    const AttnSizes rs = row_sizes(T, n_seq, Hq, Hk, d), ks = key_sizes(T, n_seq, Hq, Hk, d);
+    const AttnSizes rs = row_sizes(T, n_seq, Hq, Hk, d, true), ks = key_sizes(T, n_seq, Hq, Hk, d);
     char *ws = (char *)workspace;
     const SchedOut rows = sched_out(ws, rs), keys = sched_out(ws, ks);
     float *row_parts = (float *)ws, *key_parts = (float *)(ws += rs.part_bytes);
@@ -1099,7 +1104,7 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
         di{(const bf16_t *)dout, dout_stride};
     const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
     const unsigned magic = token_magic(sh.G);
-    const bool listed = !unlisted(rs, n_seq, Hk, tiles_of(T, kKeyTile), kMinRowChunk) || !unlisted(ks, n_seq, Hk, tiles_of((long long)T * sh.G, kRowStep), 2 * kMinKeyChunk);
+    const bool listed = rs.joins > 0 || tiles_of((long long)T * sh.G, kRowStep) > 2 * kMinKeyChunk || !unlisted(rs, n_seq, Hk) || !unlisted(ks, n_seq, Hk);
     const UnitSource row_source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
     const UnitSource key_source{listed ? keys.head : nullptr, keys.units, seq_start, seq_len, n_seq, T, err_flag};
     if (listed)
