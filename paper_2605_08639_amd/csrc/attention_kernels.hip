@@ -31,8 +31,13 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnShape {
     int T, Hq, Hk, G, d;
+    unsigned magic;                                           // for token_of
     float scale;
 };
+// r / G: for r <= 2^26 + 2^20 and G <= 64 the upper half of r * ceil(2^32 / G): its excess over r / G, below r (G - 1) / (2^32 G) < 1 / G, never reaches
+// the next integer.
+inline unsigned token_magic(int G) { return G == 1 ? 0u : (unsigned)(((1ull << 32) + G - 1) / G); }
+__device__ __forceinline__ int token_of(int r, unsigned magic) { return magic ? (int)__umulhi((unsigned)r, magic) : r; }
 // A tensor of heads: element (token, head * d + c) at p[token * ld + head * d + c].
 struct HeadsIn {
     const bf16_t *p;
@@ -44,14 +49,14 @@ struct HeadsOut {
 };
 // One block's work: rows (or keys) tile * 128 (64) .. of the sequence that starts at row0, over steps from .. to - 1 of the keys (of the packed rows), 64
 // each; into slot `slot` of the partial sums, or all there are (-1).  tile < 0: rows row0 .. row0 + len - 1 are padding.
-struct AttnUnit {
+struct alignas(16) AttnUnit {
     int row0, len, tile, from, to, slot, chunks, pad;
     __device__ __forceinline__ void make_uniform()            // (the same in every lane: scalars from here on)
     {
         for (int *x : {&row0, &len, &tile, &from, &to, &slot, &chunks}) *x = __builtin_amdgcn_readfirstlane(*x);
     }
 };
-struct AttnList {
+struct alignas(16) AttnList {
     int count, joins, pad[6];
 };
 
@@ -243,16 +248,16 @@ __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // in
 __host__ __device__ inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile); }
 
 // Steps of 64 keys of tile t: up to the token of its last row.
-__device__ __forceinline__ int row_steps(int t, int G, int len) { return tiles_of(min(((long long)t * kRowTile + kRowTile - 1) / G + 1, (long long)len), kKeyTile); }
+__device__ __forceinline__ int row_steps(int t, int G, int len, unsigned magic) { return tiles_of(token_of(min(t * kRowTile + kRowTile, len * G) - 1, magic) + 1, kKeyTile); }
 
 struct SchedOut {
     AttnList *head;
     AttnUnit *units, *joins;
-    int max_units, max_slots;                                 // (max_slots 0: no tile is shared)
+    int share;                                                // whether long tiles may be several blocks'
 };
 
 __global__ void __launch_bounds__(kSchedThreads)
-attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, int Hk, SchedOut row_out, SchedOut key_out,
+attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, unsigned magic, int Hk, SchedOut row_out, SchedOut key_out,
                   int32_t *err_flag)
 {
     const bool KEYS = blockIdx.x == 1;
@@ -279,7 +284,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
                 tiles = own + tiles_of(b - a - len, kRowTile);
                 // keys: the sum of ceil(len G / 64) - G t over the tiles t;  rows: no less than that of (128 t + 127) / (64 G) + 1
                 const long long n = own;
-                if (own) atomicAdd(&steps, (unsigned long long)(KEYS ? n * tiles_of((long long)len * G, kRowStep) - (long long)G * n * (n - 1) / 2 : n * (n + 1) / G + 1 + n));
+                if (own) atomicAdd(&steps, (unsigned long long)(KEYS ? n * tiles_of((long long)len * G, kRowStep) - (long long)G * n * (n - 1) / 2 : (long long)((double)(n * (n + 1)) / G) + 1 + n));
             }
         }
         int total;
@@ -297,7 +302,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
     const unsigned long long share = (steps * Hk + kAttnSlots - 1) / kAttnSlots;
     const int longest = KEYS ? tiles_of((long long)T * G, kRowStep) : tiles_of(T, kKeyTile);
     int chunk = longest;
-    if (to.max_slots > 0) {
+    if (to.share) {
         const unsigned long long want = !KEYS ? max(share, (unsigned long long)kMinRowChunk)
                                         : share < kFullKeyChunk ? max(share, (unsigned long long)kMinKeyChunk) : max((share + 1) / 2, (unsigned long long)kFullKeyChunk);
         chunk = (int)min(want, (unsigned long long)longest);
@@ -305,63 +310,62 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
     const int most = chunk;                                   // the largest work of a unit
     int shift = 0;
     while ((most >> shift) >= kSchedBins) ++shift;
-    // a tile's unit(s) and their work: fn(unit, work)
-    auto each = [&](int f, bool place, auto fn) __attribute__((always_inline)) {
-        int lo = 0, hi = n_seq;                               // the last sequence with before[s] <= f
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (before[mid] <= f) lo = mid;
-            else hi = mid;
-        }
-        const int a = starts[lo], b = starts[lo + 1], len = lens[lo];
-        int t = f - before[lo];
-        const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile);
-        AttnUnit u{a, len, t, 0, 0, -1, 1, 0};
-        if (t >= own) {
-            u.row0 = a + len + (t - own) * kRowTile;
-            u.len = min(kRowTile, b - u.row0);
-            u.tile = -1;
-            fn(u, 0);
-        } else {
-            const int first = KEYS ? G * t : 0;
-            const int end = KEYS ? tiles_of((long long)len * G, kRowStep) : row_steps(t, G, len);
-            const int chunks = tiles_of(end - first, chunk), per = tiles_of(end - first, chunks);
-            int slot = -1;
-            if (chunks > 1 && place) {
-                slot = atomicAdd(&n_slots, chunks);
-                if (slot + chunks > to.max_slots) slot = -1;  // (cannot be: max_slots covers the most there are)
-                else {
-                    u.slot = slot, u.chunks = chunks;
-                    to.joins[atomicAdd(&n_joins, 1)] = u;
+    const int flat = before[n_seq];
+    int total = 0;
+    // Twice over the tiles: counts of units, then their places.  (One body for both, small as it is: what the kernel waits for is its code's first arrival.)
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+        for (int f = tid; f < flat; f += kSchedThreads) {
+            int lo = 0, hi = n_seq;                           // the last sequence with before[s] <= f
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (before[mid] <= f) lo = mid;
+                else hi = mid;
+            }
+            const int a = starts[lo], len = lens[lo], t = f - before[lo], own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile);
+            AttnUnit u{a, len, t, 0, 0, -1, 1, 0};
+            int first = 0, end = 0, chunks = 1, per = 0;
+            if (t >= own) {
+                u.row0 = a + len + (t - own) * kRowTile;
+                u.len = min(kRowTile, starts[lo + 1] - u.row0);
+                u.tile = -1;
+            } else {
+                first = KEYS ? G * t : 0;
+                end = KEYS ? tiles_of((long long)len * G, kRowStep) : row_steps(t, G, len, magic);
+                per = end - first;
+                if (per > chunk) {
+                    chunks = (unsigned)(per + chunk - 1) / (unsigned)chunk;
+                    per = (unsigned)(per + chunks - 1) / (unsigned)chunks;
                 }
             }
-            for (int c = 0; c < chunks; ++c) {
+            if (!pass) {
+                atomicAdd(&bins[per >> shift], chunks);
+                continue;
+            }
+            if (chunks > 1) {
+                u.chunks = chunks;
+                u.slot = atomicAdd(&n_slots, chunks);
+                to.joins[atomicAdd(&n_joins, 1)] = u;
+            }
+            int at = atomicAdd(&bins[per >> shift], chunks);
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c, ++at) {
                 // keys: from the last rows on, so that chunks of one number begin at the same rows
                 u.from = KEYS ? max(end - (c + 1) * per, first) : c * per;
                 u.to = KEYS ? end - c * per : min(u.from + per, end);
-                u.slot = slot < 0 ? -1 : slot + c;
-                if (slot < 0 && place && chunks > 1) {
-                    if (c == 0) u.from = first, u.to = end;
-                    else u.tile = -1, u.len = 0;
-                }
-                fn(u, per);
+                to.units[at] = u;
+                if (chunks > 1) ++u.slot;
             }
         }
-    };
-    const int flat = before[n_seq];
-    for (int f = tid; f < flat; f += kSchedThreads) each(f, false, [&](const AttnUnit &, int work) { atomicAdd(&bins[work >> shift], 1); });
-    __syncthreads();
-    int total;
-    const int mine = bins[kSchedBins - 1 - tid], upto = scan1024(mine, sums, total);
-    bins[kSchedBins - 1 - tid] = upto - mine;                  // heaviest first
-    __syncthreads();
-    for (int f = tid; f < flat; f += kSchedThreads)
-        each(f, true, [&](const AttnUnit &u, int work) {
-            const int at = atomicAdd(&bins[work >> shift], 1);
-            if (at < to.max_units) to.units[at] = u;
-        });
-    __syncthreads();
-    if (tid == 0) to.head->count = min(total, to.max_units), to.head->joins = n_joins;
+        __syncthreads();
+        if (!pass) {
+            const int mine = bins[kSchedBins - 1 - tid], upto = scan1024(mine, sums, total);
+            bins[kSchedBins - 1 - tid] = upto - mine;         // heaviest first
+            __syncthreads();
+        }
+    }
+    if (tid == 0) to.head->count = total, to.head->joins = n_joins;
 }
 
 // Where a block finds its unit: in the list, or, for calls of at most 64 sequences whose tiles all run at once and are shared by nobody, from the tables
@@ -372,7 +376,7 @@ struct UnitSource {
     const int32_t *seq_start, *seq_len;
     int n_seq, T;
     int32_t *err_flag;
-    template <bool KEYS> __device__ __forceinline__ bool find(int at, int G, AttnUnit &u) const
+    template <bool KEYS> __device__ __forceinline__ bool find(int at, int G, unsigned magic, AttnUnit &u) const
     {
         if (list) {
             if (at >= list->count) return false;
@@ -398,7 +402,7 @@ struct UnitSource {
         u.slot = -1, u.chunks = 1, u.from = 0, u.to = 0, u.row0 = row0, u.len = n;
         if (t >= n_own) u.row0 = row0 + n + (t - n_own) * kRowTile, u.len = min(kRowTile, end - u.row0), u.tile = -1;
         else if (KEYS) u.tile = t, u.from = G * t, u.to = tiles_of((long long)n * G, kRowStep);
-        else u.tile = n_own - 1 - t, u.to = row_steps(u.tile, G, n);       // the longest first here, too
+        else u.tile = n_own - 1 - t, u.to = row_steps(u.tile, G, n, magic);       // the longest first here, too
         return true;
     }
 };
@@ -439,7 +443,7 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];      // keys and values, two tiles each
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     AttnUnit u;
-    if (!source.find<false>(at, sh.G, u)) return;
+    if (!source.find<false>(at, sh.G, sh.magic, u)) return;
     u.make_uniform();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
     if (u.tile < 0) {                                         // padding: zeros
@@ -450,8 +454,8 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source
         return;
     }
     const int rows = u.len * G, first = u.tile * kRowTile + wave * 32;         // (this wave's first packed row)
-    const int r = min(first + (lane & 31), rows - 1), tok = r / G, head = hk * G + r - tok * G;
-    const int wave_lo = min(first, rows - 1) / G, wave_hi = min(first + 31, rows - 1) / G;
+    const int r = min(first + (lane & 31), rows - 1), tok = token_of(r, sh.magic), head = hk * G + r - tok * G;
+    const int wave_lo = token_of(min(first, rows - 1), sh.magic), wave_hi = token_of(min(first + 31, rows - 1), sh.magic);
 
     const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
     TokenTiles<ND> kt(k, u, hk, d, wave, lane), vt(v, u, hk, d, wave, lane);
@@ -618,7 +622,7 @@ attn_join_out_kernel(AttnShape sh, const AttnList *__restrict__ list, const Attn
     if (at >= list->joins) return;
     const AttnUnit u = joins[at];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = u.len * sh.G, first = u.tile * kRowTile + wave * 32;
-    const int r = min(first + (lane & 31), rows - 1), tok = r / sh.G, head = hk * sh.G + r - tok * sh.G;
+    const int r = min(first + (lane & 31), rows - 1), tok = token_of(r, sh.magic), head = hk * sh.G + r - tok * sh.G;
     const float2 *mine = sums + (u.slot * sh.Hk + hk) * kRowTile + wave * 32 + (lane & 31);
     float top = -INFINITY, l = 0.0f;
 #pragma unroll 4
@@ -667,7 +671,7 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     AttnUnit u;
-    if (!source.find<false>(at, sh.G, u)) return;
+    if (!source.find<false>(at, sh.G, sh.magic, u)) return;
     u.make_uniform();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = sh.G, d = sh.d;
     if (u.tile < 0) {
@@ -677,8 +681,8 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
         return;
     }
     const int rows = u.len * G, first = u.tile * kRowTile + wave * 32;
-    const int r = min(first + (lane & 31), rows - 1), tok = r / G, head = hk * G + r - tok * G;
-    const int wave_lo = min(first, rows - 1) / G, wave_hi = min(first + 31, rows - 1) / G;
+    const int r = min(first + (lane & 31), rows - 1), tok = token_of(r, sh.magic), head = hk * G + r - tok * G;
+    const int wave_lo = token_of(min(first, rows - 1), sh.magic), wave_hi = token_of(min(first + 31, rows - 1), sh.magic);
     const bool live = first + (lane & 31) < rows;
 
     const uint32_t row_lane = Tile::row_lane(lane), col_lane = Tile::col_lane(lane);
@@ -760,16 +764,12 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
 }
 
 // ---------------------------------------------------------------- backward: keys and values
-// r / G: for r < 2^26 and G <= 64 the upper half of r * ceil(2^32 / G), whose excess over r / G, below r / 2^32 < 1 / G, never reaches the next integer.
-inline unsigned token_magic(int G) { return G == 1 ? 0u : (unsigned)(((1ull << 32) + G - 1) / G); }
-__device__ __forceinline__ int token_of(int r, unsigned magic) { return magic ? (int)__umulhi((unsigned)r, magic) : r; }
-
 // dk and dv of 64 keys over some of the packed rows behind the first of them.  Two waves share 32 keys: each works out p and ds for 32 of a step's
 // 64 rows, hands the other the half that it needs, and adds up one of the two gradients over all 64 rows.  A wave for itself would hold both sums,
 // 128 registers beside the operands' 64 and the scores' 32, and leave no room for a second wave on its SIMD.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
-attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ minus_delta, unsigned magic,
+attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ minus_delta,
                 UnitSource source, HeadsOut dk, HeadsOut dv, float *__restrict__ parts)
 {
     typedef AttnTile<ND, kRowStep> Tile;
@@ -778,7 +778,7 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves * 2048];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     AttnUnit u;
-    if (!source.find<true>(at, sh.G, u)) return;
+    if (!source.find<true>(at, sh.G, sh.magic, u)) return;
     u.make_uniform();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), role = wave & 1, G = sh.G, d = sh.d;   // role 0: dv, 1: dk
     if (u.tile < 0) {
@@ -798,12 +798,14 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     // quarter of a step's time.)  Other groups' and the last rows' are worked out lane by lane.
     constexpr int APART = kAttnWaves * Tile::RPB;
     const int sub = lane / Tile::SPR, col = min((lane % Tile::SPR) ^ Tile::swz(wave * Tile::RPB + sub), d / 8 - 1) * 8;
-    const bool alike = APART % G == 0;
-    const int top = u.to * kRowStep - APART + wave * Tile::RPB, top_tok = u.row0 + top / G, col0 = (hk * G + top % G) * d;
+    const unsigned magic = sh.magic;
+    const int apart = token_of(APART, magic), top = u.to * kRowStep - APART + wave * Tile::RPB, top_in = token_of(top, magic), top_tok = u.row0 + top_in;
+    const int col0 = (hk * G + top - top_in * G) * d, sub_in = token_of(sub, magic), stat_in = token_of((u.to - 1) * kRowStep + lane, magic);
+    const bool alike = apart * G == APART;
     const bf16_t *q_at = q.p + (long long)top_tok * q.ld + col0, *d_at = dout.p + (long long)top_tok * dout.ld + col0;
-    const long long q_apart = (long long)(APART / G) * q.ld, d_apart = (long long)(APART / G) * dout.ld;
-    const float *stat = wave == 0 ? lse2 : minus_delta, *stat_at = stat + (long long)(u.row0 + ((u.to - 1) * kRowStep + lane) / G) * sh.Hq + hk * G + lane % G;
-    const uint32_t q_off = (uint32_t)((sub / G) * q.ld + sub % G * d + col) * 2u, d_off = (uint32_t)((sub / G) * dout.ld + sub % G * d + col) * 2u;
+    const long long q_apart = (long long)apart * q.ld, d_apart = (long long)apart * dout.ld;
+    const float *stat = wave == 0 ? lse2 : minus_delta, *stat_at = stat + (long long)(u.row0 + stat_in) * sh.Hq + hk * G + ((u.to - 1) * kRowStep + lane - stat_in * G);
+    const uint32_t q_off = (uint32_t)(sub_in * q.ld + (sub - sub_in * G) * d + col) * 2u, d_off = (uint32_t)(sub_in * dout.ld + (sub - sub_in * G) * d + col) * 2u;
     auto load = [&](int t, int slot) __attribute__((always_inline)) {
         char *to = lds + slot * Tile::BYTES + wave * 1024, *stat_to = lds + STATS + (slot * 2 + wave) * kRowStep * 4;
         if (alike && t * kRowStep + kRowStep <= rows) {
@@ -945,7 +947,7 @@ attn_join_kernel(AttnShape sh, int row_joins, const AttnList *__restrict__ rows,
 #pragma unroll 4
     for (int c = 0; c < u.chunks; ++c) Part<ND>::add(parts, (u.slot + c) * sh.Hk + hk, wave, lane, n, 1.0f, acc[0]);
     const int first = of_keys ? u.tile * kKeyRows + (wave >> 1) * 32 : u.tile * kRowTile + wave * 32, count = of_keys ? u.len : u.len * sh.G;
-    const int mine = min(first + (lane & 31), count - 1), tok = of_keys ? mine : mine / sh.G, head = of_keys ? hk : hk * sh.G + mine - tok * sh.G;
+    const int mine = min(first + (lane & 31), count - 1), tok = of_keys ? mine : token_of(mine, sh.magic), head = of_keys ? hk : hk * sh.G + mine - tok * sh.G;
     const HeadsOut &to = !of_keys ? dq : wave & 1 ? dk : dv;
     store_row<1>(acc, of_keys && !(wave & 1) ? 1.0f : sh.scale, to.p + (long long)(u.row0 + tok) * to.ld + head * sh.d + n * 32, sh.d - n * 32, lane, first + (lane & 31) < count);
 }
@@ -953,8 +955,8 @@ attn_join_kernel(AttnShape sh, int row_joins, const AttnList *__restrict__ rows,
 // ---------------------------------------------------------------- host
 inline int attn_nd(int d) { return (d + 31) / 32; }
 // Lists: at most so many units, joined tiles and partial sums a key head, for rows and for keys.  A token is a sequence's or padding's, and padding
-// takes no more places than it would as rows or keys, but for a tile a sequence.  A chunk has at least a fair share's worth (half of it: keys) of all heads' steps, and a least number of them; tiles of two or
-// more chunks have at most twice as many as their steps make whole ones.
+// takes no more places than it would as rows or keys, but for a tile a sequence.  Chunks have at least c steps: a fair share's worth (half of it: keys) of all steps, and a
+// least number of them.  A tile of x > c steps has fewer than x / c + 1 < 2 x / c of them, all together fewer than twice their steps / c.
 struct AttnSizes {
     int units, joins, slots;
     size_t part_bytes;
@@ -1011,7 +1013,7 @@ inline SchedOut sched_out(char *&ws, const AttnSizes &s)
     AttnList *head = (AttnList *)ws;
     AttnUnit *units = (AttnUnit *)(head + 1);
     ws += s.list_bytes();
-    return SchedOut{head, units, units + s.units, s.units, s.slots};
+    return SchedOut{head, units, units + s.units, s.slots > 0};
 }
 inline int check_attn(const int32_t *seq_start, int n_seq, int T, int Hq, int Hk, int d, float scale, const int32_t *err_flag)
 {
@@ -1054,12 +1056,12 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
     const SchedOut rows = sched_out(ws, sz);
     float *parts = (float *)ws;
     float2 *sums = (float2 *)(ws + sz.part_bytes);
-    const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
+    const AttnShape sh{T, Hq, Hk, Hq / Hk, d, token_magic(Hq / Hk), scale};
     const HeadsOut oo{(bf16_t *)out, out_stride};
     const bool listed = sz.joins > 0 || !unlisted(sz, n_seq, Hk);
     const UnitSource source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
     if (listed)
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, rows, err_flag));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, sh.magic, Hk, rows, rows, err_flag));
     attn_layout(d, [&](auto nd) {
         constexpr int ND = decltype(nd)::value;
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_FWD, stream, (attn_fwd_kernel<ND><<<sz.units * Hk, kAttnThreads, 0, stream>>>(
@@ -1099,20 +1101,19 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
     const SchedOut rows = sched_out(ws, rs), keys = sched_out(ws, ks);
     float *row_parts = (float *)ws, *key_parts = (float *)(ws += rs.part_bytes);
     float *lse2 = (float *)(ws += ks.part_bytes), *delta = (float *)(ws + round256((size_t)T * Hq * sizeof(float)));
-    const AttnShape sh{T, Hq, Hk, Hq / Hk, d, scale};
+    const AttnShape sh{T, Hq, Hk, Hq / Hk, d, token_magic(Hq / Hk), scale};
     const HeadsIn qi{(const bf16_t *)q, q_stride}, ki{(const bf16_t *)k, k_stride}, vi{(const bf16_t *)v, v_stride}, oi{(const bf16_t *)out, out_stride},
         di{(const bf16_t *)dout, dout_stride};
     const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
-    const unsigned magic = token_magic(sh.G);
     const bool listed = rs.joins > 0 || tiles_of((long long)T * sh.G, kRowStep) > 2 * kMinKeyChunk || !unlisted(rs, n_seq, Hk) || !unlisted(ks, n_seq, Hk);
     const UnitSource row_source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
     const UnitSource key_source{listed ? keys.head : nullptr, keys.units, seq_start, seq_len, n_seq, T, err_flag};
     if (listed)
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<2, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, Hk, rows, keys, err_flag));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<2, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, sh.magic, Hk, rows, keys, err_flag));
     attn_layout(d, [&](auto nd) {
         constexpr int ND = decltype(nd)::value;
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, row_source, dqo, lse2, delta, row_parts)));
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, magic, key_source, dko, dvo, key_parts)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, key_source, dko, dvo, key_parts)));
         if (listed && rs.joins + ks.joins > 0)
             RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<(rs.joins + ks.joins) * Hk * ND, kAttnThreads, 0, stream>>>(
                 sh, rs.joins, rows.head, rows.joins, row_parts, dqo, keys.head, keys.joins, key_parts, dko, dvo)));
