@@ -4,12 +4,21 @@
 //   D_i = do_i . o_i;  ds_ij = p_ij (do_i . v_j - D_i);  dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij do_i
 //
 // The G query heads of a key head are rows of one matrix: packed row r of a sequence is token r / G, head r % G of the group.  A block takes
-// 128 packed rows (forward, dq) or 128 keys (dk, dv) of one key head, 32 a wave, and walks the other side in tiles of 64 through LDS, two
+// 128 packed rows (forward, dq; 32 a wave) or 64 keys (dk, dv; 32 for two waves) of one key head, and walks the other side in tiles of 64 through LDS, two
 // tiles in turn, filled by direct loads.  Products are MFMA 32x32x16 with the block's own side on the lanes: a lane then holds one row's
 // (one key's) scores in its registers, so that softmax statistics and rescaling are a lane's own work, and the exponentials, rounded
 // to bf16, are the next product's operand as they lie: MFMA does not care for the order of the contracted index as long as both sides
 // agree, so the other side is read (by transposing LDS reads) in the order that the registers have.  Everything else is fp32.  Gradients
 // are computed from the scores again in two kernels, seven products where five would do with atomics: fixed order, the same bits every call.
+//
+// Roundings: p and ds to bf16 for their products, whose operands have one type (2^-8 of a term at most; the terms' errors are independent and cost the
+// sum about what its own rounding does), and D has the error that `out` was rounded with.  dq and dk are 0.0025 to 0.0029 off (root mean square over
+// that of the result), where the last rounding alone costs 0.0017; an exact D would bring them to 0.0024, for a fourth product in the queries' kernel.
+//
+// Long calls are bound by the matrix units at the clock that the chip's power leaves them, 1.6 to 1.9 GHz of 2.4: one sequence of 16384 tokens, 32
+// heads of 4 key heads of 128, forward 2000 us, 1100 TFLOP/s; a loop of the bare products reaches 1900, with one LDS read a product 1710, with the
+// softmax's vector work as well 1460, and the library's product of 8192 x 8192 matrices 1390.  Short sequences are bound by blocks' beginnings and ends (a
+// micro-batch of 24 sequences, 16384 tokens in all, 64 heads: 462 us, 850 TFLOP/s), small calls by launches and the latency of one block's chain.
 #include "gemm_tile.h"
 #include "head_rows.h"
 #include "wave_ops.h"
@@ -20,10 +29,11 @@
 namespace relibra {
 
 constexpr int kAttnThreads = 256, kAttnWaves = 4;
-constexpr int kRowTile = 128;                                // packed rows of a block, keys of a step
-constexpr int kKeyTile = 64;
-constexpr int kKeyRows = 64;                                 // keys' gradients: keys of a block, packed rows of a step
-constexpr int kRowStep = 64;
+// Packed rows of a block and keys of a step.  Blocks of 256 rows and 8 waves: the long sequence 1.3 % faster, the packed micro-batch 3.5 % slower.
+constexpr int kRowTile = 128, kKeyTile = 64;
+// Gradients of keys: keys of a block and packed rows of a step.  128 keys and 8 waves: the long sequence's launch 1128 -> 1097 us with two tiles in
+// LDS, but 2 to 3 % slower in all with three and one barrier a step, and a packed micro-batch has too few long tiles for it.
+constexpr int kKeyRows = 64, kRowStep = 64;
 constexpr int kAttnMaxDim = 128, kAttnMaxSeq = 8192, kAttnMaxGroup = 64;
 constexpr int kAttnMaxRows = 1 << 26;                        // packed rows of a key head
 constexpr int kAttnSlots = 512;                              // blocks that run at once: two a unit
@@ -219,10 +229,15 @@ template <int ND> struct TokenTiles {
 // Lists the blocks' work, heaviest first: one block for the rows, one for the keys.  Sequences are counted (their tiles, and those of the padding behind
 // them), every thread finds the sequence of its share of the tiles by bisection, and a counting sort by work puts them in order (within a
 // bin in any order: results do not depend on it).  A table that does not ascend within [0, T], or lengths beyond their places: nothing is listed.
-// A tile with more than `chunk` steps is several blocks', whose partial sums a second kernel joins.  Rows: where a fair share of all steps is less than
-// the longest tile's, so that one long tile does not outlast the rest (8 steps at least: a join costs what four do).  Keys: two chunks to each of
-// the blocks that run at once, or one where that leaves few steps.
+// A tile with more than `chunk` steps is several blocks', whose partial sums a second kernel joins.  Rows: a fair share of all steps a block, so that one long
+// tile does not outlast the rest, 8 at least (4, 8, 16: 9 sequences in 4999 tokens of 12 heads 37.5, 35.5, 36.9 us; one of 2048 of 8 heads 37.1, 36.8, 35.9,
+// backward 79.0, 79.4, 83.4).  Keys: two chunks to each of the blocks that run at once, of 16 steps at least (8, 16, 32: that backward 89.1, 79.4, 79.8 us), or
+// one of 4 (4, 8: 5 sequences in 901 tokens of 10 heads backward 33.2, 35.1 us).
+// 8 to 11 us of latencies in a row for any table: what calls it is large, or needs shared tiles.
 constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinRowChunk = 8, kMinKeyChunk = 4, kFullKeyChunk = 16;
+// Whether rows are shared at all, from T and Hq alone: where the longest possible tile has so many steps more than the rest of the chip needs meanwhile.
+// Not shared / shared: one sequence of 16384 tokens and 1 head 259 / 106 us, 4096 of 8 heads 77 / 64, 8192 of 8 heads 174 / 169; 1024 of 32 heads 30 / 34,
+// 4096 of 16 heads 95 / 100, 8192 of 12 heads 216 / 231.
 constexpr int kShareTiles = 768, kFwdShareSteps = 24, kBwdShareSteps = 12;
 
 __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // inclusive; two barriers
@@ -284,7 +299,8 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
                 tiles = own + tiles_of(b - a - len, kRowTile);
                 // keys: the sum of ceil(len G / 64) - G t over the tiles t;  rows: no less than that of (128 t + 127) / (64 G) + 1
                 const long long n = own;
-                if (own) atomicAdd(&steps, (unsigned long long)(KEYS ? n * tiles_of((long long)len * G, kRowStep) - (long long)G * n * (n - 1) / 2 : (long long)((double)(n * (n + 1)) / G) + 1 + n));
+                const long long key_steps = n * tiles_of((long long)len * G, kRowStep) - (long long)G * n * (n - 1) / 2, row_steps = (long long)((double)(n * (n + 1)) / G) + 1 + n;
+                if (own) atomicAdd(&steps, (unsigned long long)(KEYS ? key_steps : row_steps));
             }
         }
         int total;
@@ -368,8 +384,8 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
     if (tid == 0) to.head->count = total, to.head->joins = n_joins;
 }
 
-// Where a block finds its unit: in the list, or, for calls of at most 64 sequences whose tiles all run at once and are shared by nobody, from the tables
-// itself, a sequence a lane: no scheduling launch (one prompt of 33 tokens, 32 heads: 12.5 -> 9 us).
+// Where a block finds its unit: in the list, or, where no tile is shared and sequences are few, from the tables itself, a sequence a lane, the longest
+// tiles of each sequence first: no scheduling launch (one prompt of 33 tokens, 32 heads: 14.2 -> 10.4 us; 1024 tokens of 64 heads 34.7 -> 29.1).
 struct UnitSource {
     const AttnList *list;                                     // NULL: from the tables
     const AttnUnit *units;
@@ -398,7 +414,8 @@ struct UnitSource {
         }
         const unsigned long long behind = __ballot(upto > at);
         if (!behind) return false;
-        const int mine = __builtin_ctzll(behind), t = at - __shfl(upto - tiles, mine), row0 = __shfl(a, mine), end = __shfl(b, mine), n = __shfl(len, mine), n_own = __shfl(own, mine);
+        const int mine = __builtin_ctzll(behind), t = at - __shfl(upto - tiles, mine), row0 = __shfl(a, mine), end = __shfl(b, mine), n = __shfl(len, mine);
+        const int n_own = __shfl(own, mine);
         u.slot = -1, u.chunks = 1, u.from = 0, u.to = 0, u.row0 = row0, u.len = n;
         if (t >= n_own) u.row0 = row0 + n + (t - n_own) * kRowTile, u.len = min(kRowTile, end - u.row0), u.tile = -1;
         else if (KEYS) u.tile = t, u.from = G * t, u.to = tiles_of((long long)n * G, kRowStep);
@@ -434,6 +451,8 @@ template <int ND> struct Part {
 };
 
 // ---------------------------------------------------------------- forward
+// One pass over the keys with a running maximum and sum.  A step of a wave is 32 products of 32x32x16 (d = 128), 32 exponentials a lane and 24 LDS reads; the
+// order below keeps the first two side by side (ragged batch 46.9 -> 38.5 us; long calls spend the 14 % of cycles on a lower clock: 2100 -> 2083).
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source, HeadsOut out, float *__restrict__ lse,
@@ -662,10 +681,12 @@ __device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x
 }
 
 // ---------------------------------------------------------------- backward: queries
-// dq of 128 packed rows, and for the other kernel each row's lse in powers of two and -D.
+// dq of 128 packed rows, and for the other kernel each row's lse in powers of two and -D.  Three products a step; scores are not kept, p comes from lse.
+// One sequence of 8192 tokens, 32 heads with keys of their own: 700 us, 1180 TFLOP/s of its three products.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
-attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, UnitSource source, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ minus_delta, float *__restrict__ parts)
+attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, UnitSource source, HeadsOut dq,
+               float *__restrict__ lse2, float *__restrict__ minus_delta, float *__restrict__ parts)
 {
     typedef AttnTile<ND> Tile;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
@@ -766,7 +787,8 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
 // ---------------------------------------------------------------- backward: keys and values
 // dk and dv of 64 keys over some of the packed rows behind the first of them.  Two waves share 32 keys: each works out p and ds for 32 of a step's
 // 64 rows, hands the other the half that it needs, and adds up one of the two gradients over all 64 rows.  A wave for itself would hold both sums,
-// 128 registers beside the operands' 64 and the scores' 32, and leave no room for a second wave on its SIMD.
+// 128 registers beside the operands' 64 and the scores' 32, and leave no room for a second wave on its SIMD (the long sequence 2260 -> 1190 us).
+// Four products a step, two barriers: 1100 us, 1000 TFLOP/s for 8192 tokens of 32 heads with keys of their own; without any loads it took 930.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ minus_delta,
@@ -1004,7 +1026,9 @@ size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
     const AttnSizes r = row_sizes(T, n_seq, Hq, Hk, d, true), k = key_sizes(T, n_seq, Hq, Hk, d);
     return r.list_bytes() + r.part_bytes + k.list_bytes() + k.part_bytes + 2 * round256((size_t)T * Hq * sizeof(float));
 }
-// Whether blocks may find their units themselves.
+// Whether blocks may find their units themselves.  One sequence's are in the list's order without it.  Several sequences' are not in order among each other, which
+// costs calls of many rounds of blocks what the list does (8 sequences in 4096 tokens of 64 heads, 4096 units: 98.2 with the list, 94.9 without; 24
+// in 8192 of 16 heads, 1100: 57.1 and 60.2; 8 in 2048 of 64 heads: 41.4 and 34.0).
 constexpr int kUnlisted = 4096;
 inline bool unlisted(const AttnSizes &s, int n_seq, int Hk) { return n_seq == 1 || (n_seq <= 64 && (long long)s.units * Hk <= kUnlisted); }
 // A list in the workspace, and the next free byte behind it.
@@ -1067,7 +1091,8 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_FWD, stream, (attn_fwd_kernel<ND><<<sz.units * Hk, kAttnThreads, 0, stream>>>(
             sh, HeadsIn{(const bf16_t *)q, q_stride}, HeadsIn{(const bf16_t *)k, k_stride}, HeadsIn{(const bf16_t *)v, v_stride}, source, oo, lse, parts, sums)));
         if (listed && sz.joins > 0)
-            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_out_kernel<ND><<<sz.joins * Hk * ND, kAttnThreads, 0, stream>>>(sh, rows.head, rows.joins, parts, sums, oo, lse)));
+            RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_out_kernel<ND><<<sz.joins * Hk * ND, kAttnThreads, 0, stream>>>(
+                sh, rows.head, rows.joins, parts, sums, oo, lse)));
     });
     RELIBRA_HIP_TRY(launch_check());
     return RELIBRA_OK;
@@ -1112,8 +1137,10 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<2, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, sh.magic, Hk, rows, keys, err_flag));
     attn_layout(d, [&](auto nd) {
         constexpr int ND = decltype(nd)::value;
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, oi, di, lse, row_source, dqo, lse2, delta, row_parts)));
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(sh, qi, ki, vi, di, lse2, delta, key_source, dko, dvo, key_parts)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk, kAttnThreads, 0, stream>>>(
+            sh, qi, ki, vi, oi, di, lse, row_source, dqo, lse2, delta, row_parts)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(
+            sh, qi, ki, vi, di, lse2, delta, key_source, dko, dvo, key_parts)));
         if (listed && rs.joins + ks.joins > 0)
             RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<(rs.joins + ks.joins) * Hk * ND, kAttnThreads, 0, stream>>>(
                 sh, rs.joins, rows.head, rows.joins, row_parts, dqo, keys.head, keys.joins, key_parts, dko, dvo)));
