@@ -138,13 +138,13 @@ __device__ __forceinline__ bf16x8_t pack_half(const f32x16_t &v, int j)
                                                 pack2bf(v[8 * j + 6], v[8 * j + 7])});
 }
 
-// A lane's own row as a product's operand: values kk * 16 + lane / 32 * 8 .. + 7 of `row`, zeros from d on.
+// A lane's own row as a product's operand: values kk * 16 + lane / 32 * 8 .. + 7 of `row`, zeros from d on (d > 32 (ND - 1)).
 template <int ND> __device__ __forceinline__ void load_row(bf16x8_t (&f)[2 * ND], const bf16_t *row, int d, int lane)
 {
 #pragma unroll
     for (int kk = 0; kk < 2 * ND; ++kk) {
         const int c = kk * 16 + (lane >> 5) * 8;
-        const uint4 v = c < d ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0, 0, 0, 0);
+        const uint4 v = kk < 2 * ND - 2 || c < d ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0, 0, 0, 0);
         f[kk] = __builtin_bit_cast(bf16x8_t, v);
     }
 }
@@ -161,7 +161,7 @@ template <int ND> __device__ __forceinline__ void store_row(const f32x16_t (&acc
             uint32_t b0 = pack2bf(v[8 * p + 4] * by, v[8 * p + 5] * by), b1 = pack2bf(v[8 * p + 6] * by, v[8 * p + 7] * by);
             const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
             const int c = n * 32 + p * 16 + (lane >> 5) * 8;
-            if (live && c < d) *reinterpret_cast<uint4 *>(row + c) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
+            if (live && (n < ND - 1 || c < d)) *reinterpret_cast<uint4 *>(row + c) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
         }
 }
 
