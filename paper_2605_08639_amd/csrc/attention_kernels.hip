@@ -1041,7 +1041,7 @@ inline SchedOut sched_out(char *&ws, const AttnSizes &s)
 }
 inline int check_attn(const int32_t *seq_start, int n_seq, int T, int Hq, int Hk, int d, float scale, const int32_t *err_flag)
 {
-    if (T < 0 || n_seq < 0 || Hq < 1 || Hk < 1 || Hq % Hk || d < 8 || !(scale > 0.0f) || scale > 3e38f) return RELIBRA_EINVAL;
+    if (T < 0 || n_seq < 0 || Hq < 1 || Hk < 1 || Hq % Hk || d < 8 || !(scale > 0.0f) || scale > 1e38f) return RELIBRA_EINVAL;
     if (!attn_takes(T, n_seq, Hq, Hk, d)) return RELIBRA_EUNSUPPORTED;
     if (T > 0 && n_seq > 0 && (!seq_start || !err_flag)) return RELIBRA_EINVAL;
     return RELIBRA_OK;

@@ -118,6 +118,19 @@ def test_attention_against_the_definition(name):
     check(c, run(c))
 
 
+# Long sequences of few heads: tiles that several blocks share, in both directions; many heads of short ones: lists without shared tiles.
+LONG = dict(
+    two_heads=dict(places=[1700, 300], Hk=1, G=2, d=128), threes_padded=dict(places=[900, 1150], lens=[850, 1149], Hk=2, G=3, d=80, before=5, behind=9),
+    eight_heads=dict(places=[2000], Hk=1, G=8, d=40), keys_of_their_own=dict(places=[64, 1800, 1], Hk=3, G=1, d=104), many_heads=dict(places=[300, 130, 270], lens=[300, 129, 260], Hk=512, G=1, d=8))
+
+
+@gpu
+@pytest.mark.parametrize("name", LONG)
+def test_attention_of_long_sequences_and_many_heads(name):
+    c = make(**LONG[name], seed=21)
+    check(c, run(c))
+
+
 @gpu
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("shape", ["peaked", "rising", "falling", "flat", "huge"])
@@ -296,11 +309,12 @@ def test_attention_of_as_many_sequences_as_there_may_be():
 
 
 @gpu
-def test_attention_in_a_graph_beside_eager_calls():
-    c = make([300, 129, 500], 2, 4, 128, lens=[300, 100, 481], seed=10)
+@pytest.mark.parametrize("places,lens,Hk,G", [([300, 129, 500], [300, 100, 481], 2, 4), ([1700, 200, 40], [1690, 100, 40], 1, 2)], ids=["short", "shared"])
+def test_attention_in_a_graph_beside_eager_calls(places, lens, Hk, G):
+    c = make(places, Hk, G, 128, lens=lens, seed=10)
     start, length = tables(c)
     d = {n: c[n].to(DEV) for n in ("q", "k", "v", "dout")}
-    ws = dict(f=rl.attention_fwd_workspace(c["T"], 3, 8, 2, 128), b=rl.attention_bwd_workspace(c["T"], 3, 8, 2, 128))
+    ws = dict(f=rl.attention_fwd_workspace(c["T"], 3, Hk * G, Hk, 128), b=rl.attention_bwd_workspace(c["T"], 3, Hk * G, Hk, 128))
     flag = rl.new_err_flag()
 
     def step(q, f=None, b=None):
@@ -315,7 +329,7 @@ def test_attention_in_a_graph_beside_eager_calls():
     side = torch.cuda.Stream()
     for turn in range(3):
         src.copy_(d["q"] * (turn + 1))
-        length.copy_(torch.tensor([300 - turn, 100 + turn, 481], dtype=torch.int32))       # the schedule is made on the device
+        length.copy_(torch.tensor([lens[0] - turn, lens[1] + turn, lens[2]], dtype=torch.int32))       # the schedule is made on the device
         want = step(src.clone())
         graph.replay()
         torch.cuda.synchronize()
@@ -326,6 +340,34 @@ def test_attention_in_a_graph_beside_eager_calls():
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(again, want)), turn
     assert flag.item() == 0
+
+
+@gpu
+def test_attention_of_two_streams_at_once():
+    """Calls that overlap, each with a workspace and a flag of its own, one of them with a table that is refused."""
+    c = make([1700, 300], 1, 2, 128, seed=11)
+    start, _ = tables(c)
+    bad = torch.tensor([0, 1800, 1700], dtype=torch.int32, device=DEV)
+    d = {n: c[n].to(DEV) for n in ("q", "k", "v", "dout")}
+    flags = [rl.new_err_flag() for _ in range(2)]
+
+    def step(table, flag):
+        out, lse = torch.full((c["T"], 2, 128), 3.0, dtype=BF16, device=DEV), torch.full((c["T"], 2), 3.0, device=DEV)
+        rl.relibra_attention_fwd(d["q"], d["k"], d["v"], table, out=out, lse=lse, err_flag=flag)
+        grads = [torch.full((c["T"], h, 128), 3.0, dtype=BF16, device=DEV) for h in (2, 1, 1)]
+        rl.relibra_attention_bwd(d["q"], d["k"], d["v"], out, lse, d["dout"], table, dq=grads[0], dk=grads[1], dv=grads[2], err_flag=flag)
+        return (out, lse, *grads)
+    want = step(start, flags[0])
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(5):
+        for s, table, flag in zip(side, (start, bad), flags):
+            with torch.cuda.stream(s):
+                got.append(step(table, flag))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x in got[::2] for a, b in zip(x, want)) and all(torch.all(a == 3) for x in got[1::2] for a in x)
+    assert [f.item() for f in flags] == [0, rl.ERR_SEQ_TABLE]
 
 
 @gpu
