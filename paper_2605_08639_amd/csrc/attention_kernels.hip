@@ -35,6 +35,7 @@ constexpr int kRowTile = 128, kKeyTile = 64;
 // LDS, but 2 to 3 % slower in all with three and one barrier a step, and a packed micro-batch has too few long tiles for it.
 constexpr int kKeyRows = 64, kRowStep = 64;
 constexpr int kAttnMaxDim = 128, kAttnMaxSeq = 8192, kAttnMaxGroup = 64;
+constexpr int kSelfSeq = 64;                                 // sequences of calls whose blocks find their units themselves: a lane each
 constexpr int kAttnMaxRows = 1 << 26;                        // packed rows of a key head
 constexpr int kAttnSlots = 512;                              // blocks that run at once: two a unit
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -233,14 +234,15 @@ template <int ND> struct TokenTiles {
 // tile does not outlast the rest, 8 at least (4, 8, 16: 9 sequences in 4999 tokens of 12 heads 37.5, 35.5, 36.9 us; one of 2048 of 8 heads 37.1, 36.8, 35.9,
 // backward 79.0, 79.4, 83.4).  Keys: two chunks to each of the blocks that run at once, of 16 steps at least (8, 16, 32: that backward 89.1, 79.4, 79.8 us), or
 // one of 4 (4, 8: 5 sequences in 901 tokens of 10 heads backward 33.2, 35.1 us).
-// 8 to 11 us of latencies in a row for any table: what calls it is large, or needs shared tiles.
+// 7 to 11 us of latencies in a row for any table: worth a launch where rows are shared or units are many; else it makes only the keys' list, beside dq.
 constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinRowChunk = 8, kMinKeyChunk = 4, kFullKeyChunk = 16;
-// Whether rows are shared at all, from T and Hq alone: where the longest possible tile has so many steps more than the rest of the chip needs meanwhile.
-// Not shared / shared: one sequence of 16384 tokens and 1 head 259 / 106 us, 4096 of 8 heads 77 / 64, 8192 of 8 heads 174 / 169; 1024 of 32 heads 30 / 34,
-// 4096 of 16 heads 95 / 100, 8192 of 12 heads 216 / 231.
-constexpr int kShareTiles = 768, kFwdShareSteps = 24, kBwdShareSteps = 12;
+// Whether rows are shared at all, from T and Hq alone: where the longest possible tile has so many steps more than the rest of the chip needs meanwhile
+// that it pays for the list, partial sums and (forward; the keys have it anyway) the join's launch.  One sequence, not shared / shared, us: 16384 tokens of
+// 1 head 254 / 106, 4096 of 8 heads 72 / 65, 8192 of 8 169 / 168, 2048 of 8 37 / 36, 1024 of 32 24 / 33; 8 sequences in 8192 of 4 heads 54 / 47, in 4096 of 8
+// 31 / 34, of 12 33 / 44.  Backward one of 2048 of 8 heads 86 / 72, of 16 115 / 115, of 32 168 / 172; 5 in 901 of 10 29 / 35.
+constexpr int kShareTiles = 640, kFwdShareSteps = 32, kBwdShareSteps = 24;
 
-__device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // inclusive; two barriers
+template <int THREADS> __device__ __forceinline__ int scan_block(int v, int *sums, int &total)      // inclusive; two barriers
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -252,7 +254,7 @@ __device__ __forceinline__ int scan1024(int v, int *sums, int &total)      // in
     __syncthreads();
     total = 0;
 #pragma unroll
-    for (int w = 0; w < kSchedThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < wave) v += sums[w];
         total += sums[w];
     }
@@ -271,22 +273,27 @@ struct SchedOut {
     int share;                                                // whether long tiles may be several blocks'
 };
 
-__global__ void __launch_bounds__(kSchedThreads)
-attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, unsigned magic, int Hk, SchedOut row_out, SchedOut key_out,
-                  int32_t *err_flag)
+template <int THREADS, int SEQ> struct SchedLds {
+    unsigned long long steps;
+    int before[SEQ + 1], starts[SEQ + 1], lens[SEQ];          // tiles of the sequences before; the tables
+    int bins[kSchedBins], sums[THREADS / 64], n_slots, n_joins;
+};
+
+// One block of THREADS, at most SEQ sequences.
+template <int THREADS, int SEQ>
+__device__ __forceinline__ void schedule(bool KEYS, const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, unsigned magic, int Hk,
+                                         const SchedOut &to, int32_t *err_flag, SchedLds<THREADS, SEQ> &lds)
 {
-    const bool KEYS = blockIdx.x == 1;
-    const SchedOut to = KEYS ? key_out : row_out;
-    __shared__ int before[kAttnMaxSeq + 1], starts[kAttnMaxSeq + 1], lens[kAttnMaxSeq];       // tiles of the sequences before; the tables
-    __shared__ int bins[kSchedBins], sums[kSchedThreads / 64], n_slots, n_joins;
-    __shared__ unsigned long long steps;
+    auto &[steps, before, starts, lens, bins, sums, n_slots, n_joins] = lds;
+    constexpr int PER = kSchedBins / THREADS;
     const int tid = threadIdx.x;
     if (tid == 0) steps = 0, n_slots = 0, n_joins = 0, before[0] = 0;
-    bins[tid] = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) bins[tid * PER + i] = 0;
     __syncthreads();
     bool bad = false;
     int carry = 0;
-    for (int s0 = 0; s0 < n_seq; s0 += kSchedThreads) {
+    for (int s0 = 0; s0 < n_seq; s0 += THREADS) {
         const int s = s0 + tid;
         int tiles = 0;
         if (s < n_seq) {
@@ -304,7 +311,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
             }
         }
         int total;
-        const int incl = scan1024(tiles, sums, total);
+        const int incl = scan_block<THREADS>(tiles, sums, total);
         if (s < n_seq) before[s + 1] = carry + incl;
         carry += total;
     }
@@ -332,7 +339,7 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
-        for (int f = tid; f < flat; f += kSchedThreads) {
+        for (int f = tid; f < flat; f += THREADS) {
             int lo = 0, hi = n_seq;                           // the last sequence with before[s] <= f
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -376,12 +383,29 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
         }
         __syncthreads();
         if (!pass) {
-            const int mine = bins[kSchedBins - 1 - tid], upto = scan1024(mine, sums, total);
-            bins[kSchedBins - 1 - tid] = upto - mine;         // heaviest first
+            int *mine = bins + kSchedBins - 1 - tid * PER, sum = 0;            // heaviest first
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum += mine[-i];
+            int at = scan_block<THREADS>(sum, sums, total) - sum;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int n = mine[-i];
+                mine[-i] = at;
+                at += n;
+            }
             __syncthreads();
         }
     }
     if (tid == 0) to.head->count = total, to.head->joins = n_joins;
+}
+
+__global__ void __launch_bounds__(kSchedThreads)
+attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restrict__ seq_len, int n_seq, int T, int G, unsigned magic, int Hk, SchedOut row_out, SchedOut key_out,
+                  int32_t *err_flag)
+{
+    __shared__ SchedLds<kSchedThreads, kAttnMaxSeq> lds;
+    const bool keys = blockIdx.x == 1;
+    schedule(keys, seq_start, seq_len, n_seq, T, G, magic, Hk, keys ? key_out : row_out, err_flag, lds);
 }
 
 // Where a block finds its unit: in the list, or, where no tile is shared and sequences are few, from the tables itself, a sequence a lane, the longest
@@ -685,12 +709,18 @@ __device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x
 // One sequence of 8192 tokens, 32 heads with keys of their own: 700 us, 1180 TFLOP/s of its three products.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
-attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, UnitSource source, HeadsOut dq,
-               float *__restrict__ lse2, float *__restrict__ minus_delta, float *__restrict__ parts)
+attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, UnitSource source,
+               int with_keys, SchedOut key_out, HeadsOut dq, float *__restrict__ lse2, float *__restrict__ minus_delta, float *__restrict__ parts)
 {
     typedef AttnTile<ND> Tile;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
-    const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
+    if (blockIdx.x < with_keys) {                             // the first block makes the keys' list meanwhile
+        auto &work = *reinterpret_cast<SchedLds<kAttnThreads, kSelfSeq> *>(lds);
+        static_assert(sizeof(work) <= sizeof(lds));
+        schedule(true, source.seq_start, source.seq_len, source.n_seq, sh.T, sh.G, sh.magic, sh.Hk, key_out, source.err_flag, work);
+        return;
+    }
+    const int block = blockIdx.x - with_keys, at = block / sh.Hk, hk = block - at * sh.Hk;
     AttnUnit u;
     if (!source.find<false>(at, sh.G, sh.magic, u)) return;
     u.make_uniform();
@@ -994,8 +1024,6 @@ inline AttnSizes attn_sizes(long long tiles, long long most, long long whole, in
     s.part_bytes = round256((size_t)s.slots * Hk * kAttnWaves * attn_nd(d) * 16 * 64 * sizeof(float));
     return s;
 }
-// Rows are shared where the longest tile can outlast the rest by enough steps to pay for partial sums and the join's launch, which is there
-// anyway for the keys in the backward pass.
 inline AttnSizes row_sizes(int T, int n_seq, int Hq, int Hk, int d, bool bwd)
 {
     const int G = Hq / Hk, most = tiles_of(T, kKeyTile);
@@ -1011,7 +1039,7 @@ inline AttnSizes key_sizes(int T, int n_seq, int Hq, int Hk, int d)
 inline bool attn_takes(int T, int n_seq, int Hq, int Hk, int d)
 {
     if (d % 8 || d > kAttnMaxDim || n_seq > kAttnMaxSeq || Hq / Hk > kAttnMaxGroup || Hq > 4096 || (long long)T * (Hq / Hk) > kAttnMaxRows) return false;
-    return (long long)std::max(row_sizes(T, n_seq, Hq, Hk, d, true).units, key_sizes(T, n_seq, Hq, Hk, d).units) * Hk < (1ll << 32) / kAttnThreads;
+    return (long long)std::max(row_sizes(T, n_seq, Hq, Hk, d, true).units, key_sizes(T, n_seq, Hq, Hk, d).units) * Hk < (1ll << 32) / kAttnThreads - 1;
 }
 inline size_t row_sum_bytes(const AttnSizes &s, int Hk) { return round256((size_t)s.slots * Hk * kRowTile * sizeof(float2)); }
 size_t attn_fwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
@@ -1030,7 +1058,7 @@ size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
 // costs calls of many rounds of blocks what the list does (8 sequences in 4096 tokens of 64 heads, 4096 units: 98.2 with the list, 94.9 without; 24
 // in 8192 of 16 heads, 1100: 57.1 and 60.2; 8 in 2048 of 64 heads: 41.4 and 34.0).
 constexpr int kUnlisted = 4096;
-inline bool unlisted(const AttnSizes &s, int n_seq, int Hk) { return n_seq == 1 || (n_seq <= 64 && (long long)s.units * Hk <= kUnlisted); }
+inline bool unlisted(const AttnSizes &s, int n_seq, int Hk) { return n_seq == 1 || (n_seq <= kSelfSeq && (long long)s.units * Hk <= kUnlisted); }
 // A list in the workspace, and the next free byte behind it.
 inline SchedOut sched_out(char *&ws, const AttnSizes &s)
 {
@@ -1130,18 +1158,21 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
     const HeadsIn qi{(const bf16_t *)q, q_stride}, ki{(const bf16_t *)k, k_stride}, vi{(const bf16_t *)v, v_stride}, oi{(const bf16_t *)out, out_stride},
         di{(const bf16_t *)dout, dout_stride};
     const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
-    const bool listed = rs.joins > 0 || tiles_of((long long)T * sh.G, kRowStep) > 2 * kMinKeyChunk || !unlisted(rs, n_seq, Hk) || !unlisted(ks, n_seq, Hk);
-    const UnitSource row_source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
-    const UnitSource key_source{listed ? keys.head : nullptr, keys.units, seq_start, seq_len, n_seq, T, err_flag};
-    if (listed)
+    // Rows' units are found without a list where they may be; keys' only if no tile of theirs could be shared, and their list is then made beside dq.
+    const bool rows_listed = rs.joins > 0 || !unlisted(rs, n_seq, Hk);
+    const bool keys_listed = rows_listed || tiles_of((long long)T * sh.G, kRowStep) > 2 * kMinKeyChunk || !unlisted(ks, n_seq, Hk);
+    const int beside = keys_listed && !rows_listed;
+    const UnitSource row_source{rows_listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
+    const UnitSource key_source{keys_listed ? keys.head : nullptr, keys.units, seq_start, seq_len, n_seq, T, err_flag};
+    if (rows_listed)
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<2, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, sh.magic, Hk, rows, keys, err_flag));
     attn_layout(d, [&](auto nd) {
         constexpr int ND = decltype(nd)::value;
-        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk, kAttnThreads, 0, stream>>>(
-            sh, qi, ki, vi, oi, di, lse, row_source, dqo, lse2, delta, row_parts)));
+        RELIBRA_LAUNCH(RELIBRA_K_ATTN_DQ, stream, (attn_dq_kernel<ND><<<rs.units * Hk + beside, kAttnThreads, 0, stream>>>(
+            sh, qi, ki, vi, oi, di, lse, row_source, beside, keys, dqo, lse2, delta, row_parts)));
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_DKV, stream, (attn_dkv_kernel<ND><<<ks.units * Hk, kAttnThreads, 0, stream>>>(
             sh, qi, ki, vi, di, lse2, delta, key_source, dko, dvo, key_parts)));
-        if (listed && rs.joins + ks.joins > 0)
+        if (keys_listed && rs.joins + ks.joins > 0)
             RELIBRA_LAUNCH(RELIBRA_K_ATTN_JOIN, stream, (attn_join_kernel<ND><<<(rs.joins + ks.joins) * Hk * ND, kAttnThreads, 0, stream>>>(
                 sh, rs.joins, rows.head, rows.joins, row_parts, dqo, keys.head, keys.joins, key_parts, dko, dvo)));
     });

@@ -120,8 +120,8 @@ def test_attention_against_the_definition(name):
 
 # Long sequences of few heads: tiles that several blocks share, in both directions; many heads of short ones: lists without shared tiles.
 LONG = dict(
-    two_heads=dict(places=[1700, 300], Hk=1, G=2, d=128), threes_padded=dict(places=[900, 1150], lens=[850, 1149], Hk=2, G=3, d=80, before=5, behind=9),
-    eight_heads=dict(places=[2000], Hk=1, G=8, d=40), keys_of_their_own=dict(places=[64, 1800, 1], Hk=3, G=1, d=104), many_heads=dict(places=[300, 130, 270], lens=[300, 129, 260], Hk=512, G=1, d=8))
+    two_heads=dict(places=[2100, 300], Hk=1, G=2, d=128), threes_padded=dict(places=[1300, 1400], lens=[1250, 1399], Hk=2, G=3, d=80, before=5, behind=9),
+    eight_heads=dict(places=[3000], Hk=1, G=8, d=40), keys_of_their_own=dict(places=[64, 2300, 1], Hk=3, G=1, d=104), many_heads=dict(places=[300, 130, 270], lens=[300, 129, 260], Hk=512, G=1, d=8))
 
 
 @gpu
@@ -309,7 +309,7 @@ def test_attention_of_as_many_sequences_as_there_may_be():
 
 
 @gpu
-@pytest.mark.parametrize("places,lens,Hk,G", [([300, 129, 500], [300, 100, 481], 2, 4), ([1700, 200, 40], [1690, 100, 40], 1, 2)], ids=["short", "shared"])
+@pytest.mark.parametrize("places,lens,Hk,G", [([300, 129, 500], [300, 100, 481], 2, 4), ([2200, 200, 40], [2190, 100, 40], 1, 2)], ids=["short", "shared"])
 def test_attention_in_a_graph_beside_eager_calls(places, lens, Hk, G):
     c = make(places, Hk, G, 128, lens=lens, seed=10)
     start, length = tables(c)
@@ -345,7 +345,7 @@ def test_attention_in_a_graph_beside_eager_calls(places, lens, Hk, G):
 @gpu
 def test_attention_of_two_streams_at_once():
     """Calls that overlap, each with a workspace and a flag of its own, one of them with a table that is refused."""
-    c = make([1700, 300], 1, 2, 128, seed=11)
+    c = make([2100, 300], 1, 2, 128, seed=11)
     start, _ = tables(c)
     bad = torch.tensor([0, 1800, 1700], dtype=torch.int32, device=DEV)
     d = {n: c[n].to(DEV) for n in ("q", "k", "v", "dout")}
