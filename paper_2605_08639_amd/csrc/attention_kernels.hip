@@ -12,8 +12,8 @@
 // are computed from the scores again in two kernels, seven products where five would do with atomics: fixed order, the same bits every call.
 //
 // Roundings: p and ds to bf16 for their products, whose operands have one type (2^-8 of a term at most; the terms' errors are independent and cost the
-// sum about what its own rounding does), and D has the error that `out` was rounded with.  dq and dk are 0.0025 to 0.0029 off (root mean square over
-// that of the result), where the last rounding alone costs 0.0017; an exact D would bring them to 0.0024, for a fourth product in the queries' kernel.
+// sum about what its own rounding does), and D has the error that `out` was rounded with, unless keys are few: see attn_dq_kernel.  dq and dk are 0.0024 to
+// 0.0025 off (root mean square over that of the result) for values of a normal distribution, where the last rounding alone costs 0.0017.
 //
 // Long calls are bound by the matrix units at the clock that the chip's power leaves them, 1.6 to 1.9 GHz of 2.4: one sequence of 16384 tokens, 32
 // heads of 4 key heads of 128, forward 2000 us, 1100 TFLOP/s; a loop of the bare products reaches 1900, with one LDS read a product 1710, with the
@@ -707,6 +707,10 @@ __device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x
 // ---------------------------------------------------------------- backward: queries
 // dq of 128 packed rows, and for the other kernel each row's lse in powers of two and -D.  Three products a step; scores are not kept, p comes from lse.
 // One sequence of 8192 tokens, 32 heads with keys of their own: 700 us, 1180 TFLOP/s of its three products.
+// The rounding of `out` puts an error into D that all of a row's ds share.  It is as large as ds where few keys make up `out`, so for tiles that see two steps'
+// keys D is put right first by the sum of ds, which is zero with the right one: two products more of the cheapest tiles (the long sequence 1728 -> 1731 us,
+// the packed micro-batch 1503 -> 1508), and dq and dk 0.0029 -> 0.0024 off for short sequences, 0.0026 -> 0.0025 for long ones.
+constexpr int kExactSteps = 2;                               // both steps' tiles are in LDS at once: nothing is loaded twice
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, HeadsIn dout, const float *__restrict__ lse, UnitSource source,
@@ -755,36 +759,63 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
     }
     const long long place = (long long)(u.row0 + tok) * sh.Hq + head;
     const float l2 = lse[place] * kLog2e, c = sh.scale * kLog2e;
-    if (live && lane < 32 && u.from == 0) lse2[place] = l2, minus_delta[place] = -D;
+    // a sequence's first row has one key and a constant softmax: its scores have no gradient (what rounding would leave is not stored)
+    auto mask = [&](int t, int b, f32x16_t &s) __attribute__((always_inline)) {
+        if (t * kKeyTile + kKeyTile - 1 > wave_lo) {
+            rare();
+            const int seen = (tok > 0 ? tok : -1) - t * kKeyTile - (lane >> 5) * 4;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) s[i] = -INFINITY;
+        }
+    };
+    auto tiles_in = [&](int t) __attribute__((always_inline)) {       // step t's are there; the next ones go out
+        tile_barrier();
+        if (t + 1 < u.to) {
+            kt.load_next(lds + (~t & 1) * Tile::BYTES, wave);
+            vt.load_next(lds + (2 + (~t & 1)) * Tile::BYTES, wave);
+        }
+    };
     f32x16_t minus_D;
 #pragma unroll
     for (int i = 0; i < 16; ++i) minus_D[i] = -D;
+    // Few keys: first the sum of ds, which is what D lacks.  Both steps' tiles then stay where they are.
+    const bool exact = u.to <= kExactSteps;
+    if (exact) {
+        float more = 0.0f;
+#pragma unroll 1
+        for (int t = 0; t < u.to; ++t) {
+            tiles_in(t);
+            if (t * kKeyTile > wave_hi) continue;
+            const uint32_t key_rows = lds_at(lds + (t & 1) * Tile::BYTES, row_lane), val_rows = lds_at(lds + (2 + (t & 1)) * Tile::BYTES, row_lane);
+#pragma unroll 1
+            for (int b = 0; b < 2; ++b) {
+                f32x16_t s, dp;
+                score_pair<ND>(key_rows + b * 32 * Tile::ROW, val_rows + b * 32 * Tile::ROW, qf, df, minus_D, s, dp);
+                mask(t, b, s);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) more = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)), dp[i], more);
+            }
+        }
+        D += halves_sum(more);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) minus_D[i] = -D;
+    }
+    if (live && lane < 32 && u.from == 0) lse2[place] = l2, minus_delta[place] = -D;
 
     f32x16_t acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; ++n) acc[n] = zero16();
     for (int t = u.from; t < u.to; ++t) {
-        tile_barrier();
-        const char *keys = lds + (t & 1) * Tile::BYTES, *vals = lds + (2 + (t & 1)) * Tile::BYTES;
-        if (t + 1 < u.to) {
-            kt.load_next(lds + (~t & 1) * Tile::BYTES, wave);
-            vt.load_next(lds + (2 + (~t & 1)) * Tile::BYTES, wave);
-        }
+        if (!exact) tiles_in(t);
         if (t * kKeyTile > wave_hi) continue;
-        const bool masked = t * kKeyTile + kKeyTile - 1 > wave_lo;
+        const char *keys = lds + (t & 1) * Tile::BYTES, *vals = lds + (2 + (t & 1)) * Tile::BYTES;
         const uint32_t key_rows = lds_at(keys, row_lane), val_rows = lds_at(vals, row_lane), key_cols = lds_at(keys, col_lane);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             f32x16_t s, dp;
             score_pair<ND>(key_rows + b * 32 * Tile::ROW, val_rows + b * 32 * Tile::ROW, qf, df, minus_D, s, dp);
-            if (masked) {
-                rare();
-                // a sequence's first row has one key and a constant softmax: its scores have no gradient (what rounding would leave is not stored)
-                const int seen = (tok > 0 ? tok : -1) - t * kKeyTile - (lane >> 5) * 4;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (b * 32 + (i >> 2) * 8 + (i & 3) > seen) s[i] = -INFINITY;
-            }
+            mask(t, b, s);
             bf16x8_t f[ND];
             auto fetch = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
