@@ -234,7 +234,7 @@ template <int ND> struct TokenTiles {
 // tile does not outlast the rest, 8 at least (4, 8, 16: 9 sequences in 4999 tokens of 12 heads 37.5, 35.5, 36.9 us; one of 2048 of 8 heads 37.1, 36.8, 35.9,
 // backward 79.0, 79.4, 83.4).  Keys: two chunks to each of the blocks that run at once, of 16 steps at least (8, 16, 32: that backward 89.1, 79.4, 79.8 us), or
 // one of 4 (4, 8: 5 sequences in 901 tokens of 10 heads backward 33.2, 35.1 us).
-// 7 to 11 us of latencies in a row for any table: worth a launch where rows are shared or units are many; else it makes only the keys' list, beside dq.
+// 7 to 11 us of latencies in a row for any table: a launch where rows are shared or sequences are many; else it makes only the keys' list, beside dq.
 constexpr int kSchedThreads = 1024, kSchedBins = 1024, kMinRowChunk = 8, kMinKeyChunk = 4, kFullKeyChunk = 16;
 // Whether rows are shared at all, from T and Hq alone: where the longest possible tile has so many steps more than the rest of the chip needs meanwhile
 // that it pays for the list, partial sums and (forward; the keys have it anyway) the join's launch.  One sequence, not shared / shared, us: 16384 tokens of
@@ -409,7 +409,9 @@ attn_sched_kernel(const int32_t *__restrict__ seq_start, const int32_t *__restri
 }
 
 // Where a block finds its unit: in the list, or, where no tile is shared and sequences are few, from the tables itself, a sequence a lane, the longest
-// tiles of each sequence first: no scheduling launch (one prompt of 33 tokens, 32 heads: 14.2 -> 10.4 us; 1024 tokens of 64 heads 34.7 -> 29.1).
+// tiles of each sequence first.  No scheduling launch (one prompt of 33 tokens, 32 heads: 14.2 -> 10.4 us; 1024 tokens of 64 heads 34.7 -> 29.1), and the
+// blocks of a sequence, which read the same keys, run together (60 sequences in 16384 tokens of 32 heads with keys of their own 182 -> 174 us, backward 610 ->
+// 589); without an order among sequences the last rounds of blocks are less even (24 in 8192 of 128 heads 326 -> 329).
 struct UnitSource {
     const AttnList *list;                                     // NULL: from the tables
     const AttnUnit *units;
@@ -1085,11 +1087,6 @@ size_t attn_bwd_ws_bytes(int T, int n_seq, int Hq, int Hk, int d)
     const AttnSizes r = row_sizes(T, n_seq, Hq, Hk, d, true), k = key_sizes(T, n_seq, Hq, Hk, d);
     return r.list_bytes() + r.part_bytes + k.list_bytes() + k.part_bytes + 2 * round256((size_t)T * Hq * sizeof(float));
 }
-// Whether blocks may find their units themselves.  One sequence's are in the list's order without it.  Several sequences' are not in order among each other, which
-// costs calls of many rounds of blocks what the list does (8 sequences in 4096 tokens of 64 heads, 4096 units: 98.2 with the list, 94.9 without; 24
-// in 8192 of 16 heads, 1100: 57.1 and 60.2; 8 in 2048 of 64 heads: 41.4 and 34.0).
-constexpr int kUnlisted = 4096;
-inline bool unlisted(const AttnSizes &s, int n_seq, int Hk) { return n_seq == 1 || (n_seq <= kSelfSeq && (long long)s.units * Hk <= kUnlisted); }
 // A list in the workspace, and the next free byte behind it.
 inline SchedOut sched_out(char *&ws, const AttnSizes &s)
 {
@@ -1141,7 +1138,7 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
     float2 *sums = (float2 *)(ws + sz.part_bytes);
     const AttnShape sh{T, Hq, Hk, Hq / Hk, d, token_magic(Hq / Hk), scale};
     const HeadsOut oo{(bf16_t *)out, out_stride};
-    const bool listed = sz.joins > 0 || !unlisted(sz, n_seq, Hk);
+    const bool listed = sz.joins > 0 || n_seq > kSelfSeq;
     const UnitSource source{listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
     if (listed)
         RELIBRA_LAUNCH(RELIBRA_K_ATTN_SCHED, stream, attn_sched_kernel<<<1, kSchedThreads, 0, stream>>>(seq_start, seq_len, n_seq, T, sh.G, sh.magic, Hk, rows, rows, err_flag));
@@ -1190,8 +1187,8 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
         di{(const bf16_t *)dout, dout_stride};
     const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
     // Rows' units are found without a list where they may be; keys' only if no tile of theirs could be shared, and their list is then made beside dq.
-    const bool rows_listed = rs.joins > 0 || !unlisted(rs, n_seq, Hk);
-    const bool keys_listed = rows_listed || tiles_of((long long)T * sh.G, kRowStep) > 2 * kMinKeyChunk || !unlisted(ks, n_seq, Hk);
+    const bool rows_listed = rs.joins > 0 || n_seq > kSelfSeq;
+    const bool keys_listed = rows_listed || tiles_of((long long)T * sh.G, kRowStep) > 2 * kMinKeyChunk;
     const int beside = keys_listed && !rows_listed;
     const UnitSource row_source{rows_listed ? rows.head : nullptr, rows.units, seq_start, seq_len, n_seq, T, err_flag};
     const UnitSource key_source{keys_listed ? keys.head : nullptr, keys.units, seq_start, seq_len, n_seq, T, err_flag};
