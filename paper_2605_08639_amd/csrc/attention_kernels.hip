@@ -245,11 +245,7 @@ constexpr int kShareTiles = 640, kFwdShareSteps = 32, kBwdShareSteps = 24;
 template <int THREADS> __device__ __forceinline__ int scan_block(int v, int *sums, int &total)      // inclusive; two barriers
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int below = __shfl_up(v, off);
-        if (lane >= off) v += below;
-    }
+    v = wave_scan(v);
     if (lane == 63) sums[wave] = v;
     __syncthreads();
     total = 0;
@@ -432,16 +428,12 @@ struct UnitSource {
             return false;
         }
         const int own = KEYS ? tiles_of(len, kKeyRows) : tiles_of((long long)len * G, kRowTile), tiles = lane < n_seq ? own + tiles_of(b - a - len, kRowTile) : 0;
-        int upto = tiles;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int below = __shfl_up(upto, off);
-            if (lane >= off) upto += below;
-        }
+        const int upto = wave_scan(tiles);
         const unsigned long long behind = __ballot(upto > at);
         if (!behind) return false;
-        const int mine = __builtin_ctzll(behind), t = at - __shfl(upto - tiles, mine), row0 = __shfl(a, mine), end = __shfl(b, mine), n = __shfl(len, mine);
-        const int n_own = __shfl(own, mine);
+        const int mine = __builtin_ctzll(behind);
+        auto of = [&](int v) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, mine); };
+        const int t = at - of(upto - tiles), row0 = of(a), end = of(b), n = of(len), n_own = of(own);
         u.slot = -1, u.chunks = 1, u.from = 0, u.to = 0, u.row0 = row0, u.len = n;
         if (t >= n_own) u.row0 = row0 + n + (t - n_own) * kRowTile, u.len = min(kRowTile, end - u.row0), u.tile = -1;
         else if (KEYS) u.tile = t, u.from = G * t, u.to = tiles_of((long long)n * G, kRowStep);
@@ -507,6 +499,7 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source
     kt.load_next(lds + (u.from & 1) * Tile::BYTES, wave);
     bf16x8_t qf[2 * ND];
     load_row<ND>(qf, q.p + (long long)(u.row0 + tok) * q.ld + head * d, d, lane);
+    vt.load_next(lds + (2 + (u.from & 1)) * Tile::BYTES, wave);
 
     const float c = sh.scale * kLog2e;
     float m = -INFINITY, l = 0.0f;
@@ -615,9 +608,8 @@ attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source
         });
         follow(halves_max(top));
     };
-    tile_barrier();                                           // the first keys
+    tile_barrier();                                           // the first keys and values
     if (u.from + 1 < u.to) kt.load_next(lds + (~u.from & 1) * Tile::BYTES, wave);
-    vt.load_next(lds + (2 + (u.from & 1)) * Tile::BYTES, wave);
     const int own = min(wave_hi / kKeyTile, u.to - 1);        // this wave's last step; the block's other waves may have more
     int t = u.from;
     if (t <= own) {

@@ -51,6 +51,17 @@ template <int LANES> __device__ __forceinline__ float place_sum(float v)
     return __builtin_bit_cast(float, (unsigned)s[0]) + __builtin_bit_cast(float, (unsigned)s[1]);
 }
 
+// Sums over a wave's lanes up to each lane: shifts within rows of 16, then the rows before.
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8: zeros come in
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    const int lane = threadIdx.x & 63, a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
+    return v + (lane >= 48 ? a + b + c : lane >= 32 ? a + b : lane >= 16 ? a : 0);
+}
+
 // Eight consecutive values of memory (16-byte aligned) as loaded, as fp32, and back (one rounding to bf16).
 template <class T> struct Raw8;
 template <> struct Raw8<bf16_t> {
