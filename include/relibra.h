@@ -684,8 +684,9 @@ int relibra_qk_norm_rope_bwd(const void *q_dev, int64_t q_stride, const void *k_
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ATTENTION_FWD, T, 1, Hq, n_seq, Hk, d) bytes (E, G, h, hff are Hq, n_seq, Hk, d)
  * Scores, their exponentials' sums and the result are added up in fp32; the exponentials are rounded to bf16 for their product with v, the result once.
  * A NaN or infinity stays in its sequence, reaches the rows that see it, and may reach rows up to 127 tokens before it.
- * Backward: dq, dk, dv from dout, with out and lse as the forward call left them; p and ds are rounded to bf16 for their products, the sums
- * are fp32.  A key head's gradients are summed over its group.  No atomics on values, a fixed order: the same bits every call.
+ * Backward: dq, dk, dv from dout, with out and lse as the forward call left them; p and ds are rounded to bf16 for their products (ds to twice its bits for
+ * the rows of a sequence's first 128 tokens), the sums are fp32.  A key head's gradients are summed over its group.  No atomics on values, a fixed
+ * order: the same bits every call.
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ATTENTION_BWD, T, 1, Hq, n_seq, Hk, d) bytes
  * Limits: d % 8 == 0, d <= 128, Hq % Hk == 0 (RELIBRA_EINVAL), Hq / Hk <= 64, Hq <= 4096, n_seq <= 8192, T * Hq / Hk <= 2^26, fewer than 2^24 blocks,
  * which max(T * Hq / 128, T * Hk / 64) + 2 * (n_seq + 1) * Hk + 2048 bounds (RELIBRA_EUNSUPPORTED beyond); 0 < scale <= 1e38; strides and alignment as

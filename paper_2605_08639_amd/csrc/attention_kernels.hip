@@ -12,8 +12,8 @@
 // are computed from the scores again in two kernels, seven products where five would do with atomics: fixed order, the same bits every call.
 //
 // Roundings: p and ds to bf16 for their products, whose operands have one type (2^-8 of a term at most; the terms' errors are independent and cost the
-// sum about what its own rounding does), and D has the error that `out` was rounded with, unless keys are few: see attn_dq_kernel.  dq and dk are 0.0024 to
-// 0.0025 off (root mean square over that of the result) for values of a normal distribution, where the last rounding alone costs 0.0017.
+// sum about what its own rounding does), and D has the error that `out` was rounded with; unless keys are few, see attn_dq_kernel.  dq and dk are 0.0021 to
+// 0.0024 off (root mean square over that of the result) for values of a normal distribution, where the last rounding alone costs 0.0017.
 //
 // Long calls are bound by the matrix units at the clock that the chip's power leaves them, 1.6 to 1.9 GHz of 2.4: one sequence of 16384 tokens, 32
 // heads of 4 key heads of 128, forward 2000 us, 1100 TFLOP/s; a loop of the bare products reaches 1900, with one LDS read a product 1710, with the
@@ -137,6 +137,16 @@ __device__ __forceinline__ bf16x8_t pack_half(const f32x16_t &v, int j)
     typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(bf16x8_t, u32x4_t{pack2bf(v[8 * j], v[8 * j + 1]), pack2bf(v[8 * j + 2], v[8 * j + 3]), pack2bf(v[8 * j + 4], v[8 * j + 5]),
                                                 pack2bf(v[8 * j + 6], v[8 * j + 7])});
+}
+
+// What pack_half's rounding left of them, as bf16: 16 bits together.
+__device__ __forceinline__ bf16x8_t pack_rest(const f32x16_t &v, int j)
+{
+    const bf16x8_t packed = pack_half(v, j);
+    f32x16_t rest;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = v[8 * j + i] - (float)packed[i];
+    return pack_half(rest, 0);
 }
 
 // A lane's own row as a product's operand: values kk * 16 + lane / 32 * 8 .. + 7 of `row`, zeros from d on (d > 32 (ND - 1)).
@@ -701,9 +711,10 @@ __device__ __forceinline__ void score_pair(uint32_t x0, uint32_t x1, const bf16x
 // ---------------------------------------------------------------- backward: queries
 // dq of 128 packed rows, and for the other kernel each row's lse in powers of two and -D.  Three products a step; scores are not kept, p comes from lse.
 // One sequence of 8192 tokens, 32 heads with keys of their own: 700 us, 1180 TFLOP/s of its three products.
-// The rounding of `out` puts an error into D that all of a row's ds share.  It is as large as ds where few keys make up `out`, so for tiles that see two steps'
-// keys D is put right first by the sum of ds, which is zero with the right one: two products more of the cheapest tiles (the long sequence 1728 -> 1731 us,
-// the packed micro-batch 1503 -> 1508), and dq and dk 0.0029 -> 0.0024 off for short sequences, 0.0026 -> 0.0025 for long ones.
+// Where few keys make up `out`, its rounding puts an error into D that is as large as ds, and ds' own roundings are too few to average out.  Tiles that see two
+// steps' keys therefore put D right first by the sum of ds, which is zero with the right one, and multiply what ds' rounding left, too; the other kernel
+// does that for the same rows.  For values of a normal distribution it takes dq and dk from 0.0035 to 0.0021 off in sequences of a few tokens, 0.0029 to 0.0022
+// in those of 180, 0.0026 to 0.0024 in one of 8192; the packed micro-batch 1503 -> 1522 us, the long sequence 1728 -> 1742.
 constexpr int kExactSteps = 2;                               // both steps' tiles are in LDS at once: nothing is loaded twice
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
@@ -820,16 +831,24 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
                 for (int i = 8 * j; i < 8 * j + 8; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -l2)) * dp[i];
                 return pack_half(s, j);
             };
+            auto add = [&](const bf16x8_t &x) __attribute__((always_inline)) {
+#pragma unroll
+                for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], x, acc[n]);
+            };
             fetch(0);
             const bf16x8_t ds0 = gradients(0);
             in_order();
-#pragma unroll
-            for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], ds0, acc[n]);
+            add(ds0);
             const bf16x8_t ds1 = gradients(1);
             in_order();
             fetch(1);
-#pragma unroll
-            for (int n = 0; n < ND; ++n) acc[n] = mfma16(f[n], ds1, acc[n]);
+            add(ds1);
+            if (exact) {                                      // what the rounding of ds left
+                rare();
+                add(pack_rest(s, 1));
+                fetch(0);
+                add(pack_rest(s, 0));
+            }
         }
     }
     if (u.slot >= 0) {
@@ -851,8 +870,8 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
 {
     typedef AttnTile<ND, kRowStep> Tile;
     constexpr int STATS = 4 * Tile::BYTES, TRADE = STATS + 4 * kRowStep * 4;
-    // queries and their upstream, two steps each; the rows' lse and -D, two steps each; what the waves of a pair hand each other
-    __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves * 2048];
+    // queries and their upstream, two steps each; the rows' lse and -D, two steps each; what the waves of a pair hand each other: p, or ds and its rest
+    __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves * 3072];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     AttnUnit u;
     if (!source.find<true>(at, sh.G, sh.magic, u)) return;
@@ -923,8 +942,9 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     f32x16_t acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; ++n) acc[n] = zero16();
-    char *give = lds + TRADE + wave * 2048 + lane * 16;
-    const char *take = lds + TRADE + (wave ^ 1) * 2048 + lane * 16;
+    char *give = lds + TRADE + (wave >> 1) * 6144 + (role ? 4096 : 0) + lane * 16;
+    const char *take = lds + TRADE + (wave >> 1) * 6144 + (role ? 0 : 4096) + lane * 16;
+    const int fine = kExactSteps * kKeyTile * G;              // rows before that see few keys
     // From the last rows to the first: the blocks of a head, which begin at different rows, then read the same ones at about the same time, out of L2.
     auto walk = [&](auto which) __attribute__((always_inline)) {
         constexpr int ROLE = decltype(which)::value;
@@ -987,6 +1007,17 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
                 in_order();
                 fetch(ROLE, 1);
                 add(x1);
+                if (r0 < fine) {                              // what the rounding of ds left
+                    rare();
+                    if (ROLE) {
+                        add(pack_rest(dp, 1));
+                        fetch(ROLE, 0);
+                        add(pack_rest(dp, 0));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) *reinterpret_cast<bf16x8_t *>(give + 2048 + j * 1024) = pack_rest(dp, j);
+                    }
+                }
                 fetch(ROLE ^ 1, 0);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -997,6 +1028,12 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
             add(y0);
             fetch(ROLE ^ 1, 1);
             add(y1);
+            if (ROLE && r0 < fine) {
+                rare();
+                add(*reinterpret_cast<const bf16x8_t *>(take + 3072));
+                fetch(ROLE ^ 1, 0);
+                add(*reinterpret_cast<const bf16x8_t *>(take + 2048));
+            }
         }
     };
     if (role) walk(std::integral_constant<int, 1>{});
