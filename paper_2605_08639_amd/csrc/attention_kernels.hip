@@ -18,7 +18,7 @@
 // Long calls are bound by the matrix units at the clock that the chip's power leaves them, 1.6 to 1.9 GHz of 2.4: one sequence of 16384 tokens, 32
 // heads of 4 key heads of 128, forward 2000 us, 1100 TFLOP/s; a loop of the bare products reaches 1900, with one LDS read a product 1710, with the
 // softmax's vector work as well 1460, and the library's product of 8192 x 8192 matrices 1390.  Short sequences are bound by blocks' beginnings and ends (a
-// micro-batch of 24 sequences, 16384 tokens in all, 64 heads: 462 us, 850 TFLOP/s), small calls by launches and the latency of one block's chain.
+// micro-batch of 24 sequences, 16384 tokens in all, 64 heads: 450 us, 870 TFLOP/s), small calls by launches and the latency of one block's chain.
 #include "gemm_tile.h"
 #include "head_rows.h"
 #include "wave_ops.h"

@@ -118,6 +118,43 @@ def test_attention_against_the_definition(name):
     check(c, run(c))
 
 
+@gpu
+@pytest.mark.parametrize("kw", [dict(Hk=2, G=3, d=72), dict(Hk=1, G=8, d=128), dict(Hk=2, G=1, d=32)], ids=str)
+def test_attention_gradients_of_few_keys(kw):
+    """Rows of a sequence's first 128 tokens: ds has twice bf16's bits (H^2 of it), and out's rounding is not in D.  D0, from the rounded out, is off by at most ED; D0 plus the sum
+    of p (dp - D0) is D, but for p's relative error EP, the error of dp, and n + 16 additions: (EP + (n + 20) U) sum p |dp - D0| + sum p err(dp)."""
+    c = make([1, 2, 3, 17, 64, 65, 100, 128], seed=31, **kw)
+    out, lse, dq, dk, dv = (x.cpu().double() for x in run(c))
+    G, d, s = c["G"], c["d"], c["scale"]
+    for start, end in zip(c["starts"], c["starts"][1:]):
+        rows, n = slice(start, end), end - start
+        mask = torch.ones(n, n, dtype=torch.bool).tril()
+        for h in range(c["Hk"]):
+            k, v = c["k"][rows, h].double(), c["v"][rows, h].double()
+            want_k, err_k = torch.zeros(n, d, dtype=torch.float64), torch.zeros(n, d, dtype=torch.float64)
+            for g in range(h * G, (h + 1) * G):
+                q, do = c["q"][rows, g].double(), c["dout"][rows, g].double()
+                z = (s * q @ k.T).masked_fill(~mask, -math.inf)
+                ez = ((d + 4) * U * s * (q.abs() @ k.abs().T)).masked_fill(~mask, 0).amax(1, keepdim=True)
+                top = torch.logsumexp(z, 1, keepdim=True)
+                p = torch.exp(z - top)
+                ep = ez + (ez + (n + 16) * U + 8 * U * top.abs()) + 16 * U
+                want, size = p @ v, p @ v.abs()
+                ED = (do.abs() * ((H + 2 * ez + (2 * n + 40) * U) * size + H * want.abs())).sum(1, keepdim=True)
+                dp, D = do @ v.T, (do * want).sum(1, keepdim=True)
+                err_dp = (d + 8) * U * (do.abs() @ v.abs().T + (do.abs() * size).sum(1, keepdim=True))
+                err_D = (p * ((ep + (n + 20) * U) * ((dp - D).abs() + ED) + err_dp)).sum(1, keepdim=True)
+                ds = (p * (dp - D)).masked_fill(~mask, 0)
+                ds[0] = 0                                     # one key
+                err_ds = p * (err_D + err_dp) + (2 * ep + H * H) * ds.abs()
+                want_q = s * ds @ k
+                err_q = s * (err_ds + (n + 24) * U * ds.abs()) @ k.abs() + H * want_q.abs()
+                assert torch.all((dq[rows, g] - want_q).abs() <= 1.01 * err_q + 1e-30), ("dq", n, g)
+                want_k += s * ds.T @ q
+                err_k += s * (err_ds + (n * G + 24) * U * ds.abs()).T @ q.abs()
+            assert torch.all((dk[rows, h] - want_k).abs() <= 1.01 * (err_k + H * want_k.abs()) + 1e-30), ("dk", n, h)
+
+
 # Long sequences of few heads: tiles that several blocks share, in both directions; many heads of short ones: lists without shared tiles.
 LONG = dict(
     two_heads=dict(places=[2100, 300], Hk=1, G=2, d=128), threes_padded=dict(places=[1300, 1400], lens=[1250, 1399], Hk=2, G=3, d=80, before=5, behind=9),
