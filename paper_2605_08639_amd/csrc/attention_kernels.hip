@@ -869,9 +869,9 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
                 UnitSource source, HeadsOut dk, HeadsOut dv, float *__restrict__ parts)
 {
     typedef AttnTile<ND, kRowStep> Tile;
-    constexpr int STATS = 4 * Tile::BYTES, TRADE = STATS + 4 * kRowStep * 4;
+    constexpr int STATS = 4 * Tile::BYTES, TRADE = STATS + 4 * kRowStep * 4, PAIR = 6 * 1024;
     // queries and their upstream, two steps each; the rows' lse and -D, two steps each; what the waves of a pair hand each other: p, or ds and its rest
-    __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves * 3072];
+    __shared__ __attribute__((aligned(1024))) char lds[TRADE + kAttnWaves / 2 * PAIR];
     const int at = blockIdx.x / sh.Hk, hk = blockIdx.x - at * sh.Hk;
     AttnUnit u;
     if (!source.find<true>(at, sh.G, sh.magic, u)) return;
@@ -942,8 +942,8 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
     f32x16_t acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; ++n) acc[n] = zero16();
-    char *give = lds + TRADE + (wave >> 1) * 6144 + (role ? 4096 : 0) + lane * 16;
-    const char *take = lds + TRADE + (wave >> 1) * 6144 + (role ? 0 : 4096) + lane * 16;
+    char *give = lds + TRADE + (wave >> 1) * PAIR + (role ? 4096 : 0) + lane * 16;
+    const char *take = lds + TRADE + (wave >> 1) * PAIR + (role ? 0 : 4096) + lane * 16;
     const int fine = kExactSteps * kKeyTile * G;              // rows before that see few keys
     // From the last rows to the first: the blocks of a head, which begin at different rows, then read the same ones at about the same time, out of L2.
     auto walk = [&](auto which) __attribute__((always_inline)) {
@@ -1030,7 +1030,7 @@ attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, con
             add(y1);
             if (ROLE && r0 < fine) {
                 rare();
-                add(*reinterpret_cast<const bf16x8_t *>(take + 3072));
+                add(*reinterpret_cast<const bf16x8_t *>(take + 2048 + 1024));
                 fetch(ROLE ^ 1, 0);
                 add(*reinterpret_cast<const bf16x8_t *>(take + 2048));
             }
