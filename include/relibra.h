@@ -659,8 +659,8 @@ int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const 
  * or added to with RELIBRA_QK_ACCUMULATE.  dq may be dq_out or q, dk may be dk_out or k.  A fixed order: the same bits every call.
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_QK_NORM_ROPE, T, 1, Hq, 1, Hk, d) bytes (E, h, hff are Hq, Hk, d); unused without norms
  * Limits: d % 16 == 0, d <= 256, rot % 16 == 0, Hq, Hk <= 4096, T <= 2^30 (RELIBRA_EUNSUPPORTED beyond); eps > 0 with a norm; strides are multiples
- * of 8 of at least H * d and at most 2^27, tensors 16-byte aligned.  Beside the pairs named no output may share memory with an input or the other
- * output (RELIBRA_EINVAL; tensors of one stride may interleave).
+ * of 8 of at least H * d and at most 2^27, tensors 16-byte aligned.  Beside the pairs named no output may share memory with an input (the weights and
+ * tables are such), another output (dw_q and dw_k are such) or the workspace (RELIBRA_EINVAL; tensors of one stride may interleave).
  */
 enum { RELIBRA_ROPE_ADJACENT = 1, RELIBRA_QK_ACCUMULATE = 2 };
 int relibra_qk_norm_rope_fwd(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *w_q_dev, const void *w_k_dev,

@@ -1154,10 +1154,10 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
     if (rc != RELIBRA_OK) return rc;
     if (T == 0 || n_seq == 0) return RELIBRA_OK;
     const HeadRows in[3] = {{q, q_stride, Hq * d}, {k, k_stride, Hk * d}, {v, v_stride, Hk * d}}, to{out, out_stride, Hq * d};
-    const size_t lse_bytes = (size_t)T * Hq * sizeof(float);
-    if (!to.usable() || !lse || to.overlaps(lse, lse_bytes, T)) return RELIBRA_EINVAL;
+    const Piece lse_all{lse, (size_t)T * Hq * sizeof(float)};
+    if (!to.usable() || !lse || to.overlaps(lse_all, T)) return RELIBRA_EINVAL;
     for (const HeadRows &x : in)
-        if (!x.usable() || x.overlaps(to, T) || x.overlaps(lse, lse_bytes, T)) return RELIBRA_EINVAL;
+        if (!x.usable() || x.overlaps(to, T) || x.overlaps(lse_all, T)) return RELIBRA_EINVAL;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
     if (!workspace || workspace_bytes < attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
     const AttnSizes sz = row_sizes(T, n_seq, Hq, Hk, d, false);
@@ -1194,11 +1194,12 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
     if (T == 0 || n_seq == 0) return RELIBRA_OK;
     const HeadRows in[5] = {{q, q_stride, Hq * d}, {k, k_stride, Hk * d}, {v, v_stride, Hk * d}, {out, out_stride, Hq * d}, {dout, dout_stride, Hq * d}};
     const HeadRows to[3] = {{dq, dq_stride, Hq * d}, {dk, dk_stride, Hk * d}, {dv, dv_stride, Hk * d}};
+    const Piece lse_all{lse, (size_t)T * Hq * sizeof(float)};
     if (!lse) return RELIBRA_EINVAL;
     for (const HeadRows &x : in)
         if (!x.usable()) return RELIBRA_EINVAL;
     for (int i = 0; i < 3; ++i) {
-        if (!to[i].usable() || to[i].overlaps(lse, (size_t)T * Hq * sizeof(float), T)) return RELIBRA_EINVAL;
+        if (!to[i].usable() || to[i].overlaps(lse_all, T)) return RELIBRA_EINVAL;
         for (const HeadRows &x : in)
             if (x.overlaps(to[i], T)) return RELIBRA_EINVAL;
         for (int j = 0; j < i; ++j)

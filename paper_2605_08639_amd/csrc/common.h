@@ -63,6 +63,12 @@ inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes
     return at < bt + b_bytes && bt < at + a_bytes;
 }
 
+struct Piece {
+    const void *p;                         // NULL: no such memory
+    size_t bytes;
+};
+inline bool overlap(const Piece &a, const Piece &b) { return a.p && b.p && a.bytes && b.bytes && overlap(a.p, a.bytes, b.p, b.bytes); }
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Workspace sizes of the entry points in other translation units (relibra_workspace_bytes); 0 where the call refuses the sizes.

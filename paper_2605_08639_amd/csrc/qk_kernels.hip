@@ -287,6 +287,10 @@ inline int check_qk(const void *w_q, const void *w_k, const int32_t *pos, const 
     return RELIBRA_OK;
 }
 
+// The tables' sizes, 0 where the call reads none.
+inline size_t qk_pos_bytes(int T, int n_axes, int rot) { return rot ? (size_t)n_axes * T * sizeof(int32_t) : 0; }
+inline size_t qk_freq_bytes(int rot) { return (size_t)rot / 2 * sizeof(float); }
+
 template <class Fn> void qk_layout(int lanes, bool adjacent, const Fn &fn)
 {
     auto with = [&](auto n) {
@@ -318,6 +322,8 @@ extern "C" int relibra_qk_norm_rope_fwd(const void *q, int64_t q_stride, const v
         if (in[1 - i].overlaps(out[i], T)) return RELIBRA_EINVAL;
     }
     if (out[0].overlaps(out[1], T)) return RELIBRA_EINVAL;
+    if (!pieces_apart(T, {}, {out[0], out[1]}, {{w_q, d * sizeof(bf16_t)}, {w_k, d * sizeof(bf16_t)}, {pos, qk_pos_bytes(T, n_axes, rot)}, {freq, qk_freq_bytes(rot)}}, {}))
+        return RELIBRA_EINVAL;
     const QkGrid g = qk_grid(T, Hq, Hk, d, false, sh);
     const QkTables tab{pos, freq, (const bf16_t *)w_q, (const bf16_t *)w_k};
     qk_layout(g.lanes, flags & RELIBRA_ROPE_ADJACENT, [&](auto n, auto adj) {
@@ -339,10 +345,10 @@ extern "C" int relibra_qk_norm_rope_bwd(const void *q, int64_t q_stride, const v
     const int rc = check_qk(w_q, w_k, pos, freq, axis, n_axes, T, Hq, Hk, d, rot, eps, flags, RELIBRA_ROPE_ADJACENT | RELIBRA_QK_ACCUMULATE, sh);
     if (rc != RELIBRA_OK) return rc;
     if ((w_q && !dw_q) || (w_k && !dw_k) || !aligned16(dw_q) || !aligned16(dw_k) || !aligned16(workspace)) return RELIBRA_EINVAL;
+    const HeadRows in[4] = {{dq_out, dq_out_stride, Hq * d}, {dk_out, dk_out_stride, Hk * d}, {w_q ? q : nullptr, q_stride, w_q ? Hq * d : 0},
+                            {w_k ? k : nullptr, k_stride, w_k ? Hk * d : 0}};
+    const HeadRows out[2] = {{dq, dq_stride, Hq * d}, {dk, dk_stride, Hk * d}};
     if (T > 0) {
-        const HeadRows in[4] = {{dq_out, dq_out_stride, Hq * d}, {dk_out, dk_out_stride, Hk * d}, {w_q ? q : nullptr, q_stride, w_q ? Hq * d : 0},
-                                {w_k ? k : nullptr, k_stride, w_k ? Hk * d : 0}};
-        const HeadRows out[2] = {{dq, dq_stride, Hq * d}, {dk, dk_stride, Hk * d}};
         for (const HeadRows &r : in)
             if (!r.usable()) return RELIBRA_EINVAL;
         for (int i = 0; i < 2; ++i) {
@@ -353,12 +359,18 @@ extern "C" int relibra_qk_norm_rope_bwd(const void *q, int64_t q_stride, const v
         if (out[0].overlaps(out[1], T)) return RELIBRA_EINVAL;
     }
     const bool norms = w_q || w_k;
-    if (norms && (!workspace || workspace_bytes < qk_ws_bytes(T, Hq, Hk, d))) return RELIBRA_EWORKSPACE;
+    const size_t need = norms ? qk_ws_bytes(T, Hq, Hk, d) : 0;
+    if (norms && (!workspace || workspace_bytes < need)) return RELIBRA_EWORKSPACE;
+    // (one tensor for both weights' gradients would have two blocks add to the same values at once)
+    if (!pieces_apart(T, {in[0], in[1], in[2], in[3]}, {out[0], out[1]},
+                      {{w_q, d * sizeof(bf16_t)}, {w_k, d * sizeof(bf16_t)}, {pos, qk_pos_bytes(T, n_axes, rot)}, {freq, qk_freq_bytes(rot)}},
+                      {{w_q ? dw_q : nullptr, d * sizeof(float)}, {w_k ? dw_k : nullptr, d * sizeof(float)}, {workspace, need}}))
+        return RELIBRA_EINVAL;
     const QkGrid g = qk_grid(T, Hq, Hk, d, true, sh);
     const int P = T > 0 ? g.blocks : 0, add = flags & RELIBRA_QK_ACCUMULATE ? 1 : 0;
     const bool one = P == 1;
     float *part_q = !w_q ? nullptr : one ? dw_q : (float *)workspace;
-    float *part_k = !w_k ? nullptr : one ? dw_k : (float *)((char *)workspace + qk_ws_bytes(T, Hq, Hk, d) / 2);
+    float *part_k = !w_k ? nullptr : one ? dw_k : (float *)((char *)workspace + need / 2);
     const QkTables tab{pos, freq, (const bf16_t *)w_q, (const bf16_t *)w_k};
     if (T > 0)
         qk_layout(g.lanes, flags & RELIBRA_ROPE_ADJACENT, [&](auto n, auto adj) {

@@ -310,6 +310,47 @@ def test_qk_norm_rope_backward_refuses_missing_outputs_and_small_workspaces():
     assert rl.workspace_bytes(rl.WS_QK_NORM_ROPE, 4, 1, 4, 1, 2, 72) == 0
 
 
+def test_qk_norm_rope_refuses_overlaps_of_weights_tables_and_sums():
+    """Every output against everything else that the call reads or writes, all of it apart but for the one pair."""
+    at = {n: (100 + i) << 16 for i, n in enumerate(("w_q", "w_k", "pos", "freq"))}
+    for name, a in at.items():                               # T = 4: rows of 512 and 256 bytes; weights and 32 frequencies 128 bytes, positions 16
+        for out in ("qo", "ko"):
+            assert _fwd(**dict(at, **{out: a})) == rl.EINVAL, (name, out)
+    assert _fwd(**dict(at, w_q=3 * M - 112)) == rl.EINVAL and _fwd(**dict(at, pos=3 * M + 2044)) == rl.EINVAL and _fwd(**dict(at, freq=4 * M + 1020)) == rl.EINVAL
+    need = rl.workspace_bytes(rl.WS_QK_NORM_ROPE, 4, 1, 4, 1, 2, 64)
+    sums = {n: (200 + i) << 16 for i, n in enumerate(("dw_q", "dw_k", "ws"))}
+    rows = dict(q=M, k=2 * M, gq=5 * M, gk=6 * M, qo=3 * M, ko=4 * M)
+    apart = dict(at, **sums, ws_bytes=need)
+    for flags in (0, rl.QK_ACCUMULATE):
+        for name, a in sums.items():
+            for other, b in {**at, **rows, **sums}.items():
+                if other != name:
+                    assert _bwd(**dict(apart, flags=flags, **{name: b})) == rl.EINVAL, (name, other)
+        assert _bwd(**dict(apart, flags=flags, dw_q=sums["dw_k"] + 240)) == rl.EINVAL and _bwd(**dict(apart, flags=flags, dw_k=sums["ws"] + need - 16)) == rl.EINVAL
+        assert _bwd(**dict(apart, flags=flags, T=0, dw_q=sums["dw_k"])) == rl.EINVAL
+    for name, a in at.items():
+        for out in ("qo", "ko"):
+            assert _bwd(**dict(apart, **{out: a})) == rl.EINVAL, (name, out)
+
+
+@gpu
+def test_qk_norm_rope_takes_memory_between_its_rows():
+    """Weights, tables and their gradients in the gaps between the rows of the outputs: shared by no row, and left or written as they should be."""
+    c = make(9, 3, 2, 64, seed=12)
+    want = (*rl.relibra_qk_norm_rope_fwd(dev(c["q"]), dev(c["k"]), **how(c)), *rl.relibra_qk_norm_rope_bwd(dev(c["q"]), dev(c["k"]), dev(c["up_q"]), dev(c["up_k"]), **how(c)))
+    whole = torch.zeros((9, 1024), dtype=BF16, device=DEV)
+    q, k = whole[:, :192].unflatten(1, (3, 64)), whole[:, 192:320].unflatten(1, (2, 64))
+    h = how(c)
+    gaps = dict(w_q=whole[0, 320:384], w_k=whole[1, 320:384], pos=whole[2, 320:338].view(torch.int32)[None], freq=whole[3, 320:384].view(torch.float32))
+    for name, gap in gaps.items():
+        gap.copy_(h[name])
+        h[name] = gap
+    got = rl.relibra_qk_norm_rope_fwd(dev(c["q"]), dev(c["k"]), **h, q_out=q, k_out=k)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    sums = [whole[r, 320:448].view(torch.float32) for r in (5, 6)]
+    got = rl.relibra_qk_norm_rope_bwd(dev(c["q"]), dev(c["k"]), dev(c["up_q"]), dev(c["up_k"]), **h, dq=q, dk=k, dw_q=sums[0], dw_k=sums[1])
+    assert all(torch.equal(a, b) for a, b in zip(got, want[2:])) and all(torch.equal(gap, how(c)[name]) for name, gap in gaps.items())
+
 def test_qk_norm_rope_binding_refuses_other_types_and_layouts():
     b = lambda *s, t=BF16: torch.zeros(s, dtype=t)
     freq, pos = torch.zeros(8), torch.zeros(4, dtype=torch.int32)
