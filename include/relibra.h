@@ -690,7 +690,7 @@ int relibra_qk_norm_rope_bwd(const void *q_dev, int64_t q_stride, const void *k_
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ATTENTION_BWD, T, 1, Hq, n_seq, Hk, d) bytes
  * Limits: d % 8 == 0, d <= 128, Hq % Hk == 0 (RELIBRA_EINVAL), Hq / Hk <= 64, Hq <= 4096, n_seq <= 8192, T * Hq / Hk <= 2^26, fewer than 2^24 blocks,
  * which max(T * Hq / 128, T * Hk / 64) + 2 * (n_seq + 1) * Hk + 2048 bounds (RELIBRA_EUNSUPPORTED beyond); 0 < scale <= 1e38; strides and alignment as
- * above.  No output may share memory with an input or another output (RELIBRA_EINVAL).
+ * above.  No output may share memory with an input (the tables are such), another output or the workspace (RELIBRA_EINVAL).
  */
 int relibra_attention_fwd(const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride, const void *v_dev, int64_t v_stride,
                           const int32_t *seq_start_dev, const int32_t *seq_len_dev, int n_seq, int T, int Hq, int Hk, int d, float scale,

@@ -1159,7 +1159,11 @@ extern "C" int relibra_attention_fwd(const void *q, int64_t q_stride, const void
     for (const HeadRows &x : in)
         if (!x.usable() || x.overlaps(to, T) || x.overlaps(lse_all, T)) return RELIBRA_EINVAL;
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
-    if (!workspace || workspace_bytes < attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
+    const size_t need = attn_fwd_ws_bytes(T, n_seq, Hq, Hk, d);
+    if (!workspace || workspace_bytes < need) return RELIBRA_EWORKSPACE;
+    if (!pieces_apart(T, {in[0], in[1], in[2]}, {to}, {{seq_start, (n_seq + 1) * sizeof(int32_t)}, {seq_len, n_seq * sizeof(int32_t)}},
+                      {lse_all, {workspace, need}, {err_flag, sizeof(int32_t)}}))
+        return RELIBRA_EINVAL;
     const AttnSizes sz = row_sizes(T, n_seq, Hq, Hk, d, false);
     char *ws = (char *)workspace;
     const SchedOut rows = sched_out(ws, sz);
@@ -1206,7 +1210,11 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
             if (to[j].overlaps(to[i], T)) return RELIBRA_EINVAL;
     }
     if (!aligned16(workspace)) return RELIBRA_EINVAL;
-    if (!workspace || workspace_bytes < attn_bwd_ws_bytes(T, n_seq, Hq, Hk, d)) return RELIBRA_EWORKSPACE;
+    const size_t need = attn_bwd_ws_bytes(T, n_seq, Hq, Hk, d);
+    if (!workspace || workspace_bytes < need) return RELIBRA_EWORKSPACE;
+    if (!pieces_apart(T, {in[0], in[1], in[2], in[3], in[4]}, {to[0], to[1], to[2]}, {{seq_start, (n_seq + 1) * sizeof(int32_t)}, {seq_len, n_seq * sizeof(int32_t)}, lse_all},
+                      {{workspace, need}, {err_flag, sizeof(int32_t)}}))
+        return RELIBRA_EINVAL;
     const AttnSizes rs = row_sizes(T, n_seq, Hq, Hk, d, true), ks = key_sizes(T, n_seq, Hq, Hk, d);
     char *ws = (char *)workspace;
     const SchedOut rows = sched_out(ws, rs), keys = sched_out(ws, ks);

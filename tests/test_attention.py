@@ -509,6 +509,36 @@ def test_attention_refuses_overlaps_and_small_workspaces():
         assert rl.workspace_bytes(which, 8, 1, 4, 2, 3, 64) == 0 and rl.workspace_bytes(which, 8, 1, 4, 2, 2, 136) == 0
 
 
+def test_attention_refuses_overlaps_of_tables_flag_and_workspace():
+    """Outputs over the sequences' tables would change them while blocks find their work there.  Everything apart but for one pair."""
+    small = {n: (100 + i) << 16 for i, n in enumerate(("start", "length", "lse", "flag", "ws"))}
+    fwd_rows, bwd_rows = dict(q=M, k=2 * M, v=3 * M, out=4 * M), dict(q=M, k=2 * M, v=3 * M, out=4 * M, do=5 * M, dq=6 * M, dk=7 * M, dv=8 * M)
+    for call, which, rows, outs, sums in ((_fwd, rl.WS_ATTENTION_FWD, fwd_rows, ("out",), ("lse", "ws", "flag")), (_bwd, rl.WS_ATTENTION_BWD, bwd_rows, ("dq", "dk", "dv"), ("ws", "flag"))):
+        apart = dict(small, ws_bytes=rl.workspace_bytes(which, 8, 1, 4, 2, 2, 64))
+        for name in (*outs, *sums):
+            for other, at in {**small, **rows}.items():
+                if other != name:
+                    assert call(**{**apart, name: at}) == rl.EINVAL, (name, other)
+        assert call(**{**apart, "flag": small["ws"] + apart["ws_bytes"] - 4}) == rl.EINVAL and call(**{**apart, "start": small["ws"] - 8}) == rl.EINVAL
+        assert call(**{**apart, "length": rows[outs[0]] + 7 * 512 + 508}) == rl.EINVAL and call(**{**apart, "flag": rows["v"] + 4}) == rl.EINVAL
+
+
+@gpu
+def test_attention_takes_memory_between_its_rows():
+    """lse, the tables and the flag in the gaps between the rows of the outputs: shared by no row, and left or written as they should be."""
+    c = make([30, 25], 1, 2, 64, lens=[30, 20], seed=15)
+    want = run(c)
+    whole = torch.zeros((c["T"], 2048), dtype=BF16, device=DEV)
+    out, dq, dk, dv = (whole[:, a:a + h * 64].unflatten(1, (h, 64)) for a, h in ((0, 2), (128, 2), (256, 1), (320, 1)))
+    gap = lambda row, n, t: whole[row, 384:384 + 2 * n].view(t)
+    start, length, flag, lse = gap(0, 3, torch.int32), gap(1, 2, torch.int32), gap(2, 1, torch.int32), gap(3, 110, torch.float32).view(55, 2)
+    start.copy_(torch.tensor(c["starts"], dtype=torch.int32))
+    length.copy_(torch.tensor(c["lens"], dtype=torch.int32))
+    q, k, v, do = (c[n].to(DEV) for n in ("q", "k", "v", "dout"))
+    rl.relibra_attention_fwd(q, k, v, start, seq_len=length, out=out, lse=lse, err_flag=flag)
+    rl.relibra_attention_bwd(q, k, v, out, lse, do, start, seq_len=length, dq=dq, dk=dk, dv=dv, err_flag=flag)
+    assert all(torch.equal(a, b) for a, b in zip((out, lse, dq, dk, dv), want)) and flag.item() == 0 and start.tolist() == c["starts"] and length.tolist() == c["lens"]
+
 def test_attention_takes_interleaved_parts_of_one_tensor():
     """Refused for another reason (a workspace that is too small) behind the checks of overlaps: those let the parts pass."""
     kw = dict(q=M, k=M + 512, v=M + 768, ql=512, kl=512, vl=512)
