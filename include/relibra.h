@@ -629,7 +629,8 @@ int relibra_router_bwd(const void *logits_dev, const int32_t *ids_dev, const uin
  * n comes from x' before its rounding to the stream's type.  x_out may be x, n may be y (row by row, read before it is written).
  * Backward: dx, dy, dgate, dw_post, dw_pre from dx_out (the gradient of x', NULL: 0) and dn (of n; with w_pre only), with
  * x_out as the forward call left it (x where y is NULL).  dx, dx_out in the stream's type, dy bf16, dgate like the gate, dw_post,
- * dw_pre [h] fp32: overwritten, or added to with RELIBRA_NORM_ACCUMULATE.  dx may be dx_out, dy may be y or dn.
+ * dw_pre [h] fp32: overwritten, or added to with RELIBRA_NORM_ACCUMULATE.  dx may be dx_out, dy may be y or dn; dw_post and dw_pre
+ * may not share memory (RELIBRA_EINVAL).
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_BLOCK_NORM, T, 1, 1, 1, h, 0) bytes
  * Row sums and weight gradients are added up in fp32 in a fixed order: results are reproducible bit for bit.  A row whose squares add up to
  * more than fp32 holds (h values of 2e19 / sqrt(h)) has an infinite rms, and norms of 0 as far as its values are finite.

@@ -409,6 +409,8 @@ extern "C" int relibra_block_norm_bwd(const void *x_out, const void *dx_out, con
     const NormGrid g = norm_grid(T, h, true);
     const int P = T > 0 ? g.blocks : 0;
     if ((w_post || w_pre) && (!workspace || workspace_bytes < norm_ws_bytes(T, h))) return RELIBRA_EWORKSPACE;
+    // (one tensor for both would have two blocks add to the same values at once)
+    if (w_post && w_pre && overlap(dw_post, h * sizeof(float), dw_pre, h * sizeof(float))) return RELIBRA_EINVAL;
     const bool one = P == 1;                                  // one block's sums are the gradients: no second launch
     float *part_post = !w_post ? nullptr : one ? dw_post : (float *)workspace;
     float *part_pre = !w_pre ? nullptr : one ? dw_pre : (float *)((char *)workspace + norm_ws_bytes(T, h) / 2);

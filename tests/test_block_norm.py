@@ -273,6 +273,14 @@ def test_block_norm_refuses_missing_outputs_and_small_workspaces():
     assert need > 0 and _bwd(ws_bytes=need - 1) == rl.EWORKSPACE and _bwd(ws=0) == rl.EWORKSPACE
 
 
+def test_block_norm_refuses_one_tensor_for_both_weights_gradients():
+    apart = {n: (100 + i) << 20 for i, n in enumerate(("x", "dxo", "dn", "y", "w_post", "w_pre", "gate", "dx", "dy", "dgate", "dw_post", "dw_pre", "ws"))}
+    for T in (0, 4, 700):
+        for flags in (2, 2 | rl.NORM_ACCUMULATE):
+            for off in (0, 240, -240):                        # 64 values of 4 bytes
+                assert _bwd(**dict(apart, T=T, flags=flags, dw_pre=apart["dw_post"] + off)) == rl.EINVAL, (T, flags, off)
+
+
 @gpu
 @pytest.mark.parametrize("stream", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 def test_block_norm_rows_whose_squares_pass_fp32(stream):
