@@ -656,6 +656,8 @@ int relibra_block_norm_bwd(const void *x_out_dev, const void *dx_out_dev, const 
  *   pos_dev [n_axes, T] int32, dev (any values); freq_dev [rot / 2] fp32, dev; axis_host [rot / 2] host, each below n_axes <= 4 (RELIBRA_ERANGE), or
  *   NULL: all on the first axis (several: time, height and width of images and video)
  * Angles in double, everything else in fp32 with one rounding at the end.
+ * A head whose squares add up to more than fp32 holds (d values of 2e19 / sqrt(d)) has an infinite rms: its norm, its gradient and its part of the
+ * weights' gradients are 0 as far as its values and their gradients are finite.
  * Backward: dq, dk from dq_out, dk_out and the inputs q, k of the forward call (not read without their norm), and dw_q, dw_k [d] fp32: overwritten,
  * or added to with RELIBRA_QK_ACCUMULATE.  dq may be dq_out or q, dk may be dk_out or k.  A fixed order: the same bits every call.
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_QK_NORM_ROPE, T, 1, Hq, 1, Hk, d) bytes (E, h, hff are Hq, Hk, d); unused without norms

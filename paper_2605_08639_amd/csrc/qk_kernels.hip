@@ -191,7 +191,8 @@ qk_bwd_kernel(QkShape sh, QkTables tab, const bf16_t *q, size_t q_ld, const bf16
                     sum += v0[i] * v0[i] + v1[i] * v1[i];
                     dot += w0[i] * g0[i] * v0[i] + w1[i] * g1[i] * v1[i];
                 }
-                const float r = 1.0f / sqrtf(group_sum<LANES>(sum) * inv_d + sh.eps), m = group_sum<LANES>(dot) * r * inv_d;
+                const float r = 1.0f / sqrtf(group_sum<LANES>(sum) * inv_d + sh.eps);
+                const float md = group_sum<LANES>(dot) * r * inv_d, m = r > 0.0f ? md : 0.0f;      // (an infinite rms leaves zeros, whatever the products' sum)
                 float(&acc)[16] = Q ? acc_q : acc_k;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {

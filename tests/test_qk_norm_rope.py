@@ -211,6 +211,40 @@ def test_qk_norm_rope_zeros_and_nan_stay_in_their_head():
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_qk_norm_rope_heads_whose_squares_pass_fp32(d):
+    """sqrt(3.4e38 / 256) = 1.1e18: a head of 1e19 or 3e38 has an infinite rms, its norm and its gradients are zeros; one of 1e17 is an ordinary head; no other head notices."""
+    c = make(12, 4, 2, d, seed=13)
+    g = torch.Generator().manual_seed(14)
+    sign = lambda: torch.randn(d, generator=g).sign()
+    heads = (("q", 3, 1, 1e19), ("q", 5, 0, 3e38), ("k", 7, 1, 3e38), ("q", 9, 2, 1e17))
+    for name, t, h, size in heads:
+        c[name][t, h] = (size * sign()).to(BF16)
+        c["up_" + name][t, h] = (4 * c["up_" + name][t, h].abs().float() * c[name][t, h].float().sign()).to(BF16)      # products of one sign: their sum passes fp32 for 3e38
+    c["freq"].zero_()                                         # no turn: the upstream's signs are the norm's
+    got = rl.relibra_qk_norm_rope_fwd(dev(c["q"]), dev(c["k"]), **how(c))
+    dx = rl.relibra_qk_norm_rope_bwd(dev(c["q"]), dev(c["k"]), dev(c["up_q"]), dev(c["up_k"]), **how(c))
+    for name, i in (("q", 0), ("k", 1)):
+        x, w, up, y = c[name], c["w_" + name], c["up_" + name], got[i].cpu().double()
+        leaf, wl = x.double().requires_grad_(True), w.double().requires_grad_(True)
+        kept = torch.ones(x.shape[:2], dtype=torch.bool)
+        for n, t, h, size in heads:
+            if n == name and size > 1e18:
+                kept[t, h] = False
+                assert torch.all(y[t, h] == 0) and torch.all(dx[i][t, h] == 0), (n, size)
+        want = forward(leaf, wl, c)
+        (want * up.double())[kept].sum().backward()
+        want = want.detach()
+        assert torch.all((y - want).abs()[kept] <= (HALF16 + 2 * REL) * want.abs()[kept])
+        with torch.no_grad():
+            r = 1 / torch.sqrt((x.double() ** 2).mean(2, keepdim=True) + c["eps"])
+            xh, wg = (x.double() * r).abs(), w.double().abs() * up.double().abs()
+            size = r * (wg + xh * (wg * xh).mean(2, keepdim=True))
+        assert torch.all((dx[i].cpu().double() - leaf.grad).abs()[kept] <= (HALF16 * leaf.grad.abs() + 3 * REL * size)[kept])
+        off = (dx[2 + i].cpu().double() - wl.grad).abs()
+        assert torch.all(off <= U32 * wl.grad.abs() + (2 * REL + 66 * U32) * (up.double().abs() * xh)[kept].sum(0)), float(off.max())
+
+@gpu
 def test_qk_norm_rope_writes_every_value_and_nothing_else():
     for kw in (dict(T=3, Hq=5, Hk=1, d=48), dict(T=1030, Hq=2, Hk=2, d=96, rot=32)):
         c = make(seed=8, **kw)
