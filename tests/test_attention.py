@@ -427,6 +427,95 @@ def test_attention_gradient_against_differences():
         assert abs((out_value(c1) - out_value(c2)) / 2 - slope) <= tol
 
 
+def bounds(c):
+    """(errors of out, dq, dk, dv; the values themselves) of the sequences' tokens from the definition, by the tolerances at the top; zeros elsewhere."""
+    T, Hk, G, d, s = c["T"], c["Hk"], c["G"], c["d"], c["scale"]
+    z4 = lambda: [torch.zeros(T, h, d, dtype=torch.float64) for h in (Hk * G, Hk * G, Hk, Hk)]
+    err, val = z4(), z4()
+    for start, n in zip(c["starts"], c["lens"]):
+        rows, mask = slice(start, start + n), torch.ones(n, n, dtype=torch.bool).tril()
+        for h in range(Hk):
+            k, v = c["k"][rows, h].double(), c["v"][rows, h].double()
+            for g in range(h * G, (h + 1) * G):
+                q, do = c["q"][rows, g].double(), c["dout"][rows, g].double()
+                z = (s * q @ k.T).masked_fill(~mask, -math.inf)
+                ez = ((d + 4) * U * s * (q.abs() @ k.abs().T)).masked_fill(~mask, 0).amax(1, keepdim=True)
+                lse = torch.logsumexp(z, 1, keepdim=True)
+                p = torch.exp(z - lse)
+                want, size = p @ v, p @ v.abs()
+                err_out = (H + 2 * ez + (2 * n + 40) * U) * size + H * want.abs()
+                dp, D = do @ v.T, (do * want).sum(1, keepdim=True)
+                ds = (p * (dp - D)).masked_fill(~mask, 0)
+                ep = 2 * ez + (n + 32) * U + 8 * U * lse.abs()
+                err_ds = (p * ((do.abs() * err_out).sum(1, keepdim=True) + (d + 8) * U * (do.abs() @ v.abs().T + (do.abs() * size).sum(1, keepdim=True))) + (2 * ep + H) * ds.abs()).masked_fill(~mask, 0)
+                val[0][rows, g], err[0][rows, g] = want, err_out
+                val[1][rows, g], err[1][rows, g] = s * ds @ k, s * (err_ds + (n + 24) * U * ds.abs()) @ k.abs()
+                val[2][rows, h] += s * ds.T @ q
+                val[3][rows, h] += p.T @ do
+                err[2][rows, h] += s * (err_ds + (n * G + 24) * U * ds.abs()).T @ q.abs()
+                err[3][rows, h] += ((H + ep + (n * G + 24) * U) * p).T @ do.abs()
+    for i in (1, 2, 3):
+        err[i] += H * val[i].abs()
+    return err, val
+
+
+STEPS = dict(q=1 / 4, k=1 / 4, v=1 / 4)
+
+
+def differences(c, name, out_value):
+    """(half the difference of `out_value` one step along the gradient's signs and one step back, how far it may be from the gradient's slope, the step, the definition's gradient).  Along the signs the
+    slope is the sum of the gradient's sizes.  What the curve adds to a central difference is the definition's own."""
+    i = ("q", "k", "v").index(name) + 1
+    err, val = bounds(c)
+    way = val[i].sign() * STEPS[name]
+    c1, c2 = (dict(c, **{name: (c[name].double() + s * way).to(BF16)}) for s in (1, -1))
+    moved = (c1[name].double() - c2[name].double()) / 2
+    up = c["dout"].double()
+    (e1, v1), (e2, v2) = bounds(c1), bounds(c2)
+    slope = (moved * val[i]).sum().item()
+    bend = abs(((v1[0] - v2[0]) * up).sum().item() / 2 - slope)
+    tol = bend + ((e1[0] + e2[0]) * up.abs()).sum().item() / 2 + (moved.abs() * err[i]).sum().item()
+    return (out_value(c1) - out_value(c2)) / 2, 1.01 * tol, moved, val[i]
+
+
+DIFFERENCES = [dict(places=[6], Hk=1, G=2, d=16), dict(places=[40, 90], lens=[33, 90], Hk=2, G=1, d=64), dict(places=[70], Hk=1, G=5, d=72), dict(places=[150], Hk=1, G=2, d=128)]
+
+
+def difference_case(kw):
+    """Tokens of two kinds: their keys and values point one way or the other, beside something of their own; queries and the upstream ask for one kind, scores are about 1 and -1.  What a step
+    changes then adds up over tokens and values, what is rounded does not."""
+    c = make(**kw, seed=17, peak=1.0)
+    g = torch.Generator().manual_seed(18)
+    kind = torch.randn(c["T"], 1, 1, generator=g).sign()
+    keys, values = (torch.randn(1, 1, c["d"], generator=g).sign() for _ in range(2))
+    for n, way in (("q", keys), ("k", kind * keys), ("v", kind * values), ("dout", values)):
+        c[n] = (way + 0.3 * c[n].float()).to(BF16)
+    return dict(c, scale=1 / c["d"])
+
+
+@gpu
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+@pytest.mark.parametrize("kw", DIFFERENCES, ids=str)
+def test_attention_gradient_against_its_own_differences(kw, name):
+    c = difference_case(kw)
+    up = c["dout"].double()
+    grad = run(c)[("q", "k", "v").index(name) + 2].cpu().double()
+    diff, tol, moved, _ = differences(c, name, lambda cc: (run(cc, bwd=False)[0].cpu().double() * up).sum().item())
+    assert abs(diff - (moved * grad).sum().item()) <= tol
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+@pytest.mark.parametrize("kw", DIFFERENCES, ids=str)
+def test_attention_differences_tell_wrong_gradients(kw, name):
+    """What the test above would say of other gradients, with the definition in the library's place: the right one passes; none, half of it, and one of the wrong sign do not,
+    not even if everything that may be off were off in their favour."""
+    c = difference_case(kw)
+    diff, tol, moved, grad = differences(c, name, lambda cc: (bounds(cc)[1][0] * cc["dout"].double()).sum().item())
+    right = (moved * grad).sum().item()
+    assert abs(diff - right) <= tol
+    for wrong in (0.0, 0.5, -1.0):
+        assert abs(diff - wrong * right) > 2 * tol, (wrong, diff, right, tol)
+
 def reference_out(q, k, v, s):
     kk, vv = k.repeat_interleave(q.shape[1] // k.shape[1], 1), v.repeat_interleave(q.shape[1] // k.shape[1], 1)
     z = torch.einsum("ihd,jhd->hij", q, kk) * s
