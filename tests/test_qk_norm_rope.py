@@ -136,6 +136,84 @@ def test_qk_norm_rope_gradient_against_differences():
         assert abs((value(up) - value(dn)) / (2 * step) - dq[t, h, j].item()) <= noise + bend
 
 
+STEP = 0.125
+
+
+def value(y_q, y_k, c):
+    return (y_q.cpu().double() * c["up_q"].double()).sum().item() + (y_k.cpu().double() * c["up_k"].double()).sum().item()
+
+
+def defined(c):
+    return forward(c["q"], c["w_q"], c), forward(c["k"], c["w_k"], c)
+
+
+def gradient_error(c, name, grad):
+    """What the gradient of input `name` may be off by, as in check_backward."""
+    x, w, up = (c[n] for n in (("q", "w_q", "up_q") if name in ("q", "w_q") else ("k", "w_k", "up_k")))
+    g = sizes(turn(up.double(), c, -1), c)
+    if w is None:
+        return HALF16 * grad.abs() + 3 * REL * g
+    r = 1 / torch.sqrt((x.double() ** 2).mean(2, keepdim=True) + c["eps"])
+    xh, wg = (x.double() * r).abs(), w.double().abs() * g
+    if name in ("w_q", "w_k"):
+        return U32 * grad.abs() + (2 * REL + (x.shape[0] / 8 + 64) * U32) * (g * xh).sum((0, 1))
+    return HALF16 * grad.abs() + 3 * REL * r * (wg + xh * (wg * xh).mean(2, keepdim=True))
+
+
+def difference_case(kw, name):
+    """Upstream for one side; for a weight of the normed head's own signs, so that what tokens and heads add to its gradient has one sign."""
+    c = make(seed=15, **kw)
+    c["up_k" if name in ("q", "w_q") else "up_q"].zero_()
+    if name in ("w_q", "w_k"):
+        up = "up_" + name[2]
+        c[up] = turn(c[up].double().abs() * c[name[2]].double().sign(), c).to(BF16)
+    return c
+
+
+def differences(c, name, outputs):
+    """(half the difference of the outputs' sum against the upstream one step along the signs of the definition's gradient of input `name` and one step back, how far it may be from the gradient's slope,
+    the step, the gradient, how far the library's may be off).  Along the signs the slope is the sum of the gradient's sizes; what the curve adds to a central difference is the definition's own,
+    what outputs and gradients are off by is the tolerance of the test against the definition."""
+    leaves = {n: c[n].double().requires_grad_(True) for n in ("q", "k", "w_q", "w_k") if c[n] is not None}
+    y = (forward(leaves["q"], leaves.get("w_q"), c), forward(leaves["k"], leaves.get("w_k"), c))
+    ((y[0] * c["up_q"].double()).sum() + (y[1] * c["up_k"].double()).sum()).backward()
+    grad = leaves[name].grad
+    ends = [dict(c, **{name: (c[name].double() + s * STEP * grad.sign()).to(BF16)}) for s in (1, -1)]
+    moved = (ends[0][name].double() - ends[1][name].double()) / 2
+    slope = (moved * grad).sum().item()
+    noise = 0.0
+    for e in ends:
+        for y, x, w, up in zip(defined(e), (e["q"], e["k"]), (e["w_q"], e["w_k"]), (e["up_q"], e["up_k"])):
+            noise += ((HALF16 * y.abs() + 2 * REL * sizes(forward(x, w, dict(e, freq=None)), e)) * up.double().abs()).sum().item() / 2
+    bend = abs((value(*defined(ends[0]), c) - value(*defined(ends[1]), c)) / 2 - slope)
+    own = (moved.abs() * gradient_error(c, name, grad)).sum().item()
+    return (value(*outputs(ends[0]), c) - value(*outputs(ends[1]), c)) / 2, 1.01 * (bend + noise + own), moved, grad
+
+
+DIFFERENCES = [dict(T=2, Hq=2, Hk=1, d=16), dict(T=30, Hq=5, Hk=2, d=96, rot=32, axes=3), dict(T=9, Hq=4, Hk=3, d=128, adjacent=True), dict(T=20, Hq=3, Hk=2, d=64, norm=False)]
+INPUTS = [(kw, name) for kw in DIFFERENCES for name in ("q", "k", "w_q", "w_k") if kw.get("norm", True) or name in ("q", "k")]
+
+
+@gpu
+@pytest.mark.parametrize("kw,name", INPUTS, ids=lambda x: IDS(x) if isinstance(x, dict) else x)
+def test_qk_norm_rope_gradient_against_its_own_differences(kw, name):
+    c = difference_case(kw, name)
+    got = rl.relibra_qk_norm_rope_bwd(dev(c["q"]), dev(c["k"]), dev(c["up_q"]), dev(c["up_k"]), **how(c))[("q", "k", "w_q", "w_k").index(name)].cpu().double()
+    diff, tol, moved, _ = differences(c, name, lambda e: rl.relibra_qk_norm_rope_fwd(dev(e["q"]), dev(e["k"]), **how(e)))
+    assert abs(diff - (moved * got).sum().item()) <= tol
+
+
+@pytest.mark.parametrize("kw,name", INPUTS, ids=lambda x: IDS(x) if isinstance(x, dict) else x)
+def test_qk_norm_rope_differences_tell_wrong_gradients(kw, name):
+    """What the test above would say of other gradients, with the definition in the library's place: the right one passes; none, half of it, and one of the wrong sign do not, not even if
+    everything that may be off were off in their favour."""
+    c = difference_case(kw, name)
+    diff, tol, moved, grad = differences(c, name, defined)
+    right = (moved * grad).sum().item()
+    assert abs(diff - right) <= tol
+    for wrong in (0.0, 0.5, -1.0):
+        assert abs(diff - wrong * right) > 2 * tol, (wrong, diff, right, tol)
+
 @gpu
 @pytest.mark.parametrize("kw", [dict(T=33, Hq=8, Hk=2, d=128), dict(T=700, Hq=3, Hk=2, d=80, rot=32, adjacent=True)], ids=IDS)
 def test_qk_norm_rope_of_a_fused_projection(kw):
