@@ -168,6 +168,70 @@ def test_attention_of_long_sequences_and_many_heads(name):
     check(c, run(c))
 
 
+def launches(c, **kw):
+    """What run(c) gives, and how often each of the call's kernels was launched: (forward, backward)."""
+    start, length = tables(c)
+    d = {n: c[n].to(DEV) for n in ("q", "k", "v", "dout")}
+    count = []
+    rl.prof_start(2)
+    out, lse = rl.relibra_attention_fwd(d["q"], d["k"], d["v"], start, seq_len=length, scale=c["scale"])
+    count.append({n: v[1] for n, v in rl.prof_stop().items() if v[1]})
+    rl.prof_start(2)
+    grads = rl.relibra_attention_bwd(d["q"], d["k"], d["v"], out, lse, d["dout"], start, seq_len=length, scale=c["scale"])
+    count.append({n: v[1] for n, v in rl.prof_stop().items() if v[1]})
+    return (out, lse, *grads), count
+
+
+# A call of few sequences makes a list of its rows only where several blocks share their tiles; the keys' list is made beside the queries' kernel then.
+SHARED = dict(
+    d32=(dict(places=[2300, 100], Hk=1, G=2, d=32), True, True), d24_padded=(dict(places=[2500], lens=[2433], Hk=2, G=1, d=24), True, True),
+    d8=(dict(places=[2400, 1], Hk=1, G=3, d=8), True, True), nine_heads=(dict(places=[1500, 1500, 1544], Hk=1, G=9, d=64), True, True),
+    ten_heads=(dict(places=[1700, 2000, 396], lens=[1690, 2000, 390], Hk=1, G=10, d=32), True, True), twelve_heads=(dict(places=[1700, 1692], Hk=1, G=12, d=96), False, True),
+    sixteen_heads=(dict(places=[1300, 1260], Hk=1, G=16, d=128), False, False))
+
+
+@gpu
+@pytest.mark.parametrize("name", SHARED)
+def test_attention_of_tiles_that_blocks_share(name):
+    kw, forward, backward = SHARED[name]
+    c = make(**kw, seed=22)
+    got, (fwd, bwd) = launches(c)
+    assert [fwd.get("attn_sched", 0), fwd.get("attn_join", 0), bwd.get("attn_sched", 0), bwd.get("attn_join", 0)] == [forward, forward, backward, 1]
+    check(c, got)
+
+
+# The gradients' loads of rows move by a constant where a group divides what a load takes, 16 rows of heads above 64, 32 of others: on both sides of it and
+# at it, with waves that begin inside of a group, last steps that are not whole, and padding.
+GROUPS = dict(
+    g16=dict(places=[1, 4, 5, 64, 130], Hk=1, G=16, d=128), g16_padded=dict(places=[90, 77], lens=[81, 3], Hk=2, G=16, d=128, before=4, behind=2), g16_d72=dict(places=[33, 70], Hk=2, G=16, d=72),
+    g8_d104=dict(places=[9, 130], Hk=2, G=8, d=104), g32=dict(places=[1, 2, 3, 40, 65], Hk=1, G=32, d=64), g32_padded=dict(places=[50, 31], lens=[47, 30], Hk=2, G=32, d=40),
+    g32_d128=dict(places=[7, 66], Hk=1, G=32, d=128), g24=dict(places=[20, 67], Hk=1, G=24, d=64), g64_d128=dict(places=[2, 35], Hk=1, G=64, d=128))
+
+
+@gpu
+@pytest.mark.parametrize("name", GROUPS)
+def test_attention_of_wide_groups(name):
+    c = make(**GROUPS[name], seed=23)
+    check(c, run(c))
+
+
+@gpu
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("n_seq,most", [(17, 9), (17, 90), (63, 4), (64, 5), (64, 40), (65, 5), (65, 40)])
+def test_attention_on_both_sides_of_the_sequences_that_need_no_list(n_seq, most, G):
+    """Blocks find their rows and keys in the tables for up to 64 sequences, one a lane; the keys' list of as many is made beside the queries' kernel where they are not few.  With padding and empty
+    sequences among them, the last one too."""
+    g = torch.Generator().manual_seed(n_seq + most)
+    places = [int(x) for x in torch.randint(0, most + 1, (n_seq,), generator=g)]
+    places[n_seq // 2], places[-2:] = 0, [most, 0 if G == 1 else most]
+    lens = [int(torch.randint(0, p + 1, (1,), generator=g)) for p in places]
+    lens[-2] = most
+    c = make(places, 2, G, 64, lens=lens, before=1, behind=3, seed=24)
+    got, (fwd, bwd) = launches(c)
+    few = c["T"] * G <= 512
+    assert [fwd.get("attn_sched", 0), bwd.get("attn_sched", 0), bwd.get("attn_join", 0)] == [n_seq > 64, n_seq > 64, n_seq > 64 or not few]
+    check(c, got)
+
 @gpu
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("shape", ["peaked", "rising", "falling", "flat", "huge"])
