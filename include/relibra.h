@@ -691,7 +691,9 @@ int relibra_qk_norm_rope_bwd(const void *q_dev, int64_t q_stride, const void *k_
  * the rows of a sequence's first 128 tokens), the sums are fp32.  A key head's gradients are summed over its group.  No atomics on values, a fixed
  * order: the same bits every call.
  *   workspace_dev: relibra_workspace_bytes(RELIBRA_WS_ATTENTION_BWD, T, 1, Hq, n_seq, Hk, d) bytes
- * Limits: d % 8 == 0, d <= 128, Hq % Hk == 0 (RELIBRA_EINVAL), Hq / Hk <= 64, Hq <= 4096, n_seq <= 8192, T * Hq / Hk <= 2^26, fewer than 2^24 blocks,
+ * Rows of no sequence (and with an error flag all rows) keep what was in out, lse, dq, dk and dv.
+ * Limits: d % 8 == 0, d <= 128 (a block's tiles and a wave's registers hold no more; norms and rotation take up to 256, in sixteens for their pairs of pieces),
+ * Hq % Hk == 0 (RELIBRA_EINVAL), Hq / Hk <= 64, Hq <= 4096, n_seq <= 8192, T * Hq / Hk <= 2^26, fewer than 2^24 blocks,
  * which max(T * Hq / 128, T * Hk / 64) + 2 * (n_seq + 1) * Hk + 2048 bounds (RELIBRA_EUNSUPPORTED beyond); 0 < scale <= 1e38; strides and alignment as
  * above.  No output may share memory with an input (the tables are such), another output or the workspace (RELIBRA_EINVAL).
  */

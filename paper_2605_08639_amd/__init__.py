@@ -958,7 +958,8 @@ def _attention_args(q, k, seq_start, seq_len, scale):
 def relibra_attention_fwd(q, k, v, seq_start, seq_len=None, scale=None, out=None, lse=None, workspace=None, err_flag=None):
     """Causal attention of packed sequences: q [T,Hq,d], k, v [T,Hk,d] bf16 (parts of a fused projection as they lie, or tensors of their own), sequence s
     in rows seq_start[s] .. seq_start[s+1] (int32), its first seq_len[s] (None: all) of them tokens -> out [T,Hq,d] bf16, lse [T,Hq] fp32.
-    scale: d^-1/2 unless given."""
+    scale: d^-1/2 unless given.  Rows of no sequence, and all rows with a table that err_flag refuses, keep what was in out and lse: in tensors made here, whatever
+    the memory held."""
     T, Hq, Hk, d, n_seq, scale = _attention_args(q, k, seq_start, seq_len, scale)
     out = _heads_out(out, (T, Hq, d), q)
     lse = _out(lse, (T, Hq), torch.float32, q)
@@ -975,7 +976,8 @@ def relibra_attention_fwd(q, k, v, seq_start, seq_len=None, scale=None, out=None
 
 
 def relibra_attention_bwd(q, k, v, out, lse, dout, seq_start, seq_len=None, scale=None, dq=None, dk=None, dv=None, workspace=None, err_flag=None):
-    """dout [T,Hq,d] bf16 and the forward call's inputs and outputs -> (dq [T,Hq,d], dk, dv [T,Hk,d]) bf16; they may be parts of one tensor [T, (Hq+2Hk) d]."""
+    """dout [T,Hq,d] bf16 and the forward call's inputs and outputs -> (dq [T,Hq,d], dk, dv [T,Hk,d]) bf16; they may be parts of one tensor [T, (Hq+2Hk) d].
+    Rows of no sequence, and all rows with a table that err_flag refuses, keep what was in dq, dk and dv: in tensors made here, whatever the memory held."""
     T, Hq, Hk, d, n_seq, scale = _attention_args(q, k, seq_start, seq_len, scale)
     assert lse.shape == (T, Hq) and lse.dtype is torch.float32, "lse is [T, Hq] fp32"
     dq, dk, dv = _heads_out(dq, (T, Hq, d), q), _heads_out(dk, (T, Hk, d), q), _heads_out(dv, (T, Hk, d), q)

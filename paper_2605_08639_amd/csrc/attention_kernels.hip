@@ -479,8 +479,8 @@ template <int ND> struct Part {
 };
 
 // ---------------------------------------------------------------- forward
-// One pass over the keys with a running maximum and sum.  A step of a wave is 32 products of 32x32x16 (d = 128), 32 exponentials a lane and 24 LDS reads; the
-// order below keeps the first two side by side (ragged batch 46.9 -> 38.5 us; long calls spend the 14 % of cycles on a lower clock: 2100 -> 2083).
+// One pass over the keys with a running maximum and sum.  A step of a wave is 32 products of 32x32x16 (d = 128), 32 exponentials a lane and 48 LDS reads, 32 of
+// them transposing ones of 8 bytes a lane; the order below keeps the first two side by side (ragged batch 46.9 -> 38.5 us; long calls spend the 14 % of cycles on a lower clock: 2100 -> 2083).
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source, HeadsOut out, float *__restrict__ lse,
@@ -862,7 +862,8 @@ attn_dq_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn out, Heads
 // dk and dv of 64 keys over some of the packed rows behind the first of them.  Two waves share 32 keys: each works out p and ds for 32 of a step's
 // 64 rows, hands the other the half that it needs, and adds up one of the two gradients over all 64 rows.  A wave for itself would hold both sums,
 // 128 registers beside the operands' 64 and the scores' 32, and leave no room for a second wave on its SIMD (the long sequence 2260 -> 1190 us).
-// Four products a step, two barriers: 1100 us, 1000 TFLOP/s for 8192 tokens of 32 heads with keys of their own; without any loads it took 930.
+// Four products a step, two barriers: 1100 us, 1000 TFLOP/s for 8192 tokens of 32 heads with keys of their own; without any loads it took 930.  A step of a unit's two
+// blocks takes 4200 cycles, in packed micro-batches, too; 2050 are products, and no other unit is busy for as long.  A quarter of a wave's time is waits and barriers.
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_dkv_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, HeadsIn dout, const float *__restrict__ lse2, const float *__restrict__ minus_delta,
@@ -1224,7 +1225,10 @@ extern "C" int relibra_attention_bwd(const void *q, int64_t q_stride, const void
     const HeadsIn qi{(const bf16_t *)q, q_stride}, ki{(const bf16_t *)k, k_stride}, vi{(const bf16_t *)v, v_stride}, oi{(const bf16_t *)out, out_stride},
         di{(const bf16_t *)dout, dout_stride};
     const HeadsOut dqo{(bf16_t *)dq, dq_stride}, dko{(bf16_t *)dk, dk_stride}, dvo{(bf16_t *)dv, dv_stride};
-    // Rows' units are found without a list where they may be; keys' only if no tile of theirs could be shared, and their list is then made beside dq.
+    // Rows' units are found without a list where no tile of theirs is shared.  Keys' are where no tile can have more than 8 steps: those of 5 to 8 would be
+    // shared with a list, but making it and joining costs about what that saves; beyond, the list is made beside dq.  One sequence backward, found / listed, us: 5
+    // steps (320 tokens of 8 heads) 25 / 27, 8 steps (512 tokens of 2, 8, 32, 64 heads) 33.5 / 31.5, 34 / 33, 36 / 40, 40 / 51, 16 steps (1024 of 2, 8, 32) 54 / 44,
+    // 55 / 52, 61 / 72.
     const bool rows_listed = rs.joins > 0 || n_seq > kSelfSeq;
     const bool keys_listed = rows_listed || tiles_of((long long)T * sh.G, kRowStep) > 2 * kMinKeyChunk;
     const int beside = keys_listed && !rows_listed;
