@@ -480,7 +480,8 @@ template <int ND> struct Part {
 
 // ---------------------------------------------------------------- forward
 // One pass over the keys with a running maximum and sum.  A step of a wave is 32 products of 32x32x16 (d = 128), 32 exponentials a lane and 48 LDS reads, 32 of
-// them transposing ones of 8 bytes a lane; the order below keeps the first two side by side (ragged batch 46.9 -> 38.5 us; long calls spend the 14 % of cycles on a lower clock: 2100 -> 2083).
+// them transposing ones of 8 bytes a lane; the order below keeps the first two side by side (ragged batch 46.9 -> 38.5 us; long calls spend the 14 % of cycles on
+// a lower clock: 2100 -> 2083).
 template <int ND>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 attn_fwd_kernel(AttnShape sh, HeadsIn q, HeadsIn k, HeadsIn v, UnitSource source, HeadsOut out, float *__restrict__ lse,
